@@ -411,6 +411,151 @@ int wkv_compress_group_host_rows(const wkv_shape *s, int32_t n_layers,
                                  void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
+ * ---- around the selection: rotary positions, the prompt's attention, the compact cache in use ----
+ *
+ * What an engine runs before the path above (rotary positions, the prompt's attention, whose log-sum-exp of the
+ * observation rows is what the _lse calls take) and after it (new tokens appended to the paged compact cache of section
+ * 2.1's decode phase and attending over it, rows leaving the cache by the attention weight they have received).
+ * The general conventions at the head of this file hold.  Scores are scaled by 1/sqrt(head_dim) as in Eq. 1.
+ */
+
+/* Rotary positions: of each head's first rot_dim dimensions, pairs (x_j, x_k) are turned by position * f_i,
+ *   x_j' = (x_j cos - x_k sin) * scale,  x_k' = (x_k cos + x_j sin) * scale,
+ * (j, k) = (i, i + rot_dim/2) in WKV_ROPE_HALF order, (2i, 2i + 1) in WKV_ROPE_INTERLEAVED order, i < rot_dim/2; dimensions
+ * from rot_dim on are copied.  f_i is given in turns of 2^-64: the angle is the product with the position modulo 2^64, exact at
+ * any position; computed in fp32 from there and rounded once. */
+typedef enum { WKV_ROPE_HALF = 0, WKV_ROPE_INTERLEAVED = 1 } wkv_rope_order;
+/* How f_i = base^(-2i/rot_dim) is changed for contexts longer than the model was trained on: not at all; divided by factor
+ * (LINEAR); base times factor^(rot_dim/(rot_dim-2)) (BASE); by bands (BANDS): with t = (original_length * f_i / 2 pi - low) /
+ * (high - low) limited to 0..1, f_i (t + (1 - t)/factor), so that pairs which turn often keep their angle. */
+typedef enum { WKV_ROPE_NONE = 0, WKV_ROPE_LINEAR = 1, WKV_ROPE_BASE = 2, WKV_ROPE_BANDS = 3 } wkv_rope_scaling;
+typedef struct {
+    uint32_t struct_size;      /* sizeof(wkv_rope), checked */
+    int32_t rot_dim;           /* even, 2 .. head_dim */
+    int32_t order;             /* wkv_rope_order */
+    float scale;               /* factor of the turned dimensions, finite (1 where the model has none) */
+    const uint64_t *turns;     /* DEVICE [rot_dim/2], as wkv_rope_frequencies writes them on the host */
+} wkv_rope;
+/* Host function, no device work: f_i in turns of 2^-64, HOST out [rot_dim/2].  factor, original_length, low and high are read
+ * where the scaling uses them.  WKV_ERR_SHAPE for an odd or non-positive rot_dim, base <= 0, factor <= 0, high <= low,
+ * original_length <= 0 or an unknown scaling. */
+int wkv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_length, double low,
+                         double high, uint64_t *turns_out);
+
+/*
+ * Rotary positions of a prompt's queries and keys, before they are attended over and scored.
+ *   q, q_out   DEVICE  queries, element (b, hq, i, c) at q[(off_b + i)*q_strides[2] + b*q_strides[0] + hq*q_strides[1] + c], off_b
+ *              as for K/V (q_strides[0] is not used when packed); HOST array of three strides, for both
+ *   k, k_out   DEVICE  keys in the layout of `s`
+ *   positions  DEVICE int32 or NULL (then a token's position is its place in its sequence): [T] packed, [B, max_seqlen] dense
+ * Either pair may be NULL (both of it); an output may be its input, and may not overlap it otherwise.
+ */
+int wkv_rotate_prompt(const wkv_shape *s, const wkv_rope *rope, const void *q, void *q_out, const int64_t *q_strides,
+                      const void *k, void *k_out, const int32_t *positions, void *cuda_stream);
+
+/*
+ * Causal attention of whole prompts with grouped heads (Eq. 1's softmax for every row, times V): query i of a sequence attends
+ * to its keys 0..i.
+ *   q, out     DEVICE  as in wkv_rotate_prompt, with strides of their own (HOST arrays of three)
+ *   k, v       DEVICE  in the layout of `s`
+ *   lse        DEVICE out or NULL, float [B, H_q, max_seqlen]: natural log of every row's sum of exponentials; entries behind a
+ *              sequence's end are not written
+ *   lse_obs    DEVICE out or NULL, float [B, H_q, alpha]: the same of the observation rows, as wkv_score_windows_lse and the
+ *              others take it; -infinity where the sequence has fewer than alpha tokens and the row does not exist
+ *   status     DEVICE int32 or NULL, OR-ed with 1 if a bounded wait inside the kernel expired (the outputs are invalid then)
+ * What stands in K or V behind a row's position (infinities and NaN included) does not reach the row.  head_dim up to 256.
+ */
+int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_strides, const void *k, const void *v, void *out,
+                      const int64_t *out_strides, float *lse, float *lse_obs, int32_t *status, void *cuda_stream);
+
+/*
+ * A paged cache as wkv_gather_kv_paged fills it: row r of unit (b, h) is slot r % page_size of page block_table[b][r / page_size],
+ * element c of it at pool[page*page_stride + h*head_stride + slot*row_stride + c].  A table entry outside [0, num_pages) is no
+ * page: its rows are neither read nor written, and nothing attends to them.  Lengths are per unit, as kept_len.
+ * The chunk of new tokens: max_new for every sequence ([B, heads, max_new, d], strides given with each tensor), or packed
+ * [T, heads, d] with cu_new (0 .. max_new tokens per sequence; HOST and DEVICE copies as for cu_seqlens).
+ */
+typedef struct {
+    uint32_t struct_size;        /* sizeof(wkv_paged), checked */
+    int32_t dtype;               /* wkv_dtype of Q, K, V and the pools */
+    int32_t batch, n_q_heads, n_kv_heads, head_dim;
+    int32_t max_new;             /* >= 1 */
+    int32_t page_size, num_pages, max_pages;
+    int32_t reserved[2];         /* must be 0 */
+    const int32_t *cu_new_host;  /* HOST [B+1] or NULL */
+    const int32_t *cu_new_dev;   /* DEVICE copy (required iff the host one is given) */
+    const int32_t *block_table;  /* DEVICE [B, max_pages] */
+    int64_t page_stride, head_stride, row_stride;   /* elements, multiples of 16 bytes */
+} wkv_paged;
+/* Bytes of DEVICE scratch that wkv_attend_paged and wkv_evict_kv_paged need for this cache (256-byte aligned base expected);
+ * 0 for an invalid description.  Its first int32 is a status word as elsewhere (zero it once); the rest need not be
+ * zeroed.  One workspace serves one call at a time, calls on one stream in turn. */
+size_t wkv_paged_workspace_bytes(const wkv_paged *c);
+
+/*
+ * New tokens into the cache: keys (turned by `rope` if given) and values go to rows lengths[b][h] .. of their unit, queries are
+ * turned into q_out.
+ *   k_new, v_new   DEVICE  [B, H_kv, max_new, d] or packed, element (b, h, i, c) at x[i*kv_strides[2] + b*kv_strides[0] +
+ *                  h*kv_strides[1] + c], packed x[(off_b + i)*kv_strides[2] + h*kv_strides[1] + c]; HOST array, for both
+ *   q, q_out       DEVICE or both NULL; q_strides for both; q_out may be q
+ *   positions      DEVICE int32 [T] or [B, max_new]: positions of the new tokens; NULL only without `rope` and row_positions
+ *   lengths        DEVICE int32 [B, H_kv]: rows of every unit before the call
+ *   lengths_out    DEVICE out or NULL, int32 [B, H_kv]: lengths plus new tokens; not `lengths` itself
+ *   row_positions  DEVICE out or NULL, int32 [B, H_kv, max_pages*page_size]: the new rows' positions
+ *   row_weights    DEVICE out or NULL, float [same]: 0 for the new rows
+ * Rows behind max_pages*page_size are dropped (and lengths_out ends there).
+ */
+int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_new, const void *v_new,
+                        const int64_t *kv_strides, const void *q, void *q_out, const int64_t *q_strides,
+                        const int32_t *positions, const int32_t *lengths, void *k_pool, void *v_pool, int32_t *lengths_out,
+                        int32_t *row_positions, float *row_weights, void *cuda_stream);
+
+/*
+ * Attention of the new tokens over the cache, their own rows (the last ones) included: with n = lengths[b][h] rows and m new tokens,
+ * query i attends to rows 0 .. n - m + i of its unit.  A query that has no row to attend to gives 0 and -infinity.
+ *   q, out         DEVICE  [B, H_q, max_new, d] or packed [T, H_q, d], strides as for q above
+ *   lengths        DEVICE int32 [B, H_kv]: rows of every unit, new tokens included
+ *   lse            DEVICE out or NULL, float [B, H_q, max_new]; entries behind a sequence's new tokens are not written
+ *   weights_in     DEVICE or NULL (then zeros), float [B, H_kv, max_pages*page_size]
+ *   weights_out    DEVICE out or NULL, float [same]: weights_in plus the weight that the row has received from the new tokens of all
+ *                  query heads of its group (the sum of the softmax entries of its column); may be weights_in; entries from
+ *                  the unit's length on are not written
+ * What stands in rows that a query does not attend to does not reach it.  head_dim up to 256.
+ */
+int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides, const void *k_pool, const void *v_pool,
+                     const int32_t *lengths, void *out, const int64_t *out_strides, float *lse, const float *weights_in,
+                     float *weights_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Rows leave the cache by the weight they have received, for all layers of a group, which share the block table and the rows'
+ * state as they share their indices (section 2.2.2): of a unit's n rows the first keep = min(n, budget) stay, in the order (position
+ * > newest position - recent first, weight from high to low, row from low to high); a NaN weight is the lowest.  The i-th
+ * row that leaves in front of row `keep` takes over the i-th that stays behind it, so that rows 0 .. keep-1 are those that
+ * stay and only rows that change places are moved.  Their order is then no longer that of their positions: attention does not ask for it.
+ *   k_pools, v_pools   HOST arrays [n_layers] of DEVICE pool pointers, read and written; v_pools may be NULL
+ *   budget             rows kept per unit, >= 0;  budgets: DEVICE int32 [B] or NULL: per sequence instead
+ *   recent             >= 0
+ *   weights, positions DEVICE [B, H_kv, max_pages*page_size] as wkv_attend_paged and wkv_append_kv_paged write them
+ *   lengths            DEVICE int32 [B, H_kv]
+ *   weights_out, positions_out, lengths_out   DEVICE out; each may be its input.  Entries from row `keep` on are not written
+ * Rows in pages that are no pages keep their place in the order, their K and V are not moved.
+ */
+int wkv_evict_kv_paged(const wkv_paged *c, int32_t n_layers, void *const *k_pools, void *const *v_pools, int32_t budget,
+                       const int32_t *budgets, int32_t recent, const float *weights, const int32_t *positions,
+                       const int32_t *lengths, float *weights_out, int32_t *positions_out, int32_t *lengths_out,
+                       void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * The rows' state behind wkv_gather_kv / wkv_gather_kv_paged: for each retained row of a unit, in the compact cache's order,
+ *   positions     DEVICE out or NULL, int32 [B, H_kv, row_capacity]: its place in the prompt
+ *   weights       DEVICE out or NULL, float [same]: its token score (Eq. 2), 0 for the observation rows and without token_scores
+ * window_idx as written by the selection; token_scores: DEVICE [B, H_kv, max(1, max_seqlen - alpha)] as written by
+ * wkv_score_windows, or NULL.  row_capacity >= wkv_keep_max().  Rows from kept_len on are not written.
+ */
+int wkv_seed_rows(const wkv_shape *s, const int32_t *window_idx, const float *token_scores, int32_t row_capacity,
+                  int32_t *positions, float *weights, void *cuda_stream);
+
+/*
  * Measurement aid (no counterpart in the paper): launches a kernel that does nothing but evaluate
  * ex2.approx.ftz.f32 (the exponential of Eq. 1 in base 2, the instruction that bounds the score
  * stage) in eight independent chains per thread, `iters` times.  Timing the launch with CUDA events

@@ -27,7 +27,8 @@ EXPORTED_SYMBOLS = [
     "wkv_workspace_bytes", "wkv_score_windows", "wkv_score_windows_static", "wkv_select_topk_windows", "wkv_gather_kv", "wkv_gather_kv_paged", "wkv_compact_kv_inplace",
     "wkv_compress_group", "wkv_compress_group_host", "wkv_compress_group_host_rows", "wkv_score_windows_lse", "wkv_compress_group_lse",
     "wkv_select_leader_windows", "wkv_probe_ex2_rate", "wkv_probe_colsum_rate", "wkv_probe_published_select", "wkv_probe_impatient_select", "wkv_group_plan_create", "wkv_group_plan_launch", "wkv_group_plan_destroy", "wkv_status_string", "wkv_last_error_detail",
-    "wkv_launch_count",
+    "wkv_launch_count", "wkv_rope_frequencies", "wkv_rotate_prompt", "wkv_attend_prompt", "wkv_paged_workspace_bytes", "wkv_append_kv_paged",
+    "wkv_attend_paged", "wkv_evict_kv_paged", "wkv_seed_rows",
 ]
 
 
@@ -58,6 +59,40 @@ class WkvShape(ctypes.Structure):
         ("q_stride_b", ctypes.c_int64),
         ("q_stride_h", ctypes.c_int64),
         ("q_stride_t", ctypes.c_int64),
+    ]
+
+
+class WkvRope(ctypes.Structure):
+    """Mirror of `wkv_rope`."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("rot_dim", ctypes.c_int32),
+        ("order", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("turns", ctypes.c_void_p),
+    ]
+
+
+class WkvPaged(ctypes.Structure):
+    """Mirror of `wkv_paged`."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("max_new", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("reserved", ctypes.c_int32 * 2),
+        ("cu_new_host", ctypes.c_void_p),
+        ("cu_new_dev", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
     ]
 
 
@@ -144,6 +179,23 @@ def lib() -> ctypes.CDLL:
     L.wkv_last_error_detail.argtypes = []
     L.wkv_launch_count.restype = ctypes.c_uint64
     L.wkv_launch_count.argtypes = []
+    dbl, rp, pp = ctypes.c_double, ctypes.POINTER(WkvRope), ctypes.POINTER(WkvPaged)
+    L.wkv_rope_frequencies.restype = ctypes.c_int
+    L.wkv_rope_frequencies.argtypes = [i32, dbl, i32, dbl, dbl, dbl, dbl, vp]
+    L.wkv_rotate_prompt.restype = ctypes.c_int
+    L.wkv_rotate_prompt.argtypes = [sp, rp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_attend_prompt.restype = ctypes.c_int
+    L.wkv_attend_prompt.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_paged_workspace_bytes.restype = sz
+    L.wkv_paged_workspace_bytes.argtypes = [pp]
+    L.wkv_append_kv_paged.restype = ctypes.c_int
+    L.wkv_append_kv_paged.argtypes = [pp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_attend_paged.restype = ctypes.c_int
+    L.wkv_attend_paged.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.wkv_evict_kv_paged.restype = ctypes.c_int
+    L.wkv_evict_kv_paged.argtypes = [pp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.wkv_seed_rows.restype = ctypes.c_int
+    L.wkv_seed_rows.argtypes = [sp, vp, vp, i32, vp, vp, vp]
     _lib = L
     return L
 
@@ -506,6 +558,250 @@ def wkv_compress_group_host(prob: Problem, q_obs_host, k_layers_host, v_layers_h
         _ptr_array(v_layers_dev), _ptr_array(k_out_dev), _ptr_array(v_out_dev), _ptr(window_idx_dev),
         _ptr(kept_len_dev), keep_capacity, _ptr(workspace), workspace.numel(), _stream(stream)),
         "wkv_compress_group_host")
+
+
+# ---- around the selection: rotary positions, the prompt's attention, the paged cache in use ----
+WKV_ROPE_HALF, WKV_ROPE_INTERLEAVED = 0, 1
+_ROPE_ORDERS = {"half": WKV_ROPE_HALF, "interleaved": WKV_ROPE_INTERLEAVED}
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+def wkv_rope_frequencies(rot_dim: int, base: float, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
+                         low: float = 1.0, high: float = 4.0) -> np.ndarray:
+    """Angle per position of every rotated pair, in turns of 2^-64 (host arithmetic): uint64 [rot_dim / 2]."""
+    out = np.zeros(max(rot_dim // 2, 1), dtype=np.uint64)
+    _check(lib().wkv_rope_frequencies(rot_dim, base, _ROPE_SCALINGS[scaling], factor, original_length, low, high, out.ctypes.data),
+           "wkv_rope_frequencies")
+    return out
+
+
+class Rope:
+    """A `wkv_rope` with its table on the device (kept alive here)."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, *, order: str = "half", scaling: str = "none", factor: float = 1.0,
+                 original_length: float = 0.0, low: float = 1.0, high: float = 4.0, scale: float = 1.0, device=None):
+        import torch
+        self.turns_host = wkv_rope_frequencies(rot_dim, base, scaling, factor, original_length, low, high)
+        self.device = device if device is not None else torch.device("cuda", torch.cuda.current_device())
+        self.turns = torch.from_numpy(self.turns_host.view(np.int64)).to(self.device)
+        self.struct = WkvRope(ctypes.sizeof(WkvRope), rot_dim, _ROPE_ORDERS[order], scale, self.turns.data_ptr())
+
+
+class PagedCache:
+    """A `wkv_paged` together with the arrays it points to (kept alive here).  `layout`: "phsd" for pools [pages, H_kv, page_size, d],
+    "pshd" for [pages, page_size, H_kv, d]; or (page, head, row) strides in elements."""
+
+    def __init__(self, *, dtype: str, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, page_size: int, num_pages: int,
+                 block_table, max_new: int = 1, cu_new: Optional[Sequence[int]] = None, layout="phsd"):
+        import torch
+        self.dtype = dtype
+        self.torch_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
+        self.device = block_table.device
+        if block_table.dtype != torch.int32 or not block_table.is_contiguous() or block_table.dim() != 2 or block_table.shape[0] != batch:
+            raise ValueError("block_table: contiguous int32 [batch, max_pages]")
+        self.block_table = block_table
+        s = WkvPaged()
+        s.struct_size = ctypes.sizeof(WkvPaged)
+        s.dtype = WKV_F32 if dtype == "f32" else WKV_BF16
+        s.batch, s.n_q_heads, s.n_kv_heads, s.head_dim = batch, n_q_heads, n_kv_heads, head_dim
+        s.max_new, s.page_size, s.num_pages, s.max_pages = max_new, page_size, num_pages, block_table.shape[1]
+        s.block_table = block_table.data_ptr()
+        if layout == "phsd":
+            s.page_stride, s.head_stride, s.row_stride = n_kv_heads * page_size * head_dim, page_size * head_dim, head_dim
+        elif layout == "pshd":
+            s.page_stride, s.head_stride, s.row_stride = n_kv_heads * page_size * head_dim, head_dim, n_kv_heads * head_dim
+        else:
+            s.page_stride, s.head_stride, s.row_stride = layout
+        self.packed = cu_new is not None
+        self.cu_host = self.cu_dev = None
+        if self.packed:
+            self.cu_host = np.ascontiguousarray(cu_new, dtype=np.int32)
+            if len(self.cu_host) != batch + 1:
+                raise ValueError("cu_new: batch + 1 entries")
+            self.cu_dev = torch.from_numpy(self.cu_host).to(self.device)
+            s.cu_new_host, s.cu_new_dev = self.cu_host.ctypes.data, self.cu_dev.data_ptr()
+        self.shape = s
+        self.capacity = page_size * block_table.shape[1]
+        self.workspace_bytes = lib().wkv_paged_workspace_bytes(ctypes.byref(s))
+        if self.workspace_bytes == 0:
+            raise WkvError(-1, "wkv_paged", lib().wkv_last_error_detail().decode())
+
+    def alloc_workspace(self):
+        """Scratch; its first int32 is the device status word (see `device_status`)."""
+        import torch
+        ws = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+        ws[:256].zero_()
+        return ws
+
+
+def _head_strides(t, packed: bool, what: str):
+    """Element strides (batch, head, token) of [B, heads, tokens, d] or packed [T, heads, d], as a C array."""
+    if t is None:
+        return None
+    if t.dim() != (3 if packed else 4) or t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError(f"{what}: {'packed [T, heads, d]' if packed else '[B, heads, tokens, d]'} with contiguous rows expected")
+    st = t.stride()
+    return (ctypes.c_int64 * 3)(*((0, st[1], st[0]) if packed else st[:3]))
+
+
+def _check_heads(t, heads: int, prob_dtype, head_dim: int, packed: bool, batch: int, tokens: int, what: str) -> None:
+    """Shape and type of a [B, heads, tokens, d] or packed [T, heads, d] tensor: the C side sees an address and strides only."""
+    want = (tokens, heads, head_dim) if packed else (batch, heads, tokens, head_dim)
+    if tuple(t.shape) != want or t.dtype != prob_dtype:
+        raise ValueError(f"{what}: {want} of {prob_dtype} expected, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _check_state(t, shape, dtype: str, what: str) -> None:
+    """A contiguous tensor of the expected shape and type (or None)."""
+    if t is not None and (tuple(t.shape) != tuple(shape) or str(t.dtype) != "torch." + dtype or not t.is_contiguous()):
+        raise ValueError(f"{what}: contiguous {tuple(shape)} of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _check_same_layout(a, b, what: str) -> None:
+    if a is not None and b is not None and (a.stride() != b.stride() or a.shape != b.shape):
+        raise ValueError(f"{what}: both need the same shape and strides")
+
+
+def _check_kv_layout(prob: "Problem", t, what: str) -> None:
+    """Keys or values in the layout that the problem describes."""
+    s = prob.shape
+    if t.dtype != prob.torch_dtype or t.shape[-1] != s.head_dim or t.stride(-1) != 1 and s.head_dim != 1:
+        raise ValueError(f"{what}: rows of {s.head_dim} {prob.torch_dtype} expected")
+
+
+def prepare_rotate_prompt(prob: Problem, rope: Rope, q, k, q_out, k_out, positions=None, stream=None) -> PreparedCall:
+    """Rotary positions of a prompt: q, q_out [B, H_q, N, d] (any strides) or packed [T, H_q, d]; k, k_out in the problem's layout.
+    Either pair may be None; an output may be its input."""
+    s = prob.shape
+    tokens = int(prob.cu_host[-1]) if prob.packed else s.max_seqlen
+    for t, what in ((q, "q"), (q_out, "q_out")):
+        if t is not None:
+            _check_heads(t, s.n_q_heads, prob.torch_dtype, s.head_dim, prob.packed, s.batch, tokens, what)
+    _check_same_layout(q, q_out, "q and q_out")
+    for t, what in ((k, "k"), (k_out, "k_out")):
+        if t is not None:
+            _check_kv_layout(prob, t, what)
+    _check_state(positions, (tokens,) if prob.packed else (s.batch, s.max_seqlen), "int32", "positions")
+    qs = _head_strides(q, prob.packed, "q")
+    args = (ctypes.byref(s), ctypes.byref(rope.struct), _ptr(q), _ptr(q_out), qs, _ptr(k), _ptr(k_out), _ptr(positions), _stream(stream))
+    return PreparedCall(lib().wkv_rotate_prompt, "wkv_rotate_prompt", args, (prob, rope, q, q_out, qs, k, k_out, positions))
+
+
+def wkv_rotate_prompt(prob: Problem, rope: Rope, q, k, q_out, k_out, positions=None, stream=None) -> None:
+    prepare_rotate_prompt(prob, rope, q, k, q_out, k_out, positions, stream).run()
+
+
+def prepare_attend_prompt(prob: Problem, q, k, v, out, lse=None, lse_obs=None, status=None, stream=None) -> PreparedCall:
+    """Causal attention of whole prompts: q, out [B, H_q, N, d] (any strides) or packed [T, H_q, d]; k, v in the problem's layout;
+    lse float [B, H_q, max_seqlen], lse_obs float [B, H_q, alpha] as the _lse calls take it; status int32 [1]."""
+    s = prob.shape
+    tokens = int(prob.cu_host[-1]) if prob.packed else s.max_seqlen
+    for t, what in ((q, "q"), (out, "out")):
+        _check_heads(t, s.n_q_heads, prob.torch_dtype, s.head_dim, prob.packed, s.batch, tokens, what)
+    for t, what in ((k, "k"), (v, "v")):
+        _check_kv_layout(prob, t, what)
+    _check_state(lse, (s.batch, s.n_q_heads, s.max_seqlen), "float32", "lse")
+    _check_state(lse_obs, (s.batch, s.n_q_heads, s.l_obs), "float32", "lse_obs")
+    qs, os_ = _head_strides(q, prob.packed, "q"), _head_strides(out, prob.packed, "out")
+    args = (ctypes.byref(s), _ptr(q), qs, _ptr(k), _ptr(v), _ptr(out), os_, _ptr(lse), _ptr(lse_obs), _ptr(status), _stream(stream))
+    return PreparedCall(lib().wkv_attend_prompt, "wkv_attend_prompt", args, (prob, q, qs, k, v, out, os_, lse, lse_obs, status))
+
+
+def wkv_attend_prompt(prob: Problem, q, k, v, out, lse=None, lse_obs=None, status=None, stream=None) -> None:
+    prepare_attend_prompt(prob, q, k, v, out, lse, lse_obs, status, stream).run()
+
+
+def _chunk_tokens(cache: PagedCache) -> int:
+    return int(cache.cu_host[-1]) if cache.packed else cache.shape.max_new
+
+
+def prepare_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_pool, q=None, q_out=None, positions=None, rope=None,
+                            lengths_out=None, row_positions=None, row_weights=None, stream=None) -> PreparedCall:
+    """New tokens into the cache, behind lengths[b, h] rows: k_new, v_new [B, H_kv, max_new, d] or packed [T, H_kv, d] (same strides);
+    q likewise, turned into q_out; positions int32 [B, max_new] or [T]."""
+    s, tokens = cache.shape, _chunk_tokens(cache)
+    for t, heads, what in ((k_new, s.n_kv_heads, "k_new"), (v_new, s.n_kv_heads, "v_new"), (q, s.n_q_heads, "q"), (q_out, s.n_q_heads, "q_out")):
+        if t is not None:
+            _check_heads(t, heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
+    _check_same_layout(k_new, v_new, "k_new and v_new")
+    _check_same_layout(q, q_out, "q and q_out")
+    units = (s.batch, s.n_kv_heads)
+    _check_state(lengths, units, "int32", "lengths")
+    _check_state(lengths_out, units, "int32", "lengths_out")
+    _check_state(row_positions, units + (cache.capacity,), "int32", "row_positions")
+    _check_state(row_weights, units + (cache.capacity,), "float32", "row_weights")
+    _check_state(positions, (tokens,) if cache.packed else (s.batch, s.max_new), "int32", "positions")
+    ks, qs = _head_strides(k_new, cache.packed, "k_new"), _head_strides(q, cache.packed, "q")
+    args = (ctypes.byref(s), ctypes.byref(rope.struct) if rope is not None else None, _ptr(k_new), _ptr(v_new), ks, _ptr(q), _ptr(q_out), qs,
+            _ptr(positions), _ptr(lengths), _ptr(k_pool), _ptr(v_pool), _ptr(lengths_out), _ptr(row_positions), _ptr(row_weights),
+            _stream(stream))
+    return PreparedCall(lib().wkv_append_kv_paged, "wkv_append_kv_paged", args,
+                        (cache, rope, k_new, v_new, ks, q, q_out, qs, positions, lengths, k_pool, v_pool, lengths_out, row_positions,
+                         row_weights))
+
+
+def wkv_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_pool, **kw) -> None:
+    prepare_append_kv_paged(cache, k_new, v_new, lengths, k_pool, v_pool, **kw).run()
+
+
+def prepare_attend_paged(cache: PagedCache, q, k_pool, v_pool, lengths, out, workspace, lse=None, weights_in=None, weights_out=None,
+                         stream=None) -> PreparedCall:
+    """Attention of the new tokens over the cache (their own rows, the last of lengths[b, h], included): q, out [B, H_q, max_new, d]
+    or packed [T, H_q, d]; lse float [B, H_q, max_new]; weights float [B, H_kv, capacity], weights_out may be weights_in."""
+    s, tokens = cache.shape, _chunk_tokens(cache)
+    for t, what in ((q, "q"), (out, "out")):
+        _check_heads(t, s.n_q_heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
+    units = (s.batch, s.n_kv_heads)
+    _check_state(lengths, units, "int32", "lengths")
+    _check_state(lse, (s.batch, s.n_q_heads, s.max_new), "float32", "lse")
+    _check_state(weights_in, units + (cache.capacity,), "float32", "weights_in")
+    _check_state(weights_out, units + (cache.capacity,), "float32", "weights_out")
+    qs, os_ = _head_strides(q, cache.packed, "q"), _head_strides(out, cache.packed, "out")
+    args = (ctypes.byref(s), _ptr(q), qs, _ptr(k_pool), _ptr(v_pool), _ptr(lengths), _ptr(out), os_, _ptr(lse), _ptr(weights_in),
+            _ptr(weights_out), _ptr(workspace), workspace.numel(), _stream(stream))
+    return PreparedCall(lib().wkv_attend_paged, "wkv_attend_paged", args,
+                        (cache, q, qs, k_pool, v_pool, lengths, out, os_, lse, weights_in, weights_out, workspace))
+
+
+def wkv_attend_paged(cache: PagedCache, q, k_pool, v_pool, lengths, out, workspace, **kw) -> None:
+    prepare_attend_paged(cache, q, k_pool, v_pool, lengths, out, workspace, **kw).run()
+
+
+def prepare_evict_kv_paged(cache: PagedCache, k_pools, v_pools, weights, positions, lengths, budget: int, recent: int, weights_out,
+                           positions_out, lengths_out, workspace, budgets=None, stream=None) -> PreparedCall:
+    """Rows of least weight leave the cache, for all layers given; outputs may be their inputs.  budgets: int32 [B] on the device."""
+    s = cache.shape
+    units = (s.batch, s.n_kv_heads)
+    for t, what in ((weights, "weights"), (weights_out, "weights_out")):
+        _check_state(t, units + (cache.capacity,), "float32", what)
+    for t, what in ((positions, "positions"), (positions_out, "positions_out")):
+        _check_state(t, units + (cache.capacity,), "int32", what)
+    for t, what in ((lengths, "lengths"), (lengths_out, "lengths_out")):
+        _check_state(t, units, "int32", what)
+    _check_state(budgets, (s.batch,), "int32", "budgets")
+    arrs = (_ptr_array(k_pools), _ptr_array(v_pools))
+    args = (ctypes.byref(s), len(k_pools), arrs[0], arrs[1], budget, _ptr(budgets), recent, _ptr(weights), _ptr(positions), _ptr(lengths),
+            _ptr(weights_out), _ptr(positions_out), _ptr(lengths_out), _ptr(workspace), workspace.numel(), _stream(stream))
+    return PreparedCall(lib().wkv_evict_kv_paged, "wkv_evict_kv_paged", args,
+                        (cache, arrs, k_pools, v_pools, weights, positions, lengths, weights_out, positions_out, lengths_out, workspace,
+                         budgets))
+
+
+def wkv_evict_kv_paged(cache: PagedCache, k_pools, v_pools, weights, positions, lengths, budget: int, recent: int, weights_out,
+                       positions_out, lengths_out, workspace, budgets=None, stream=None) -> None:
+    prepare_evict_kv_paged(cache, k_pools, v_pools, weights, positions, lengths, budget, recent, weights_out, positions_out, lengths_out,
+                           workspace, budgets, stream).run()
+
+
+def wkv_seed_rows(prob: Problem, window_idx, token_scores, positions, weights, stream=None) -> None:
+    """The rows' state behind a gather: positions int32 and weights float [B, H_kv, row_capacity] (either may be None)."""
+    capacity = (positions if positions is not None else weights).shape[-1]
+    units = (prob.shape.batch, prob.shape.n_kv_heads)
+    _check_state(positions, units + (capacity,), "int32", "positions")
+    _check_state(weights, units + (capacity,), "float32", "weights")
+    _check_state(token_scores, units + (prob.nr_max,), "float32", "token_scores")
+    _check(lib().wkv_seed_rows(ctypes.byref(prob.shape), _ptr(window_idx), _ptr(token_scores), capacity, _ptr(positions), _ptr(weights),
+                               _stream(stream)), "wkv_seed_rows")
 
 
 def wkv_keep_len(n: int, alpha: int, omega: int, budget: int):

@@ -6,8 +6,11 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -16,7 +19,7 @@ LIB = os.path.join(PKG, "libwkv.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+    "-Xcompiler", "-fPIC",
 ]
 
 
@@ -40,13 +43,23 @@ def _stale() -> bool:
 def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [_nvcc()] + NVCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    flags = [_nvcc()] + NVCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += ["-o", tmp] + sources() + ["-ldl"]
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+        flags += ["-Xptxas", "-v"]
+    # one compiler per source, as many at a time as there are cores
+    objects = tempfile.mkdtemp(prefix="wkv-build-")
+    try:
+        def compile_one(src: str) -> str:
+            obj = os.path.join(objects, os.path.basename(src) + ".o")
+            subprocess.check_call(flags + ["-c", "-o", obj, src])
+            return obj
+        with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as pool:
+            objs = list(pool.map(compile_one, sources()))
+        tmp = LIB + f".tmp{os.getpid()}"
+        subprocess.check_call([_nvcc()] + NVCC_FLAGS[:2] + ["-shared", "-cudart", "static", "-o", tmp] + objs + ["-ldl"])
+        os.replace(tmp, LIB)
+    finally:
+        shutil.rmtree(objects, ignore_errors=True)
     return LIB
 
 

@@ -1,0 +1,400 @@
+// Attention on the CUDA cores: fp32 inputs, and the shapes that the tensor-core kernels do not take.  One block holds ROWS rows
+// of one unit in shared memory and walks over the unit's keys in tiles of 64 with a running maximum and sum per row;
+// everything is fp32, products in plain multiply-adds.
+//
+// With S key splits a block walks over one of S parts of the keys and leaves (maximum, sum, unnormalised output) per row for
+// the joining kernel.  A row's sums are taken in one order whatever else the launch holds, so results do not depend
+// on the other sequences of a batch.
+#include "attn.cuh"
+
+namespace wkv {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kKeys = 64;
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_float(float &y, float x) { y = x; }
+__device__ __forceinline__ void from_float(__nv_bfloat16 &y, float x) { y = __float2bfloat16_rn(x); }
+
+// one row of d elements into shared memory as fp32, zero from d to DP; `p` null: zeros.  16-byte vectors, lanes of a row together.
+template <typename T, int DP>
+__device__ __forceinline__ void load_row_part(float *dst, const T *p, int d, int part)
+{
+    constexpr int kVec = 16 / sizeof(T);
+    const int c = part * kVec;
+    float x[kVec];
+    if (p && c < d) {
+        const int4 raw = *reinterpret_cast<const int4 *>(p + c);
+        const T *e = reinterpret_cast<const T *>(&raw);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = to_float(e[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; i += 4) *reinterpret_cast<float4 *>(dst + c + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+}
+
+template <int DP, int ROWS>
+struct SimtSmem {
+    float q[ROWS][DP + 4];
+    float k[kKeys][DP + 4];
+    float v[kKeys][DP];
+    float p[ROWS][kKeys + 4];
+    int present[kKeys];       // the key's page is one
+};
+
+// the keys (and values) of one tile; rows from n on and rows without a page are zeros
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ void load_keys(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int b, int h, long long off, int n, int j0, bool values)
+{
+    constexpr int kVec = 16 / sizeof(T), kParts = DP / kVec;
+    for (int x = threadIdx.x; x < kKeys * kParts; x += kThreads) {
+        const int r = x / kParts, part = x - r * kParts, j = j0 + r;
+        const long long at = j < n ? attn_row(a, b, h, off, j) : -1;
+        load_row_part<T, DP>(sm.k[r], at >= 0 ? static_cast<const T *>(a.k) + at : nullptr, a.d, part);
+        if (values) load_row_part<T, DP>(sm.v[r], at >= 0 ? static_cast<const T *>(a.v) + at : nullptr, a.d, part);
+        if (part == 0) sm.present[r] = at >= 0;
+    }
+}
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ void load_queries(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int b, int h, long long off, int row0, int rows)
+{
+    constexpr int kVec = 16 / sizeof(T), kParts = DP / kVec;
+    for (int x = threadIdx.x; x < ROWS * kParts; x += kThreads) {
+        const int r = x / kParts, part = x - r * kParts, row = row0 + r, i = row / a.G, g = row - i * a.G;
+        const T *p = row < rows ? static_cast<const T *>(a.q) + (off + i) * a.qt + b * a.qb + (long long)(h * a.G + g) * a.qh : nullptr;
+        load_row_part<T, DP>(sm.q[r], p, a.d, part);
+    }
+}
+// logits (base 2) of rows ty*RT.. against keys tx + 16 j
+template <int DP, int ROWS>
+__device__ __forceinline__ void logits(const SimtSmem<DP, ROWS> &sm, int ty, int tx, float c, float (&s)[ROWS / 16][4])
+{
+    constexpr int RT = ROWS / 16;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[r][j] = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < DP; e += 4) {
+        float4 qv[RT], kv[4];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) qv[r] = *reinterpret_cast<const float4 *>(&sm.q[ty * RT + r][e]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4 *>(&sm.k[tx + 16 * j][e]);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[r][j] = fmaf(qv[r].x, kv[j].x, s[r][j]);
+                s[r][j] = fmaf(qv[r].y, kv[j].y, s[r][j]);
+                s[r][j] = fmaf(qv[r].z, kv[j].z, s[r][j]);
+                s[r][j] = fmaf(qv[r].w, kv[j].w, s[r][j]);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[r][j] *= c;
+}
+
+template <typename T, int DP, int ROWS>
+__global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_constant__ AttnArgs a)
+{
+    extern __shared__ __align__(16) unsigned char raw[];
+    SimtSmem<DP, ROWS> &sm = *reinterpret_cast<SimtSmem<DP, ROWS> *>(raw);
+    constexpr int RT = ROWS / 16, CT = DP / 64;
+    pdl_trigger();
+    pdl_wait();
+    const int units = a.batch * a.hkv;
+    // the last rows of a prompt have the most keys: they are taken first
+    const int tiles = (int)gridDim.x / units, unit = (int)blockIdx.x % units, tile = tiles - 1 - (int)blockIdx.x / units;
+    const int b = unit / a.hkv, h = unit - b * a.hkv;
+    const AttnSeq sq = attn_seq(a, b, h);
+    const int rows = sq.m * a.G, row0 = tile * ROWS;
+    if (row0 >= rows) return;
+    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+    const int base = sq.n - sq.m + 1;                                    // keys that query 0 attends to (may be negative)
+    const int most = min(base + (min(row0 + ROWS, rows) - 1) / a.G, sq.n);
+    const int all_tiles = (max(most, 0) + kKeys - 1) / kKeys;
+    const int split = blockIdx.y;
+    const int t0 = (int)((long long)all_tiles * split / a.splits), t1 = (int)((long long)all_tiles * (split + 1) / a.splits);
+    int limit[RT];
+    float m[RT], l[RT];
+    float4 o[RT][CT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        limit[r] = base + (row0 + ty * RT + r) / a.G;
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int x = 0; x < CT; ++x) o[r][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    load_queries<T, DP, ROWS>(a, sm, b, h, sq.q_off, row0, rows);
+    const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
+    for (int t = t0; t < t1; ++t) {
+        const int j0 = t * kKeys;
+        load_keys<T, DP, ROWS>(a, sm, b, h, sq.q_off, sq.n, j0, true);
+        __syncthreads();
+        float s[RT][4];
+        logits<DP, ROWS>(sm, ty, tx, a.scale_log2, s);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = m[r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j0 + tx + 16 * j >= limit[r] || !sm.present[tx + 16 * j]) s[r][j] = -INFINITY;
+                top = fmaxf(top, s[r][j]);
+            }
+#pragma unroll
+            for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            const float ref = top == -INFINITY ? 0.f : top;              // nothing to attend to so far
+            const float keep = exp2f(m[r] - ref);
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float p = exp2f(s[r][j] - ref);
+                sm.p[ty * RT + r][tx + 16 * j] = p;
+                sum += p;
+            }
+#pragma unroll
+            for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+            l[r] = l[r] * keep + sum;
+            m[r] = top;
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                o[r][x].x *= keep;
+                o[r][x].y *= keep;
+                o[r][x].z *= keep;
+                o[r][x].w *= keep;
+            }
+        }
+        __syncwarp();                                                    // a row's 16 threads are in one warp
+        const bool guarded = j0 + kKeys > plain;
+#pragma unroll 4
+        for (int j = 0; j < kKeys; ++j) {
+            float4 vv[CT];
+#pragma unroll
+            for (int x = 0; x < CT; ++x) vv[x] = *reinterpret_cast<const float4 *>(&sm.v[j][tx * 4 + 64 * x]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float p = sm.p[ty * RT + r][j];
+                // what stands behind a row's position may be infinite or NaN: 0 times it is not 0
+                if (guarded && p == 0.f) continue;
+#pragma unroll
+                for (int x = 0; x < CT; ++x) {
+                    o[r][x].x = fmaf(p, vv[x].x, o[r][x].x);
+                    o[r][x].y = fmaf(p, vv[x].y, o[r][x].y);
+                    o[r][x].z = fmaf(p, vv[x].z, o[r][x].z);
+                    o[r][x].w = fmaf(p, vv[x].w, o[r][x].w);
+                }
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = row0 + ty * RT + r;
+        if (row >= rows) continue;
+        const int i = row / a.G, hq = h * a.G + row - i * a.G;
+        if (a.splits > 1) {
+            const long long at = ((long long)unit * a.rows_max + row) * a.splits + split;
+            if (tx == 0) a.part_ml[at] = make_float2(m[r], l[r]);
+#pragma unroll
+            for (int x = 0; x < CT; ++x) {
+                const int c = tx * 4 + 64 * x;
+                if (c < a.d) *reinterpret_cast<float4 *>(a.part_o + at * a.d + c) = o[r][x];
+            }
+            continue;
+        }
+        if (tx == 0) attn_store_lse(a, b, hq, i, sq.m, l[r] > 0.f || l[r] != l[r] ? m[r] + log2f(l[r]) : -INFINITY);
+        const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+        T *dst = static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh;
+#pragma unroll
+        for (int x = 0; x < CT; ++x) {
+            const int c = tx * 4 + 64 * x;
+            if (c >= a.d) continue;
+            T y[4];
+            from_float(y[0], o[r][x].x * inv);
+            from_float(y[1], o[r][x].y * inv);
+            from_float(y[2], o[r][x].z * inv);
+            from_float(y[3], o[r][x].w * inv);
+            if (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst + c) = *reinterpret_cast<float4 *>(y);
+            else *reinterpret_cast<uint2 *>(dst + c) = *reinterpret_cast<uint2 *>(y);
+        }
+    }
+}
+
+// Weights that the rows of the cache receive: one block per 64 rows of a unit sums exp2(logit - lse) over all of the unit's
+// queries.  The logits are computed once more, from the normalisers that the attention has written; sums in a fixed order.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr int ROWS = 64, RT = ROWS / 16;
+    extern __shared__ __align__(16) unsigned char raw[];
+    SimtSmem<DP, ROWS> &sm = *reinterpret_cast<SimtSmem<DP, ROWS> *>(raw);
+    pdl_trigger();
+    pdl_wait();
+    const int units = a.batch * a.hkv, unit = (int)blockIdx.x % units, j0 = (int)blockIdx.x / units * kKeys;
+    const int b = unit / a.hkv, h = unit - b * a.hkv;
+    const AttnSeq sq = attn_seq(a, b, h);
+    if (j0 >= sq.n) return;
+    const int rows = sq.m * a.G, base = sq.n - sq.m + 1;
+    const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+    load_keys<T, DP, ROWS>(a, sm, b, h, sq.q_off, sq.n, j0, false);
+    float got[4] = {0.f, 0.f, 0.f, 0.f};
+    // queries in front of the tile's first key do not attend to any of it
+    const long long first = base > j0 ? 0 : (long long)(j0 - base + 1) * a.G;
+    for (int row0 = (int)(first / ROWS * ROWS); row0 < rows; row0 += ROWS) {
+        __syncthreads();
+        load_queries<T, DP, ROWS>(a, sm, b, h, sq.q_off, row0, rows);
+        __syncthreads();
+        float s[RT][4];
+        logits<DP, ROWS>(sm, ty, tx, a.scale_log2, s);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int row = row0 + ty * RT + r, i = row / a.G, hq = h * a.G + row - i * a.G;
+            if (row >= rows) continue;
+            const float lse2 = a.lse[((long long)b * a.hq + hq) * a.max_q + i] * 1.44269504088896341f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j0 + tx + 16 * j < base + i && sm.present[tx + 16 * j]) got[j] += exp2f(s[r][j] - lse2);
+        }
+    }
+    __syncthreads();
+    float(*sums)[kKeys + 1] = reinterpret_cast<float(*)[kKeys + 1]>(&sm.p[0][0]);     // [16][65]
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[ty][tx + 16 * j] = got[j];
+    __syncthreads();
+    if (threadIdx.x < kKeys && j0 + (int)threadIdx.x < sq.n) {
+        float w = 0.f;
+#pragma unroll
+        for (int y = 0; y < 16; ++y) w += sums[y][threadIdx.x];
+        const long long at = (long long)unit * a.cap + j0 + threadIdx.x;
+        a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + w;
+    }
+}
+
+// Joins the parts of every row: o = sum exp2(m_s - M) o_s / sum exp2(m_s - M) l_s.  A warp per row, splits in order.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_constant__ AttnArgs a)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x % (a.batch * a.hkv), b = unit / a.hkv, h = unit - b * a.hkv;
+    const int lane = threadIdx.x & 31, row = (int)(blockIdx.x / (a.batch * a.hkv)) * (kThreads / 32) + (threadIdx.x >> 5);
+    const AttnSeq sq = attn_seq(a, b, h);
+    if (row >= sq.m * a.G) return;
+    const int i = row / a.G, hq = h * a.G + row - i * a.G;
+    const long long at = ((long long)unit * a.rows_max + row) * a.splits;
+    float top = -INFINITY;
+    for (int s = lane; s < a.splits; s += 32) top = fmaxf(top, a.part_ml[at + s].x);
+#pragma unroll
+    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float l = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = a.part_ml[at + s];
+        l += ml.y * exp2f(ml.x - ref);
+    }
+    if (lane == 0) attn_store_lse(a, b, hq, i, sq.m, l > 0.f || l != l ? top + log2f(l) : -INFINITY);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *dst = static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh;
+    for (int c = lane * 4; c < a.d; c += 128) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < a.splits; ++s) {
+            const float2 ml = a.part_ml[at + s];
+            if (ml.y == 0.f) continue;                                   // a part without a key of the row
+            const float w = exp2f(ml.x - ref);
+            const float4 p = *reinterpret_cast<const float4 *>(a.part_o + (at + s) * a.d + c);
+            o.x = fmaf(w, p.x, o.x);
+            o.y = fmaf(w, p.y, o.y);
+            o.z = fmaf(w, p.z, o.z);
+            o.w = fmaf(w, p.w, o.w);
+        }
+        T y[4];
+        from_float(y[0], o.x * inv);
+        from_float(y[1], o.y * inv);
+        from_float(y[2], o.z * inv);
+        from_float(y[3], o.w * inv);
+        if (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst + c) = *reinterpret_cast<float4 *>(y);
+        else *reinterpret_cast<uint2 *>(dst + c) = *reinterpret_cast<uint2 *>(y);
+    }
+}
+
+// -infinity where an observation row would lie in front of its sequence
+__global__ void lse_obs_fill_kernel(const __grid_constant__ AttnArgs a)
+{
+    pdl_trigger();
+    pdl_wait();
+    const long long x = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    if (x >= (long long)a.batch * a.hq * a.alpha) return;
+    const int i = (int)(x % a.alpha), b = (int)(x / ((long long)a.alpha * a.hq));
+    if (i < a.alpha - attn_seq(a, b, 0).m) a.lse_obs[x] = -INFINITY;
+}
+
+template <typename K>
+int launch(K kernel, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t stream, const char *what)
+{
+    cudaError_t err = smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    if (err == cudaSuccess) err = launch_pdl(kernel, grid, kThreads, smem, stream, 1, a);
+    if (err == cudaSuccess) count_launches(1);
+    return check_cuda(err, what);
+}
+template <typename T, int ROWS>
+int launch_rows(const AttnArgs &a, cudaStream_t stream)
+{
+    const long long tiles = ((long long)a.max_q * a.G + ROWS - 1) / ROWS, blocks = tiles * a.batch * a.hkv;
+    if (blocks > 0x7fffffffLL || a.splits > 65535) {
+        set_error_detail("attention: %lld blocks", blocks);
+        return WKV_ERR_LIMIT;
+    }
+    const dim3 grid((unsigned)blocks, a.splits);
+    if (a.d <= 64) return launch(attn_simt_kernel<T, 64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel");
+    if (a.d <= 128) return launch(attn_simt_kernel<T, 128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel");
+    return launch(attn_simt_kernel<T, 256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel");
+}
+template <typename T>
+int launch_weights(const AttnArgs &a, cudaStream_t stream)
+{
+    const long long blocks = ((long long)a.cap + kKeys - 1) / kKeys * a.batch * a.hkv;
+    if (blocks > 0x7fffffffLL) {
+        set_error_detail("attention weights: %lld blocks", blocks);
+        return WKV_ERR_LIMIT;
+    }
+    const dim3 grid((unsigned)blocks);
+    if (a.d <= 64) return launch(attn_weights_kernel<T, 64>, grid, sizeof(SimtSmem<64, 64>), a, stream, "attention weights kernel");
+    if (a.d <= 128) return launch(attn_weights_kernel<T, 128>, grid, sizeof(SimtSmem<128, 64>), a, stream, "attention weights kernel");
+    return launch(attn_weights_kernel<T, 256>, grid, sizeof(SimtSmem<256, 64>), a, stream, "attention weights kernel");
+}
+
+}  // namespace
+
+int launch_attn_simt(const AttnArgs &a, int dtype, cudaStream_t stream)
+{
+    const bool few = (long long)a.max_q * a.G <= 16;
+    if (dtype == WKV_F32) return few ? launch_rows<float, 16>(a, stream) : launch_rows<float, 64>(a, stream);
+    return few ? launch_rows<__nv_bfloat16, 16>(a, stream) : launch_rows<__nv_bfloat16, 64>(a, stream);
+}
+int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream)
+{
+    return dtype == WKV_F32 ? launch_weights<float>(a, stream) : launch_weights<__nv_bfloat16>(a, stream);
+}
+int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
+{
+    const long long per = kThreads / 32, blocks = ((long long)a.rows_max + per - 1) / per * a.batch * a.hkv;
+    const dim3 grid((unsigned)blocks);
+    return dtype == WKV_F32 ? launch(attn_join_kernel<float>, grid, 0, a, stream, "attention joining kernel")
+                            : launch(attn_join_kernel<__nv_bfloat16>, grid, 0, a, stream, "attention joining kernel");
+}
+int launch_attn_lse_obs_fill(const AttnArgs &a, cudaStream_t stream)
+{
+    const long long n = (long long)a.batch * a.hq * a.alpha;
+    return launch(lse_obs_fill_kernel, dim3((unsigned)((n + kThreads - 1) / kThreads)), 0, a, stream, "log-sum-exp fill kernel");
+}
+
+}  // namespace wkv

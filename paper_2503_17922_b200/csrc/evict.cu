@@ -1,0 +1,279 @@
+// Eviction from the paged cache by accumulated attention weight, and the state that it goes by.
+//
+// First kernel, a block per unit: rows get 32-bit keys in the order of eviction, the key of the keep-th is found by a radix
+// select of 8 bits per pass, and one walk over the rows lists those that leave in front of row `keep` and those that stay
+// behind it, pairwise.  Ties go to the lower row.
+// Second kernel: every listed row of every layer's K and V is copied over its counterpart.  Targets lie in front of row `keep`
+// and sources behind it, so the copies depend on nothing and a call repeated on the same lengths and weights does the same.
+#include "attn.cuh"
+#include "topk_block.cuh"
+
+namespace wkv {
+namespace {
+
+constexpr int kSelThreads = 1024;
+constexpr int kMoveThreads = 256;
+constexpr int kHeldKeys = 48 * 1024;        // keys that a block holds in shared memory (192 KB); longer lists are re-read
+
+struct SelectSmem {
+    int hist[256];
+    int warp_sums[2][32];
+    int newest[32], recent[32];
+    unsigned prefix;
+    int remaining;
+};
+
+// A row's place in the order as a key.  With fewer recent rows than stay, they all do and have the highest key; with more,
+// they alone are chosen among and all others have the lowest.  A weight's own key lies between (NaN: 1; -infinity's is 0x007fffff, infinity's
+// 0xff800000).
+__device__ __forceinline__ unsigned evict_key(float w, bool is_recent, bool among_recent)
+{
+    if (is_recent != among_recent) return is_recent ? 0xffffffffu : 0u;
+    return w != w ? 1u : topk_order_key(w);
+}
+
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs a)
+{
+    extern __shared__ unsigned held[];
+    __shared__ SelectSmem sm;
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x, b = unit / a.hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int n = min(max(a.lengths[unit], 0), a.cap), budget = max(a.budgets ? a.budgets[b] : a.budget, 0), keep = min(n, budget);
+    const float *w = a.weights + (long long)unit * a.cap;
+    const int *pos = a.positions + (long long)unit * a.cap;
+    float *w_out = a.weights_out + (long long)unit * a.cap;
+    int *pos_out = a.positions_out + (long long)unit * a.cap;
+    if (w_out != w)
+        for (int j = tid; j < keep; j += kSelThreads) w_out[j] = w[j];
+    if (pos_out != pos)
+        for (int j = tid; j < keep; j += kSelThreads) pos_out[j] = pos[j];
+    int moved = 0;
+    if (keep < n && keep > 0) {
+        int newest = INT_MIN;
+        for (int j = tid; j < n; j += kSelThreads) newest = max(newest, pos[j]);
+        newest = __reduce_max_sync(0xffffffffu, newest);
+        if (lane == 0) sm.newest[warp] = newest;
+        if (tid < 256) sm.hist[tid] = 0;
+        __syncthreads();
+        newest = __reduce_max_sync(0xffffffffu, sm.newest[lane]);
+        const long long recent_from = (long long)newest - a.recent;
+        int n_recent = 0;
+        for (int j = tid; j < n; j += kSelThreads) n_recent += (long long)pos[j] > recent_from;
+        n_recent = __reduce_add_sync(0xffffffffu, n_recent);
+        if (lane == 0) sm.recent[warp] = n_recent;
+        __syncthreads();
+        const bool among_recent = __reduce_add_sync(0xffffffffu, sm.recent[lane]) >= keep;
+        const bool hold = n <= kHeldKeys;
+        auto fresh_key = [&](int j) { return evict_key(w[j], (long long)pos[j] > recent_from, among_recent); };
+        auto key_at = [&](int j) { return hold ? held[j] : fresh_key(j); };
+        if (hold)
+            for (int j = tid; j < n; j += kSelThreads) held[j] = fresh_key(j);
+        // radix select of the keep-th largest, 8 bits at a time
+        unsigned prefix = 0u;
+        int remaining = keep;
+#pragma unroll 1
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            const unsigned mask = shift == 24 ? 0u : ~0u << (shift + 8);
+            for (int j = tid; j < n; j += kSelThreads) {
+                const unsigned key = key_at(j);
+                if ((key & mask) == prefix) atomicAdd(&sm.hist[(key >> shift) & 255u], 1);
+            }
+            __syncthreads();
+            if (warp == 0) {
+                int c[8], mine = 0;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    c[x] = sm.hist[lane * 8 + x];
+                    mine += c[x];
+                }
+                int upto = mine;                       // in this lane's bins and the higher lanes'
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int t = __shfl_down_sync(0xffffffffu, upto, o);
+                    if (lane + o < 32) upto += t;
+                }
+                int above = upto - mine;
+                if (above < remaining && remaining <= upto) {
+#pragma unroll
+                    for (int x = 7; x >= 0; --x) {
+                        if (above < remaining && remaining <= above + c[x]) {
+                            sm.prefix = prefix | (unsigned)(lane * 8 + x) << shift;
+                            sm.remaining = remaining - above;
+                        }
+                        above += c[x];
+                    }
+                }
+            }
+            __syncthreads();
+            prefix = sm.prefix;
+            remaining = sm.remaining;
+            if (tid < 256) sm.hist[tid] = 0;
+            __syncthreads();
+        }
+        // rows in order, kSelThreads at a time: which stay, and the two lists
+        int2 *moves = a.moves + (long long)unit * a.moves_max;
+        int equal_before = 0, holes = 0, fills = 0;
+        for (int j0 = 0; j0 < n; j0 += kSelThreads) {
+            const int j = j0 + tid;
+            const unsigned key = j < n ? key_at(j) : 0u;
+            const bool equal = j < n && key == prefix;
+            unsigned votes = __ballot_sync(0xffffffffu, equal);
+            if (lane == 0) sm.warp_sums[0][warp] = __popc(votes);
+            __syncthreads();
+            int sum = sm.warp_sums[0][lane];
+            const int before = equal_before + __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0) + __popc(votes & ((1u << lane) - 1u));
+            equal_before += __reduce_add_sync(0xffffffffu, sum);
+            const bool stays = j < n && (key > prefix || (equal && before < remaining));
+            const bool hole = j < keep && !stays, fill = j >= keep && stays;
+            // holes and fills in one count: low and high half of a word (at most 1,024 of each here)
+            const unsigned hv = __ballot_sync(0xffffffffu, hole), fv = __ballot_sync(0xffffffffu, fill);
+            if (lane == 0) sm.warp_sums[1][warp] = __popc(hv) | __popc(fv) << 16;
+            __syncthreads();
+            sum = sm.warp_sums[1][lane];
+            const int ahead = __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0), total = __reduce_add_sync(0xffffffffu, sum);
+            if (hole) {
+                const int at = holes + (ahead & 0xffff) + __popc(hv & ((1u << lane) - 1u));
+                if (at < a.moves_max) moves[at].x = j;
+            }
+            if (fill) {
+                const int at = fills + (ahead >> 16) + __popc(fv & ((1u << lane) - 1u));
+                if (at < a.moves_max) moves[at].y = j;
+            }
+            holes += total & 0xffff;
+            fills += total >> 16;
+        }
+        moved = min(min(holes, fills), a.moves_max);
+        __syncthreads();                               // the lists are complete (and the copies above)
+        for (int x = tid; x < moved; x += kSelThreads) {
+            const int2 mv = moves[x];
+            w_out[mv.x] = w[mv.y];
+            pos_out[mv.x] = pos[mv.y];
+        }
+    }
+    __syncthreads();                                   // lengths_out may be lengths: all have read it
+    if (tid == 0) {
+        a.counts[unit] = moved;
+        a.lengths_out[unit] = keep;
+    }
+}
+
+// a quarter, half or whole warp per row (`lanes` of them), four vectors in flight each
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ PoolTable pools,
+                                                                  int lanes_shift)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x / a.n_tensors, tensor = blockIdx.x % a.n_tensors, b = unit / a.hkv, h = unit - b * a.hkv;
+    const int moved = a.counts[unit], lanes = 1 << lanes_shift, lane = threadIdx.x & (lanes - 1);
+    const int step = (int)gridDim.y * (kMoveThreads >> lanes_shift), vecs = a.d * a.elem_bytes / 16;
+    const int2 *moves = a.moves + (long long)unit * a.moves_max;
+    const int *table = a.table + (long long)b * a.max_pages;
+    int4 *pool = static_cast<int4 *>(pools.ptr[tensor]);
+    const long long page_vecs = a.page_stride * a.elem_bytes / 16, head_vecs = a.head_stride * a.elem_bytes / 16,
+                    row_vecs = a.row_stride * a.elem_bytes / 16;
+    auto place = [&](int row) -> int4 * {
+        const int pg = row / a.page_size, page = __ldg(table + pg);
+        if ((unsigned)page >= (unsigned)a.num_pages) return nullptr;
+        return pool + page * page_vecs + h * head_vecs + (long long)(row - pg * a.page_size) * row_vecs;
+    };
+    constexpr int kAhead = 4;
+    for (int x0 = (int)blockIdx.y * (kMoveThreads >> lanes_shift) + (threadIdx.x >> lanes_shift); x0 < moved; x0 += step * kAhead) {
+        int4 *to[kAhead];
+        const int4 *from[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int x = x0 + u * step;
+            to[u] = nullptr;
+            from[u] = nullptr;
+            if (x < moved) {
+                const int2 mv = moves[x];
+                to[u] = place(mv.x);
+                from[u] = place(mv.y);
+            }
+        }
+        for (int v = lane; v < vecs; v += lanes) {
+            int4 y[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (to[u] && from[u]) y[u] = from[u][v];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (to[u] && from[u]) to[u][v] = y[u];
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256) seed_rows_kernel(const __grid_constant__ KShape s, const int *window_idx, const float *token_scores,
+                                                        int row_capacity, int *positions, float *weights)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.y, b = unit / s.hkv;
+    const SeqInfo si = seq_info(s, b);
+    const int n_r = si.n > s.alpha ? si.n - s.alpha : 0, kw = num_windows(si.n, s.alpha, s.omega);
+    const int k = num_selected_capped(si.n, s.alpha, s.omega, si.budget, s.k_max);
+    const int *idx = window_idx + (long long)unit * s.k_max;
+    int review = k * s.omega;
+    if (k > 0 && idx[k - 1] == kw - 1) review -= kw * s.omega - n_r;      // the sequence's short last window
+    review = min(review, n_r);
+    for (int r = blockIdx.x * blockDim.x + threadIdx.x; r < review + si.n - n_r && r < row_capacity; r += gridDim.x * blockDim.x) {
+        int at;
+        float w = 0.f;
+        if (r < review) {
+            const int wi = idx[r / s.omega];
+            at = wi * s.omega + r % s.omega;
+            if (wi < 0 || wi >= kw || at >= n_r) continue;                // no window of the sequence: the row stays as it is
+            if (token_scores) w = token_scores[(long long)unit * s.nr_max + at];
+        } else {
+            at = n_r + (r - review);
+        }
+        if (positions) positions[(long long)unit * row_capacity + r] = at;
+        if (weights) weights[(long long)unit * row_capacity + r] = w;
+    }
+}
+
+}  // namespace
+
+int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream)
+{
+    const int units = a.batch * a.hkv;
+    const size_t smem = (size_t)(a.cap < kHeldKeys ? a.cap : kHeldKeys) * sizeof(unsigned);
+    cudaError_t err = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldKeys * 4);
+    if (err == cudaSuccess) err = launch_pdl(evict_select_kernel, dim3(units), kSelThreads, smem, stream, 1, a);
+    if (err != cudaSuccess) return check_cuda(err, "eviction kernel");
+    count_launches(1);
+    int lanes_shift = 5;
+    const int vecs = a.d * a.elem_bytes / 16;
+    while (lanes_shift > 2 && (1 << (lanes_shift - 1)) >= vecs) --lanes_shift;
+    // as many blocks as the GPU holds (eight of 256 threads per SM) and a few more, however many units there are
+    const long long pairs = (long long)units * a.n_tensors;
+    if (pairs > 0x7fffffffLL) {
+        set_error_detail("eviction: %lld (unit, tensor) pairs", pairs);
+        return WKV_ERR_LIMIT;
+    }
+    long long slices = (148 * 16 + pairs - 1) / pairs;
+    const long long most = (a.moves_max + (kMoveThreads >> lanes_shift) - 1) / (kMoveThreads >> lanes_shift);
+    if (slices > most) slices = most;
+    if (slices < 1) slices = 1;
+    err = launch_pdl(evict_move_kernel, dim3((unsigned)pairs, (unsigned)slices), kMoveThreads, 0, stream, 1, a, pools, lanes_shift);
+    if (err == cudaSuccess) count_launches(1);
+    return check_cuda(err, "eviction kernel (rows)");
+}
+
+int launch_seed_rows(const KShape &ks, const int *window_idx, const float *token_scores, int row_capacity, int *positions,
+                     float *weights, cudaStream_t stream)
+{
+    const int units = ks.batch * ks.hkv;
+    if (units > 65535) {
+        set_error_detail("%d (sequence, KV head) pairs", units);
+        return WKV_ERR_LIMIT;
+    }
+    const int blocks = row_capacity > 256 * 16 ? 16 : (row_capacity + 255) / 256;
+    const cudaError_t err = launch_pdl(seed_rows_kernel, dim3(blocks < 1 ? 1 : blocks, units), 256, 0, stream, 1, ks, window_idx, token_scores,
+                                       row_capacity, positions, weights);
+    if (err == cudaSuccess) count_launches(1);
+    return check_cuda(err, "row state kernel");
+}
+
+}  // namespace wkv

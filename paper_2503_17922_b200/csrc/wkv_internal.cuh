@@ -235,8 +235,8 @@ constexpr int kStatusWaitExpired = 1;   // a bounded wait inside a kernel ran ou
 // ended.  It must call pdl_wait() before it touches global memory; the wait ends when the kernel before it
 // has completed and its writes are visible.  Because every kernel launched this way waits, "the kernel
 // before it has completed" includes everything earlier in the stream.  Exceptions to waiting first: the CUDA-core
-// score kernel reads Q, K and the lengths (which no kernel of this library writes) ahead of its wait, because the statistics
-// kernel in front of it triggers only after its own wait, behind which everything that wrote them lies; what the
+// score kernel reads Q, K and the lengths ahead of its wait, because the statistics
+// kernel in front of it triggers only after its own wait, behind which everything that wrote them (rotary positions, say) lies; what the
 // statistics kernel writes is read, and anything is written, after the wait.  And the kernels that fetch rows into L2 ahead
 // of theirs (fetch_window here, fetch_ahead in score_tc.cu) read lengths and indices for it, from L2 and for nothing else.
 // Takes about 2 us off the gap

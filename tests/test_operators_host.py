@@ -1,0 +1,224 @@
+"""CPU-only checks of the entry points around the selection: struct mirrors, the frequency table, refusals before any device work."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+import operators_util as ou
+from paper_2503_17922_b200 import binding, build
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build_library()
+    return binding.lib()
+
+
+P = 0x1000      # an aligned address that nothing follows: every call here is refused on the host
+
+
+def shape(**kw):
+    s = binding.WkvShape()
+    s.struct_size = ctypes.sizeof(binding.WkvShape)
+    s.dtype, s.batch, s.n_q_heads, s.n_kv_heads, s.head_dim = binding.WKV_BF16, 1, 4, 2, 64
+    s.l_obs, s.window, s.top_p, s.task, s.max_seqlen, s.budget = 8, 8, 0, 0, 1024, 128
+    s.stride_b, s.stride_h, s.stride_t = 2 * 1024 * 64, 1024 * 64, 64
+    s.q_stride_b, s.q_stride_h, s.q_stride_t = 4 * 8 * 64, 8 * 64, 64
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+def paged(**kw):
+    c = binding.WkvPaged()
+    c.struct_size = ctypes.sizeof(binding.WkvPaged)
+    c.dtype, c.batch, c.n_q_heads, c.n_kv_heads, c.head_dim = binding.WKV_BF16, 2, 4, 2, 64
+    c.max_new, c.page_size, c.num_pages, c.max_pages = 3, 16, 20, 8
+    c.block_table = P
+    c.page_stride, c.head_stride, c.row_stride = 2 * 16 * 64, 16 * 64, 64
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def rope(**kw):
+    r = binding.WkvRope(ctypes.sizeof(binding.WkvRope), 64, 0, 1.0, P)
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+def strides(*st):
+    return (ctypes.c_int64 * 3)(*st)
+
+
+QS = strides(4 * 1024 * 64, 1024 * 64, 64)
+BIG = 1 << 40
+
+
+def test_struct_mirrors():
+    assert ctypes.sizeof(binding.WkvPaged) == 12 * 4 + 3 * 8 + 3 * 8
+    assert ctypes.sizeof(binding.WkvRope) == 4 * 4 + 8
+
+
+@pytest.mark.parametrize("rot,base,scaling,factor,original", [
+    (128, 10000.0, "none", 1.0, 0.0), (64, 500000.0, "linear", 8.0, 0.0), (128, 500000.0, "base", 4.0, 0.0),
+    (2, 10000.0, "base", 4.0, 0.0), (128, 500000.0, "bands", 8.0, 8192.0), (80, 10000.0, "bands", 32.0, 4096.0),
+])
+def test_frequencies_in_turns(L, rot, base, scaling, factor, original):
+    got = binding.wkv_rope_frequencies(rot, base, scaling, factor, original)
+    ref = ou.frequencies(rot, base, scaling, factor, original)
+    # the reference is in 64 bits: relative 2^-50 of rounding errors, and half a unit of 2^-64 turns
+    for g, f in zip(got, ref):
+        assert abs(int(g) * 2.0 ** -64 - f / (2 * math.pi)) <= f * 2.0 ** -48 + 2.0 ** -64
+
+
+def test_frequencies_wrap_whole_turns(L):
+    got = binding.wkv_rope_frequencies(2, 1.0, "linear", 1.0 / (2 * math.pi * 3.25))
+    assert abs(int(got[0]) * 2.0 ** -64 - 0.25) < 1e-12
+
+
+@pytest.mark.parametrize("args", [
+    (3, 1e4, "none", 1.0), (0, 1e4, "none", 1.0), (64, 0.0, "none", 1.0), (64, -1.0, "none", 1.0), (64, 1e4, "linear", 0.0),
+    (64, 1e4, "bands", 2.0, 0.0), (64, 1e4, "bands", 2.0, 8192.0, 4.0, 4.0), (64, float("nan"), "none", 1.0), (64, 1e4, "linear", float("inf")),
+])
+def test_frequency_refusals(L, args):
+    with pytest.raises(binding.WkvError) as e:
+        binding.wkv_rope_frequencies(*args)
+    assert e.value.status == 2
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(struct_size=8), 2), (dict(dtype=5), 3), (dict(batch=0), 2), (dict(n_q_heads=3), 2), (dict(head_dim=4), 6),
+    (dict(max_new=0), 2), (dict(page_size=0), 2), (dict(num_pages=0), 2), (dict(max_pages=0), 2), (dict(block_table=None), 1),
+    (dict(row_stride=60), 6), (dict(row_stride=56), 2), (dict(page_stride=-64), 6), (dict(cu_new_host=P), 1), (dict(cu_new_dev=P), 1),
+    (dict(max_pages=1 << 27), 9), (dict(page_size=1 << 30, max_pages=2), 9),
+])
+def test_paged_description_refusals(L, kw, status):
+    c = paged(**kw)
+    assert L.wkv_paged_workspace_bytes(ctypes.byref(c)) == 0
+    ptrs = (ctypes.c_void_p * 2)(P, 2 * P)
+    st = strides(4 * 3 * 64, 3 * 64, 64)
+    calls = [
+        L.wkv_append_kv_paged(ctypes.byref(c), None, P, P, st, None, None, None, P, P, P, 2 * P, None, None, None, None),
+        L.wkv_attend_paged(ctypes.byref(c), P, st, P, P, P, 2 * P, st, None, None, None, P, BIG, None),
+        L.wkv_evict_kv_paged(ctypes.byref(c), 2, ptrs, None, 1, None, 0, P, P, P, P, P, P, P, BIG, None),
+    ]
+    assert calls == [status] * 3, L.wkv_last_error_detail()
+    assert L.wkv_last_error_detail()
+
+
+def test_reserved_words(L):
+    c = paged()
+    c.reserved[1] = 1
+    assert L.wkv_paged_workspace_bytes(ctypes.byref(c)) == 0
+    assert L.wkv_paged_workspace_bytes(ctypes.byref(paged())) > 0
+    assert L.wkv_paged_workspace_bytes(None) == 0
+
+
+@pytest.mark.parametrize("cu", [[0, 4, 5], [1, 2, 3], [0, 2, 1]])
+def test_chunk_lengths(L, cu):
+    a = np.array(cu, dtype=np.int32)
+    c = paged(cu_new_host=a.ctypes.data, cu_new_dev=P)
+    assert L.wkv_paged_workspace_bytes(ctypes.byref(c)) == 0
+    a[:] = [0, 0, 3]
+    assert L.wkv_paged_workspace_bytes(ctypes.byref(c)) > 0
+
+
+def test_attend_paged_refusals(L):
+    c = paged()
+    need = L.wkv_paged_workspace_bytes(ctypes.byref(c))
+    st = strides(4 * 3 * 64, 3 * 64, 64)
+
+    def call(q=P, qs=st, k=P, v=P, n=P, out=2 * P, os=st, lse=None, win=None, wout=None, ws=P, size=need, desc=c):
+        return L.wkv_attend_paged(ctypes.byref(desc), q, qs, k, v, n, out, os, lse, win, wout, ws, size, None)
+
+    assert [call(q=None), call(k=None), call(v=None), call(n=None), call(out=None), call(qs=None), call(os=None)] == [1] * 7
+    assert [call(q=P + 8), call(k=P + 8), call(out=P + 8), call(qs=strides(64, 4, 64))] == [6] * 4
+    assert [call(ws=None), call(size=need - 1), call(ws=P + 16)] == [5] * 3
+    assert call(win=P) == 1 and call(out=P) == 2 and call(qs=strides(64, 64, 56)) == 2
+    assert call(desc=paged(head_dim=264, page_stride=2 * 16 * 264, head_stride=16 * 264, row_stride=264), qs=strides(0, 264, 264), os=strides(0, 264, 264)) == 7
+
+
+def test_append_refusals(L):
+    c = paged()
+    st = strides(2 * 3 * 64, 3 * 64, 64)
+
+    def call(r=None, k=P, v=P, ks=st, q=None, qo=None, qs=None, pos=P, n=P, kp=P, vp=2 * P, no=None, rp=None, rw=None):
+        return L.wkv_append_kv_paged(ctypes.byref(c), ctypes.byref(r) if r is not None else None, k, v, ks, q, qo, qs, pos, n, kp, vp, no, rp,
+                                     rw, None)
+
+    assert [call(k=None), call(v=None), call(ks=None), call(n=None), call(kp=None), call(vp=None), call(q=P), call(qo=P)] == [1] * 8
+    assert [call(pos=None, r=rope()), call(pos=None, rp=P), call(q=P, qo=P, qs=None), call(r=rope(turns=None))] == [1] * 4
+    assert [call(k=P + 8), call(kp=P + 8), call(ks=strides(0, 4, 64))] == [6] * 3
+    assert [call(no=P), call(vp=P), call(ks=strides(0, 64, 32))] == [2] * 3
+    assert [call(r=rope(struct_size=1)), call(r=rope(rot_dim=3)), call(r=rope(rot_dim=66)), call(r=rope(rot_dim=0)), call(r=rope(order=2)),
+            call(r=rope(scale=math.inf)), call(r=rope(scale=math.nan))] == [2] * 7
+
+
+def test_evict_refusals(L):
+    c = paged()
+    need = L.wkv_paged_workspace_bytes(ctypes.byref(c))
+    ptrs = (ctypes.c_void_p * 40)(*([P] * 40))
+
+    def call(layers=1, k=ptrs, v=None, budget=4, recent=0, w=P, p=P, n=P, wo=P, po=P, no=P, ws=P, size=need):
+        return L.wkv_evict_kv_paged(ctypes.byref(c), layers, k, v, budget, None, recent, w, p, n, wo, po, no, ws, size, None)
+
+    assert [call(layers=0), call(layers=33)] == [9] * 2
+    assert [call(k=None), call(w=None), call(p=None), call(n=None), call(wo=None), call(po=None), call(no=None)] == [1] * 7
+    assert call(budget=-1) == 4 and call(recent=-1) == 2
+    assert [call(ws=None), call(size=need - 1), call(ws=P + 128)] == [5] * 3
+    assert call(k=(ctypes.c_void_p * 1)(P + 8)) == 6 and call(k=(ctypes.c_void_p * 1)(None)) == 1
+
+
+def test_prompt_refusals(L):
+    def attend(s=None, q=P, qs=QS, k=P, v=P, out=2 * P, os=QS):
+        return L.wkv_attend_prompt(ctypes.byref(s if s is not None else shape()), q, qs, k, v, out, os, None, None, None, None)
+
+    assert [attend(q=None), attend(k=None), attend(v=None), attend(out=None), attend(qs=None), attend(os=None)] == [1] * 6
+    assert [attend(q=P + 4), attend(v=P + 8), attend(qs=strides(0, 4, 64)), attend(qs=strides(-64, 64, 64))] == [6] * 4
+    assert [attend(out=P), attend(qs=strides(0, 64, 32)), attend(s=shape(batch=0))] == [2] * 3
+    assert attend(s=shape(head_dim=264, stride_t=264, q_stride_t=264), qs=strides(0, 264, 264), os=strides(0, 264, 264)) == 7
+
+    def rotate(r=None, q=P, qo=P, qs=QS, k=P, ko=P, s=None):
+        return L.wkv_rotate_prompt(ctypes.byref(s if s is not None else shape()), ctypes.byref(r if r is not None else rope()), q, qo, qs, k, ko,
+                                   None, None)
+
+    assert [rotate(q=None), rotate(ko=None), rotate(qs=None), rotate(q=None, qo=None, k=None, ko=None), rotate(r=rope(turns=None))] == [1] * 5
+    assert [rotate(q=P + 8), rotate(k=P + 8)] == [6] * 2
+    assert [rotate(r=rope(rot_dim=66)), rotate(r=rope(order=-1)), rotate(qs=strides(0, 64, 8))] == [2] * 3
+    assert L.wkv_rotate_prompt(ctypes.byref(shape()), None, P, P, QS, P, P, None, None) == 1
+
+
+def test_seed_refusals(L):
+    s = shape()
+    assert L.wkv_keep_max(ctypes.byref(s)) == 128
+    assert L.wkv_seed_rows(ctypes.byref(s), None, None, 128, P, P, None) == 1
+    assert L.wkv_seed_rows(ctypes.byref(s), P, None, 128, None, None, None) == 1
+    assert L.wkv_seed_rows(ctypes.byref(s), P, None, 127, P, P, None) == 2
+
+
+def test_nothing_was_launched(L):
+    assert L.wkv_launch_count() == 0
+
+
+def test_python_side_checks_shapes():
+    torch = pytest.importorskip("torch")
+    t = torch.zeros((2, 4, 3, 64), dtype=torch.bfloat16)
+    assert list(binding._head_strides(t, False, "q")) == [768, 192, 64]
+    assert list(binding._head_strides(t[0].transpose(0, 1), True, "q")) == [0, 192, 64]
+    with pytest.raises(ValueError):
+        binding._head_strides(t[0], False, "q")
+    with pytest.raises(ValueError):
+        binding._head_strides(t.transpose(2, 3), False, "q")
+    with pytest.raises(ValueError):
+        binding._check_heads(t, 4, torch.float32, 64, False, 2, 3, "q")
+    with pytest.raises(ValueError):
+        binding._check_heads(t, 4, torch.bfloat16, 64, False, 2, 4, "q")
+    with pytest.raises(ValueError):
+        binding._check_state(torch.zeros((2, 2), dtype=torch.int64), (2, 2), "int32", "lengths")
+    with pytest.raises(ValueError):
+        binding._check_state(torch.zeros((2, 4), dtype=torch.int32)[:, ::2], (2, 2), "int32", "lengths")
+    with pytest.raises(ValueError):
+        binding._check_same_layout(t, t.transpose(1, 2), "q and q_out")
