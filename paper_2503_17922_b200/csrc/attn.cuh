@@ -7,6 +7,8 @@
 
 #include "wkv_internal.cuh"
 
+#include <atomic>
+
 namespace wkv {
 
 constexpr int kAttnMaxHeadDim = 256;
@@ -80,7 +82,26 @@ __device__ __forceinline__ void attn_store_lse(const AttnArgs &a, int b, int hq,
     if (a.lse_obs && i >= m - a.alpha) a.lse_obs[row * a.alpha + (i - m + a.alpha)] = l;
 }
 
+// Dynamic shared memory beyond 48 KB has to be asked for once per kernel and device; `asked` remembers for one kernel.
+struct SmemAsked {
+    std::atomic<uint64_t> devices{0};
+};
+template <typename K>
+inline cudaError_t allow_smem(K kernel, size_t bytes, SmemAsked &asked)
+{
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    const uint64_t bit = dev < kMaxDevices ? 1ull << dev : 0;
+    if (asked.devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (err == cudaSuccess) asked.devices.fetch_or(bit, std::memory_order_release);
+    return err;
+}
+
 // kernels (each returns a wkv_status)
+bool attn_tc_supported(const AttnArgs &a, int dtype);
+int launch_attn_tc(const AttnArgs &a, cudaStream_t stream);          // WKV_ERR_UNSUPPORTED: a layout that no tensor map describes
 int launch_attn_simt(const AttnArgs &a, int dtype, cudaStream_t stream);
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream);
 int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream);    // reads a.lse

@@ -1,0 +1,638 @@
+// Attention on the tensor cores (tcgen05, tensor memory, TMA): bf16, head dimension 64 or 128, whole prompts and chunks of new
+// tokens over a paged cache.
+//
+// An item is two query tiles of up to 128 rows of one unit (row = position x query head of the group, so one key tile serves
+// every head that shares it), against the unit's keys in tiles of 128, in ascending order:
+//   S = Q K^T    128 x 128 per query tile, in tensor memory
+//   P = exp2(S c - m c), in bf16 over S's first columns; one thread per row keeps the maximum m and the sum of P
+//   O += P V     128 x d in tensor memory
+// The two query tiles alternate: while one's P is computed, the tensor cores work on the other.  m follows the row's maximum
+// only when that has grown by more than 2^8: a sum that is too large by at most that factor loses nothing in fp32, and O has to
+// be read, scaled and written back only then.
+//
+// P is rounded to bf16 for the product (as its operand has to be); sum, maximum and O are fp32, the sum of the unrounded P.
+//
+// Warps: 0-3 and 4-7 the softmax of the two query tiles (thread = row), 8 issues the MMAs, 9 the TMA loads (keys and values of a
+// tile in turn through one ring), 10 and 11 look through the values of tiles that hold rows which some query does not see: P is 0 there,
+// but 0 times an infinity or NaN is not.  Such elements are replaced by 0 in shared memory, and the rows that do see them
+// get them added at the end.
+//
+// Blocks are persistent, one per SM; the items come in order of descending work and are dealt to the blocks back and forth.
+// Every wait is bounded; on expiry the block sets bit 0 of the status word, lets its loads land, frees its tensor memory and returns.
+#include "attn.cuh"
+#include "score_math.cuh"
+#include "tc_common.cuh"
+#include "tensor_map.cuh"
+
+namespace wkv {
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 128;
+constexpr int kThreads = 384;
+constexpr int kRegion = kTile * 128;          // bytes of 64 columns of a tile
+constexpr uint32_t kTmemCols = 512;           // all of it: S/P of the two query tiles (128 columns each), O of both (128 each)
+constexpr int kMaxStages = 8;
+constexpr int kMaskSlots = 8;
+constexpr float kLazy = 8.f;                  // exponent by which the maximum may be outgrown
+__host__ __device__ constexpr int stages_for(int kb) { return kb == 2 ? 5 : 8; }
+struct TcAttnArgs {
+    AttnArgs a;
+    int ppt;                 // positions of a query tile: 128 / G
+    int max_pairs;           // items of a unit at most
+    long long items;
+    int k_slot[3];           // tensor-map coordinates of (token, head, batch) / (slot, head, page)
+    int box_rows;            // rows of a key box
+};
+
+struct Shared {
+    uint64_t q_full, q_empty;
+    uint64_t full[kMaxStages], empty[kMaxStages], look[kMaxStages], clean[kMaxStages];
+    uint64_t s_full[2], p_full[2], pv_done[2], o_free[2];
+    uint32_t tmem_base;
+    int abort;
+    int poison[kMaskSlots];                        // item whose values held an infinity or NaN in a tile that was looked through
+    uint4 present[kMaskSlots];                     // of the tiles' 128 rows: those with a page
+};
+
+struct Item {
+    int unit, b, h;
+    AttnSeq sq;
+    int pos0;                // first position of the first query tile
+    int rows[2];             // positions in each
+    int tiles[2];            // key tiles of each
+    int base;                // keys that query 0 sees
+    int looked;              // key tiles from here on are looked through
+    int n_tiles;
+};
+__device__ __forceinline__ bool get_item(const TcAttnArgs &t, long long k, Item &im)
+{
+    const AttnArgs &a = t.a;
+    const int units = a.batch * a.hkv;
+    const int rank = (int)(k / units);
+    im.unit = (int)(k - (long long)rank * units);
+    im.b = im.unit / a.hkv;
+    im.h = im.unit - im.b * a.hkv;
+    im.sq = attn_seq(a, im.b, im.h);
+    const int per = 2 * t.ppt, pairs = (im.sq.m + per - 1) / per, pair = pairs - 1 - rank;
+    if (pair < 0) return false;
+    im.pos0 = pair * per;
+    im.base = im.sq.n - im.sq.m + 1;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int first = im.pos0 + x * t.ppt;
+        im.rows[x] = min(max(im.sq.m - first, 0), t.ppt);
+        const int most = im.rows[x] > 0 ? min(im.base + first + im.rows[x] - 1, im.sq.n) : 0;
+        im.tiles[x] = (max(most, 0) + kTile - 1) / kTile;
+    }
+    im.looked = max(im.base + im.pos0, 0) / kTile;       // every row sees all of the tiles in front of this one
+    im.n_tiles = max(im.tiles[0], im.tiles[1]);
+    return true;
+}
+// a block's items, back and forth over the list
+struct Walk {
+    long long k0 = 0;
+    int round = 0, seq = 0;       // seq: items with key tiles so far
+    __device__ __forceinline__ bool next(const TcAttnArgs &t, Item &im)
+    {
+        while (k0 < t.items) {
+            const long long k = k0 + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+            k0 += gridDim.x;
+            ++round;
+            if (k < t.items && get_item(t, k, im)) return true;
+        }
+        return false;
+    }
+};
+
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int lane)
+{
+    int ok = 1;
+    if (lane == 0) ok = mbar_wait(bar, parity, abort_flag) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
+// ---- tensor memory and MMA forms that only this kernel uses -------------------------------------
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+                 "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void umma_bf16_ta_if(uint32_t leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                                uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t"
+                 "setp.ne.b32 p, %4, 0;\n\t"
+                 "setp.ne.b32 q, %5, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 :
+                 : "r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader)
+                 : "memory");
+}
+// Values as B operand: N (the head dimension) runs along the 128-byte rows, K (the keys) across them.  Stride byte offset: 8 keys
+// (1024 bytes); leading byte offset: the next 64 columns (a region).
+__device__ __forceinline__ uint64_t value_desc(uint32_t smem_addr)
+{
+    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | ((uint64_t)(kRegion >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+constexpr uint32_t kBTransposed = 1u << 16;
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// ---- the softmax of one query tile ------------------------------------------------------------
+template <int KB, int x>
+__device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, uint32_t tmem)
+{
+    constexpr int D = KB * 64;
+    const AttnArgs &a = t.a;
+    const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3, row = quarter * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t s_addr = lanes + x * kTile, o_addr = lanes + 2 * kTile + x * kTile;
+    const int place = row / a.G, head = row - place * a.G;
+    const bool of_tile = row < t.ppt * a.G;
+    const float c = a.scale_log2;
+    uint32_t turn = 0, tiles_before = 0;            // tiles of S taken so far; key tiles of the items so far
+    volatile int *const abort_flag = &sh.abort;
+    Walk walk;
+    Item im;
+    while (walk.next(t, im)) {
+        const int pos = im.pos0 + x * t.ppt + place;
+        const bool mine = of_tile && place < im.rows[x];
+        const int limit = mine ? min(im.base + pos, im.sq.n) : 0;
+        const int plain = (im.base + im.pos0 + x * t.ppt) / kTile;         // tiles that every row of this query tile sees all of
+        float m = -INFINITY, l = 0.f;
+        for (int u = 0; u < im.tiles[x]; ++u, ++turn) {
+            if (!warp_wait(&sh.s_full[x], turn & 1, abort_flag, lane)) return;
+            tc_fence_after_sync();
+            float s[4][32];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) tmem_ld32_issue(s_addr + y * 32, s[y]);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) tmem_ld_wait(s[y]);
+            if (a.table) {
+                const uint4 have = sh.present[(tiles_before + u) % kMaskSlots];
+                if ((have.x & have.y & have.z & have.w) != ~0u) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        if (!(have.x >> j & 1u)) s[0][j] = -INFINITY;
+                        if (!(have.y >> j & 1u)) s[1][j] = -INFINITY;
+                        if (!(have.z >> j & 1u)) s[2][j] = -INFINITY;
+                        if (!(have.w >> j & 1u)) s[3][j] = -INFINITY;
+                    }
+                }
+            }
+            if (u >= plain) {
+                const int in_tile = limit - u * kTile;
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (y * 32 + j >= in_tile) s[y][j] = -INFINITY;
+            }
+            float top[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                top[y] = s[y][0];
+#pragma unroll
+                for (int j = 1; j < 32; ++j) top[y] = fmaxf(top[y], s[y][j]);
+            }
+            const float grown = fmaxf(fmaxf(m, fmaxf(top[0], top[1])), fmaxf(top[2], top[3]));
+            const bool follow = (grown - m) * c > kLazy;          // (also from -infinity on)
+            if (u == 0) {
+                m = grown;
+            } else if (__any_sync(0xffffffffu, follow)) {
+                if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag, lane)) return;
+                tc_fence_after_sync();
+                const float f = follow ? exp2f((m - grown) * c) : 1.f;
+                if (follow) m = grown;
+                l *= f;
+#pragma unroll 1
+                for (int y = 0; y < D / 16; ++y) {
+                    float o[16];
+                    tmem_ld16(o_addr + y * 16, o);
+                    uint32_t w[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) w[j] = __float_as_uint(o[j] * f);
+                    tmem_st16(o_addr + y * 16, w);
+                }
+            }
+            const float ref = m == -INFINITY ? 0.f : -m * c;
+            const unsigned long long c2 = pair_of(c, c), ref2 = pair_of(ref, ref);
+            unsigned long long sum[2] = {0ull, 0ull};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                uint32_t p[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float *v = &s[y][2 * j];
+                    const float2 e = halves_of(fma_pair(pair_of(v[0], v[1]), c2, ref2));
+                    const float p0 = fast_exp2(e.x), p1 = fast_exp2(e.y);
+                    sum[j & 1] = add_pair(sum[j & 1], pair_of(p0, p1));
+                    p[j] = pack_bf16(p0, p1);
+                }
+                tmem_st16(s_addr + y * 16, p);
+            }
+            tmem_st_wait();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.p_full[x]);
+            const float2 s0 = halves_of(sum[0]), s1 = halves_of(sum[1]);
+            l += (s0.x + s0.y) + (s1.x + s1.y);
+        }
+        // ---- the item's rows: O / l -------------------------------------------------------------
+        const bool any = im.tiles[x] > 0;
+        const int hq = im.h * a.G + head;
+        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (im.sq.q_off + pos) * a.ot + im.b * a.ob + (long long)hq * a.oh;
+        if (any) {
+            if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag, lane)) return;
+            tc_fence_after_sync();
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const bool poisoned = any && *static_cast<volatile int *>(&sh.poison[walk.seq % kMaskSlots]) == walk.seq + 1;
+#pragma unroll 1
+        for (int y = 0; y < D / 32; ++y) {
+            float o[32];
+            if (any) {
+                tmem_ld32(o_addr + y * 32, o);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] = l == 0.f ? 0.f : o[j] * inv;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) o[j] = 0.f;
+            }
+            if (poisoned) {
+                for (int j = im.looked * kTile; j < limit; ++j) {
+                    const long long at = attn_row(a, im.b, im.h, im.sq.q_off, j);
+                    if (at < 0) continue;
+                    const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + at + y * 32;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float ve = __bfloat162float(v[e]);
+                        if (!(fabsf(ve) < INFINITY)) o[e] += ve;
+                    }
+                }
+            }
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8)
+                    *reinterpret_cast<uint4 *>(dst + y * 32 + j) = make_uint4(pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]),
+                                                                              pack_bf16(o[j + 4], o[j + 5]), pack_bf16(o[j + 6], o[j + 7]));
+            }
+        }
+        if (any) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.o_free[x]);
+        }
+        if (mine) attn_store_lse(a, im.b, hq, pos, im.sq.m, l > 0.f || l != l ? m * c + log2f(l) : -INFINITY);
+        walk.seq += im.n_tiles > 0;
+        tiles_before += im.n_tiles;
+    }
+}
+
+// ---- MMAs --------------------------------------------------------------------------------------
+template <int KB>
+__device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, uint32_t tmem)
+{
+    constexpr int NS = stages_for(KB), kStage = KB * kRegion;
+    const int lane = threadIdx.x & 31;
+    const uint32_t leader = elect_one();
+    volatile int *const abort_flag = &sh.abort;
+    const uint64_t q_desc0 = umma_desc_sw128(smem_u32(q_img)), k_desc0 = umma_desc_sw128(smem_u32(ring)), v_desc0 = value_desc(smem_u32(ring));
+    constexpr uint32_t s_idesc = umma_idesc_bf16(kTile, kTile), o_idesc = umma_idesc_bf16(kTile, KB * 64) | kBTransposed;
+    uint32_t entry = 0, clean_phase = 0;               // ring entries so far; parity per stage of the looked-through tiles
+    uint32_t turn[2] = {0, 0}, outs[2] = {0, 0};       // tiles and items of each query tile so far
+    Walk walk;
+    Item im;
+    auto scores = [&](int x, int stage) {
+        const uint64_t kd = k_desc0 + (uint64_t)((uint32_t)(stage * kStage) >> 4), qd = q_desc0 + (uint64_t)((uint32_t)(x * kStage) >> 4);
+#pragma unroll
+        for (int ks = 0; ks < KB * 4; ++ks) {
+            const uint32_t at = (uint32_t)((ks >> 2) * kRegion + (ks & 3) * 32) >> 4;
+            umma_bf16_if(leader, tmem + x * kTile, qd + at, kd + at, s_idesc, ks > 0);
+        }
+        umma_commit_if(leader, &sh.s_full[x]);
+    };
+    while (walk.next(t, im)) {
+        if (im.n_tiles == 0) continue;
+        if (!warp_wait(&sh.q_full, walk.seq & 1, abort_flag, lane)) return;
+        int stage = entry % NS;
+        if (!warp_wait(&sh.full[stage], (entry / NS) & 1, abort_flag, lane)) return;
+        tc_fence_after_sync();
+        // (S of the last item's last tile has been read: its P was waited for)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (im.tiles[x] > 0) scores(x, stage);
+        umma_commit_if(leader, &sh.empty[stage]);
+        if (im.n_tiles == 1) umma_commit_if(leader, &sh.q_empty);
+        ++entry;
+        for (int u = 0; u < im.n_tiles; ++u) {
+            const int v_stage = entry % NS;
+            if (!warp_wait(&sh.full[v_stage], (entry / NS) & 1, abort_flag, lane)) return;
+            const bool looked = u >= im.looked;
+            if (looked && lane == 0) mbar_arrive(&sh.look[v_stage]);
+            ++entry;
+            const bool more = u + 1 < im.n_tiles;
+            const int k_stage = entry % NS;
+            if (more && !warp_wait(&sh.full[k_stage], (entry / NS) & 1, abort_flag, lane)) return;
+            if (looked) {
+                if (!warp_wait(&sh.clean[v_stage], clean_phase >> v_stage & 1u, abort_flag, lane)) return;
+                clean_phase ^= 1u << v_stage;
+            }
+            const uint64_t vd = v_desc0 + (uint64_t)((uint32_t)(v_stage * kStage) >> 4);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (u >= im.tiles[x]) continue;
+                if (u == 0) {
+                    if (outs[x] > 0 && !warp_wait(&sh.o_free[x], (outs[x] - 1) & 1, abort_flag, lane)) return;
+                    ++outs[x];
+                }
+                if (!warp_wait(&sh.p_full[x], turn[x] & 1, abort_flag, lane)) return;
+                ++turn[x];
+                tc_fence_after_sync();
+#pragma unroll
+                for (int ks = 0; ks < kTile / 16; ++ks)
+                    umma_bf16_ta_if(leader, tmem + 2 * kTile + x * kTile, tmem + x * kTile + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc,
+                                    u > 0 || ks > 0);
+                umma_commit_if(leader, &sh.pv_done[x]);
+                if (u + 1 < im.tiles[x]) scores(x, k_stage);
+            }
+            umma_commit_if(leader, &sh.empty[v_stage]);
+            if (more) {
+                umma_commit_if(leader, &sh.empty[k_stage]);
+                ++entry;
+                if (u + 2 == im.n_tiles) umma_commit_if(leader, &sh.q_empty);
+            }
+        }
+        ++walk.seq;
+    }
+}
+
+// ---- loads --------------------------------------------------------------------------------------
+template <int KB>
+__device__ __forceinline__ uint32_t load_warp(const TcAttnArgs &t, Shared &sh, const CUtensorMap *k_map, const CUtensorMap *v_map, uint8_t *ring)
+{
+    constexpr int NS = stages_for(KB), kStage = KB * kRegion;
+    const AttnArgs &a = t.a;
+    const int lane = threadIdx.x & 31;
+    volatile int *const abort_flag = &sh.abort;
+    uint32_t entry = 0;
+    Walk walk;
+    Item im;
+    const int boxes = kTile / t.box_rows;             // of a tile
+    const uint32_t leader = elect_one();
+    // One box into a stage.  One lane issues, and every operand is the same in all lanes: the instruction takes them from
+    // uniform registers, so that an address which varies from lane to lane is another lane's.
+    auto put_box = [&](const CUtensorMap *map, int stage, int box, int tok, int h, int third) {
+        const int c1 = t.k_slot[0] == 1 ? tok : (t.k_slot[1] == 1 ? h : third);
+        const int c2 = t.k_slot[0] == 2 ? tok : (t.k_slot[1] == 2 ? h : third);
+        const int c3 = t.k_slot[0] == 3 ? tok : (t.k_slot[1] == 3 ? h : third);
+        uint8_t *to = ring + stage * kStage + box * t.box_rows * 128;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) tma_load_4d_if(leader, to + kb * kRegion, map, &sh.full[stage], kb * 64, c1, c2, c3);
+    };
+    while (walk.next(t, im)) {
+        for (int u = 0; u < im.n_tiles; ++u) {
+            // Where the tile's rows are: dense, one box; paged, one box per page or part of one, and rows without a page are
+            // zeros (a page beyond the pool's).  Lane i looks up box i.
+            int tok = (int)im.sq.q_off + u * kTile, third = a.cu_q ? 0 : im.b;
+            if (a.table) {
+                const int row = u * kTile + lane * t.box_rows;
+                int page = -1;
+                tok = 0;
+                if (lane < boxes && row < im.sq.n) {
+                    const int pg = row / a.page_size;
+                    page = __ldg(a.table + (long long)im.b * a.max_pages + pg);
+                    tok = row - pg * a.page_size;
+                }
+                const bool have = (unsigned)page < (unsigned)a.num_pages;
+                third = have ? page : a.num_pages;
+                // bit j of word w: row 32 w + j has a page (rows from the length on: no matter)
+                const uint32_t votes = __ballot_sync(0xffffffffu, have), all = (1u << boxes) - 1u;
+                uint32_t bits = ~0u;
+                if ((votes & all) != all) {
+                    if (boxes >= 4) {
+                        bits = 0;
+                        for (int j = 0; j < 32; ++j) bits |= (votes >> (((lane & 3) * 32 + j) / t.box_rows) & 1u) << j;
+                    } else {
+                        bits = votes >> ((lane & 3) * boxes / 4) & 1u ? ~0u : 0u;
+                    }
+                }
+                if (lane < 4) reinterpret_cast<uint32_t *>(&sh.present[(entry >> 1) % kMaskSlots])[lane] = bits;
+                __syncwarp();
+            }
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                const int stage = entry % NS;
+                if (entry >= NS && !warp_wait(&sh.empty[stage], (entry / NS - 1) & 1, abort_flag, lane)) return entry;
+                mbar_arrive_expect_tx_if(leader, &sh.full[stage], kStage);
+                for (int box = 0; box < boxes; ++box) {
+                    const int bt = __shfl_sync(0xffffffffu, tok, box), b3 = __shfl_sync(0xffffffffu, third, box);
+                    if (kv == 0) put_box(k_map, stage, box, bt, im.h, b3);
+                    else put_box(v_map, stage, box, bt, im.h, b3);
+                }
+                ++entry;
+            }
+        }
+    }
+    return entry;
+}
+
+// ---- queries, and values of tiles that some row does not see whole -----------------------------------
+// Rows of the two query tiles into shared memory, in the 128-byte swizzle that the MMAs read; rows that no query has are zeros.
+template <int KB>
+__device__ __forceinline__ void load_queries(const TcAttnArgs &t, const Item &im, uint8_t *q_img, int which, int lane)
+{
+    constexpr int kChunks = KB * 8;                    // of 16 bytes, in a row
+    const AttnArgs &a = t.a;
+    const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q) + im.sq.q_off * a.qt + im.b * a.qb + (long long)im.h * a.G * a.qh;
+    const int chunk = lane % kChunks;
+    for (int r = which * (32 / kChunks) + lane / kChunks; r < 2 * kTile; r += 64 / kChunks) {
+        const int x = r / kTile, row = r - x * kTile, place = row / a.G, head = row - place * a.G;
+        const bool there = place < t.ppt && place < (x ? im.rows[1] : im.rows[0]);
+        const __nv_bfloat16 *from = there ? q + (long long)(im.pos0 + x * t.ppt + place) * a.qt + head * a.qh + chunk * 8 : q;
+        uint8_t *to = q_img + x * KB * kRegion + (chunk >> 3) * kRegion + swz128_offset(row, chunk & 7);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+template <int KB>
+__device__ __forceinline__ void helper_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, int which)
+{
+    constexpr int NS = stages_for(KB), kStage = KB * kRegion;
+    const int lane = threadIdx.x & 31;
+    volatile int *const abort_flag = &sh.abort;
+    uint32_t entry = 0, look_phase = 0;
+    Walk walk;
+    Item im;
+    while (walk.next(t, im)) {
+        if (im.n_tiles == 0) continue;
+        if (walk.seq > 0 && !warp_wait(&sh.q_empty, (walk.seq - 1) & 1, abort_flag, lane)) return;
+        load_queries<KB>(t, im, q_img, which, lane);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_full);
+        for (int u = 0; u < im.n_tiles; ++u, entry += 2) {
+            if (u < im.looked) continue;
+            const int stage = (entry + 1) % NS;
+            // The MMA warp says when: it has seen the tile land and does not go on before this is done, so that the stage's
+            // barrier stands at this entry's phase and not two away.
+            if (!warp_wait(&sh.look[stage], look_phase >> stage & 1u, abort_flag, lane)) return;
+            look_phase ^= 1u << stage;
+            if (!warp_wait(&sh.full[stage], ((entry + 1) / NS) & 1, abort_flag, lane)) return;
+            uint4 *tile = reinterpret_cast<uint4 *>(ring + stage * kStage) + which * (kStage / 32);
+            uint32_t found = 0;
+#pragma unroll 4
+            for (int y = lane; y < kStage / 32; y += 32) {
+                const uint4 v = tile[y];
+                const uint32_t e = 0x7f807f80u;
+                const uint32_t bx = __vcmpeq2(v.x & e, e), by = __vcmpeq2(v.y & e, e), bz = __vcmpeq2(v.z & e, e), bw = __vcmpeq2(v.w & e, e);
+                if (bx | by | bz | bw) {
+                    found = 1;
+                    tile[y] = make_uint4(v.x & ~bx, v.y & ~by, v.z & ~bz, v.w & ~bw);
+                }
+            }
+            if (found) *static_cast<volatile int *>(&sh.poison[walk.seq % kMaskSlots]) = walk.seq + 1;
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.clean[stage]);
+        }
+        ++walk.seq;
+    }
+}
+
+template <int KB>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ TcAttnArgs t)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Shared sh;
+    constexpr int NS = stages_for(KB), kStage = KB * kRegion;
+    uint8_t *q_img = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023u) & ~uintptr_t(1023u));
+    uint8_t *ring = q_img + 2 * kStage;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_trigger();
+    if (threadIdx.x == 0) {
+        mbar_init(&sh.q_full, 2);
+        mbar_init(&sh.q_empty, 1);
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 1);
+            mbar_init(&sh.look[i], 1);
+            mbar_init(&sh.clean[i], 2);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sh.s_full[x], 1);
+            mbar_init(&sh.p_full[x], 4);
+            mbar_init(&sh.pv_done[x], 1);
+            mbar_init(&sh.o_free[x], 4);
+        }
+        fence_barrier_init();
+        sh.abort = 0;
+        for (int i = 0; i < kMaskSlots; ++i) sh.poison[i] = 0;
+    }
+    // Tensor memory only behind the wait: the kernel in front may still need all of it on this SM.
+    pdl_wait();
+    if (warp == 8) tmem_alloc(&sh.tmem_base, kTmemCols);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = sh.tmem_base;
+    if (warp < 4) {
+        softmax_warps<KB, 0>(t, sh, tmem);
+    } else if (warp < 8) {
+        softmax_warps<KB, 1>(t, sh, tmem);
+    } else if (warp == 8) {
+        mma_warp<KB>(t, sh, q_img, ring, tmem);
+    } else if (warp == 9) {
+        if (lane == 0) {
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&v_map);
+        }
+        const uint32_t issued = load_warp<KB>(t, sh, &k_map, &v_map, ring);
+        // nothing of this block may be in flight when it ends: the last MMAs must have released their stages; after a
+        // failed wait, the loads already issued must still land
+        for (uint32_t e = issued > NS ? issued - NS : 0; e < issued; ++e) {
+            const int st = e % NS;
+            if (!warp_wait(&sh.empty[st], (e / NS) & 1, &sh.abort, lane)) {
+                volatile int never = 0;
+                warp_wait(&sh.full[st], (e / NS) & 1, &never, lane);
+            }
+        }
+        if (lane == 0 && *static_cast<volatile int *>(&sh.abort) && t.a.status) atomicOr(t.a.status, kStatusWaitExpired);
+    } else {
+        helper_warp<KB>(t, sh, q_img, ring, warp - 10);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 8) tmem_dealloc(sh.tmem_base, kTmemCols);
+}
+
+template <int KB>
+int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream)
+{
+    constexpr size_t smem = 1024 + (size_t)(2 + stages_for(KB)) * KB * kRegion;
+    static_assert(smem + sizeof(Shared) <= 232448, "shared memory of a block");
+    static SmemAsked asked;
+    int dev = 0, sms = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (err == cudaSuccess) err = allow_smem(attn_tc_kernel<KB>, smem, asked);
+    const long long grid = t.items < sms ? t.items : sms;
+    if (err == cudaSuccess) err = launch_pdl(attn_tc_kernel<KB>, dim3((unsigned)grid), kThreads, smem, stream, 1, k_map, v_map, t);
+    if (err == cudaSuccess) count_launches(1);
+    return check_cuda(err, "tensor-core attention kernel");
+}
+
+}  // namespace
+
+// Shapes that the kernel takes; a layout that no tensor map describes is found out at launch (WKV_ERR_UNSUPPORTED).
+bool attn_tc_supported(const AttnArgs &a, int dtype)
+{
+    if (dtype != WKV_BF16 || (a.d != 64 && a.d != 128) || a.G > kTile) return false;
+    // a key tile is one box: tensors of fewer rows are left to the other kernels, which are as fast there
+    if (!a.table && (a.cu_q ? a.total_q : a.max_q) < kTile) return false;
+    // a tile's rows come in boxes of whole pages or parts of one; the swizzle's pattern repeats every eight rows
+    if (a.table && !(a.page_size % kTile == 0 || (kTile % a.page_size == 0 && a.page_size >= 8))) return false;
+    int dev = 0, major = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return false;
+    }
+    return major == 10;
+}
+
+int launch_attn_tc(const AttnArgs &a, cudaStream_t stream)
+{
+    TcAttnArgs t;
+    t.a = a;
+    t.ppt = kTile / a.G;
+    const long long units = (long long)a.batch * a.hkv;
+    t.max_pairs = (a.max_q + 2 * t.ppt - 1) / (2 * t.ppt);
+    t.items = units * t.max_pairs;
+    t.box_rows = a.table && a.page_size < kTile ? a.page_size : kTile;
+    alignas(64) CUtensorMap k_map, v_map;
+    const unsigned long long tokens = a.cu_q ? a.total_q : a.max_q, batch = a.cu_q ? 1 : a.batch;
+    if (a.cu_q && a.total_q == 0) return WKV_OK;
+    const RowDim k_dims[3] = {{a.table ? (unsigned long long)a.page_size : tokens, (unsigned long long)a.kt * 2, (unsigned)t.box_rows},
+                              {(unsigned long long)a.hkv, (unsigned long long)a.kh * 2, 1},
+                              {a.table ? (unsigned long long)a.num_pages : batch, (unsigned long long)a.kb * 2, 1}};
+    if (!make_row_tensor_map(a.k, a.d, k_dims, &k_map, t.k_slot) || !make_row_tensor_map(a.v, a.d, k_dims, &v_map, t.k_slot))
+        return WKV_ERR_UNSUPPORTED;
+    return a.d == 128 ? launch_kb<2>(t, k_map, v_map, stream) : launch_kb<1>(t, k_map, v_map, stream);
+}
+
+}  // namespace wkv

@@ -339,6 +339,7 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
             shorter |= (s->cu_seqlens_host ? s->cu_seqlens_host[b + 1] - s->cu_seqlens_host[b] : s->max_seqlen) < s->l_obs;
         if (shorter && (st = launch_attn_lse_obs_fill(a, stream)) != WKV_OK) return st;
     }
+    if (attn_tc_supported(a, s->dtype) && (st = launch_attn_tc(a, stream)) != WKV_ERR_UNSUPPORTED) return st;
     return launch_attn_simt(a, s->dtype, stream);
 }
 
@@ -484,8 +485,12 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
     a.weights_in = weights_in;
     a.weights_out = weights_out;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if ((st = launch_attn_simt(a, c->dtype, stream)) != WKV_OK) return st;
-    if (a.splits > 1 && (st = launch_attn_join(a, c->dtype, stream)) != WKV_OK) return st;
+    st = p.rows_max > 32 && attn_tc_supported(a, c->dtype) ? launch_attn_tc(a, stream) : WKV_ERR_UNSUPPORTED;
+    if (st == WKV_ERR_UNSUPPORTED) {
+        st = launch_attn_simt(a, c->dtype, stream);
+        if (st == WKV_OK && a.splits > 1) st = launch_attn_join(a, c->dtype, stream);
+    }
+    if (st != WKV_OK) return st;
     if (weights_out) return launch_attn_weights(a, c->dtype, stream);
     return WKV_OK;
 }
