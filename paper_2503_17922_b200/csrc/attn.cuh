@@ -37,7 +37,8 @@ struct AttnArgs {
     float *part_o;               // [units][rows_max][splits][d]: not yet normalised
     float2 *part_ml;             // [units][rows_max][splits]: (maximum in base 2, sum)
     int rows_max;                // max_q * G
-    float *logits;               // [units][rows_max][cap] in base 2, or null: for the weights
+    float *logits;               // [units][rows_max][logit_stride] in base 2, or null: for the weights
+    long long logit_stride;      // cap, rounded up to a multiple of four
     const float *weights_in;     // [units][cap] or null
     float *weights_out;          // [units][cap] or null
 };
@@ -102,8 +103,9 @@ inline cudaError_t allow_smem(K kernel, size_t bytes, SmemAsked &asked)
 // kernels (each returns a wkv_status)
 bool attn_tc_supported(const AttnArgs &a, int dtype);
 int launch_attn_tc(const AttnArgs &a, cudaStream_t stream);          // WKV_ERR_UNSUPPORTED: a layout that no tensor map describes
+int launch_attn_mma(const AttnArgs &a, cudaStream_t stream);         // bf16
 int launch_attn_simt(const AttnArgs &a, int dtype, cudaStream_t stream);
-int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream);
+int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream);       // with a.logits: and the weights
 int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream);    // reads a.lse
 int launch_attn_lse_obs_fill(const AttnArgs &a, cudaStream_t stream);
 

@@ -204,6 +204,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         if (a.splits > 1) {
             const long long at = ((long long)unit * a.rows_max + row) * a.splits + split;
             if (tx == 0) a.part_ml[at] = make_float2(m[r], l[r]);
+            if (l[r] == 0.f) continue;
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
                 const int c = tx * 4 + 64 * x;
@@ -281,14 +282,8 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
 
 // Joins the parts of every row: o = sum exp2(m_s - M) o_s / sum exp2(m_s - M) l_s.  A warp per row, splits in order.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_constant__ AttnArgs a)
+__device__ __forceinline__ float join_row(const AttnArgs &a, const AttnSeq &sq, int unit, int b, int h, int row, int lane, bool write)
 {
-    pdl_trigger();
-    pdl_wait();
-    const int unit = blockIdx.x % (a.batch * a.hkv), b = unit / a.hkv, h = unit - b * a.hkv;
-    const int lane = threadIdx.x & 31, row = (int)(blockIdx.x / (a.batch * a.hkv)) * (kThreads / 32) + (threadIdx.x >> 5);
-    const AttnSeq sq = attn_seq(a, b, h);
-    if (row >= sq.m * a.G) return;
     const int i = row / a.G, hq = h * a.G + row - i * a.G;
     const long long at = ((long long)unit * a.rows_max + row) * a.splits;
     float top = -INFINITY;
@@ -296,16 +291,22 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_consta
 #pragma unroll
     for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
     const float ref = top == -INFINITY ? 0.f : top;
+    // every lane its splits, then over the lanes: one order, whatever the launch
     float l = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
+    for (int s = lane; s < a.splits; s += 32) {
         const float2 ml = a.part_ml[at + s];
         l += ml.y * exp2f(ml.x - ref);
     }
-    if (lane == 0) attn_store_lse(a, b, hq, i, sq.m, l > 0.f || l != l ? top + log2f(l) : -INFINITY);
+#pragma unroll
+    for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    const float lse2 = l > 0.f || l != l ? top + log2f(l) : -INFINITY;
+    if (!write) return lse2;
+    if (lane == 0) attn_store_lse(a, b, hq, i, sq.m, lse2);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T *dst = static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh;
     for (int c = lane * 4; c < a.d; c += 128) {
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
         for (int s = 0; s < a.splits; ++s) {
             const float2 ml = a.part_ml[at + s];
             if (ml.y == 0.f) continue;                                   // a part without a key of the row
@@ -324,6 +325,54 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_consta
         if (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst + c) = *reinterpret_cast<float4 *>(y);
         else *reinterpret_cast<uint2 *>(dst + c) = *reinterpret_cast<uint2 *>(y);
     }
+    return lse2;
+}
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_constant__ AttnArgs a)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x % (a.batch * a.hkv), b = unit / a.hkv, h = unit - b * a.hkv;
+    const int lane = threadIdx.x & 31, row = (int)(blockIdx.x / (a.batch * a.hkv)) * (kThreads / 32) + (threadIdx.x >> 5);
+    const AttnSeq sq = attn_seq(a, b, h);
+    if (row < sq.m * a.G) join_row<T>(a, sq, unit, b, h, row, lane, true);
+}
+// The same for up to 16 rows whose logits are in the workspace: block (unit, y) also adds up the weights of kJoinKeys keys.  Every
+// block of a unit needs the rows' normalisers and joins the few parts for itself; block 0 writes the rows.
+constexpr int kJoinKeys = 4 * kThreads;
+template <typename T>
+__global__ void __launch_bounds__(kThreads) attn_join_weights_kernel(const __grid_constant__ AttnArgs a)
+{
+    __shared__ float lse2[16];
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x, b = unit / a.hkv, h = unit - b * a.hkv;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const AttnSeq sq = attn_seq(a, b, h);
+    const int rows = sq.m * a.G;
+    if (blockIdx.y > 0 && (int)blockIdx.y * kJoinKeys >= sq.n) return;
+    for (int row = warp; row < rows; row += kThreads / 32) {
+        const float x = join_row<T>(a, sq, unit, b, h, row, lane, blockIdx.y == 0);
+        if (lane == 0) lse2[row] = x;
+    }
+    __syncthreads();
+    const int j = (int)blockIdx.y * kJoinKeys + threadIdx.x * 4;
+    if (j >= sq.n) return;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    const float *x = a.logits + (long long)unit * a.rows_max * a.logit_stride + j;
+    for (int row = 0; row < rows; ++row) {
+        const float ref = lse2[row];
+        if (ref == -INFINITY) continue;                                  // the row attends to nothing
+        const float4 s = *reinterpret_cast<const float4 *>(x + row * a.logit_stride);
+        w[0] += exp2f(s.x - ref);
+        w[1] += exp2f(s.y - ref);
+        w[2] += exp2f(s.z - ref);
+        w[3] += exp2f(s.w - ref);
+    }
+    const long long at = (long long)unit * a.cap + j;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (j + e < sq.n) a.weights_out[at + e] = (a.weights_in ? a.weights_in[at + e] : 0.f) + w[e];
 }
 
 // -infinity where an observation row would lie in front of its sequence
@@ -386,7 +435,22 @@ int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream)
 }
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
 {
-    const long long per = kThreads / 32, blocks = ((long long)a.rows_max + per - 1) / per * a.batch * a.hkv;
+    const int units = a.batch * a.hkv;
+    if (a.logits) {
+        const int blocks = (a.cap + kJoinKeys - 1) / kJoinKeys;
+        if (blocks > 65535) {
+            set_error_detail("attention weights: %d rows of a unit", a.cap);
+            return WKV_ERR_LIMIT;
+        }
+        const dim3 grid(units, blocks);
+        return dtype == WKV_F32 ? launch(attn_join_weights_kernel<float>, grid, 0, a, stream, "attention joining kernel")
+                                : launch(attn_join_weights_kernel<__nv_bfloat16>, grid, 0, a, stream, "attention joining kernel");
+    }
+    const long long per = kThreads / 32, blocks = ((long long)a.rows_max + per - 1) / per * units;
+    if (blocks > 0x7fffffffLL) {
+        set_error_detail("attention: %lld blocks", blocks);
+        return WKV_ERR_LIMIT;
+    }
     const dim3 grid((unsigned)blocks);
     return dtype == WKV_F32 ? launch(attn_join_kernel<float>, grid, 0, a, stream, "attention joining kernel")
                             : launch(attn_join_kernel<__nv_bfloat16>, grid, 0, a, stream, "attention joining kernel");

@@ -119,33 +119,41 @@ int resolve_paged(const wkv_paged *c, Paged &p)
 // Workspace of the paged entry points: status word, then what an attention or an eviction leaves between its kernels.
 struct PagedWorkspace {
     int splits;
-    size_t lse_off, ml_off, o_off, counts_off, moves_off, total;
+    size_t lse_off, ml_off, o_off, logits_off, counts_off, moves_off, total;
+    long long logit_stride;      // 0: the weights are computed from K once more
     int moves_max;
 };
-// Key splits: so many blocks that every SM has two, but none with fewer than 256 keys.
-constexpr int kSplitBlocks = 2 * 148, kSplitKeys = 256;
-int plan_splits(const wkv_paged *c, const Paged &p)
+// Key splits of the kernels that take one tile of rows per block: two blocks for every SM, where each then has a tile of 64
+// keys at least; and with 1,024 keys or more to each, up to four times as many, so that sequences of different lengths
+// even out.
+constexpr int kSplitBlocks = 2 * 148, kSplitKeys = 64, kSplitEven = 1024;
+int plan_splits(const Paged &p)
 {
-    (void)c;
     const int tile = p.rows_max <= 16 ? 16 : 64;
     const long long blocks = ((long long)p.rows_max + tile - 1) / tile * p.units;
     long long s = (kSplitBlocks + blocks - 1) / blocks;
-    const long long most = (p.cap + kSplitKeys - 1) / kSplitKeys;
-    if (s > most) s = most;
+    if (s > (p.cap + kSplitKeys - 1) / kSplitKeys) s = (p.cap + kSplitKeys - 1) / kSplitKeys;
+    while (blocks * s < 4 * kSplitBlocks && p.cap / (s + 1) >= kSplitEven) ++s;
     return s < 1 ? 1 : (int)s;
 }
+// Rows per unit whose logits are kept for the weights: 4 bytes for each beside the 2 * d * 2 of K and V, written and read.
+constexpr int kLogitRows = 16;
 PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
 {
     PagedWorkspace w;
-    w.splits = plan_splits(c, p);
+    w.splits = plan_splits(p);
     size_t off = 256;
     w.lse_off = off;
     off = align_up(off + (size_t)c->batch * c->n_q_heads * c->max_new * sizeof(float), 256);
-    const size_t parts = w.splits > 1 ? (size_t)p.units * p.rows_max * w.splits : 0;
+    const bool keeps_logits = c->dtype == WKV_BF16 && p.rows_max <= kLogitRows;
+    const size_t parts = w.splits > 1 || keeps_logits ? (size_t)p.units * p.rows_max * w.splits : 0;
     w.ml_off = off;
     off = align_up(off + parts * sizeof(float2), 256);
     w.o_off = off;
     off = align_up(off + parts * c->head_dim * sizeof(float), 256);
+    w.logits_off = off;
+    w.logit_stride = keeps_logits ? ((long long)p.cap + 3) / 4 * 4 : 0;
+    off = align_up(off + (size_t)p.units * p.rows_max * w.logit_stride * sizeof(float), 256);
     w.total = off;
     w.moves_max = p.cap / 2 + 1;
     off = 256;
@@ -340,7 +348,7 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
         if (shorter && (st = launch_attn_lse_obs_fill(a, stream)) != WKV_OK) return st;
     }
     if (attn_tc_supported(a, s->dtype) && (st = launch_attn_tc(a, stream)) != WKV_ERR_UNSUPPORTED) return st;
-    return launch_attn_simt(a, s->dtype, stream);
+    return s->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, s->dtype, stream);
 }
 
 size_t wkv_paged_workspace_bytes(const wkv_paged *c)
@@ -485,13 +493,18 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
     a.weights_in = weights_in;
     a.weights_out = weights_out;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (weights_out && w.logit_stride) {
+        a.logits = reinterpret_cast<float *>(ws + w.logits_off);
+        a.logit_stride = w.logit_stride;
+    }
+    // Up to 16 rows are one tile of the warp-level kernel, whose time is that of the loads.
     st = p.rows_max > 32 && attn_tc_supported(a, c->dtype) ? launch_attn_tc(a, stream) : WKV_ERR_UNSUPPORTED;
     if (st == WKV_ERR_UNSUPPORTED) {
-        st = launch_attn_simt(a, c->dtype, stream);
-        if (st == WKV_OK && a.splits > 1) st = launch_attn_join(a, c->dtype, stream);
+        st = c->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, c->dtype, stream);
+        if (st == WKV_OK && (a.splits > 1 || a.logits)) st = launch_attn_join(a, c->dtype, stream);
     }
     if (st != WKV_OK) return st;
-    if (weights_out) return launch_attn_weights(a, c->dtype, stream);
+    if (weights_out && !a.logits) return launch_attn_weights(a, c->dtype, stream);
     return WKV_OK;
 }
 
