@@ -151,8 +151,32 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 }
 
 // ---- the softmax of one query tile ------------------------------------------------------------
-template <int KB, int x>
-__device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, uint32_t tmem)
+// S is read twice, 32 columns at a time, for the maximum and for the exponentials: a row of 128 in registers takes more of them than
+// a thread has, and the code of a row in one piece more than the instruction cache holds (8,192 tokens of 32 heads: 1,010 us).
+struct RowMask {
+    uint4 bits;              // of the tile's 128 keys: those that the row sees
+    __device__ __forceinline__ uint32_t of(int y) const { return y == 0 ? bits.x : (y == 1 ? bits.y : (y == 2 ? bits.z : bits.w)); }
+};
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u); }
+__device__ __forceinline__ void hide(float (&v)[32], uint32_t seen)
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = seen >> j & 1u ? v[j] : -INFINITY;
+}
+
+__device__ __forceinline__ float largest(float top, const float (&v)[32])
+{
+    float t0 = top, t1 = v[0];
+#pragma unroll
+    for (int j = 1; j < 31; j += 2) {
+        if (j & 2) t0 = fmaxf(t0, fmaxf(v[j], v[j + 1]));
+        else t1 = fmaxf(t1, fmaxf(v[j], v[j + 1]));
+    }
+    return fmaxf(t0, fmaxf(t1, v[31]));
+}
+
+template <int KB>
+__device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, int x, uint32_t tmem)
 {
     constexpr int D = KB * 64;
     const AttnArgs &a = t.a;
@@ -162,52 +186,56 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, u
     const int place = row / a.G, head = row - place * a.G;
     const bool of_tile = row < t.ppt * a.G;
     const float c = a.scale_log2;
+    const unsigned long long c2 = pair_of(c, c);
     uint32_t turn = 0, tiles_before = 0;            // tiles of S taken so far; key tiles of the items so far
     volatile int *const abort_flag = &sh.abort;
     Walk walk;
     Item im;
     while (walk.next(t, im)) {
-        const int pos = im.pos0 + x * t.ppt + place;
-        const bool mine = of_tile && place < im.rows[x];
+        const int pos = im.pos0 + x * t.ppt + place, tiles = x ? im.tiles[1] : im.tiles[0];
+        const bool mine = of_tile && place < (x ? im.rows[1] : im.rows[0]);
         const int limit = mine ? min(im.base + pos, im.sq.n) : 0;
         const int plain = (im.base + im.pos0 + x * t.ppt) / kTile;         // tiles that every row of this query tile sees all of
         float m = -INFINITY, l = 0.f;
-        for (int u = 0; u < im.tiles[x]; ++u, ++turn) {
+        for (int u = 0; u < tiles; ++u, ++turn) {
             if (!warp_wait(&sh.s_full[x], turn & 1, abort_flag, lane)) return;
             tc_fence_after_sync();
-            float s[4][32];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) tmem_ld32_issue(s_addr + y * 32, s[y]);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) tmem_ld_wait(s[y]);
+            RowMask seen = {make_uint4(~0u, ~0u, ~0u, ~0u)};
+            bool masked = u >= plain;
             if (a.table) {
-                const uint4 have = sh.present[(tiles_before + u) % kMaskSlots];
-                if ((have.x & have.y & have.z & have.w) != ~0u) {
+                seen.bits = sh.present[(tiles_before + u) % kMaskSlots];
+                masked |= (seen.bits.x & seen.bits.y & seen.bits.z & seen.bits.w) != ~0u;
+            }
+            if (masked) {
+                const int in_tile = limit - u * kTile;
+                seen.bits.x &= first_bits(in_tile);
+                seen.bits.y &= first_bits(in_tile - 32);
+                seen.bits.z &= first_bits(in_tile - 64);
+                seen.bits.w &= first_bits(in_tile - 96);
+            }
+            // (A load in flight never crosses a branch: its registers must not be touched, or moved, before the wait.)
+            float grown = m;
+            if (!masked) {
+                float v0[32], v1[32];
+                tmem_ld32_issue(s_addr, v0);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        if (!(have.x >> j & 1u)) s[0][j] = -INFINITY;
-                        if (!(have.y >> j & 1u)) s[1][j] = -INFINITY;
-                        if (!(have.z >> j & 1u)) s[2][j] = -INFINITY;
-                        if (!(have.w >> j & 1u)) s[3][j] = -INFINITY;
-                    }
+                for (int y = 0; y < 4; y += 2) {
+                    tmem_ld_wait(v0);
+                    tmem_ld32_issue(s_addr + y * 32 + 32, v1);
+                    grown = largest(grown, v0);
+                    tmem_ld_wait(v1);
+                    if (y == 0) tmem_ld32_issue(s_addr + 64, v0);
+                    grown = largest(grown, v1);
+                }
+            } else {
+#pragma unroll 1
+                for (int y = 0; y < 4; ++y) {
+                    float v[32];
+                    tmem_ld32(s_addr + y * 32, v);
+                    hide(v, seen.of(y));
+                    grown = largest(grown, v);
                 }
             }
-            if (u >= plain) {
-                const int in_tile = limit - u * kTile;
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (y * 32 + j >= in_tile) s[y][j] = -INFINITY;
-            }
-            float top[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                top[y] = s[y][0];
-#pragma unroll
-                for (int j = 1; j < 32; ++j) top[y] = fmaxf(top[y], s[y][j]);
-            }
-            const float grown = fmaxf(fmaxf(m, fmaxf(top[0], top[1])), fmaxf(top[2], top[3]));
             const bool follow = (grown - m) * c > kLazy;          // (also from -infinity on)
             if (u == 0) {
                 m = grown;
@@ -228,30 +256,50 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, u
                 }
             }
             const float ref = m == -INFINITY ? 0.f : -m * c;
-            const unsigned long long c2 = pair_of(c, c), ref2 = pair_of(ref, ref);
-            unsigned long long sum[2] = {0ull, 0ull};
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
+            const unsigned long long ref2 = pair_of(ref, ref);
+            unsigned long long sum0 = 0ull, sum1 = 0ull;
+            auto weights = [&](float(&v)[32], int y) {
                 uint32_t p[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float *v = &s[y][2 * j];
-                    const float2 e = halves_of(fma_pair(pair_of(v[0], v[1]), c2, ref2));
+                    const float2 e = halves_of(fma_pair(pair_of(v[2 * j], v[2 * j + 1]), c2, ref2));
                     const float p0 = fast_exp2(e.x), p1 = fast_exp2(e.y);
-                    sum[j & 1] = add_pair(sum[j & 1], pair_of(p0, p1));
+                    if (j & 1) sum1 = add_pair(sum1, pair_of(p0, p1));
+                    else sum0 = add_pair(sum0, pair_of(p0, p1));
                     p[j] = pack_bf16(p0, p1);
                 }
                 tmem_st16(s_addr + y * 16, p);
+            };
+            if (!masked) {
+                float v0[32], v1[32];
+                tmem_ld32_issue(s_addr, v0);
+#pragma unroll
+                for (int y = 0; y < 4; y += 2) {
+                    tmem_ld_wait(v0);
+                    tmem_ld32_issue(s_addr + y * 32 + 32, v1);
+                    weights(v0, y);
+                    tmem_ld_wait(v1);
+                    if (y == 0) tmem_ld32_issue(s_addr + 64, v0);
+                    weights(v1, y + 1);
+                }
+            } else {
+#pragma unroll 1
+                for (int y = 0; y < 4; ++y) {
+                    float v[32];
+                    tmem_ld32(s_addr + y * 32, v);
+                    hide(v, seen.of(y));
+                    weights(v, y);
+                }
             }
             tmem_st_wait();
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.p_full[x]);
-            const float2 s0 = halves_of(sum[0]), s1 = halves_of(sum[1]);
+            const float2 s0 = halves_of(sum0), s1 = halves_of(sum1);
             l += (s0.x + s0.y) + (s1.x + s1.y);
         }
         // ---- the item's rows: O / l -------------------------------------------------------------
-        const bool any = im.tiles[x] > 0;
+        const bool any = tiles > 0;
         const int hq = im.h * a.G + head;
         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (im.sq.q_off + pos) * a.ot + im.b * a.ob + (long long)hq * a.oh;
         if (any) {
@@ -550,10 +598,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
-    if (warp < 4) {
-        softmax_warps<KB, 0>(t, sh, tmem);
-    } else if (warp < 8) {
-        softmax_warps<KB, 1>(t, sh, tmem);
+    if (warp < 8) {
+        softmax_warps<KB>(t, sh, warp >> 2, tmem);
     } else if (warp == 8) {
         mma_warp<KB>(t, sh, q_img, ring, tmem);
     } else if (warp == 9) {
