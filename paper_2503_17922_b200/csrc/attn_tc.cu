@@ -13,8 +13,8 @@
 // P is rounded to bf16 for the product (as its operand has to be); sum, maximum and O are fp32, the sum of the unrounded P.
 //
 // Warps: 0-3 and 4-7 the softmax of the two query tiles (thread = row), 8 issues the MMAs, 9 the TMA loads (keys and values of a
-// tile in turn through one ring), 10 and 11 look through the values of tiles that hold rows which some query does not see: P is 0 there,
-// but 0 times an infinity or NaN is not.  Such elements are replaced by 0 in shared memory, and the rows that do see them
+// tile in turn through one ring), 10 and 11 load the queries and look through the values of tiles that hold rows which some query
+// does not see: P is 0 there, but 0 times an infinity or NaN is not.  Such elements are replaced by 0 in shared memory, and the rows that do see them
 // get them added at the end.
 //
 // Blocks are persistent, one per SM; the items come in order of descending work and are dealt to the blocks back and forth.
@@ -23,6 +23,8 @@
 #include "score_math.cuh"
 #include "tc_common.cuh"
 #include "tensor_map.cuh"
+
+#include <type_traits>
 
 namespace wkv {
 namespace {
@@ -35,6 +37,8 @@ constexpr int kRegion = kTile * 128;          // bytes of 64 columns of a tile
 constexpr uint32_t kTmemCols = 512;           // all of it: S/P of the two query tiles (128 columns each), O of both (128 each)
 constexpr int kMaxStages = 8;
 constexpr int kMaskSlots = 8;
+constexpr int kFmaEvery = 8;                  // one pair of exponentials in so many on the FMA pipe (measured below)
+constexpr int kFirst = 2;                     // 32-key pieces of a tile whose product begins while the others' weights are computed
 constexpr float kLazy = 8.f;                  // exponent by which the maximum may be outgrown
 __host__ __device__ constexpr int stages_for(int kb) { return kb == 2 ? 5 : 8; }
 struct TcAttnArgs {
@@ -49,7 +53,7 @@ struct TcAttnArgs {
 struct Shared {
     uint64_t q_full, q_empty;
     uint64_t full[kMaxStages], empty[kMaxStages], look[kMaxStages], clean[kMaxStages];
-    uint64_t s_full[2], p_full[2], pv_done[2], o_free[2];
+    uint64_t s_full[2], p_part[2], p_full[2], pv_done[2], o_free[2];
     uint32_t tmem_base;
     int abort;
     int poison[kMaskSlots];                        // item whose values held an infinity or NaN in a tile that was looked through
@@ -106,9 +110,9 @@ struct Walk {
     }
 };
 
-// A whole warp waits.  The phase is looked at without suspending the thread: with a suspended wait the MMA warp, which waits
-// five times per key tile, came back as much as 2,000 cycles after the phase had completed.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int)
+// A whole warp waits.  The phase is looked at without suspending the thread: a suspended one came back as much as 2,000 cycles
+// after the phase had completed, and the MMA warp waits five times per key tile.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
 {
     const uint32_t addr = smem_u32(bar);
     unsigned long long t0 = 0;
@@ -182,6 +186,29 @@ __device__ __forceinline__ void hide(float (&v)[32], uint32_t seen)
     for (int j = 0; j < 32; ++j) v[j] = seen >> j & 1u ? v[j] : -INFINITY;
 }
 
+// 2^x of two values on the FMA pipe: 2^t * 2^f with t the nearest integer, 2^f by a polynomial of degree five (a Remez fit of the
+// relative error on [-1/2, 1/2], 7.5e-8; evaluated in fp32 2.1e-7).  x is at most kLazy; below -126 it counts as -126, so
+// that a weight of 0 comes out as 1e-38 (rows that see nothing of a tile do not come here); a NaN stays one.
+__device__ __forceinline__ unsigned long long exp2_pair_fma(unsigned long long x2)
+{
+    float2 x = halves_of(x2);
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(x.x));      // -126
+    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(x.y));
+    auto both = [](float v) { return pair_of(v, v); };
+    x2 = pair_of(x.x, x.y);
+    const unsigned long long shifted = add_pair(x2, both(12582912.f));            // 1.5 * 2^23: the integer is in the low bits
+    const unsigned long long f = fma_pair(add_pair(shifted, both(-12582912.f)), both(-1.f), x2);
+    unsigned long long p = both(1.3276472e-3f);
+    p = fma_pair(p, f, both(9.675541e-3f));
+    p = fma_pair(p, f, both(5.550713e-2f));
+    p = fma_pair(p, f, both(2.402212e-1f));
+    p = fma_pair(p, f, both(6.9314694e-1f));
+    p = fma_pair(p, f, both(1.0000001f));
+    const float2 s = halves_of(shifted);
+    return fma_pair(p, pair_of(__int_as_float((__float_as_int(s.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(s.y) << 23) + 0x3f800000)),
+                    0ull);
+}
+
 __device__ __forceinline__ float largest(float top, const float (&v)[32])
 {
     float t0 = top, t1 = v[0];
@@ -216,7 +243,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
         const int plain = (im.base + im.pos0 + x * t.ppt) / kTile;         // tiles that every row of this query tile sees all of
         float m = -INFINITY, l = 0.f;
         for (int u = 0; u < tiles; ++u, ++turn) {
-            if (!warp_wait(&sh.s_full[x], turn & 1, abort_flag, lane)) return;
+            if (!warp_wait(&sh.s_full[x], turn & 1, abort_flag)) return;
             tc_fence_after_sync();
             RowMask seen = {make_uint4(~0u, ~0u, ~0u, ~0u)};
             bool masked = u >= plain;
@@ -258,7 +285,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
             if (u == 0) {
                 m = grown;
             } else if (__any_sync(0xffffffffu, follow)) {
-                if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag, lane)) return;
+                if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag)) return;
                 tc_fence_after_sync();
                 const float f = follow ? exp2f((m - grown) * c) : 1.f;
                 if (follow) m = grown;
@@ -276,17 +303,24 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
             const float ref = m == -INFINITY ? 0.f : -m * c;
             const unsigned long long ref2 = pair_of(ref, ref);
             unsigned long long sum0 = 0ull, sum1 = 0ull;
-            auto weights = [&](float(&v)[32], int y) {
+            auto weights = [&](float(&v)[32], int y, auto all_seen) {
                 uint32_t p[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float2 e = halves_of(fma_pair(pair_of(v[2 * j], v[2 * j + 1]), c2, ref2));
-                    const float p0 = fast_exp2(e.x), p1 = fast_exp2(e.y);
-                    if (j & 1) sum1 = add_pair(sum1, pair_of(p0, p1));
-                    else sum0 = add_pair(sum0, pair_of(p0, p1));
-                    p[j] = pack_bf16(p0, p1);
+                    const unsigned long long e2 = fma_pair(pair_of(v[2 * j], v[2 * j + 1]), c2, ref2), w2 = decltype(all_seen)::value && j % kFmaEvery == kFmaEvery - 1 ? exp2_pair_fma(e2) : exp2_pair(e2);
+                    if (j & 1) sum1 = add_pair(sum1, w2);
+                    else sum0 = add_pair(sum0, w2);
+                    const float2 w = halves_of(w2);
+                    p[j] = pack_bf16(w.x, w.y);
                 }
                 tmem_st16(s_addr + y * 16, p);
+            };
+            // the product of the first keys may begin while the others' weights are computed
+            auto first_part = [&]() {
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.p_part[x]);
             };
             if (!masked) {
                 float v0[32], v1[32];
@@ -295,10 +329,12 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                 for (int y = 0; y < 4; y += 2) {
                     tmem_ld_wait(v0);
                     tmem_ld32_issue(s_addr + y * 32 + 32, v1);
-                    weights(v0, y);
+                    weights(v0, y, std::true_type{});
+                    if (y + 1 == kFirst) first_part();
                     tmem_ld_wait(v1);
                     if (y == 0) tmem_ld32_issue(s_addr + 64, v0);
-                    weights(v1, y + 1);
+                    weights(v1, y + 1, std::true_type{});
+                    if (y + 2 == kFirst) first_part();
                 }
             } else {
 #pragma unroll 1
@@ -306,7 +342,8 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                     float v[32];
                     tmem_ld32(s_addr + y * 32, v);
                     hide(v, seen.of(y));
-                    weights(v, y);
+                    weights(v, y, std::false_type{});
+                    if (y + 1 == kFirst) first_part();
                 }
             }
             tmem_st_wait();
@@ -321,7 +358,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
         const int hq = im.h * a.G + head;
         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (im.sq.q_off + pos) * a.ot + im.b * a.ob + (long long)hq * a.oh;
         if (any) {
-            if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag, lane)) return;
+            if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag)) return;
             tc_fence_after_sync();
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -368,6 +405,8 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
 }
 
 // ---- MMAs --------------------------------------------------------------------------------------
+// One warp issues for both query tiles in turn, which keeps them half a step apart: with a warp for each they fell into step, both
+// at their exponentials or both at their products (8,192 tokens of 32 heads: 683 us against 617).
 template <int KB>
 __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, uint32_t tmem)
 {
@@ -392,46 +431,51 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
     };
     while (walk.next(t, im)) {
         if (im.n_tiles == 0) continue;
-        if (!warp_wait(&sh.q_full, walk.seq & 1, abort_flag, lane)) return;
-        int stage = entry % NS;
-        if (!warp_wait(&sh.full[stage], (entry / NS) & 1, abort_flag, lane)) return;
+        if (!warp_wait(&sh.q_full, walk.seq & 1, abort_flag)) return;
+        const int first = entry % NS;
+        if (!warp_wait(&sh.full[first], (entry / NS) & 1, abort_flag)) return;
         tc_fence_after_sync();
         // (S of the last item's last tile has been read: its P was waited for)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-            if (im.tiles[x] > 0) scores(x, stage);
-        umma_commit_if(leader, &sh.empty[stage]);
+            if (im.tiles[x] > 0) scores(x, first);
+        umma_commit_if(leader, &sh.empty[first]);
         if (im.n_tiles == 1) umma_commit_if(leader, &sh.q_empty);
         ++entry;
         for (int u = 0; u < im.n_tiles; ++u) {
             const int v_stage = entry % NS;
-            if (!warp_wait(&sh.full[v_stage], (entry / NS) & 1, abort_flag, lane)) return;
+            if (!warp_wait(&sh.full[v_stage], (entry / NS) & 1, abort_flag)) return;
             const bool looked = u >= im.looked;
             if (looked && lane == 0) mbar_arrive(&sh.look[v_stage]);
             ++entry;
             const bool more = u + 1 < im.n_tiles;
             const int k_stage = entry % NS;
-            if (more && !warp_wait(&sh.full[k_stage], (entry / NS) & 1, abort_flag, lane)) return;
+            if (more && !warp_wait(&sh.full[k_stage], (entry / NS) & 1, abort_flag)) return;
             if (looked) {
-                if (!warp_wait(&sh.clean[v_stage], clean_phase >> v_stage & 1u, abort_flag, lane)) return;
+                if (!warp_wait(&sh.clean[v_stage], clean_phase >> v_stage & 1u, abort_flag)) return;
                 clean_phase ^= 1u << v_stage;
             }
             const uint64_t vd = v_desc0 + (uint64_t)((uint32_t)(v_stage * kStage) >> 4);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 if (u >= im.tiles[x]) continue;
+                const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 2 * kTile + x * kTile;
                 if (u == 0) {
-                    if (outs[x] > 0 && !warp_wait(&sh.o_free[x], (outs[x] - 1) & 1, abort_flag, lane)) return;
+                    if (outs[x] > 0 && !warp_wait(&sh.o_free[x], (outs[x] - 1) & 1, abort_flag)) return;
                     ++outs[x];
                 }
-                if (!warp_wait(&sh.p_full[x], turn[x] & 1, abort_flag, lane)) return;
-                ++turn[x];
+                if (!warp_wait(&sh.p_part[x], turn[x] & 1, abort_flag)) return;
                 tc_fence_after_sync();
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks)
-                    umma_bf16_ta_if(leader, tmem + 2 * kTile + x * kTile, tmem + x * kTile + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc,
-                                    u > 0 || ks > 0);
+                for (int ks = 0; ks < 2 * kFirst; ++ks)
+                    umma_bf16_ta_if(leader, o_tmem, s_tmem + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc, u > 0 || ks > 0);
+                if (!warp_wait(&sh.p_full[x], turn[x] & 1, abort_flag)) return;
+                tc_fence_after_sync();
+#pragma unroll
+                for (int ks = 2 * kFirst; ks < kTile / 16; ++ks)
+                    umma_bf16_ta_if(leader, o_tmem, s_tmem + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc, 1);
                 umma_commit_if(leader, &sh.pv_done[x]);
+                ++turn[x];
                 if (u + 1 < im.tiles[x]) scores(x, k_stage);
             }
             umma_commit_if(leader, &sh.empty[v_stage]);
@@ -501,7 +545,7 @@ __device__ __forceinline__ uint32_t load_warp(const TcAttnArgs &t, Shared &sh, c
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const int stage = entry % NS;
-                if (entry >= NS && !warp_wait(&sh.empty[stage], (entry / NS - 1) & 1, abort_flag, lane)) return entry;
+                if (entry >= NS && !warp_wait(&sh.empty[stage], (entry / NS - 1) & 1, abort_flag)) return entry;
                 mbar_arrive_expect_tx_if(leader, &sh.full[stage], kStage);
                 for (int box = 0; box < boxes; ++box) {
                     const int bt = __shfl_sync(0xffffffffu, tok, box), b3 = __shfl_sync(0xffffffffu, third, box);
@@ -545,7 +589,7 @@ __device__ __forceinline__ void helper_warp(const TcAttnArgs &t, Shared &sh, uin
     Item im;
     while (walk.next(t, im)) {
         if (im.n_tiles == 0) continue;
-        if (walk.seq > 0 && !warp_wait(&sh.q_empty, (walk.seq - 1) & 1, abort_flag, lane)) return;
+        if (walk.seq > 0 && !warp_wait(&sh.q_empty, (walk.seq - 1) & 1, abort_flag)) return;
         load_queries<KB>(t, im, q_img, which, lane);
         fence_proxy_async_smem();
         __syncwarp();
@@ -555,12 +599,12 @@ __device__ __forceinline__ void helper_warp(const TcAttnArgs &t, Shared &sh, uin
             const int stage = (entry + 1) % NS;
             // The MMA warp says when: it has seen the tile land and does not go on before this is done, so that the stage's
             // barrier stands at this entry's phase and not two away.
-            if (!warp_wait(&sh.look[stage], look_phase >> stage & 1u, abort_flag, lane)) return;
+            if (!warp_wait(&sh.look[stage], look_phase >> stage & 1u, abort_flag)) return;
             look_phase ^= 1u << stage;
-            if (!warp_wait(&sh.full[stage], ((entry + 1) / NS) & 1, abort_flag, lane)) return;
+            if (!warp_wait(&sh.full[stage], ((entry + 1) / NS) & 1, abort_flag)) return;
             uint4 *tile = reinterpret_cast<uint4 *>(ring + stage * kStage) + which * (kStage / 32);
             uint32_t found = 0;
-#pragma unroll 4
+#pragma unroll 8
             for (int y = lane; y < kStage / 32; y += 32) {
                 const uint4 v = tile[y];
                 const uint32_t e = 0x7f807f80u;
@@ -601,6 +645,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(&sh.s_full[x], 1);
+            mbar_init(&sh.p_part[x], 4);
             mbar_init(&sh.p_full[x], 4);
             mbar_init(&sh.pv_done[x], 1);
             mbar_init(&sh.o_free[x], 4);
@@ -630,9 +675,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
         // failed wait, the loads already issued must still land
         for (uint32_t e = issued > NS ? issued - NS : 0; e < issued; ++e) {
             const int st = e % NS;
-            if (!warp_wait(&sh.empty[st], (e / NS) & 1, &sh.abort, lane)) {
+            if (!warp_wait(&sh.empty[st], (e / NS) & 1, &sh.abort)) {
                 volatile int never = 0;
-                warp_wait(&sh.full[st], (e / NS) & 1, &never, lane);
+                warp_wait(&sh.full[st], (e / NS) & 1, &never);
             }
         }
         if (lane == 0 && *static_cast<volatile int *>(&sh.abort) && t.a.status) atomicOr(t.a.status, kStatusWaitExpired);
