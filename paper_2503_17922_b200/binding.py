@@ -657,6 +657,12 @@ def _check_state(t, shape, dtype: str, what: str) -> None:
         raise ValueError(f"{what}: contiguous {tuple(shape)} of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
 
 
+def _check_positions(t, shape) -> None:
+    """Positions of the expected shape, or the same number of them in one dimension."""
+    flat = (int(np.prod(shape)),)
+    _check_state(t, flat if t is not None and t.dim() == 1 else shape, "int32", "positions")
+
+
 def _check_same_layout(a, b, what: str) -> None:
     if a is not None and b is not None and (a.stride() != b.stride() or a.shape != b.shape):
         raise ValueError(f"{what}: both need the same shape and strides")
@@ -681,7 +687,7 @@ def prepare_rotate_prompt(prob: Problem, rope: Rope, q, k, q_out, k_out, positio
     for t, what in ((k, "k"), (k_out, "k_out")):
         if t is not None:
             _check_kv_layout(prob, t, what)
-    _check_state(positions, (tokens,) if prob.packed else (s.batch, s.max_seqlen), "int32", "positions")
+    _check_positions(positions, (tokens,) if prob.packed else (s.batch, s.max_seqlen))
     qs = _head_strides(q, prob.packed, "q")
     args = (ctypes.byref(s), ctypes.byref(rope.struct), _ptr(q), _ptr(q_out), qs, _ptr(k), _ptr(k_out), _ptr(positions), _stream(stream))
     return PreparedCall(lib().wkv_rotate_prompt, "wkv_rotate_prompt", args, (prob, rope, q, q_out, qs, k, k_out, positions))
@@ -730,7 +736,7 @@ def prepare_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_
     _check_state(lengths_out, units, "int32", "lengths_out")
     _check_state(row_positions, units + (cache.capacity,), "int32", "row_positions")
     _check_state(row_weights, units + (cache.capacity,), "float32", "row_weights")
-    _check_state(positions, (tokens,) if cache.packed else (s.batch, s.max_new), "int32", "positions")
+    _check_positions(positions, (tokens,) if cache.packed else (s.batch, s.max_new))
     ks, qs = _head_strides(k_new, cache.packed, "k_new"), _head_strides(q, cache.packed, "q")
     args = (ctypes.byref(s), ctypes.byref(rope.struct) if rope is not None else None, _ptr(k_new), _ptr(v_new), ks, _ptr(q), _ptr(q_out), qs,
             _ptr(positions), _ptr(lengths), _ptr(k_pool), _ptr(v_pool), _ptr(lengths_out), _ptr(row_positions), _ptr(row_weights),

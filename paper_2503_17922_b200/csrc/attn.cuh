@@ -102,7 +102,10 @@ inline cudaError_t allow_smem(K kernel, size_t bytes, SmemAsked &asked)
 
 // kernels (each returns a wkv_status)
 bool attn_tc_supported(const AttnArgs &a, int dtype);
-int launch_attn_tc(const AttnArgs &a, cudaStream_t stream);          // WKV_ERR_UNSUPPORTED: a layout that no tensor map describes
+// WKV_ERR_UNSUPPORTED: a layout that no tensor map describes.  piece_o, piece_ml, line: room for attn_tc_pieces() * rows rows of d
+// (256-byte aligned) and of one, and for items + 1 words, or null; with them the blocks share the work evenly where there are few items.
+int launch_attn_tc(const AttnArgs &a, float *piece_o, float2 *piece_ml, long long *line, cudaStream_t stream);
+int attn_tc_pieces(long long units, int max_q, int G, int cap, int *rows, int *items);
 int launch_attn_mma(const AttnArgs &a, cudaStream_t stream);         // bf16
 int launch_attn_simt(const AttnArgs &a, int dtype, cudaStream_t stream);
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream);       // with a.logits: and the weights

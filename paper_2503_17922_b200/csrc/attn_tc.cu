@@ -48,6 +48,11 @@ struct TcAttnArgs {
     long long items;
     int k_slot[3];           // tensor-map coordinates of (token, head, batch) / (slot, head, page)
     int box_rows;            // rows of a key box
+    bool wide_out;           // rows of the output begin on 32 bytes
+    int by_work;             // blocks that share the items' key tiles evenly (0: items are dealt out whole)
+    float *piece_o;          // by_work: [2 * blocks][256][d] and
+    float2 *piece_ml;        // [2 * blocks][256], what a block has of an item that it does not have all of
+    long long *line;         // [items + 1]: where the items begin on the line of work, for the joining kernel
 };
 
 struct Shared {
@@ -69,6 +74,8 @@ struct Item {
     int base;                // keys that query 0 sees
     int looked;              // key tiles from here on are looked through
     int n_tiles;
+    int begin, end;          // key tiles that this block takes
+    int piece;               // where it leaves what it has of the item, -1: it has all of it
 };
 __device__ __forceinline__ bool get_item(const TcAttnArgs &t, long long k, Item &im)
 {
@@ -92,19 +99,110 @@ __device__ __forceinline__ bool get_item(const TcAttnArgs &t, long long k, Item 
     }
     im.looked = max(im.base + im.pos0, 0) / kTile;       // every row sees all of the tiles in front of this one
     im.n_tiles = max(im.tiles[0], im.tiles[1]);
+    im.begin = 0;
+    im.end = im.n_tiles;
+    im.piece = -1;
     return true;
 }
-// a block's items, back and forth over the list
+
+// Sharing by work: the items, one after the other, are a line of (tiles + kItemCost) each, of which every block takes an equal length.
+// An item that lies across blocks is computed in pieces and joined by the kernel behind this one, which finds the pieces by the same
+// arithmetic.
+constexpr int kItemCost = 4;            // what an item costs beside its key tiles, in tiles
+constexpr int kWorkItems = 4 * 148;     // with more items than this they are dealt out whole
+constexpr int kWorkKeys = 2048;         // ... and where a unit has fewer keys at most
+constexpr int kWorkBlocks = 148;
+__device__ __forceinline__ long long item_cost(const TcAttnArgs &t, long long k)
+{
+    Item im;
+    return k < t.items && get_item(t, k, im) ? im.n_tiles + kItemCost : 0;
+}
+// By a whole warp, 32 items at a time: the length of the line; and, at a place on it, the item there and where that begins.
+__device__ __forceinline__ long long line_length(const TcAttnArgs &t, int lane)
+{
+    long long sum = 0;
+    for (int x = lane; x < t.items; x += 32) sum += item_cost(t, x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
+template <typename F>
+__device__ __forceinline__ void walk_line(const TcAttnArgs &t, int lane, F visit)      // visit(item, where it begins, where it ends): enough?
+{
+    long long before = 0;
+    for (int x0 = 0; x0 < t.items; x0 += 32) {
+        const long long c = item_cost(t, x0 + lane);
+        long long end = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, end, o);
+            if (lane >= o) end += v;
+        }
+        end += before;
+        if (visit(x0 + lane, end - c, end)) return;
+        before = __shfl_sync(0xffffffffu, end, 31);
+    }
+}
+// what block c has of an item at `at` on a line of `total`: tiles begin .. end - 1
+__device__ __forceinline__ void piece_of(const TcAttnArgs &t, long long total, int c, long long at, int n_tiles, int &begin, int &end)
+{
+    const long long lo = total * c / t.by_work - at, hi = total * (c + 1) / t.by_work - at;
+    begin = (int)min(max(lo - kItemCost, 0ll), (long long)n_tiles);
+    end = (int)min(max(hi - kItemCost, 0ll), (long long)n_tiles);
+}
+__device__ __forceinline__ int piece_slot(int c, int begin) { return 2 * c + (begin == 0); }
+
+// a block's items: back and forth over the list, or its share of the line
 struct Walk {
     long long k0 = 0;
     int round = 0, seq = 0;       // seq: items with key tiles so far
+    long long at = 0, total = -1;
     __device__ __forceinline__ bool next(const TcAttnArgs &t, Item &im)
     {
+        if (t.by_work) return next_share(t, im);
         while (k0 < t.items) {
             const long long k = k0 + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
             k0 += gridDim.x;
             ++round;
             if (k < t.items && get_item(t, k, im)) return true;
+        }
+        return false;
+    }
+    __device__ __forceinline__ bool next_share(const TcAttnArgs &t, Item &im)
+    {
+        if (total < 0) {
+            const int lane = threadIdx.x & 31;
+            total = line_length(t, lane);
+            const long long lo = total * blockIdx.x / t.by_work;
+            long long k = t.items, from = 0;
+            walk_line(t, lane, [&](int item, long long start, long long end) {
+                const unsigned there = __ballot_sync(0xffffffffu, end > lo);
+                if (!there) return false;
+                k = __shfl_sync(0xffffffffu, item, __ffs(there) - 1);
+                from = __shfl_sync(0xffffffffu, start, __ffs(there) - 1);
+                return true;
+            });
+            k0 = k;
+            at = from;
+        }
+        const long long lo = total * blockIdx.x / t.by_work, hi = total * (blockIdx.x + 1) / t.by_work;
+        while (k0 < t.items && at < hi) {
+            if (!get_item(t, k0, im)) {
+                ++k0;
+                continue;
+            }
+            const long long here = at;
+            ++k0;
+            at += im.n_tiles + kItemCost;
+            if (at <= lo) continue;
+            piece_of(t, total, blockIdx.x, here, im.n_tiles, im.begin, im.end);
+            if (im.n_tiles == 0) {
+                if (here >= lo) return true;              // nothing to see: its rows are written where it begins
+                continue;
+            }
+            if (im.begin >= im.end) continue;
+            if (im.end - im.begin < im.n_tiles) im.piece = piece_slot(blockIdx.x, im.begin);
+            return true;
         }
         return false;
     }
@@ -172,6 +270,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return r;
 }
 
+__device__ __forceinline__ void store32(void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h)
+                 : "memory");
+}
+__device__ __forceinline__ void store32(float *p, float a, float b, float c, float d, float e, float f, float g, float h)
+{
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(a), "f"(b), "f"(c), "f"(d), "f"(e), "f"(f), "f"(g), "f"(h)
+                 : "memory");
+}
+
 // ---- the softmax of one query tile ------------------------------------------------------------
 // S is read twice, 32 columns at a time, for the maximum and for the exponentials: a row of 128 in registers takes more of them than
 // a thread has, and the code of a row in one piece more than the instruction cache holds (8,192 tokens of 32 heads: 1,010 us).
@@ -237,18 +346,18 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
     Walk walk;
     Item im;
     while (walk.next(t, im)) {
-        const int pos = im.pos0 + x * t.ppt + place, tiles = x ? im.tiles[1] : im.tiles[0];
+        const int pos = im.pos0 + x * t.ppt + place, tiles = min(x ? im.tiles[1] : im.tiles[0], im.end);
         const bool mine = of_tile && place < (x ? im.rows[1] : im.rows[0]);
         const int limit = mine ? min(im.base + pos, im.sq.n) : 0;
         const int plain = (im.base + im.pos0 + x * t.ppt) / kTile;         // tiles that every row of this query tile sees all of
         float m = -INFINITY, l = 0.f;
-        for (int u = 0; u < tiles; ++u, ++turn) {
+        for (int u = im.begin; u < tiles; ++u, ++turn) {
             if (!warp_wait(&sh.s_full[x], turn & 1, abort_flag)) return;
             tc_fence_after_sync();
             RowMask seen = {make_uint4(~0u, ~0u, ~0u, ~0u)};
             bool masked = u >= plain;
             if (a.table) {
-                seen.bits = sh.present[(tiles_before + u) % kMaskSlots];
+                seen.bits = sh.present[(tiles_before + u - im.begin) % kMaskSlots];
                 masked |= (seen.bits.x & seen.bits.y & seen.bits.z & seen.bits.w) != ~0u;
             }
             if (masked) {
@@ -282,7 +391,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                 }
             }
             const bool follow = (grown - m) * c > kLazy;          // (also from -infinity on)
-            if (u == 0) {
+            if (u == im.begin) {
                 m = grown;
             } else if (__any_sync(0xffffffffu, follow)) {
                 if (!warp_wait(&sh.pv_done[x], (turn - 1) & 1, abort_flag)) return;
@@ -354,7 +463,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
             l += (s0.x + s0.y) + (s1.x + s1.y);
         }
         // ---- the item's rows: O / l -------------------------------------------------------------
-        const bool any = tiles > 0;
+        const bool any = tiles > im.begin;
         const int hq = im.h * a.G + head;
         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (im.sq.q_off + pos) * a.ot + im.b * a.ob + (long long)hq * a.oh;
         if (any) {
@@ -363,19 +472,21 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const bool poisoned = any && *static_cast<volatile int *>(&sh.poison[walk.seq % kMaskSlots]) == walk.seq + 1;
+        const long long left = ((long long)im.piece * 2 * kTile + x * kTile + row);      // row of the pieces
 #pragma unroll 1
         for (int y = 0; y < D / 32; ++y) {
             float o[32];
             if (any) {
                 tmem_ld32(o_addr + y * 32, o);
+                const float f = im.piece >= 0 ? 1.f : inv;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] = l == 0.f ? 0.f : o[j] * inv;
+                for (int j = 0; j < 32; ++j) o[j] = l == 0.f ? 0.f : o[j] * f;
             } else {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) o[j] = 0.f;
             }
             if (poisoned) {
-                for (int j = im.looked * kTile; j < limit; ++j) {
+                for (int j = max(im.looked, im.begin) * kTile; j < min(limit, im.end * kTile); ++j) {
                     const long long at = attn_row(a, im.b, im.h, im.sq.q_off, j);
                     if (at < 0) continue;
                     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + at + y * 32;
@@ -386,7 +497,19 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                     }
                 }
             }
-            if (mine) {
+            if (!mine) continue;
+            if (im.piece >= 0) {
+                float *to = t.piece_o + left * D + y * 32;
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) store32(to + j, o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+            } else if (t.wide_out) {
+                // (32 bytes a store are whole sectors: 16 take twice as many of L2's write cycles)
+#pragma unroll
+                for (int j = 0; j < 32; j += 16)
+                    store32(dst + y * 32 + j, pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]), pack_bf16(o[j + 4], o[j + 5]),
+                            pack_bf16(o[j + 6], o[j + 7]), pack_bf16(o[j + 8], o[j + 9]), pack_bf16(o[j + 10], o[j + 11]),
+                            pack_bf16(o[j + 12], o[j + 13]), pack_bf16(o[j + 14], o[j + 15]));
+            } else {
 #pragma unroll
                 for (int j = 0; j < 32; j += 8)
                     *reinterpret_cast<uint4 *>(dst + y * 32 + j) = make_uint4(pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]),
@@ -398,9 +521,12 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.o_free[x]);
         }
-        if (mine) attn_store_lse(a, im.b, hq, pos, im.sq.m, l > 0.f || l != l ? m * c + log2f(l) : -INFINITY);
-        walk.seq += im.n_tiles > 0;
-        tiles_before += im.n_tiles;
+        if (mine) {
+            if (im.piece >= 0) t.piece_ml[left] = make_float2(m * c, l);
+            else attn_store_lse(a, im.b, hq, pos, im.sq.m, l > 0.f || l != l ? m * c + log2f(l) : -INFINITY);
+        }
+        walk.seq += im.end > im.begin;
+        tiles_before += im.end - im.begin;
     }
 }
 
@@ -430,7 +556,8 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
         umma_commit_if(leader, &sh.s_full[x]);
     };
     while (walk.next(t, im)) {
-        if (im.n_tiles == 0) continue;
+        if (im.end == im.begin) continue;
+        const int tiles[2] = {min(im.tiles[0], im.end), min(im.tiles[1], im.end)};
         if (!warp_wait(&sh.q_full, walk.seq & 1, abort_flag)) return;
         const int first = entry % NS;
         if (!warp_wait(&sh.full[first], (entry / NS) & 1, abort_flag)) return;
@@ -438,17 +565,17 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
         // (S of the last item's last tile has been read: its P was waited for)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-            if (im.tiles[x] > 0) scores(x, first);
+            if (tiles[x] > im.begin) scores(x, first);
         umma_commit_if(leader, &sh.empty[first]);
-        if (im.n_tiles == 1) umma_commit_if(leader, &sh.q_empty);
+        if (im.end - im.begin == 1) umma_commit_if(leader, &sh.q_empty);
         ++entry;
-        for (int u = 0; u < im.n_tiles; ++u) {
+        for (int u = im.begin; u < im.end; ++u) {
             const int v_stage = entry % NS;
             if (!warp_wait(&sh.full[v_stage], (entry / NS) & 1, abort_flag)) return;
             const bool looked = u >= im.looked;
             if (looked && lane == 0) mbar_arrive(&sh.look[v_stage]);
             ++entry;
-            const bool more = u + 1 < im.n_tiles;
+            const bool more = u + 1 < im.end;
             const int k_stage = entry % NS;
             if (more && !warp_wait(&sh.full[k_stage], (entry / NS) & 1, abort_flag)) return;
             if (looked) {
@@ -458,9 +585,9 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
             const uint64_t vd = v_desc0 + (uint64_t)((uint32_t)(v_stage * kStage) >> 4);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                if (u >= im.tiles[x]) continue;
+                if (u >= tiles[x]) continue;
                 const uint32_t s_tmem = tmem + x * kTile, o_tmem = tmem + 2 * kTile + x * kTile;
-                if (u == 0) {
+                if (u == im.begin) {
                     if (outs[x] > 0 && !warp_wait(&sh.o_free[x], (outs[x] - 1) & 1, abort_flag)) return;
                     ++outs[x];
                 }
@@ -468,7 +595,7 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
                 tc_fence_after_sync();
 #pragma unroll
                 for (int ks = 0; ks < 2 * kFirst; ++ks)
-                    umma_bf16_ta_if(leader, o_tmem, s_tmem + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc, u > 0 || ks > 0);
+                    umma_bf16_ta_if(leader, o_tmem, s_tmem + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc, u > im.begin || ks > 0);
                 if (!warp_wait(&sh.p_full[x], turn[x] & 1, abort_flag)) return;
                 tc_fence_after_sync();
 #pragma unroll
@@ -476,13 +603,13 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
                     umma_bf16_ta_if(leader, o_tmem, s_tmem + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc, 1);
                 umma_commit_if(leader, &sh.pv_done[x]);
                 ++turn[x];
-                if (u + 1 < im.tiles[x]) scores(x, k_stage);
+                if (u + 1 < tiles[x]) scores(x, k_stage);
             }
             umma_commit_if(leader, &sh.empty[v_stage]);
             if (more) {
                 umma_commit_if(leader, &sh.empty[k_stage]);
                 ++entry;
-                if (u + 2 == im.n_tiles) umma_commit_if(leader, &sh.q_empty);
+                if (u + 2 == im.end) umma_commit_if(leader, &sh.q_empty);
             }
         }
         ++walk.seq;
@@ -513,7 +640,7 @@ __device__ __forceinline__ uint32_t load_warp(const TcAttnArgs &t, Shared &sh, c
         for (int kb = 0; kb < KB; ++kb) tma_load_4d_if(leader, to + kb * kRegion, map, &sh.full[stage], kb * 64, c1, c2, c3);
     };
     while (walk.next(t, im)) {
-        for (int u = 0; u < im.n_tiles; ++u) {
+        for (int u = im.begin; u < im.end; ++u) {
             // Where the tile's rows are: dense, one box; paged, one box per page or part of one, and rows without a page are
             // zeros (a page beyond the pool's).  Lane i looks up box i.
             int tok = (int)im.sq.q_off + u * kTile, third = a.cu_q ? 0 : im.b;
@@ -587,14 +714,20 @@ __device__ __forceinline__ void helper_warp(const TcAttnArgs &t, Shared &sh, uin
     uint32_t entry = 0, look_phase = 0;
     Walk walk;
     Item im;
+    if (t.by_work && blockIdx.x == 0 && which == 1)
+        walk_line(t, lane, [&](int item, long long start, long long end) {
+            if (item < t.items) t.line[item] = start;
+            if (item == t.items - 1) t.line[item + 1] = end;
+            return false;
+        });
     while (walk.next(t, im)) {
-        if (im.n_tiles == 0) continue;
+        if (im.end == im.begin) continue;
         if (walk.seq > 0 && !warp_wait(&sh.q_empty, (walk.seq - 1) & 1, abort_flag)) return;
         load_queries<KB>(t, im, q_img, which, lane);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.q_full);
-        for (int u = 0; u < im.n_tiles; ++u, entry += 2) {
+        for (int u = im.begin; u < im.end; ++u, entry += 2) {
             if (u < im.looked) continue;
             const int stage = (entry + 1) % NS;
             // The MMA warp says when: it has seen the tile land and does not go on before this is done, so that the stage's
@@ -690,6 +823,62 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     if (warp == 8) tmem_dealloc(sh.tmem_base, kTmemCols);
 }
 
+// Joins the pieces of the items that lie across blocks: block (item, y) takes 64 of its 256 rows, a warp per row in turn.
+constexpr int kJoinRows = 64;
+__global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant__ TcAttnArgs t)
+{
+    pdl_trigger();
+    pdl_wait();
+    const AttnArgs &a = t.a;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Item im;
+    if (!get_item(t, blockIdx.x, im) || im.n_tiles == 0) return;
+    const long long at = t.line[blockIdx.x], total = t.line[t.items];
+    // blocks that have some of it
+    int c0 = (int)(at * t.by_work / total), begin, end;
+    while (c0 > 0 && total * c0 / t.by_work > at) --c0;
+    while (total * (c0 + 1) / t.by_work <= at) ++c0;
+    int c1 = c0;
+    while (c1 + 1 < t.by_work && total * (c1 + 1) / t.by_work < at + im.n_tiles + kItemCost) ++c1;
+    for (int c = c0; c <= c1; ++c) {
+        piece_of(t, total, c, at, im.n_tiles, begin, end);
+        if (end - begin == im.n_tiles) return;            // one has it whole
+    }
+    for (int r = blockIdx.y * kJoinRows + warp; r < (int)(blockIdx.y + 1) * kJoinRows; r += 8) {
+        const int x = r / kTile, row = r - x * kTile, place = row / a.G, head = row - place * a.G;
+        if (place >= t.ppt || place >= (x ? im.rows[1] : im.rows[0])) continue;
+        float top = -INFINITY;
+        for (int c = c0; c <= c1; ++c) {
+            piece_of(t, total, c, at, im.n_tiles, begin, end);
+            if (begin < end) top = fmaxf(top, t.piece_ml[(long long)piece_slot(c, begin) * 2 * kTile + r].x);
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        float l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = c0; c <= c1; ++c) {
+            piece_of(t, total, c, at, im.n_tiles, begin, end);
+            if (begin >= end) continue;
+            const long long left = (long long)piece_slot(c, begin) * 2 * kTile + r;
+            const float2 ml = t.piece_ml[left];
+            if (ml.y == 0.f) continue;
+            const float f = exp2f(ml.x - ref);
+            l += f * ml.y;
+            if (lane * 4 < a.d) {
+                const float4 p = *reinterpret_cast<const float4 *>(t.piece_o + left * a.d + lane * 4);
+                o.x = fmaf(f, p.x, o.x);
+                o.y = fmaf(f, p.y, o.y);
+                o.z = fmaf(f, p.z, o.z);
+                o.w = fmaf(f, p.w, o.w);
+            }
+        }
+        const int pos = im.pos0 + x * t.ppt + place, hq = im.h * a.G + head;
+        if (lane == 0) attn_store_lse(a, im.b, hq, pos, im.sq.m, l > 0.f || l != l ? top + log2f(l) : -INFINITY);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (im.sq.q_off + pos) * a.ot + im.b * a.ob + (long long)hq * a.oh;
+        if (lane * 4 < a.d) *reinterpret_cast<uint2 *>(dst + lane * 4) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    }
+}
+
 template <int KB>
 int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream)
 {
@@ -700,9 +889,13 @@ int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &
     cudaError_t err = cudaGetDevice(&dev);
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (err == cudaSuccess) err = allow_smem(attn_tc_kernel<KB>, smem, asked);
-    const long long grid = t.items < sms ? t.items : sms;
+    const long long grid = t.by_work ? t.by_work : (t.items < sms ? t.items : sms);
     if (err == cudaSuccess) err = launch_pdl(attn_tc_kernel<KB>, dim3((unsigned)grid), kThreads, smem, stream, 1, k_map, v_map, t);
     if (err == cudaSuccess) count_launches(1);
+    if (err == cudaSuccess && t.by_work) {
+        err = launch_pdl(attn_tc_join_kernel, dim3((unsigned)t.items, 2 * kTile / kJoinRows), 256, 0, stream, 1, t);
+        if (err == cudaSuccess) count_launches(1);
+    }
     return check_cuda(err, "tensor-core attention kernel");
 }
 
@@ -724,7 +917,15 @@ bool attn_tc_supported(const AttnArgs &a, int dtype)
     return major == 10;
 }
 
-int launch_attn_tc(const AttnArgs &a, cudaStream_t stream)
+int attn_tc_pieces(long long units, int max_q, int G, int cap, int *rows, int *items)
+{
+    const int ppt = kTile / G;
+    *rows = 2 * kTile;
+    *items = kWorkItems;
+    return units * ((max_q + 2 * ppt - 1) / (2 * ppt)) <= kWorkItems && cap >= kWorkKeys ? 2 * kWorkBlocks : 0;
+}
+
+int launch_attn_tc(const AttnArgs &a, float *piece_o, float2 *piece_ml, long long *line, cudaStream_t stream)
 {
     TcAttnArgs t;
     t.a = a;
@@ -733,6 +934,12 @@ int launch_attn_tc(const AttnArgs &a, cudaStream_t stream)
     t.max_pairs = (a.max_q + 2 * t.ppt - 1) / (2 * t.ppt);
     t.items = units * t.max_pairs;
     t.box_rows = a.table && a.page_size < kTile ? a.page_size : kTile;
+    t.wide_out = (reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ot * 2) | (uintptr_t)(a.oh * 2) | (uintptr_t)(a.ob * 2)) % 32 == 0;
+    int rows = 0, most = 0;
+    t.by_work = piece_o && attn_tc_pieces(units, a.max_q, a.G, a.cap, &rows, &most) ? kWorkBlocks : 0;
+    t.piece_o = piece_o;
+    t.piece_ml = piece_ml;
+    t.line = line;
     alignas(64) CUtensorMap k_map, v_map;
     const unsigned long long tokens = a.cu_q ? a.total_q : a.max_q, batch = a.cu_q ? 1 : a.batch;
     if (a.cu_q && a.total_q == 0) return WKV_OK;

@@ -121,6 +121,8 @@ struct PagedWorkspace {
     int splits;
     size_t lse_off, ml_off, o_off, logits_off, counts_off, moves_off, total;
     long long logit_stride;      // 0: the weights are computed from K once more
+    int pieces;                  // of the tensor-core kernel
+    size_t line_off, piece_o_off, piece_ml_off;
     int moves_max;
 };
 // Key splits of the kernels that take one tile of rows per block: two blocks for every SM, where each then has a tile of 64
@@ -136,6 +138,8 @@ int plan_splits(const Paged &p)
     while (blocks * s < 4 * kSplitBlocks && p.cap / (s + 1) >= kSplitEven) ++s;
     return s < 1 ? 1 : (int)s;
 }
+// More rows than this go to the tensor-core kernel where it takes the shape.
+constexpr int kFewRows = 32;
 // Rows per unit whose logits are kept for the weights: 4 bytes for each beside the 2 * d * 2 of K and V, written and read.
 constexpr int kLogitRows = 16;
 PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
@@ -155,6 +159,19 @@ PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
     w.logit_stride = keeps_logits ? ((long long)p.cap + 3) / 4 * 4 : 0;
     off = align_up(off + (size_t)p.units * p.rows_max * w.logit_stride * sizeof(float), 256);
     w.total = off;
+    // (in the place of the parts above: a call runs one kernel or the other)
+    off = w.ml_off;
+    int rows = 0, items = 0;
+    const int G = c->n_q_heads / c->n_kv_heads;
+    w.pieces = c->dtype == WKV_BF16 && p.rows_max > kFewRows && G <= 128 && (c->head_dim == 64 || c->head_dim == 128)
+                   ? attn_tc_pieces(p.units, c->max_new, G, p.cap, &rows, &items) : 0;
+    w.line_off = off;
+    off = align_up(off + (w.pieces ? (size_t)(items + 1) * sizeof(long long) : 0), 256);
+    w.piece_ml_off = off;
+    off = align_up(off + (size_t)w.pieces * rows * sizeof(float2), 256);
+    w.piece_o_off = off;
+    off = align_up(off + (size_t)w.pieces * rows * c->head_dim * sizeof(float), 256);
+    if (off > w.total) w.total = off;
     w.moves_max = p.cap / 2 + 1;
     off = 256;
     w.counts_off = off;
@@ -347,7 +364,7 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
             shorter |= (s->cu_seqlens_host ? s->cu_seqlens_host[b + 1] - s->cu_seqlens_host[b] : s->max_seqlen) < s->l_obs;
         if (shorter && (st = launch_attn_lse_obs_fill(a, stream)) != WKV_OK) return st;
     }
-    if (attn_tc_supported(a, s->dtype) && (st = launch_attn_tc(a, stream)) != WKV_ERR_UNSUPPORTED) return st;
+    if (attn_tc_supported(a, s->dtype) && (st = launch_attn_tc(a, nullptr, nullptr, nullptr, stream)) != WKV_ERR_UNSUPPORTED) return st;
     return s->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, s->dtype, stream);
 }
 
@@ -498,7 +515,10 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
         a.logit_stride = w.logit_stride;
     }
     // Up to 16 rows are one tile of the warp-level kernel, whose time is that of the loads.
-    st = p.rows_max > 32 && attn_tc_supported(a, c->dtype) ? launch_attn_tc(a, stream) : WKV_ERR_UNSUPPORTED;
+    st = WKV_ERR_UNSUPPORTED;
+    if (p.rows_max > kFewRows && attn_tc_supported(a, c->dtype))
+        st = launch_attn_tc(a, w.pieces ? reinterpret_cast<float *>(ws + w.piece_o_off) : nullptr, reinterpret_cast<float2 *>(ws + w.piece_ml_off),
+                            reinterpret_cast<long long *>(ws + w.line_off), stream);
     if (st == WKV_ERR_UNSUPPORTED) {
         st = c->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, c->dtype, stream);
         if (st == WKV_OK && (a.splits > 1 || a.logits)) st = launch_attn_join(a, c->dtype, stream);
