@@ -829,47 +829,53 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
 {
     pdl_trigger();
     pdl_wait();
+    __shared__ int slots[kWorkBlocks];
+    __shared__ int n_slots;
     const AttnArgs &a = t.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Item im;
     if (!get_item(t, blockIdx.x, im) || im.n_tiles == 0) return;
     const long long at = t.line[blockIdx.x], total = t.line[t.items];
-    // blocks that have some of it
-    int c0 = (int)(at * t.by_work / total), begin, end;
-    while (c0 > 0 && total * c0 / t.by_work > at) --c0;
-    while (total * (c0 + 1) / t.by_work <= at) ++c0;
-    int c1 = c0;
-    while (c1 + 1 < t.by_work && total * (c1 + 1) / t.by_work < at + im.n_tiles + kItemCost) ++c1;
-    for (int c = c0; c <= c1; ++c) {
-        piece_of(t, total, c, at, im.n_tiles, begin, end);
-        if (end - begin == im.n_tiles) return;            // one has it whole
+    // the pieces, in order: 32 blocks at a time, by the first warp
+    if (warp == 0) {
+        int n = 0, whole = 0;
+        for (int c0 = 0; c0 < t.by_work; c0 += 32) {
+            const int c = c0 + lane;
+            int begin = 0, end = 0;
+            if (c < t.by_work) piece_of(t, total, c, at, im.n_tiles, begin, end);
+            const unsigned some = __ballot_sync(0xffffffffu, begin < end);
+            whole |= __any_sync(0xffffffffu, end - begin == im.n_tiles);
+            if (begin < end) slots[n + __popc(some & ((1u << lane) - 1u))] = piece_slot(c, begin);
+            n += __popc(some);
+        }
+        if (lane == 0) n_slots = whole ? 0 : n;           // (one block has it whole, and has written its rows)
     }
+    __syncthreads();
+    const int n = n_slots;
+    if (n == 0) return;
     for (int r = blockIdx.y * kJoinRows + warp; r < (int)(blockIdx.y + 1) * kJoinRows; r += 8) {
         const int x = r / kTile, row = r - x * kTile, place = row / a.G, head = row - place * a.G;
         if (place >= t.ppt || place >= (x ? im.rows[1] : im.rows[0])) continue;
         float top = -INFINITY;
-        for (int c = c0; c <= c1; ++c) {
-            piece_of(t, total, c, at, im.n_tiles, begin, end);
-            if (begin < end) top = fmaxf(top, t.piece_ml[(long long)piece_slot(c, begin) * 2 * kTile + r].x);
-        }
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, t.piece_ml[(long long)slots[i] * 2 * kTile + r].x);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const float ref = top == -INFINITY ? 0.f : top;
         float l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = c0; c <= c1; ++c) {
-            piece_of(t, total, c, at, im.n_tiles, begin, end);
-            if (begin >= end) continue;
-            const long long left = (long long)piece_slot(c, begin) * 2 * kTile + r;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const long long left = (long long)slots[i] * 2 * kTile + r;
             const float2 ml = t.piece_ml[left];
-            if (ml.y == 0.f) continue;
-            const float f = exp2f(ml.x - ref);
+            float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (lane * 4 < a.d) p = *reinterpret_cast<const float4 *>(t.piece_o + left * a.d + lane * 4);
+            const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - ref);
+            if (f == 0.f) continue;
             l += f * ml.y;
-            if (lane * 4 < a.d) {
-                const float4 p = *reinterpret_cast<const float4 *>(t.piece_o + left * a.d + lane * 4);
-                o.x = fmaf(f, p.x, o.x);
-                o.y = fmaf(f, p.y, o.y);
-                o.z = fmaf(f, p.z, o.z);
-                o.w = fmaf(f, p.w, o.w);
-            }
+            o.x = fmaf(f, p.x, o.x);
+            o.y = fmaf(f, p.y, o.y);
+            o.z = fmaf(f, p.z, o.z);
+            o.w = fmaf(f, p.w, o.w);
         }
         const int pos = im.pos0 + x * t.ppt + place, hq = im.h * a.G + head;
         if (lane == 0) attn_store_lse(a, im.b, hq, pos, im.sq.m, l > 0.f || l != l ? top + log2f(l) : -INFINITY);

@@ -686,3 +686,36 @@ def test_decode_step_captured_and_replayed(dtype, new):
     for x, y in zip(*results):
         assert torch.equal(x.view(torch.uint8) if x.dtype != torch.int32 else x, y.view(torch.uint8) if y.dtype != torch.int32 else y)
     assert wkv.device_status(a.ws) == 0
+
+
+@pytest.mark.parametrize("case", [
+    # few items over long caches: blocks share items and join their pieces
+    ("bf16", 8, 2, 128, 64, "pshd", [[5000, 4990], [2100, 700], [1, 0], [3, 2600]], [40, 300, 0, 200], True),
+    ("bf16", 4, 1, 64, 128, "phsd", [[9000]], [33], False),
+    ("bf16", 12, 1, 128, 16, "phsd", [[2500], [4100]], [500, 7], True),
+    ("bf16", 64, 1, 128, 32, "phsd", [[3333]], [1], False),
+], ids=["ragged", "one", "g6", "token"])
+def test_attend_shared_work(case):
+    a = Attend(*case)
+    assert a.c.cap >= 2048
+    a.run()
+    a.check()
+
+
+def test_attend_shared_work_with_infinities_and_missing_pages():
+    a = Attend("bf16", 8, 2, 128, 64, "phsd", [[4000, 3990]], [200], False)
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    clean = a.out.clone()
+    a.c.slot(a.c.v[0], 0, 0, 3900)[3] = NAN
+    a.c.slot(a.c.v[0], 0, 1, 3890)[5] = INF
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    assert torch.equal(a.out[:, :4, :100], clean[:, :4, :100]) and torch.isnan(a.out[:, :4, 100:, 3]).all()
+    assert torch.equal(a.out[:, 4:, :100], clean[:, 4:, :100]) and (a.out[:, 4:, 100:, 5] == INF).all()
+    assert torch.equal(a.out[:, :4, :, 4:], clean[:, :4, :, 4:])
+    a.c.slot(a.c.v[0], 0, 0, 3900)[3] = 0.5
+    a.c.slot(a.c.v[0], 0, 1, 3890)[5] = 0.5
+    a.c.table[0, 20:40] = -1
+    a.run()
+    a.check()
