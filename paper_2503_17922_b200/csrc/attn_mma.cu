@@ -70,7 +70,10 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
     extern __shared__ __align__(128) unsigned char raw[];
     MmaSmem<DP> &sm = *reinterpret_cast<MmaSmem<DP> *>(raw);
     constexpr int NS = stages_for(DP), kRows = FEW ? 16 : 64, kSteps = DP / 16, kGroups = FEW ? 1 : 4;   // 16-key groups per warp
-    pdl_trigger();
+    // The joining kernel may be placed now.  Another of this kind is not to be before this one ends: its blocks would crowd onto the
+    // SMs that have room at that time.
+    const bool parts = a.splits > 1 || a.logits;
+    if (parts) pdl_trigger();
     pdl_wait();
     const int units = a.batch * a.hkv;
     // the last rows of a prompt have the most keys: they are taken first
@@ -86,7 +89,6 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
     const int split = blockIdx.y;
     const int t0 = (int)((long long)all_tiles * split / a.splits), t1 = (int)((long long)all_tiles * (split + 1) / a.splits);
     const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
-    const bool parts = a.splits > 1 || a.logits;
 
     // rows of this thread: `quad` and quad + 8 of the warp's sixteen
     const int my_row[2] = {row0 + (FEW ? 0 : warp * 16) + quad, row0 + (FEW ? 0 : warp * 16) + quad + 8};
@@ -283,6 +285,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
         l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (!parts) pdl_trigger();
     if (FEW) {
         // ---- the four warps' sums, in order -------------------------------------------------------
         __syncthreads();

@@ -1,6 +1,9 @@
-// Attention on the CUDA cores: fp32 inputs, and the shapes that the tensor-core kernels do not take.  One block holds ROWS rows
-// of one unit in shared memory and walks over the unit's keys in tiles of 64 with a running maximum and sum per row;
-// everything is fp32, products in plain multiply-adds.
+// Attention on the CUDA cores for fp32, and the joining and weights kernels of all types.  One block holds ROWS rows of one
+// unit in shared memory and walks over the unit's keys in tiles of 64 with a running maximum and sum per row; everything is
+// fp32, products in plain multiply-adds, which bound it (2 * 64 * d per row and tile).  A tile's keys and values come by asynchronous copies
+// while the one before is worked on.
+//
+// ROWS is the largest of 64, 32 and 16 that gives every SM a block (4 heads of 1,024 tokens, d = 64: 122 us with 64 rows in 64 blocks).
 //
 // With S key splits a block walks over one of S parts of the keys and leaves (maximum, sum, unnormalised output) per row for
 // the joining kernel.  A row's sums are taken in one order whatever else the launch holds, so results do not depend
@@ -38,41 +41,64 @@ __device__ __forceinline__ void load_row_part(float *dst, const T *p, int d, int
     for (int i = 0; i < kVec; i += 4) *reinterpret_cast<float4 *>(dst + c + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 
+// Stages of key tiles: two where they fit.
+__host__ __device__ constexpr int simt_stages(int dp) { return dp <= 128 ? 2 : 1; }
 template <int DP, int ROWS>
 struct SimtSmem {
     float q[ROWS][DP + 4];
-    float k[kKeys][DP + 4];
-    float v[kKeys][DP];
+    float k[simt_stages(DP)][kKeys][DP + 4];
+    float v[simt_stages(DP)][kKeys][DP];
     float p[ROWS][kKeys + 4];
-    int present[kKeys];       // the key's page is one
+    int present[simt_stages(DP)][kKeys];       // the key's page is one
+};
+template <int DP>
+struct WeightsSmem {
+    float q[64][DP + 4];
+    float k[kKeys][DP + 4];
+    float sums[16][kKeys + 1];
+    int present[kKeys];
 };
 
-// the keys (and values) of one tile; rows from n on and rows without a page are zeros
-template <typename T, int DP, int ROWS>
-__device__ __forceinline__ void load_keys(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int b, int h, long long off, int n, int j0, bool values)
+// the keys and values of one tile, on their way; rows from n on and rows without a page are zeros
+template <int DP, int ROWS>
+__device__ __forceinline__ void fetch_keys(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int st, int b, int h, long long off, int n, int j0)
+{
+    constexpr int kParts = DP / 4;
+    for (int x = threadIdx.x; x < kKeys * kParts; x += kThreads) {
+        const int r = x / kParts, c = (x - r * kParts) * 4, j = j0 + r;
+        const long long at = j < n ? attn_row(a, b, h, off, j) : -1;
+        const bool have = at >= 0 && c < a.d;
+        const int size = have ? 16 : 0;
+        const float *kp = static_cast<const float *>(a.k) + (have ? at + c : 0), *vp = static_cast<const float *>(a.v) + (have ? at + c : 0);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&sm.k[st][r][c]))), "l"(kp), "r"(size) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&sm.v[st][r][c]))), "l"(vp), "r"(size) : "memory");
+        if (c == 0) sm.present[st][r] = at >= 0;
+    }
+}
+template <typename T, int DP>
+__device__ __forceinline__ void load_keys(const AttnArgs &a, WeightsSmem<DP> &sm, int b, int h, long long off, int n, int j0)
 {
     constexpr int kVec = 16 / sizeof(T), kParts = DP / kVec;
     for (int x = threadIdx.x; x < kKeys * kParts; x += kThreads) {
         const int r = x / kParts, part = x - r * kParts, j = j0 + r;
         const long long at = j < n ? attn_row(a, b, h, off, j) : -1;
         load_row_part<T, DP>(sm.k[r], at >= 0 ? static_cast<const T *>(a.k) + at : nullptr, a.d, part);
-        if (values) load_row_part<T, DP>(sm.v[r], at >= 0 ? static_cast<const T *>(a.v) + at : nullptr, a.d, part);
         if (part == 0) sm.present[r] = at >= 0;
     }
 }
 template <typename T, int DP, int ROWS>
-__device__ __forceinline__ void load_queries(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int b, int h, long long off, int row0, int rows)
+__device__ __forceinline__ void load_queries(const AttnArgs &a, float (&q)[ROWS][DP + 4], int b, int h, long long off, int row0, int rows)
 {
     constexpr int kVec = 16 / sizeof(T), kParts = DP / kVec;
     for (int x = threadIdx.x; x < ROWS * kParts; x += kThreads) {
         const int r = x / kParts, part = x - r * kParts, row = row0 + r, i = row / a.G, g = row - i * a.G;
         const T *p = row < rows ? static_cast<const T *>(a.q) + (off + i) * a.qt + b * a.qb + (long long)(h * a.G + g) * a.qh : nullptr;
-        load_row_part<T, DP>(sm.q[r], p, a.d, part);
+        load_row_part<T, DP>(q[r], p, a.d, part);
     }
 }
 // logits (base 2) of rows ty*RT.. against keys tx + 16 j
 template <int DP, int ROWS>
-__device__ __forceinline__ void logits(const SimtSmem<DP, ROWS> &sm, int ty, int tx, float c, float (&s)[ROWS / 16][4])
+__device__ __forceinline__ void logits(const float (&q)[ROWS][DP + 4], const float (&k)[kKeys][DP + 4], int ty, int tx, float c, float (&s)[ROWS / 16][4])
 {
     constexpr int RT = ROWS / 16;
 #pragma unroll
@@ -83,9 +109,9 @@ __device__ __forceinline__ void logits(const SimtSmem<DP, ROWS> &sm, int ty, int
     for (int e = 0; e < DP; e += 4) {
         float4 qv[RT], kv[4];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) qv[r] = *reinterpret_cast<const float4 *>(&sm.q[ty * RT + r][e]);
+        for (int r = 0; r < RT; ++r) qv[r] = *reinterpret_cast<const float4 *>(&q[ty * RT + r][e]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4 *>(&sm.k[tx + 16 * j][e]);
+        for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4 *>(&k[tx + 16 * j][e]);
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -102,13 +128,16 @@ __device__ __forceinline__ void logits(const SimtSmem<DP, ROWS> &sm, int ty, int
         for (int j = 0; j < 4; ++j) s[r][j] *= c;
 }
 
-template <typename T, int DP, int ROWS>
+template <int DP, int ROWS>
 __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
     SimtSmem<DP, ROWS> &sm = *reinterpret_cast<SimtSmem<DP, ROWS> *>(raw);
-    constexpr int RT = ROWS / 16, CT = DP / 64;
-    pdl_trigger();
+    constexpr int RT = ROWS / 16, CT = DP / 64, NS = simt_stages(DP);
+    // The joining kernel may be placed now.  Another of this kind is not to be before this one ends: its blocks would crowd onto the
+    // SMs that have room at that time.
+    const bool parts = a.splits > 1 || a.logits;
+    if (parts) pdl_trigger();
     pdl_wait();
     const int units = a.batch * a.hkv;
     // the last rows of a prompt have the most keys: they are taken first
@@ -134,21 +163,31 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
 #pragma unroll
         for (int x = 0; x < CT; ++x) o[r][x] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    load_queries<T, DP, ROWS>(a, sm, b, h, sq.q_off, row0, rows);
+    if (t0 < t1) fetch_keys(a, sm, 0, b, h, sq.q_off, sq.n, t0 * kKeys);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    load_queries<float, DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
     const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
     for (int t = t0; t < t1; ++t) {
-        const int j0 = t * kKeys;
-        load_keys<T, DP, ROWS>(a, sm, b, h, sq.q_off, sq.n, j0, true);
+        const int j0 = t * kKeys, st = NS == 2 ? (t - t0) & 1 : 0;
+        if (NS == 2 && t + 1 < t1) fetch_keys(a, sm, st ^ 1, b, h, sq.q_off, sq.n, j0 + kKeys);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(NS - 1) : "memory");
         __syncthreads();
         float s[RT][4];
-        logits<DP, ROWS>(sm, ty, tx, a.scale_log2, s);
+        logits<DP, ROWS>(sm.q, sm.k[st], ty, tx, a.scale_log2, s);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             float top = m[r];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (j0 + tx + 16 * j >= limit[r] || !sm.present[tx + 16 * j]) s[r][j] = -INFINITY;
+                if (j0 + tx + 16 * j >= limit[r] || !sm.present[st][tx + 16 * j]) s[r][j] = -INFINITY;
                 top = fmaxf(top, s[r][j]);
+            }
+            if (ROWS == 16 && a.logits && row0 + ty < rows) {
+                float *to = a.logits + ((long long)unit * a.rows_max + row0 + ty) * a.logit_stride + j0 + tx;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j0 + tx + 16 * j < sq.n) to[16 * j] = s[r][j];
             }
 #pragma unroll
             for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
@@ -175,33 +214,41 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         }
         __syncwarp();                                                    // a row's 16 threads are in one warp
         const bool guarded = j0 + kKeys > plain;
-#pragma unroll 4
-        for (int j = 0; j < kKeys; ++j) {
-            float4 vv[CT];
+#pragma unroll 2
+        for (int j = 0; j < kKeys; j += 4) {
+            float4 pp[RT];
 #pragma unroll
-            for (int x = 0; x < CT; ++x) vv[x] = *reinterpret_cast<const float4 *>(&sm.v[j][tx * 4 + 64 * x]);
+            for (int r = 0; r < RT; ++r) pp[r] = *reinterpret_cast<const float4 *>(&sm.p[ty * RT + r][j]);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const float p = sm.p[ty * RT + r][j];
-                // what stands behind a row's position may be infinite or NaN: 0 times it is not 0
-                if (guarded && p == 0.f) continue;
+            for (int e = 0; e < 4; ++e) {
+                float4 vv[CT];
 #pragma unroll
-                for (int x = 0; x < CT; ++x) {
-                    o[r][x].x = fmaf(p, vv[x].x, o[r][x].x);
-                    o[r][x].y = fmaf(p, vv[x].y, o[r][x].y);
-                    o[r][x].z = fmaf(p, vv[x].z, o[r][x].z);
-                    o[r][x].w = fmaf(p, vv[x].w, o[r][x].w);
+                for (int x = 0; x < CT; ++x) vv[x] = *reinterpret_cast<const float4 *>(&sm.v[st][j + e][tx * 4 + 64 * x]);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const float p = e == 0 ? pp[r].x : (e == 1 ? pp[r].y : (e == 2 ? pp[r].z : pp[r].w));
+                    // what stands behind a row's position may be infinite or NaN: 0 times it is not 0
+                    if (guarded && p == 0.f) continue;
+#pragma unroll
+                    for (int x = 0; x < CT; ++x) {
+                        o[r][x].x = fmaf(p, vv[x].x, o[r][x].x);
+                        o[r][x].y = fmaf(p, vv[x].y, o[r][x].y);
+                        o[r][x].z = fmaf(p, vv[x].z, o[r][x].z);
+                        o[r][x].w = fmaf(p, vv[x].w, o[r][x].w);
+                    }
                 }
             }
         }
         __syncthreads();
+        if (NS == 1 && t + 1 < t1) fetch_keys(a, sm, 0, b, h, sq.q_off, sq.n, j0 + kKeys);
     }
+    if (!parts) pdl_trigger();
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = row0 + ty * RT + r;
         if (row >= rows) continue;
         const int i = row / a.G, hq = h * a.G + row - i * a.G;
-        if (a.splits > 1) {
+        if (parts) {
             const long long at = ((long long)unit * a.rows_max + row) * a.splits + split;
             if (tx == 0) a.part_ml[at] = make_float2(m[r], l[r]);
             if (l[r] == 0.f) continue;
@@ -214,18 +261,11 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         }
         if (tx == 0) attn_store_lse(a, b, hq, i, sq.m, l[r] > 0.f || l[r] != l[r] ? m[r] + log2f(l[r]) : -INFINITY);
         const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-        T *dst = static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh;
+        float *dst = static_cast<float *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh;
 #pragma unroll
         for (int x = 0; x < CT; ++x) {
             const int c = tx * 4 + 64 * x;
-            if (c >= a.d) continue;
-            T y[4];
-            from_float(y[0], o[r][x].x * inv);
-            from_float(y[1], o[r][x].y * inv);
-            from_float(y[2], o[r][x].z * inv);
-            from_float(y[3], o[r][x].w * inv);
-            if (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst + c) = *reinterpret_cast<float4 *>(y);
-            else *reinterpret_cast<uint2 *>(dst + c) = *reinterpret_cast<uint2 *>(y);
+            if (c < a.d) *reinterpret_cast<float4 *>(dst + c) = make_float4(o[r][x].x * inv, o[r][x].y * inv, o[r][x].z * inv, o[r][x].w * inv);
         }
     }
 }
@@ -237,8 +277,7 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
 {
     constexpr int ROWS = 64, RT = ROWS / 16;
     extern __shared__ __align__(16) unsigned char raw[];
-    SimtSmem<DP, ROWS> &sm = *reinterpret_cast<SimtSmem<DP, ROWS> *>(raw);
-    pdl_trigger();
+    WeightsSmem<DP> &sm = *reinterpret_cast<WeightsSmem<DP> *>(raw);
     pdl_wait();
     const int units = a.batch * a.hkv, unit = (int)blockIdx.x % units, j0 = (int)blockIdx.x / units * kKeys;
     const int b = unit / a.hkv, h = unit - b * a.hkv;
@@ -246,16 +285,16 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
     if (j0 >= sq.n) return;
     const int rows = sq.m * a.G, base = sq.n - sq.m + 1;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    load_keys<T, DP, ROWS>(a, sm, b, h, sq.q_off, sq.n, j0, false);
+    load_keys<T, DP>(a, sm, b, h, sq.q_off, sq.n, j0);
     float got[4] = {0.f, 0.f, 0.f, 0.f};
     // queries in front of the tile's first key do not attend to any of it
     const long long first = base > j0 ? 0 : (long long)(j0 - base + 1) * a.G;
     for (int row0 = (int)(first / ROWS * ROWS); row0 < rows; row0 += ROWS) {
         __syncthreads();
-        load_queries<T, DP, ROWS>(a, sm, b, h, sq.q_off, row0, rows);
+        load_queries<T, DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
         __syncthreads();
         float s[RT][4];
-        logits<DP, ROWS>(sm, ty, tx, a.scale_log2, s);
+        logits<DP, ROWS>(sm.q, sm.k, ty, tx, a.scale_log2, s);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int row = row0 + ty * RT + r, i = row / a.G, hq = h * a.G + row - i * a.G;
@@ -266,15 +305,14 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
                 if (j0 + tx + 16 * j < base + i && sm.present[tx + 16 * j]) got[j] += exp2f(s[r][j] - lse2);
         }
     }
-    __syncthreads();
-    float(*sums)[kKeys + 1] = reinterpret_cast<float(*)[kKeys + 1]>(&sm.p[0][0]);     // [16][65]
+    pdl_trigger();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sums[ty][tx + 16 * j] = got[j];
+    for (int j = 0; j < 4; ++j) sm.sums[ty][tx + 16 * j] = got[j];
     __syncthreads();
     if (threadIdx.x < kKeys && j0 + (int)threadIdx.x < sq.n) {
         float w = 0.f;
 #pragma unroll
-        for (int y = 0; y < 16; ++y) w += sums[y][threadIdx.x];
+        for (int y = 0; y < 16; ++y) w += sm.sums[y][threadIdx.x];
         const long long at = (long long)unit * a.cap + j0 + threadIdx.x;
         a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + w;
     }
@@ -394,18 +432,18 @@ int launch(K kernel, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t str
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, what);
 }
-template <typename T, int ROWS>
+template <int ROWS>
 int launch_rows(const AttnArgs &a, cudaStream_t stream)
 {
-    const long long tiles = ((long long)a.max_q * a.G + ROWS - 1) / ROWS, blocks = tiles * a.batch * a.hkv;
+    const long long tiles = ((long long)a.rows_max + ROWS - 1) / ROWS, blocks = tiles * a.batch * a.hkv;
     if (blocks > 0x7fffffffLL || a.splits > 65535) {
         set_error_detail("attention: %lld blocks", blocks);
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)blocks, a.splits);
-    if (a.d <= 64) return launch(attn_simt_kernel<T, 64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel");
-    if (a.d <= 128) return launch(attn_simt_kernel<T, 128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel");
-    return launch(attn_simt_kernel<T, 256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel");
+    if (a.d <= 64) return launch(attn_simt_kernel<64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel");
+    if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel");
+    return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel");
 }
 template <typename T>
 int launch_weights(const AttnArgs &a, cudaStream_t stream)
@@ -416,18 +454,18 @@ int launch_weights(const AttnArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)blocks);
-    if (a.d <= 64) return launch(attn_weights_kernel<T, 64>, grid, sizeof(SimtSmem<64, 64>), a, stream, "attention weights kernel");
-    if (a.d <= 128) return launch(attn_weights_kernel<T, 128>, grid, sizeof(SimtSmem<128, 64>), a, stream, "attention weights kernel");
-    return launch(attn_weights_kernel<T, 256>, grid, sizeof(SimtSmem<256, 64>), a, stream, "attention weights kernel");
+    if (a.d <= 64) return launch(attn_weights_kernel<T, 64>, grid, sizeof(WeightsSmem<64>), a, stream, "attention weights kernel");
+    if (a.d <= 128) return launch(attn_weights_kernel<T, 128>, grid, sizeof(WeightsSmem<128>), a, stream, "attention weights kernel");
+    return launch(attn_weights_kernel<T, 256>, grid, sizeof(WeightsSmem<256>), a, stream, "attention weights kernel");
 }
 
 }  // namespace
 
-int launch_attn_simt(const AttnArgs &a, int dtype, cudaStream_t stream)
+int launch_attn_simt(const AttnArgs &a, cudaStream_t stream)
 {
-    const bool few = (long long)a.max_q * a.G <= 16;
-    if (dtype == WKV_F32) return few ? launch_rows<float, 16>(a, stream) : launch_rows<float, 64>(a, stream);
-    return few ? launch_rows<__nv_bfloat16, 16>(a, stream) : launch_rows<__nv_bfloat16, 64>(a, stream);
+    const long long units = (long long)a.batch * a.hkv * a.splits, enough = 148;
+    if (a.rows_max <= 16 || ((long long)a.rows_max + 31) / 32 * units < enough) return launch_rows<16>(a, stream);
+    return ((long long)a.rows_max + 63) / 64 * units < enough ? launch_rows<32>(a, stream) : launch_rows<64>(a, stream);
 }
 int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream)
 {

@@ -149,7 +149,7 @@ PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
     size_t off = 256;
     w.lse_off = off;
     off = align_up(off + (size_t)c->batch * c->n_q_heads * c->max_new * sizeof(float), 256);
-    const bool keeps_logits = c->dtype == WKV_BF16 && p.rows_max <= kLogitRows;
+    const bool keeps_logits = p.rows_max <= kLogitRows;
     const size_t parts = w.splits > 1 || keeps_logits ? (size_t)p.units * p.rows_max * w.splits : 0;
     w.ml_off = off;
     off = align_up(off + parts * sizeof(float2), 256);
@@ -365,7 +365,7 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
         if (shorter && (st = launch_attn_lse_obs_fill(a, stream)) != WKV_OK) return st;
     }
     if (attn_tc_supported(a, s->dtype) && (st = launch_attn_tc(a, nullptr, nullptr, nullptr, stream)) != WKV_ERR_UNSUPPORTED) return st;
-    return s->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, s->dtype, stream);
+    return s->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, stream);
 }
 
 size_t wkv_paged_workspace_bytes(const wkv_paged *c)
@@ -520,7 +520,7 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
         st = launch_attn_tc(a, w.pieces ? reinterpret_cast<float *>(ws + w.piece_o_off) : nullptr, reinterpret_cast<float2 *>(ws + w.piece_ml_off),
                             reinterpret_cast<long long *>(ws + w.line_off), stream);
     if (st == WKV_ERR_UNSUPPORTED) {
-        st = c->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, c->dtype, stream);
+        st = c->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, stream);
         if (st == WKV_OK && (a.splits > 1 || a.logits)) st = launch_attn_join(a, c->dtype, stream);
     }
     if (st != WKV_OK) return st;
