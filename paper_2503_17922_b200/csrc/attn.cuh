@@ -34,6 +34,7 @@ struct AttnArgs {
     int *status;                 // or null
     // key splits: `splits` > 1 leaves partial results for the joining kernel
     int splits;
+    bool clustered;              // the splits are the blocks of a cluster, which join them: no partial results in memory
     float *part_o;               // [units][rows_max][splits][d]: not yet normalised
     float2 *part_ml;             // [units][rows_max][splits]: (maximum in base 2, sum)
     int rows_max;                // max_q * G

@@ -12,14 +12,14 @@
 //
 // Where weights are wanted (FEW), the logits go to the workspace (4 bytes per row and key beside the 512 of K and V) and the joining
 // kernel adds up exp2(logit - lse), instead of K being read once more.
-#include "attn.cuh"
+#include "attn_cluster.cuh"
 
 namespace wkv {
 namespace {
 
 constexpr int kThreads = 128;
 constexpr int kKeys = 64;
-__host__ __device__ constexpr int stages_for(int dp) { return dp == 64 ? 4 : 3; }
+__host__ __device__ constexpr int stages_for(int dp) { return dp == 64 ? 4 : 2; }
 
 template <int DP>
 struct MmaSmem {
@@ -27,7 +27,7 @@ struct MmaSmem {
     __align__(128) __nv_bfloat16 v[stages_for(DP)][kKeys][DP];
     long long at[2][kKeys];                    // element offsets of a tile's rows, -1: none
     int missing[stages_for(DP) + 1][2];        // of a tile's two halves: some row has no page
-    float m[4][16], l[4][16];
+    float m[4][16], l[4][16], lse2[16];
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -72,22 +72,25 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
     constexpr int NS = stages_for(DP), kRows = FEW ? 16 : 64, kSteps = DP / 16, kGroups = FEW ? 1 : 4;   // 16-key groups per warp
     // The joining kernel may be placed now.  Another of this kind is not to be before this one ends: its blocks would crowd onto the
     // SMs that have room at that time.
-    const bool parts = a.splits > 1 || a.logits;
+    const bool clustered = FEW && a.clustered, parts = !clustered && (a.splits > 1 || a.logits);
     if (parts) pdl_trigger();
     pdl_wait();
     const int units = a.batch * a.hkv;
     // the last rows of a prompt have the most keys: they are taken first
-    const int tiles = (int)gridDim.x / units, unit = (int)blockIdx.x % units, tile = tiles - 1 - (int)blockIdx.x / units;
+    const int splits = a.splits, place_of = (int)blockIdx.x / splits, split = (int)blockIdx.x - place_of * splits;
+    const int tiles = (int)gridDim.x / splits / units, unit = place_of % units, tile = tiles - 1 - place_of / units;
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttnSeq sq = attn_seq(a, b, h);
     const int rows = sq.m * a.G, row0 = tile * kRows;
-    if (row0 >= rows) return;
+    if (row0 >= rows) {
+        if (clustered) carry_weights(a, unit, (int)((long long)sq.n * split / splits), (int)((long long)sq.n * (split + 1) / splits), kThreads);
+        return;
+    }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane >> 2, ql = lane & 3;
     const int base = sq.n - sq.m + 1;                                    // keys that query 0 attends to (may be negative)
     const int most = min(base + (min(row0 + kRows, rows) - 1) / a.G, sq.n);
     const int all_tiles = (max(most, 0) + kKeys - 1) / kKeys;
-    const int split = blockIdx.y;
-    const int t0 = (int)((long long)all_tiles * split / a.splits), t1 = (int)((long long)all_tiles * (split + 1) / a.splits);
+    const int t0 = (int)((long long)all_tiles * split / splits), t1 = (int)((long long)all_tiles * (split + 1) / splits);
     const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
 
     // rows of this thread: `quad` and quad + 8 of the warp's sixteen
@@ -165,19 +168,23 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
 #pragma unroll
         for (int grp = 0; grp < kGroups; ++grp) {
             const int key0 = (FEW ? warp : grp) * 16;
-            float s[2][4] = {};
+            // (two sums over every other step of the head dimension: half the chain of dependent instructions)
+            float s[2][4] = {}, s1[2][4] = {};
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) {
-                uint32_t kf[4];
+            for (int c = 0; c < kSteps; c += 2) {
+                uint32_t kf[4], kg[4];
                 ldmatrix4(chunk_addr<DP>(ks, key0 + (lane & 7) + ((lane >> 4) << 3), 2 * c + ((lane >> 3) & 1)), kf);
+                ldmatrix4(chunk_addr<DP>(ks, key0 + (lane & 7) + ((lane >> 4) << 3), 2 * c + 2 + ((lane >> 3) & 1)), kg);
                 mma(s[0], q[c], kf[0], kf[1]);
                 mma(s[1], q[c], kf[2], kf[3]);
+                mma(s1[0], q[c + 1], kg[0], kg[1]);
+                mma(s1[1], q[c + 1], kg[2], kg[3]);
             }
             bool unseen = false;              // some key that exists is not seen by some row
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[y][e] *= a.scale_log2;
+                for (int e = 0; e < 4; ++e) s[y][e] = (s[y][e] + s1[y][e]) * a.scale_log2;
             if (masked) {
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
@@ -321,6 +328,10 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
                 y.z = fmaf(f, part.z, y.z);
                 y.w = fmaf(f, part.w, y.w);
             }
+            if (clustered) {
+                *reinterpret_cast<float4 *>(all + r * kPad + c) = y;          // (in the place of the first warp's, which this thread has read)
+                continue;
+            }
             const int row = row0 + r, i = row / a.G, hq = h * a.G + row - i * a.G;
             if (parts) {
                 const long long at = ((long long)unit * a.rows_max + row) * a.splits + split;
@@ -333,6 +344,20 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh + c;
             *reinterpret_cast<uint2 *>(dst) = make_uint2(pack(y.x * inv, y.y * inv), pack(y.z * inv, y.w * inv));
+        }
+        if (clustered) {
+            __syncthreads();
+            float top = 0.f, sum = 0.f;
+            if (tid < 16) {
+                top = fmaxf(fmaxf(sm.m[0][tid], sm.m[1][tid]), fmaxf(sm.m[2][tid], sm.m[3][tid]));
+                const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sum += ex2(sm.m[w][tid] - ref) * sm.l[w][tid];
+                sm.m[0][tid] = top;
+                sm.l[0][tid] = sum;
+            }
+            cluster_join<__nv_bfloat16, kThreads>(a, sq, unit, b, h, row0, live, split, sm.m[0], sm.l[0], all, kPad, sm.lse2, t0 * kKeys,
+                                                  min(t1 * kKeys, sq.n));
         }
     } else {
 #pragma unroll
@@ -364,13 +389,14 @@ int launch_dp(const AttnArgs &a, cudaStream_t stream)
 {
     static SmemAsked asked;
     constexpr int kRows = FEW ? 16 : 64;
-    const long long tiles = ((long long)a.rows_max + kRows - 1) / kRows, blocks = tiles * a.batch * a.hkv;
-    if (blocks > 0x7fffffffLL || a.splits > 65535) {
+    const long long tiles = ((long long)a.rows_max + kRows - 1) / kRows, blocks = tiles * a.batch * a.hkv * a.splits;
+    if (blocks > 0x7fffffffLL) {
         set_error_detail("attention: %lld blocks", blocks);
         return WKV_ERR_LIMIT;
     }
     cudaError_t err = allow_smem(attn_mma_kernel<DP, FEW>, sizeof(MmaSmem<DP>), asked);
-    if (err == cudaSuccess) err = launch_pdl(attn_mma_kernel<DP, FEW>, dim3((unsigned)blocks, a.splits), kThreads, sizeof(MmaSmem<DP>), stream, 1, a);
+    if (err == cudaSuccess) err = launch_pdl(attn_mma_kernel<DP, FEW>, dim3((unsigned)blocks), kThreads, sizeof(MmaSmem<DP>), stream,
+                                             FEW && a.clustered ? a.splits : 1, a);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "attention kernel");
 }

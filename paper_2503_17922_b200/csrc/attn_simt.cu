@@ -8,7 +8,7 @@
 // With S key splits a block walks over one of S parts of the keys and leaves (maximum, sum, unnormalised output) per row for
 // the joining kernel.  A row's sums are taken in one order whatever else the launch holds, so results do not depend
 // on the other sequences of a batch.
-#include "attn.cuh"
+#include "attn_cluster.cuh"
 
 namespace wkv {
 namespace {
@@ -50,6 +50,7 @@ struct SimtSmem {
     float v[simt_stages(DP)][kKeys][DP];
     float p[ROWS][kKeys + 4];
     int present[simt_stages(DP)][kKeys];       // the key's page is one
+    float m[16], l[16], lse2[16];
 };
 template <int DP>
 struct WeightsSmem {
@@ -63,16 +64,24 @@ struct WeightsSmem {
 template <int DP, int ROWS>
 __device__ __forceinline__ void fetch_keys(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int st, int b, int h, long long off, int n, int j0)
 {
-    constexpr int kParts = DP / 4;
-    for (int x = threadIdx.x; x < kKeys * kParts; x += kThreads) {
-        const int r = x / kParts, c = (x - r * kParts) * 4, j = j0 + r;
-        const long long at = j < n ? attn_row(a, b, h, off, j) : -1;
-        const bool have = at >= 0 && c < a.d;
+    // a row's vectors lie in neighbouring threads; the rows' places first, so that their looking up (a trip to memory where paged) overlaps
+    constexpr int kParts = DP / 4, kEach = kKeys * kParts / kThreads;
+    const int c = (int)(threadIdx.x % kParts) * 4, r0 = threadIdx.x / kParts;
+    long long at[kEach];
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) {
+        const int j = j0 + r0 + x * (kThreads / kParts);
+        at[x] = j < n ? attn_row(a, b, h, off, j) : -1;
+    }
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) {
+        const int r = r0 + x * (kThreads / kParts);
+        const bool have = at[x] >= 0 && c < a.d;
         const int size = have ? 16 : 0;
-        const float *kp = static_cast<const float *>(a.k) + (have ? at + c : 0), *vp = static_cast<const float *>(a.v) + (have ? at + c : 0);
+        const float *kp = static_cast<const float *>(a.k) + (have ? at[x] + c : 0), *vp = static_cast<const float *>(a.v) + (have ? at[x] + c : 0);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&sm.k[st][r][c]))), "l"(kp), "r"(size) : "memory");
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&sm.v[st][r][c]))), "l"(vp), "r"(size) : "memory");
-        if (c == 0) sm.present[st][r] = at >= 0;
+        if (c == 0) sm.present[st][r] = at[x] >= 0;
     }
 }
 template <typename T, int DP>
@@ -136,22 +145,25 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     constexpr int RT = ROWS / 16, CT = DP / 64, NS = simt_stages(DP);
     // The joining kernel may be placed now.  Another of this kind is not to be before this one ends: its blocks would crowd onto the
     // SMs that have room at that time.
-    const bool parts = a.splits > 1 || a.logits;
+    const bool clustered = ROWS == 16 && a.clustered, parts = !clustered && (a.splits > 1 || a.logits);
     if (parts) pdl_trigger();
     pdl_wait();
     const int units = a.batch * a.hkv;
     // the last rows of a prompt have the most keys: they are taken first
-    const int tiles = (int)gridDim.x / units, unit = (int)blockIdx.x % units, tile = tiles - 1 - (int)blockIdx.x / units;
+    const int splits = a.splits, place = (int)blockIdx.x / splits, split = (int)blockIdx.x - place * splits;
+    const int tiles = (int)gridDim.x / splits / units, unit = place % units, tile = tiles - 1 - place / units;
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttnSeq sq = attn_seq(a, b, h);
     const int rows = sq.m * a.G, row0 = tile * ROWS;
-    if (row0 >= rows) return;
+    if (row0 >= rows) {
+        if (clustered) carry_weights(a, unit, (int)((long long)sq.n * split / splits), (int)((long long)sq.n * (split + 1) / splits), kThreads);
+        return;
+    }
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
     const int base = sq.n - sq.m + 1;                                    // keys that query 0 attends to (may be negative)
     const int most = min(base + (min(row0 + ROWS, rows) - 1) / a.G, sq.n);
     const int all_tiles = (max(most, 0) + kKeys - 1) / kKeys;
-    const int split = blockIdx.y;
-    const int t0 = (int)((long long)all_tiles * split / a.splits), t1 = (int)((long long)all_tiles * (split + 1) / a.splits);
+    const int t0 = (int)((long long)all_tiles * split / splits), t1 = (int)((long long)all_tiles * (split + 1) / splits);
     int limit[RT];
     float m[RT], l[RT];
     float4 o[RT][CT];
@@ -243,6 +255,20 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
         if (NS == 1 && t + 1 < t1) fetch_keys(a, sm, 0, b, h, sq.q_off, sq.n, j0 + kKeys);
     }
     if (!parts) pdl_trigger();
+    if (clustered) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+        float *const all = &sm.k[0][0][0];                               // [16][DP + 4]
+        if (tx == 0) {
+            sm.m[ty] = m[0];
+            sm.l[ty] = l[0];
+        }
+#pragma unroll
+        for (int x = 0; x < CT; ++x) *reinterpret_cast<float4 *>(all + ty * (DP + 4) + tx * 4 + 64 * x) = o[0][x];
+        cluster_join<float, kThreads>(a, sq, unit, b, h, row0, min(16, rows - row0), split, sm.m, sm.l, all, DP + 4, sm.lse2, t0 * kKeys,
+                                      min(t1 * kKeys, sq.n));
+        return;
+    }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = row0 + ty * RT + r;
@@ -318,62 +344,92 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
     }
 }
 
-// Joins the parts of every row: o = sum exp2(m_s - M) o_s / sum exp2(m_s - M) l_s.  A warp per row, splits in order.
+// Joins the parts of up to 16 rows: o = sum exp2(m_s - M) o_s / sum exp2(m_s - M) l_s.  The parts' factors first, a warp per row; then
+// every thread sums four columns of a row over the parts, in order, several of them in flight (one after the other 16 parts
+// took 12 us, of which the memory's latency was all).
+constexpr int kJoinParts = 64;               // factors in shared memory at a time
+struct JoinSmem {
+    float factor[16][kJoinParts];
+    float top[16], sum[16], lse2[16];
+};
 template <typename T>
-__device__ __forceinline__ float join_row(const AttnArgs &a, const AttnSeq &sq, int unit, int b, int h, int row, int lane, bool write)
+__device__ __forceinline__ void join_rows(const AttnArgs &a, JoinSmem &sm, const AttnSeq &sq, int unit, int b, int h, int row0, int n, bool write)
 {
-    const int i = row / a.G, hq = h * a.G + row - i * a.G;
-    const long long at = ((long long)unit * a.rows_max + row) * a.splits;
-    float top = -INFINITY;
-    for (int s = lane; s < a.splits; s += 32) top = fmaxf(top, a.part_ml[at + s].x);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int r = warp; r < n; r += kThreads / 32) {
+        const long long at = ((long long)unit * a.rows_max + row0 + r) * a.splits;
+        float top = -INFINITY, l = 0.f;
+        for (int s = lane; s < a.splits; s += 32) top = fmaxf(top, a.part_ml[at + s].x);
 #pragma unroll
-    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-    const float ref = top == -INFINITY ? 0.f : top;
-    // every lane its splits, then over the lanes: one order, whatever the launch
-    float l = 0.f;
-    for (int s = lane; s < a.splits; s += 32) {
-        const float2 ml = a.part_ml[at + s];
-        l += ml.y * exp2f(ml.x - ref);
-    }
-#pragma unroll
-    for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-    const float lse2 = l > 0.f || l != l ? top + log2f(l) : -INFINITY;
-    if (!write) return lse2;
-    if (lane == 0) attn_store_lse(a, b, hq, i, sq.m, lse2);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T *dst = static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh;
-    for (int c = lane * 4; c < a.d; c += 128) {
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) {
+        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        const float ref = top == -INFINITY ? 0.f : top;
+        // every lane its parts, then over the lanes: one order, whatever the launch
+        for (int s = lane; s < a.splits; s += 32) {
             const float2 ml = a.part_ml[at + s];
-            if (ml.y == 0.f) continue;                                   // a part without a key of the row
-            const float w = exp2f(ml.x - ref);
-            const float4 p = *reinterpret_cast<const float4 *>(a.part_o + (at + s) * a.d + c);
-            o.x = fmaf(w, p.x, o.x);
-            o.y = fmaf(w, p.y, o.y);
-            o.z = fmaf(w, p.z, o.z);
-            o.w = fmaf(w, p.w, o.w);
+            l += ml.y * exp2f(ml.x - ref);
         }
+#pragma unroll
+        for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+        if (lane == 0) {
+            sm.top[r] = ref;
+            sm.sum[r] = l;
+            sm.lse2[r] = l > 0.f || l != l ? top + log2f(l) : -INFINITY;
+        }
+    }
+    __syncthreads();
+    if (!write) return;
+    const int cols = a.d / 4;
+    for (int x0 = 0; x0 < n * cols; x0 += kThreads) {
+        const int x = x0 + threadIdx.x, r = x / cols, c = (x - r * cols) * 4;
+        const long long at = ((long long)unit * a.rows_max + row0 + r) * a.splits;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s0 = 0; s0 < a.splits; s0 += kJoinParts) {
+            const int parts = min(kJoinParts, a.splits - s0);
+            __syncthreads();
+            for (int y = threadIdx.x; y < n * parts; y += kThreads) {
+                const int fr = y / parts, fs = y - fr * parts;
+                const float2 ml = a.part_ml[((long long)unit * a.rows_max + row0 + fr) * a.splits + s0 + fs];
+                sm.factor[fr][fs] = ml.y == 0.f ? 0.f : exp2f(ml.x - sm.top[fr]);       // (a part without a key of the row has no output)
+            }
+            __syncthreads();
+            if (x >= n * cols) continue;
+            const float *from = a.part_o + (at + s0) * a.d + c;
+#pragma unroll 8
+            for (int s = 0; s < parts; ++s) {
+                const float f = sm.factor[r][s];
+                float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (f != 0.f) p = *reinterpret_cast<const float4 *>(from + (long long)s * a.d);
+                o.x = fmaf(f, p.x, o.x);
+                o.y = fmaf(f, p.y, o.y);
+                o.z = fmaf(f, p.z, o.z);
+                o.w = fmaf(f, p.w, o.w);
+            }
+        }
+        if (x >= n * cols) continue;
+        const int row = row0 + r, i = row / a.G, hq = h * a.G + row - i * a.G;
+        if (c == 0) attn_store_lse(a, b, hq, i, sq.m, sm.lse2[r]);
+        const float l = sm.sum[r], inv = l == 0.f ? 0.f : 1.f / l;
+        T *dst = static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh + c;
         T y[4];
         from_float(y[0], o.x * inv);
         from_float(y[1], o.y * inv);
         from_float(y[2], o.z * inv);
         from_float(y[3], o.w * inv);
-        if (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst + c) = *reinterpret_cast<float4 *>(y);
-        else *reinterpret_cast<uint2 *>(dst + c) = *reinterpret_cast<uint2 *>(y);
+        if (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst) = *reinterpret_cast<float4 *>(y);
+        else *reinterpret_cast<uint2 *>(dst) = *reinterpret_cast<uint2 *>(y);
     }
-    return lse2;
 }
+// block (unit, y): 16 rows from 16 y on
 template <typename T>
 __global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_constant__ AttnArgs a)
 {
+    __shared__ JoinSmem sm;
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.x % (a.batch * a.hkv), b = unit / a.hkv, h = unit - b * a.hkv;
-    const int lane = threadIdx.x & 31, row = (int)(blockIdx.x / (a.batch * a.hkv)) * (kThreads / 32) + (threadIdx.x >> 5);
+    const int unit = blockIdx.x % (a.batch * a.hkv), b = unit / a.hkv, h = unit - b * a.hkv, row0 = (int)(blockIdx.x / (a.batch * a.hkv)) * 16;
     const AttnSeq sq = attn_seq(a, b, h);
-    if (row < sq.m * a.G) join_row<T>(a, sq, unit, b, h, row, lane, true);
+    const int n = min(16, sq.m * a.G - row0);
+    if (n > 0) join_rows<T>(a, sm, sq, unit, b, h, row0, n, true);
 }
 // The same for up to 16 rows whose logits are in the workspace: block (unit, y) also adds up the weights of kJoinKeys keys.  Every
 // block of a unit needs the rows' normalisers and joins the few parts for itself; block 0 writes the rows.
@@ -381,25 +437,24 @@ constexpr int kJoinKeys = 4 * kThreads;
 template <typename T>
 __global__ void __launch_bounds__(kThreads) attn_join_weights_kernel(const __grid_constant__ AttnArgs a)
 {
-    __shared__ float lse2[16];
+    __shared__ JoinSmem sm;
     pdl_trigger();
     pdl_wait();
     const int unit = blockIdx.x, b = unit / a.hkv, h = unit - b * a.hkv;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const AttnSeq sq = attn_seq(a, b, h);
-    const int rows = sq.m * a.G;
-    if (blockIdx.y > 0 && (int)blockIdx.y * kJoinKeys >= sq.n) return;
-    for (int row = warp; row < rows; row += kThreads / 32) {
-        const float x = join_row<T>(a, sq, unit, b, h, row, lane, blockIdx.y == 0);
-        if (lane == 0) lse2[row] = x;
+    const int rows = sq.m * a.G, j = ((int)blockIdx.y - 1) * kJoinKeys + threadIdx.x * 4;
+    if (blockIdx.y == 0) {                                               // the first block writes the rows, the others weights
+        join_rows<T>(a, sm, sq, unit, b, h, 0, rows, true);
+        return;
     }
-    __syncthreads();
-    const int j = (int)blockIdx.y * kJoinKeys + threadIdx.x * 4;
+    if (((int)blockIdx.y - 1) * kJoinKeys >= sq.n) return;
+    join_rows<T>(a, sm, sq, unit, b, h, 0, rows, false);
     if (j >= sq.n) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     const float *x = a.logits + (long long)unit * a.rows_max * a.logit_stride + j;
+#pragma unroll 4
     for (int row = 0; row < rows; ++row) {
-        const float ref = lse2[row];
+        const float ref = sm.lse2[row];
         if (ref == -INFINITY) continue;                                  // the row attends to nothing
         const float4 s = *reinterpret_cast<const float4 *>(x + row * a.logit_stride);
         w[0] += exp2f(s.x - ref);
@@ -425,25 +480,26 @@ __global__ void lse_obs_fill_kernel(const __grid_constant__ AttnArgs a)
 }
 
 template <typename K>
-int launch(K kernel, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t stream, const char *what)
+int launch(K kernel, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t stream, const char *what, int cluster = 1)
 {
     cudaError_t err = smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-    if (err == cudaSuccess) err = launch_pdl(kernel, grid, kThreads, smem, stream, 1, a);
+    if (err == cudaSuccess) err = launch_pdl(kernel, grid, kThreads, smem, stream, cluster, a);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, what);
 }
 template <int ROWS>
 int launch_rows(const AttnArgs &a, cudaStream_t stream)
 {
-    const long long tiles = ((long long)a.rows_max + ROWS - 1) / ROWS, blocks = tiles * a.batch * a.hkv;
-    if (blocks > 0x7fffffffLL || a.splits > 65535) {
+    const long long tiles = ((long long)a.rows_max + ROWS - 1) / ROWS, blocks = tiles * a.batch * a.hkv * a.splits;
+    if (blocks > 0x7fffffffLL) {
         set_error_detail("attention: %lld blocks", blocks);
         return WKV_ERR_LIMIT;
     }
-    const dim3 grid((unsigned)blocks, a.splits);
-    if (a.d <= 64) return launch(attn_simt_kernel<64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel");
-    if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel");
-    return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel");
+    const dim3 grid((unsigned)blocks);
+    const int cluster = ROWS == 16 && a.clustered ? a.splits : 1;
+    if (a.d <= 64) return launch(attn_simt_kernel<64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel", cluster);
+    if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
+    return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel", cluster);
 }
 template <typename T>
 int launch_weights(const AttnArgs &a, cudaStream_t stream)
@@ -463,7 +519,7 @@ int launch_weights(const AttnArgs &a, cudaStream_t stream)
 
 int launch_attn_simt(const AttnArgs &a, cudaStream_t stream)
 {
-    const long long units = (long long)a.batch * a.hkv * a.splits, enough = 148;
+    const long long units = (long long)a.batch * a.hkv * a.splits, enough = 120;
     if (a.rows_max <= 16 || ((long long)a.rows_max + 31) / 32 * units < enough) return launch_rows<16>(a, stream);
     return ((long long)a.rows_max + 63) / 64 * units < enough ? launch_rows<32>(a, stream) : launch_rows<64>(a, stream);
 }
@@ -475,7 +531,7 @@ int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
 {
     const int units = a.batch * a.hkv;
     if (a.logits) {
-        const int blocks = (a.cap + kJoinKeys - 1) / kJoinKeys;
+        const int blocks = 1 + (a.cap + kJoinKeys - 1) / kJoinKeys;
         if (blocks > 65535) {
             set_error_detail("attention weights: %d rows of a unit", a.cap);
             return WKV_ERR_LIMIT;
@@ -484,7 +540,7 @@ int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
         return dtype == WKV_F32 ? launch(attn_join_weights_kernel<float>, grid, 0, a, stream, "attention joining kernel")
                                 : launch(attn_join_weights_kernel<__nv_bfloat16>, grid, 0, a, stream, "attention joining kernel");
     }
-    const long long per = kThreads / 32, blocks = ((long long)a.rows_max + per - 1) / per * units;
+    const long long blocks = ((long long)a.rows_max + 15) / 16 * units;
     if (blocks > 0x7fffffffLL) {
         set_error_detail("attention: %lld blocks", blocks);
         return WKV_ERR_LIMIT;

@@ -1,6 +1,6 @@
 // Host side of the entry points around the selection: rotary positions, the prompt's attention, and the paged cache in use
 // (append, attend, evict, row state).  Validation, workspace carve-up and kernel choice; no device memory is allocated here.
-#include "attn.cuh"
+#include "attn_cluster.cuh"
 
 #include <math.h>
 #include <string.h>
@@ -119,6 +119,7 @@ int resolve_paged(const wkv_paged *c, Paged &p)
 // Workspace of the paged entry points: status word, then what an attention or an eviction leaves between its kernels.
 struct PagedWorkspace {
     int splits;
+    bool clustered;
     size_t lse_off, ml_off, o_off, logits_off, counts_off, moves_off, total;
     long long logit_stride;      // 0: the weights are computed from K once more
     int pieces;                  // of the tensor-core kernel
@@ -128,15 +129,24 @@ struct PagedWorkspace {
 // Key splits of the kernels that take one tile of rows per block: two blocks for every SM, where each then has a tile of 64
 // keys at least; and with 1,024 keys or more to each, up to four times as many, so that sequences of different lengths
 // even out.
+// With up to 16 rows, a power of two up to eight is preferred: those are clusters, which join their splits themselves, as long as
+// all of them run at once (32 sequences of 8 heads x 4-8 K rows: 267 us as clusters of eight, 188 as five splits and a joining
+// kernel; one sequence of 8 heads x 992 rows 8.8 and 12.6) and a block has no more than kClusterBytes of keys and values to read.
 constexpr int kSplitBlocks = 2 * 148, kSplitKeys = 64, kSplitEven = 1024;
-int plan_splits(const Paged &p)
+constexpr long long kClusterBytes = 512 << 10;
+int plan_splits(const wkv_paged *c, const Paged &p, bool &clustered)
 {
     const int tile = p.rows_max <= 16 ? 16 : 64;
     const long long blocks = ((long long)p.rows_max + tile - 1) / tile * p.units;
     long long s = (kSplitBlocks + blocks - 1) / blocks;
     if (s > (p.cap + kSplitKeys - 1) / kSplitKeys) s = (p.cap + kSplitKeys - 1) / kSplitKeys;
     while (blocks * s < 4 * kSplitBlocks && p.cap / (s + 1) >= kSplitEven) ++s;
-    return s < 1 ? 1 : (int)s;
+    if (s < 1) s = 1;
+    long long power = 1;
+    while (power < s && power < kClusterSplits) power *= 2;
+    clustered = tile == 16 && blocks * power <= kSplitBlocks &&
+                (s <= power || 2ll * p.cap * c->head_dim * p.eb / kClusterSplits <= kClusterBytes);
+    return (int)(clustered ? power : s);
 }
 // More rows than this go to the tensor-core kernel where it takes the shape.
 constexpr int kFewRows = 32;
@@ -145,12 +155,12 @@ constexpr int kLogitRows = 16;
 PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
 {
     PagedWorkspace w;
-    w.splits = plan_splits(p);
+    w.splits = plan_splits(c, p, w.clustered);
     size_t off = 256;
     w.lse_off = off;
     off = align_up(off + (size_t)c->batch * c->n_q_heads * c->max_new * sizeof(float), 256);
     const bool keeps_logits = p.rows_max <= kLogitRows;
-    const size_t parts = w.splits > 1 || keeps_logits ? (size_t)p.units * p.rows_max * w.splits : 0;
+    const size_t parts = !w.clustered && (w.splits > 1 || keeps_logits) ? (size_t)p.units * p.rows_max * w.splits : 0;
     w.ml_off = off;
     off = align_up(off + parts * sizeof(float2), 256);
     w.o_off = off;
@@ -504,6 +514,7 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
     a.lse = lse ? lse : (weights_out ? reinterpret_cast<float *>(ws + w.lse_off) : nullptr);
     a.status = reinterpret_cast<int *>(ws);
     a.splits = w.splits;
+    a.clustered = w.clustered;
     a.part_ml = reinterpret_cast<float2 *>(ws + w.ml_off);
     a.part_o = reinterpret_cast<float *>(ws + w.o_off);
     a.rows_max = p.rows_max;
@@ -521,7 +532,7 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
                             reinterpret_cast<long long *>(ws + w.line_off), stream);
     if (st == WKV_ERR_UNSUPPORTED) {
         st = c->dtype == WKV_BF16 ? launch_attn_mma(a, stream) : launch_attn_simt(a, stream);
-        if (st == WKV_OK && (a.splits > 1 || a.logits)) st = launch_attn_join(a, c->dtype, stream);
+        if (st == WKV_OK && !a.clustered && (a.splits > 1 || a.logits)) st = launch_attn_join(a, c->dtype, stream);
     }
     if (st != WKV_OK) return st;
     if (weights_out && !a.logits) return launch_attn_weights(a, c->dtype, stream);

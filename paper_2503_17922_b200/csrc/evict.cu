@@ -19,11 +19,12 @@ struct SelectSmem {
     int hist[256];
     int warp_sums[2][32];
     int newest[32], recent[32];
+    unsigned lowest[32], highest[32];
     unsigned prefix;
     int remaining;
 };
 
-// A row's place in the order as a key.  With fewer recent rows than stay, they all do and have the highest key; with more,
+// A row's place in the order as a key.  With no more recent rows than stay, they all do and have the highest key; with more,
 // they alone are chosen among and all others have the lowest.  A weight's own key lies between (NaN: 1; -infinity's is 0x007fffff, infinity's
 // 0xff800000).
 __device__ __forceinline__ unsigned evict_key(float w, bool is_recent, bool among_recent)
@@ -63,21 +64,42 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
         n_recent = __reduce_add_sync(0xffffffffu, n_recent);
         if (lane == 0) sm.recent[warp] = n_recent;
         __syncthreads();
-        const bool among_recent = __reduce_add_sync(0xffffffffu, sm.recent[lane]) >= keep;
+        const int all_recent = __reduce_add_sync(0xffffffffu, sm.recent[lane]);
+        const bool among_recent = all_recent > keep;
         const bool hold = n <= kHeldKeys;
         auto fresh_key = [&](int j) { return evict_key(w[j], (long long)pos[j] > recent_from, among_recent); };
         auto key_at = [&](int j) { return hold ? held[j] : fresh_key(j); };
         if (hold)
             for (int j = tid; j < n; j += kSelThreads) held[j] = fresh_key(j);
-        // radix select of the keep-th largest, 8 bits at a time
-        unsigned prefix = 0u;
-        int remaining = keep;
+        // Radix select among the rows that are chosen among (keys that are neither lowest nor highest), 8 bits at a time over the bits in
+        // which they differ: counted from the top of all 32, nearly all weights share the first eight, and with them
+        // one counter (8,192 rows: 26 us).
+        unsigned lo = 0xffffffffu, hi = 0u;
+        for (int j = tid; j < n; j += kSelThreads) {
+            const unsigned key = key_at(j);
+            if (key == 0u || key == 0xffffffffu) continue;
+            lo = min(lo, key);
+            hi = max(hi, key);
+        }
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        if (lane == 0) {
+            sm.lowest[warp] = lo;
+            sm.highest[warp] = hi;
+        }
+        __syncthreads();
+        lo = __reduce_min_sync(0xffffffffu, sm.lowest[lane]);
+        hi = __reduce_max_sync(0xffffffffu, sm.highest[lane]);
+        unsigned prefix = 0u, mask = 0u;                          // of key - lo: bits that are known, and which
+        int remaining = among_recent ? keep : keep - all_recent, top = lo <= hi ? 32 - __clz(hi - lo) : 0;
+        const bool none = remaining == 0;                         // the recent ones are just as many as stay
 #pragma unroll 1
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            const unsigned mask = shift == 24 ? 0u : ~0u << (shift + 8);
+        while (top > 0 && !none) {
+            const int low = top > 8 ? top - 8 : 0;
+            const unsigned digit = (1u << (top - low)) - 1u;
             for (int j = tid; j < n; j += kSelThreads) {
-                const unsigned key = key_at(j);
-                if ((key & mask) == prefix) atomicAdd(&sm.hist[(key >> shift) & 255u], 1);
+                const unsigned key = key_at(j), rk = key - lo;
+                if (key != 0u && key != 0xffffffffu && (rk & mask) == prefix) atomicAdd(&sm.hist[(rk >> low) & digit], 1);
             }
             __syncthreads();
             if (warp == 0) {
@@ -98,7 +120,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
 #pragma unroll
                     for (int x = 7; x >= 0; --x) {
                         if (above < remaining && remaining <= above + c[x]) {
-                            sm.prefix = prefix | (unsigned)(lane * 8 + x) << shift;
+                            sm.prefix = prefix | (unsigned)(lane * 8 + x) << low;
                             sm.remaining = remaining - above;
                         }
                         above += c[x];
@@ -110,21 +132,26 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
             remaining = sm.remaining;
             if (tid < 256) sm.hist[tid] = 0;
             __syncthreads();
+            mask |= digit << low;
+            top = low;
         }
+        // the threshold, and how many of the rows that equal it stay (the lower ones)
+        const unsigned threshold = none ? 0xffffffffu : prefix + lo;
+        if (none) remaining = keep;
         // rows in order, kSelThreads at a time: which stay, and the two lists
         int2 *moves = a.moves + (long long)unit * a.moves_max;
         int equal_before = 0, holes = 0, fills = 0;
         for (int j0 = 0; j0 < n; j0 += kSelThreads) {
             const int j = j0 + tid;
             const unsigned key = j < n ? key_at(j) : 0u;
-            const bool equal = j < n && key == prefix;
+            const bool equal = j < n && key == threshold;
             unsigned votes = __ballot_sync(0xffffffffu, equal);
             if (lane == 0) sm.warp_sums[0][warp] = __popc(votes);
             __syncthreads();
             int sum = sm.warp_sums[0][lane];
             const int before = equal_before + __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0) + __popc(votes & ((1u << lane) - 1u));
             equal_before += __reduce_add_sync(0xffffffffu, sum);
-            const bool stays = j < n && (key > prefix || (equal && before < remaining));
+            const bool stays = j < n && (key > threshold || (equal && before < remaining));
             const bool hole = j < keep && !stays, fill = j >= keep && stays;
             // holes and fills in one count: low and high half of a word (at most 1,024 of each here)
             const unsigned hv = __ballot_sync(0xffffffffu, hole), fv = __ballot_sync(0xffffffffu, fill);
@@ -164,7 +191,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
 {
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.x / a.n_tensors, tensor = blockIdx.x % a.n_tensors, b = unit / a.hkv, h = unit - b * a.hkv;
+    const int units = a.batch * a.hkv, unit = blockIdx.x % units, tensor = blockIdx.x / units, b = unit / a.hkv, h = unit - b * a.hkv;
     const int moved = a.counts[unit], lanes = 1 << lanes_shift, lane = threadIdx.x & (lanes - 1);
     const int step = (int)gridDim.y * (kMoveThreads >> lanes_shift), vecs = a.d * a.elem_bytes / 16;
     const int2 *moves = a.moves + (long long)unit * a.moves_max;

@@ -1,8 +1,8 @@
 // Rotary positions of queries and keys, of a prompt in its tensors or of new tokens on their way into the paged cache.
 //
 // A block takes a few tokens: cosines and sines of a token's rot/2 pairs are computed once (sincospif of the angle in half
-// turns) and serve all of its heads; then every thread turns one 16-byte vector of first partners with the vector of
-// second partners (HALF order) or one vector of whole pairs (INTERLEAVED).  The angle is position * turns mod 2^64 in
+// turns) and serve all of its heads; then every thread turns vectors of first partners with the vectors of second
+// partners (HALF order) or vectors of whole pairs (INTERLEAVED).  The angle is position * turns mod 2^64 in
 // integers: exact at any position, where the product in fp32 would be off by 2^-24 of itself, 0.04 radians at position 10^6.
 // Each thread reads what it writes, so an output may be its input.  Bound by memory.
 #include "attn.cuh"
@@ -47,43 +47,29 @@ __device__ __forceinline__ bool find_token(const RopeArgs &a, long long t, Token
     return first >= 0 && t < last && tok.i < tok.m;
 }
 
-// VEC elements of 16 bytes (fast path), or single elements
+// VEC elements as they stand in memory: 2 to 16 bytes
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { typedef unsigned short type; };
+template <> struct Bits<4> { typedef unsigned type; };
+template <> struct Bits<8> { typedef uint2 type; };
+template <> struct Bits<16> { typedef uint4 type; };
 template <typename T, int VEC>
-__device__ __forceinline__ void load(const T *p, float (&x)[VEC])
-{
-    if (VEC == 1) {
-        x[0] = to_float(p[0]);
-    } else {
-        const int4 raw = *reinterpret_cast<const int4 *>(p);
-        const T *e = reinterpret_cast<const T *>(&raw);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[i] = to_float(e[i]);
-    }
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void store(T *p, const float (&x)[VEC])
-{
-    if (VEC == 1) {
-        from_float(p[0], x[0]);
-    } else {
-        int4 raw;
-        T *e = reinterpret_cast<T *>(&raw);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) from_float(e[i], x[i]);
-        *reinterpret_cast<int4 *>(p) = raw;
-    }
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void copy(const T *p, T *q)
-{
-    if (VEC == 1) q[0] = p[0];
-    else *reinterpret_cast<int4 *>(q) = *reinterpret_cast<const int4 *>(p);
-}
+struct Vec {
+    typedef typename Bits<VEC * sizeof(T)>::type Raw;
+    Raw raw;
+    __device__ __forceinline__ void load(const T *p) { raw = *reinterpret_cast<const Raw *>(p); }
+    __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<Raw *>(p) = raw; }
+    __device__ __forceinline__ float get(int i) const { return to_float(reinterpret_cast<const T *>(&raw)[i]); }
+    __device__ __forceinline__ void set(int i, float x) { from_float(reinterpret_cast<T *>(&raw)[i], x); }
+};
 
-// VEC = 16 bytes where vectors do not straddle the two halves or the end of the turned part; else single elements
-// (single pairs in INTERLEAVED order).
-template <typename T, int VEC>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a, int tokens_per_block, long long tokens)
+// A thread keeps to one piece of the rows and takes them kBatch at a time, loads first.  Pieces of a row: HALF order: half / VEC
+// pairs of vectors; INTERLEAVED: rot / VEC vectors of pairs (rot / 2 pairs of elements if VEC = 1); then the rest, copied.  VEC is
+// the largest of which the two halves, or the turned part, are whole multiples.
+constexpr int kBatch = 4;
+// PAIRS: vectors of whole pairs, one to a piece
+template <typename T, int VEC, bool PAIRS>
+__global__ void __launch_bounds__(kThreads, PAIRS ? 4 : 3) rope_kernel(const __grid_constant__ RopeArgs a, int tokens_per_block, long long tokens)
 {
     __shared__ float2 turn[kMaxPairs];
     __shared__ Token token[16];
@@ -116,89 +102,85 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         turn[x] = make_float2(cosine * a.scale, sine * a.scale);
     }
     __syncthreads();
-    // pieces of a row: HALF: `half/VEC` pairs of vectors; INTERLEAVED: rot/VEC vectors of pairs (rot/2 pairs if VEC = 1); the rest copied
     const bool inter = a.order == WKV_ROPE_INTERLEAVED;
-    const int turned = inter && VEC > 1 ? rot / VEC : half / VEC, pieces = turned + (a.d - rot) / VEC;
-    const int v_pieces = a.v ? a.d / VEC : 0;
-    const int hq = a.q ? a.hq : 0, hk = a.k ? a.hkv : 0;
-    const int per_token = (hq + hk) * pieces + hk * v_pieces;
-    for (int x = threadIdx.x; x < n * per_token; x += kThreads) {
-        const int w = x / per_token;
-        int y = x - w * per_token;
-        if (!there[w]) continue;
-        const Token tok = token[w];
-        int kind = 0, head, piece;
-        if (y < hq * pieces) {
-            head = y / pieces;
-            piece = y - head * pieces;
-        } else if ((y -= hq * pieces) < hk * pieces) {
-            kind = 1;
-            head = y / pieces;
-            piece = y - head * pieces;
-        } else {
-            y -= hk * pieces;
-            kind = 2;
-            head = y / v_pieces;
-            piece = y - head * v_pieces;
-        }
-        const T *src;
-        T *dst;
-        if (kind == 0) {
-            const long long at = (tok.off + tok.i) * a.qt + tok.b * a.qb + head * a.qh;
-            src = static_cast<const T *>(a.q) + at;
-            dst = static_cast<T *>(a.q_out) + at;
-        } else {
-            const long long at = (tok.off + tok.i) * a.kt + tok.b * a.kb + head * a.kh;
-            src = static_cast<const T *>(kind == 1 ? a.k : a.v) + at;
-            if (a.table) {
-                const long long unit = (long long)tok.b * a.hkv + head, row = (long long)max(a.lengths[unit], 0) + tok.i;
-                if (row >= a.cap) continue;
-                const int pg = (int)row / a.page_size, page = __ldg(a.table + (long long)tok.b * a.max_pages + pg);
-                if (kind == 1 && piece == 0) {
-                    if (a.row_positions) a.row_positions[unit * a.cap + row] = a.positions[t0 + w];
-                    if (a.row_weights) a.row_weights[unit * a.cap + row] = 0.f;
+    const int turned = PAIRS ? rot / VEC : half / VEC, pieces = turned + (a.d - rot) / VEC;
+    const int hq = a.q ? a.hq : 0, hk = a.k ? a.hkv : 0, hv = a.v ? a.hkv : 0, rows = hq + hk + hv;
+    // values are copied whole: with `turned` pieces of two vectors a thread takes two of theirs as well
+    const int width = min(pieces, kThreads), step = kThreads / width;
+    if ((int)threadIdx.x >= step * width) return;
+    for (int piece = threadIdx.x % width; piece < pieces; piece += width) {
+        const bool turns = piece < turned;
+        const int j = !turns ? rot + (piece - turned) * VEC : (PAIRS || !inter ? piece * VEC : 2 * piece);
+        const int k = turns && !PAIRS ? (inter ? j + 1 : j + half) : -1;              // the second vector of a pair
+        for (int y0 = threadIdx.x / width; y0 < n * rows; y0 += step * kBatch) {
+            Vec<T, VEC> first[kBatch], second[PAIRS ? 1 : kBatch];
+            T *dst[kBatch];
+            int at[kBatch];                                     // token, and bit 8: a row of values
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int y = y0 + u * step;
+                dst[u] = nullptr;
+                at[u] = 0;
+                if (y >= n * rows) continue;
+                const int w = y / rows, row = y - w * rows;
+                if (!there[w]) continue;
+                const Token tok = token[w];
+                const T *src;
+                if (row < hq) {
+                    const long long off = (tok.off + tok.i) * a.qt + tok.b * a.qb + row * a.qh;
+                    src = static_cast<const T *>(a.q) + off;
+                    dst[u] = static_cast<T *>(a.q_out) + off;
+                } else {
+                    const bool value = row >= hq + hk;
+                    const int head = row - hq - (value ? hk : 0);
+                    const long long off = (tok.off + tok.i) * a.kt + tok.b * a.kb + head * a.kh;
+                    src = static_cast<const T *>(value ? a.v : a.k) + off;
+                    if (a.table) {
+                        const long long unit = (long long)tok.b * a.hkv + head, r = (long long)max(a.lengths[unit], 0) + tok.i;
+                        if (r >= a.cap) continue;
+                        const int pg = (int)r / a.page_size, page = __ldg(a.table + (long long)tok.b * a.max_pages + pg);
+                        if (!value && piece == 0) {
+                            if (a.row_positions) a.row_positions[unit * a.cap + r] = a.positions[t0 + w];
+                            if (a.row_weights) a.row_weights[unit * a.cap + r] = 0.f;
+                        }
+                        if ((unsigned)page >= (unsigned)a.num_pages) continue;
+                        dst[u] = static_cast<T *>(value ? a.v_out : a.k_out) + page * a.page_stride + head * a.head_stride +
+                                 (r - (long long)pg * a.page_size) * a.row_stride;
+                    } else {
+                        dst[u] = static_cast<T *>(a.k_out) + off;
+                    }
+                    if (value) at[u] = 256;
                 }
-                if ((unsigned)page >= (unsigned)a.num_pages) continue;
-                dst = static_cast<T *>(kind == 1 ? a.k_out : a.v_out) + page * a.page_stride + head * a.head_stride +
-                      (row - (long long)pg * a.page_size) * a.row_stride;
-            } else {
-                dst = static_cast<T *>(a.k_out) + at;
+                at[u] |= w;
+                first[u].load(src + j);
+                if (!PAIRS && k >= 0) second[PAIRS ? 0 : u].load(src + k);
             }
-        }
-        if (kind == 2) {
-            copy<T, VEC>(src + piece * VEC, dst + piece * VEC);
-            continue;
-        }
-        if (piece >= turned) {
-            const int c = rot + (piece - turned) * VEC;
-            if (src != dst) copy<T, VEC>(src + c, dst + c);
-            continue;
-        }
-        const float2 *tr = turn + w * half;
-        if (!inter || VEC == 1) {
-            const int j = inter ? 2 * piece : piece * VEC, k = inter ? j + 1 : j + half;
-            float p[VEC], q[VEC], u[VEC], v[VEC];
-            load<T, VEC>(src + j, p);
-            load<T, VEC>(src + k, q);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float2 cs = tr[piece * VEC + e];
-                u[e] = p[e] * cs.x - q[e] * cs.y;
-                v[e] = q[e] * cs.x + p[e] * cs.y;
-            }
-            store<T, VEC>(dst + j, u);
-            store<T, VEC>(dst + k, v);
-        } else {
-            constexpr int kPairs = VEC > 1 ? VEC / 2 : 1;
-            float p[VEC], u[VEC];
-            load<T, VEC>(src + piece * VEC, p);
+            for (int u = 0; u < kBatch; ++u) {
+                if (!dst[u]) continue;
+                if (turns && at[u] < 256) {
+                    const float2 *tr = turn + at[u] * half;
+                    if (PAIRS) {
 #pragma unroll
-            for (int e = 0; e < kPairs; ++e) {
-                const float2 cs = tr[piece * kPairs + e];
-                u[2 * e] = p[2 * e] * cs.x - p[(2 * e + 1) % VEC] * cs.y;
-                u[(2 * e + 1) % VEC] = p[(2 * e + 1) % VEC] * cs.x + p[2 * e] * cs.y;
+                        for (int e = 0; e + 1 < VEC; e += 2) {
+                            const float2 cs = tr[piece * (VEC / 2) + e / 2];
+                            const float p = first[u].get(e), q = first[u].get(e + 1);
+                            first[u].set(e, p * cs.x - q * cs.y);
+                            first[u].set(e + 1, q * cs.x + p * cs.y);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            const float2 cs = tr[piece * VEC + e];
+                            const float p = first[u].get(e), q = second[PAIRS ? 0 : u].get(e);
+                            first[u].set(e, p * cs.x - q * cs.y);
+                            second[PAIRS ? 0 : u].set(e, q * cs.x + p * cs.y);
+                        }
+                    }
+                }
+                first[u].store(dst[u] + j);
+                if (!PAIRS && k >= 0) second[PAIRS ? 0 : u].store(dst[u] + k);
             }
-            store<T, VEC>(dst + piece * VEC, u);
         }
     }
 }
@@ -209,8 +191,6 @@ int launch(const RopeArgs &a, cudaStream_t stream)
     constexpr int kVec = 16 / sizeof(T);
     const int half = a.turns ? a.rot / 2 : 0;
     const long long tokens = a.cu_q ? a.total_q : (long long)a.batch * a.max_q;
-    // vectors must end where the turned part does, and in HALF order where its first half does
-    const bool vectors = a.order == WKV_ROPE_HALF ? half % kVec == 0 : (2 * half) % kVec == 0;
     // Tokens of a block: several where there are plenty, so that the threads that have no pair to compute angles for wait less
     long long per = tokens / (148 * 8);
     per = per < 1 ? 1 : (per > 4 ? 4 : per);
@@ -221,8 +201,15 @@ int launch(const RopeArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)(blocks > 0 ? blocks : 1));
-    const cudaError_t err = vectors ? launch_pdl(rope_kernel<T, kVec>, grid, kThreads, 0, stream, 1, a, (int)per, tokens)
-                                    : launch_pdl(rope_kernel<T, 1>, grid, kThreads, 0, stream, 1, a, (int)per, tokens);
+    // vectors must end where the turned part does, and in HALF order where its first half does
+    const bool pairs = a.order == WKV_ROPE_INTERLEAVED;
+    const int part = pairs ? 2 * half : half;
+    auto go = [&](auto kernel) { return launch_pdl(kernel, grid, kThreads, 0, stream, 1, a, (int)per, tokens); };
+    cudaError_t err;
+    if (part % kVec == 0) err = pairs ? go(rope_kernel<T, kVec, true>) : go(rope_kernel<T, kVec, false>);
+    else if (part % (kVec / 2) == 0) err = pairs ? go(rope_kernel<T, kVec / 2, true>) : go(rope_kernel<T, kVec / 2, false>);
+    else if (part % 2 == 0) err = pairs ? go(rope_kernel<T, 2, true>) : go(rope_kernel<T, 2, false>);
+    else err = go(rope_kernel<T, 1, false>);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "rotary positions kernel");
 }
