@@ -4,13 +4,19 @@
 // turns) and serve all of its heads; then every thread turns vectors of first partners with the vectors of second
 // partners (HALF order) or vectors of whole pairs (INTERLEAVED).  The angle is position * turns mod 2^64 in
 // integers: exact at any position, where the product in fp32 would be off by 2^-24 of itself, 0.04 radians at position 10^6.
-// Each thread reads what it writes, so an output may be its input.  Bound by memory.
+// Each thread reads what it writes, so an output may be its input.
+//
+// Bound by memory: 32,768 tokens of 40 rows of 128 in bf16, 64 of each turned, take 114 us, 5.9 TB/s read and written, and 118 us
+// with all 128 turned in HALF order.  Two rows in flight per thread leave room for seven or eight blocks per SM; four rows (half as
+// many blocks) took 128 us, one 122; four tokens per block: eight took 117.  When each thread worked out its own addresses,
+// piece by piece, the divisions and strides took as long as the memory (186 us).
 #include "attn.cuh"
 
 namespace wkv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBatch = 2;                // rows that a thread has in flight
 constexpr int kMaxPairs = 2048;          // rot/2 at most, per block: cosines and sines in shared memory (16 KB)
 
 __device__ __forceinline__ float to_float(float x) { return x; }
@@ -63,15 +69,24 @@ struct Vec {
     __device__ __forceinline__ void set(int i, float x) { from_float(reinterpret_cast<T *>(&raw)[i], x); }
 };
 
-// A thread keeps to one piece of the rows and takes them kBatch at a time, loads first.  Pieces of a row: HALF order: half / VEC
-// pairs of vectors; INTERLEAVED: rot / VEC vectors of pairs (rot / 2 pairs of elements if VEC = 1); then the rest, copied.  VEC is
-// the largest of which the two halves, or the turned part, are whole multiples.
-constexpr int kBatch = 4;
+// A row on its way: where it is read and written (null: nowhere), and its token's cosines and sines (-1: copied as it is)
+struct Row {
+    const void *src;
+    void *dst;
+};
+
+// The rows of a block's tokens are listed in shared memory, one per thread and kThreads at a time: the divisions, the strides
+// and the look-up of the page are done once for a row, not once for each of its pieces.  A thread keeps to one piece of the rows and
+// takes them kBatch at a time, loads first.  Pieces of a row: HALF order: half / VEC pairs of vectors; INTERLEAVED: rot / VEC
+// vectors of pairs (rot / 2 pairs of elements if VEC = 1); then the rest, copied.  VEC is the largest of which the two halves, or
+// the turned part, are whole multiples.
 // PAIRS: vectors of whole pairs, one to a piece
 template <typename T, int VEC, bool PAIRS>
-__global__ void __launch_bounds__(kThreads, PAIRS ? 4 : 3) rope_kernel(const __grid_constant__ RopeArgs a, int tokens_per_block, long long tokens)
+__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a, int tokens_per_block, long long tokens)
 {
-    __shared__ float2 turn[kMaxPairs];
+    __shared__ __align__(16) float2 turn[kMaxPairs];
+    __shared__ Row list[kThreads];
+    __shared__ int list_token[kThreads];
     __shared__ Token token[16];
     __shared__ int there[16];
     pdl_trigger();
@@ -101,87 +116,93 @@ __global__ void __launch_bounds__(kThreads, PAIRS ? 4 : 3) rope_kernel(const __g
         sincospif((float)(int)(angle >> 32) * (1.f / 2147483648.f), &sine, &cosine);      // angle in half turns, -1 .. 1
         turn[x] = make_float2(cosine * a.scale, sine * a.scale);
     }
-    __syncthreads();
     const bool inter = a.order == WKV_ROPE_INTERLEAVED;
     const int turned = PAIRS ? rot / VEC : half / VEC, pieces = turned + (a.d - rot) / VEC;
     const int hq = a.q ? a.hq : 0, hk = a.k ? a.hkv : 0, hv = a.v ? a.hkv : 0, rows = hq + hk + hv;
-    // values are copied whole: with `turned` pieces of two vectors a thread takes two of theirs as well
-    const int width = min(pieces, kThreads), step = kThreads / width;
-    if ((int)threadIdx.x >= step * width) return;
-    for (int piece = threadIdx.x % width; piece < pieces; piece += width) {
-        const bool turns = piece < turned;
-        const int j = !turns ? rot + (piece - turned) * VEC : (PAIRS || !inter ? piece * VEC : 2 * piece);
-        const int k = turns && !PAIRS ? (inter ? j + 1 : j + half) : -1;              // the second vector of a pair
-        for (int y0 = threadIdx.x / width; y0 < n * rows; y0 += step * kBatch) {
-            Vec<T, VEC> first[kBatch], second[PAIRS ? 1 : kBatch];
-            T *dst[kBatch];
-            int at[kBatch];                                     // token, and bit 8: a row of values
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int y = y0 + u * step;
-                dst[u] = nullptr;
-                at[u] = 0;
-                if (y >= n * rows) continue;
-                const int w = y / rows, row = y - w * rows;
-                if (!there[w]) continue;
-                const Token tok = token[w];
-                const T *src;
+    const int width = min(pieces, kThreads), step = kThreads / width, slot = threadIdx.x / width;
+    for (int y0 = 0; y0 < n * rows; y0 += kThreads) {
+        const int listed = min(n * rows - y0, kThreads);
+        if (y0 > 0) __syncthreads();
+        if ((int)threadIdx.x < listed) {
+            const int y = y0 + threadIdx.x, w = y / rows, row = y - w * rows;
+            const Token tok = token[w];
+            Row r = {nullptr, nullptr};
+            int kind = w;
+            if (there[w]) {
                 if (row < hq) {
                     const long long off = (tok.off + tok.i) * a.qt + tok.b * a.qb + row * a.qh;
-                    src = static_cast<const T *>(a.q) + off;
-                    dst[u] = static_cast<T *>(a.q_out) + off;
+                    r.src = static_cast<const T *>(a.q) + off;
+                    r.dst = static_cast<T *>(a.q_out) + off;
                 } else {
                     const bool value = row >= hq + hk;
                     const int head = row - hq - (value ? hk : 0);
                     const long long off = (tok.off + tok.i) * a.kt + tok.b * a.kb + head * a.kh;
-                    src = static_cast<const T *>(value ? a.v : a.k) + off;
+                    r.src = static_cast<const T *>(value ? a.v : a.k) + off;
+                    if (value) kind = -1;
                     if (a.table) {
-                        const long long unit = (long long)tok.b * a.hkv + head, r = (long long)max(a.lengths[unit], 0) + tok.i;
-                        if (r >= a.cap) continue;
-                        const int pg = (int)r / a.page_size, page = __ldg(a.table + (long long)tok.b * a.max_pages + pg);
-                        if (!value && piece == 0) {
-                            if (a.row_positions) a.row_positions[unit * a.cap + r] = a.positions[t0 + w];
-                            if (a.row_weights) a.row_weights[unit * a.cap + r] = 0.f;
-                        }
-                        if ((unsigned)page >= (unsigned)a.num_pages) continue;
-                        dst[u] = static_cast<T *>(value ? a.v_out : a.k_out) + page * a.page_stride + head * a.head_stride +
-                                 (r - (long long)pg * a.page_size) * a.row_stride;
-                    } else {
-                        dst[u] = static_cast<T *>(a.k_out) + off;
-                    }
-                    if (value) at[u] = 256;
-                }
-                at[u] |= w;
-                first[u].load(src + j);
-                if (!PAIRS && k >= 0) second[PAIRS ? 0 : u].load(src + k);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                if (!dst[u]) continue;
-                if (turns && at[u] < 256) {
-                    const float2 *tr = turn + at[u] * half;
-                    if (PAIRS) {
-#pragma unroll
-                        for (int e = 0; e + 1 < VEC; e += 2) {
-                            const float2 cs = tr[piece * (VEC / 2) + e / 2];
-                            const float p = first[u].get(e), q = first[u].get(e + 1);
-                            first[u].set(e, p * cs.x - q * cs.y);
-                            first[u].set(e + 1, q * cs.x + p * cs.y);
+                        const long long unit = (long long)tok.b * a.hkv + head, at = (long long)max(a.lengths[unit], 0) + tok.i;
+                        if (at < a.cap) {
+                            const int pg = (int)at / a.page_size, page = __ldg(a.table + (long long)tok.b * a.max_pages + pg);
+                            if (!value) {
+                                if (a.row_positions) a.row_positions[unit * a.cap + at] = a.positions[t0 + w];
+                                if (a.row_weights) a.row_weights[unit * a.cap + at] = 0.f;
+                            }
+                            if ((unsigned)page < (unsigned)a.num_pages)
+                                r.dst = static_cast<T *>(value ? a.v_out : a.k_out) + page * a.page_stride + head * a.head_stride +
+                                        (at - (long long)pg * a.page_size) * a.row_stride;
                         }
                     } else {
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            const float2 cs = tr[piece * VEC + e];
-                            const float p = first[u].get(e), q = second[PAIRS ? 0 : u].get(e);
-                            first[u].set(e, p * cs.x - q * cs.y);
-                            second[PAIRS ? 0 : u].set(e, q * cs.x + p * cs.y);
-                        }
+                        r.dst = static_cast<T *>(a.k_out) + off;
                     }
                 }
-                first[u].store(dst[u] + j);
-                if (!PAIRS && k >= 0) second[PAIRS ? 0 : u].store(dst[u] + k);
             }
+            list[threadIdx.x] = r;
+            list_token[threadIdx.x] = kind;
         }
+        __syncthreads();
+        if (slot < step)
+            for (int piece = threadIdx.x - slot * width; piece < pieces; piece += width) {
+                const bool turns = piece < turned;
+                const int j = !turns ? rot + (piece - turned) * VEC : (PAIRS || !inter ? piece * VEC : 2 * piece);
+                const int k = inter ? j + 1 : j + half;                       // the second vector of a pair
+                const float2 *tr = turn + (PAIRS ? piece * (VEC / 2) : piece * VEC);
+                for (int x0 = slot; x0 < listed; x0 += step * kBatch) {
+                    Vec<T, VEC> first[kBatch], second[PAIRS ? 1 : kBatch];
+                    T *dst[kBatch];
+                    int w[kBatch];
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {
+                        const int x = x0 + u * step;
+                        dst[u] = nullptr;
+                        w[u] = -1;
+                        if (x >= listed) continue;
+                        const T *src = static_cast<const T *>(list[x].src);
+                        dst[u] = static_cast<T *>(list[x].dst);
+                        w[u] = list_token[x];
+                        if (!dst[u]) continue;
+                        first[u].load(src + j);
+                        if (!PAIRS && turns) second[PAIRS ? 0 : u].load(src + k);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {
+                        if (!dst[u]) continue;
+                        if (turns && w[u] >= 0) {
+                            const float2 *cs = tr + w[u] * half;
+#pragma unroll
+                            for (int e = 0; e < VEC; e += PAIRS ? 2 : 1) {
+                                Vec<T, VEC> &to = PAIRS ? first[u] : second[PAIRS ? 0 : u];
+                                constexpr int kNext = PAIRS ? 1 : 0;
+                                const float2 t = cs[PAIRS ? e / 2 : e];
+                                const float p = first[u].get(e), q = to.get(e + kNext);
+                                first[u].set(e, p * t.x - q * t.y);
+                                to.set(e + kNext, q * t.x + p * t.y);
+                            }
+                        }
+                        first[u].store(dst[u] + j);
+                        if (!PAIRS && turns) second[PAIRS ? 0 : u].store(dst[u] + k);
+                    }
+                }
+            }
     }
 }
 
