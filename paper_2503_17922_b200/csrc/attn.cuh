@@ -110,7 +110,8 @@ int attn_tc_pieces(long long units, int max_q, int G, int cap, int *rows, int *i
 int launch_attn_mma(const AttnArgs &a, cudaStream_t stream);         // bf16
 int launch_attn_simt(const AttnArgs &a, cudaStream_t stream);         // fp32
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream);       // with a.logits: and the weights
-int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream);    // reads a.lse
+int launch_attn_weights(const AttnArgs &a, cudaStream_t stream);      // fp32; reads a.lse
+int launch_attn_mma_weights(const AttnArgs &a, cudaStream_t stream);  // bf16; reads a.lse
 int launch_attn_lse_obs_fill(const AttnArgs &a, cudaStream_t stream);
 
 // rotary positions

@@ -1,6 +1,6 @@
 // Attention on warp-level matrix instructions (m16n8k16, bf16): single tokens and short chunks over the paged cache, where the
-// bytes of K and V bound the time, and the shapes that the tcgen05 kernel does not take (head dimensions other than 64 and 128,
-// pages of odd sizes).
+// bytes of K and V bound the time, and the shapes that the tcgen05 kernel does not take (head dimensions beyond 128,
+// pages of sizes that eight does not divide).
 //
 // A block of four warps walks over the keys of one unit (or a split of them) in tiles of 64, which come through a ring of
 // asynchronous 16-byte copies: two or three tiles are in flight while one is worked on.  Rows (position x head of the group) sit
@@ -384,6 +384,136 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
     }
 }
 
+// ---- weights that the rows of the cache receive from longer chunks --------------------------------
+// A block takes WARPS * 16 * F keys of a unit and sums exp2(logit - lse) over all of the unit's queries that see them: the logits are
+// computed once more, from the normalisers that the attention has written.  The keys sit on the M side of the instruction and
+// stay in registers, 16 F for each warp; the queries come through a ring in tiles of 64, and every fragment of them serves F
+// instructions.  Sums are fp32, over a thread's queries in order and then over the four threads of a key: one order, no atomics.
+//
+// Bound by the instructions: 2 * keys * rows * d.  Four sequences of 10-16 K rows and up to 512 new tokens of 32 heads, d = 128: 545 us
+// (on the CUDA cores 4,650); of up to 64 tokens 102 us (660).
+constexpr int kWeightRows = 64, kWeightStages = 3;
+template <int DP>
+struct WeightsSmem {
+    __align__(128) __nv_bfloat16 q[kWeightStages][kWeightRows][DP];
+    __align__(16) float lse[kWeightStages][kWeightRows];
+    __align__(16) int limit[kWeightStages][kWeightRows];           // keys that the row sees; 0: there is no such row
+};
+template <int DP, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) attn_mma_weights_kernel(const __grid_constant__ AttnArgs a)
+{
+    extern __shared__ __align__(128) unsigned char raw[];
+    WeightsSmem<DP> &sm = *reinterpret_cast<WeightsSmem<DP> *>(raw);
+    constexpr int F = DP == 256 ? 1 : 2, NS = kWeightStages, kSteps = DP / 16, kBlockKeys = WARPS * 16 * F, kBlock = WARPS * 32;
+    pdl_wait();
+    const int units = a.batch * a.hkv, unit = (int)blockIdx.x % units, j0 = (int)blockIdx.x / units * kBlockKeys;
+    const int b = unit / a.hkv, h = unit - b * a.hkv;
+    const AttnSeq sq = attn_seq(a, b, h);
+    if (j0 >= sq.n) return;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane >> 2, ql = lane & 3;
+    const int rows = sq.m * a.G, base = sq.n - sq.m + 1;
+    const int key0 = j0 + warp * 16 * F + quad;                    // this thread's keys: key0 + 16 f + 8 x
+
+    // queries in front of the block's first key do not attend to any of it
+    const int first = base > j0 ? 0 : (int)min((long long)(j0 - base + 1) * a.G, (long long)rows), tiles = (rows - first + kWeightRows - 1) / kWeightRows;
+    constexpr int kChunks = DP / 8, kRowsAtOnce = kBlock / kChunks;
+    const int chunk = tid % kChunks;
+    auto load = [&](int t) {
+        if (t < tiles) {
+            const int st = t % NS;
+            const uint32_t qs = smem_addr(&sm.q[st][0][0]);
+#pragma unroll
+            for (int r = tid / kChunks; r < kWeightRows; r += kRowsAtOnce) {
+                const int row = first + t * kWeightRows + r, i = row / a.G, g = row - i * a.G;
+                const bool have = row < rows && chunk * 8 < a.d;
+                const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(a.q);
+                if (have) p += (sq.q_off + i) * a.qt + b * a.qb + (long long)(h * a.G + g) * a.qh + chunk * 8;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(chunk_addr<DP>(qs, r, chunk)), "l"(p), "r"(have ? 16 : 0) : "memory");
+            }
+            if (tid < kWeightRows) {
+                const int row = first + t * kWeightRows + tid, i = row / a.G, g = row - i * a.G;
+                const float *p = a.lse;
+                if (row < rows) p += ((long long)b * a.hq + h * a.G + g) * a.max_q + i;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_addr(&sm.lse[st][tid])), "l"(p), "r"(row < rows ? 4 : 0) : "memory");
+                sm.limit[st][tid] = row < rows ? base + i : 0;
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int x = 0; x < NS - 1; ++x) load(x);
+
+    uint32_t k[F][kSteps][4];
+    bool there[F][2];
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int j = key0 + 16 * f + 8 * x;
+            const long long at = j < sq.n ? attn_row(a, b, h, sq.q_off, j) : -1;
+            there[f][x] = at >= 0;
+            const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(a.k) + (at >= 0 ? at : 0);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int c = s * 16 + y * 8 + ql * 2;
+                    k[f][s][2 * y + x] = at >= 0 && c < a.d ? __ldg(reinterpret_cast<const uint32_t *>(p + c)) : 0u;
+                }
+        }
+    float sum[F][2] = {};
+    for (int t = 0; t < tiles; ++t) {
+        const int st = t % NS, row0 = first + t * kWeightRows;
+        asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
+        __syncthreads();                      // tile t has landed for all; the stage of tile t - 1 is free
+        load(t + NS - 1);
+        const bool masked = j0 + kBlockKeys > base + row0 / a.G || row0 + kWeightRows > rows;
+        const uint32_t qs = smem_addr(&sm.q[st][0][0]);
+#pragma unroll 1
+        for (int g = 0; g < kWeightRows; g += 16) {
+            float s[F][2][4] = {};
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) {
+                uint32_t qf[4];
+                ldmatrix4(chunk_addr<DP>(qs, g + (lane & 7) + ((lane >> 4) << 3), 2 * c + ((lane >> 3) & 1)), qf);
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    mma(s[f][0], k[f][c], qf[0], qf[1]);
+                    mma(s[f][1], k[f][c], qf[2], qf[3]);
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int r = g + y * 8 + ql * 2;
+                const float2 lse = *reinterpret_cast<const float2 *>(&sm.lse[st][r]);
+                const float ref[2] = {lse.x * 1.44269504088896341f, lse.y * 1.44269504088896341f};
+                const int2 limit = masked ? *reinterpret_cast<const int2 *>(&sm.limit[st][r]) : make_int2(INT_MAX, INT_MAX);
+#pragma unroll
+                for (int f = 0; f < F; ++f)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int j = key0 + 16 * f + 8 * x;
+                        const float w0 = ex2(fmaf(s[f][y][2 * x], a.scale_log2, -ref[0])), w1 = ex2(fmaf(s[f][y][2 * x + 1], a.scale_log2, -ref[1]));
+                        if (j < limit.x) sum[f][x] += w0;
+                        if (j < limit.y) sum[f][x] += w1;
+                    }
+            }
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    pdl_trigger();
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            float w = sum[f][x];
+            w += __shfl_xor_sync(0xffffffffu, w, 1);
+            w += __shfl_xor_sync(0xffffffffu, w, 2);
+            const int j = key0 + 16 * f + 8 * x;
+            const long long at = (long long)unit * a.cap + j;
+            if (ql == 0 && j < sq.n) a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + (there[f][x] ? w : 0.f);
+        }
+}
+
 template <int DP, bool FEW>
 int launch_dp(const AttnArgs &a, cudaStream_t stream)
 {
@@ -401,8 +531,30 @@ int launch_dp(const AttnArgs &a, cudaStream_t stream)
     return check_cuda(err, "attention kernel");
 }
 
+template <int DP, int WARPS>
+int launch_weights(const AttnArgs &a, cudaStream_t stream)
+{
+    static SmemAsked asked;
+    constexpr int kBlockKeys = WARPS * 16 * (DP == 256 ? 1 : 2);
+    const long long blocks = ((long long)a.cap + kBlockKeys - 1) / kBlockKeys * a.batch * a.hkv;
+    // (half as many keys to a block where that leaves SMs without one)
+    if (WARPS > 4 && blocks < 2 * 148) return launch_weights<DP, 4>(a, stream);
+    if (blocks > 0x7fffffffLL) {
+        set_error_detail("attention weights: %lld blocks", blocks);
+        return WKV_ERR_LIMIT;
+    }
+    cudaError_t err = allow_smem(attn_mma_weights_kernel<DP, WARPS>, sizeof(WeightsSmem<DP>), asked);
+    if (err == cudaSuccess) err = launch_pdl(attn_mma_weights_kernel<DP, WARPS>, dim3((unsigned)blocks), WARPS * 32, sizeof(WeightsSmem<DP>), stream, 1, a);
+    if (err == cudaSuccess) count_launches(1);
+    return check_cuda(err, "attention weights kernel");
+}
+
 }  // namespace
 
+int launch_attn_mma_weights(const AttnArgs &a, cudaStream_t stream)
+{
+    return a.d <= 64 ? launch_weights<64, 8>(a, stream) : a.d <= 128 ? launch_weights<128, 8>(a, stream) : launch_weights<256, 8>(a, stream);
+}
 int launch_attn_mma(const AttnArgs &a, cudaStream_t stream)
 {
     if (a.rows_max <= 16) return a.d <= 64 ? launch_dp<64, true>(a, stream) : a.d <= 128 ? launch_dp<128, true>(a, stream) : launch_dp<256, true>(a, stream);

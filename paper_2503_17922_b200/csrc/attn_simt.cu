@@ -1,4 +1,4 @@
-// Attention on the CUDA cores for fp32, and the joining and weights kernels of all types.  One block holds ROWS rows of one
+// Attention on the CUDA cores for fp32, its weights kernel, and the joining kernels of all types.  One block holds ROWS rows of one
 // unit in shared memory and walks over the unit's keys in tiles of 64 with a running maximum and sum per row; everything is
 // fp32, products in plain multiply-adds, which bound it (2 * 64 * d per row and tile).  A tile's keys and values come by asynchronous copies
 // while the one before is worked on.
@@ -16,29 +16,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kKeys = 64;
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_float(float &y, float x) { y = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16 &y, float x) { y = __float2bfloat16_rn(x); }
 
-// one row of d elements into shared memory as fp32, zero from d to DP; `p` null: zeros.  16-byte vectors, lanes of a row together.
-template <typename T, int DP>
-__device__ __forceinline__ void load_row_part(float *dst, const T *p, int d, int part)
+// four elements of a row of d into shared memory, zeros from d on; `p` null: zeros
+template <int DP>
+__device__ __forceinline__ void load_row_part(float *dst, const float *p, int d, int part)
 {
-    constexpr int kVec = 16 / sizeof(T);
-    const int c = part * kVec;
-    float x[kVec];
-    if (p && c < d) {
-        const int4 raw = *reinterpret_cast<const int4 *>(p + c);
-        const T *e = reinterpret_cast<const T *>(&raw);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = to_float(e[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kVec; i += 4) *reinterpret_cast<float4 *>(dst + c + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    const int c = part * 4;
+    *reinterpret_cast<float4 *>(dst + c) = p && c < d ? *reinterpret_cast<const float4 *>(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
 // Stages of key tiles: two where they fit.
@@ -84,25 +70,25 @@ __device__ __forceinline__ void fetch_keys(const AttnArgs &a, SimtSmem<DP, ROWS>
         if (c == 0) sm.present[st][r] = at[x] >= 0;
     }
 }
-template <typename T, int DP>
+template <int DP>
 __device__ __forceinline__ void load_keys(const AttnArgs &a, WeightsSmem<DP> &sm, int b, int h, long long off, int n, int j0)
 {
-    constexpr int kVec = 16 / sizeof(T), kParts = DP / kVec;
+    constexpr int kParts = DP / 4;
     for (int x = threadIdx.x; x < kKeys * kParts; x += kThreads) {
         const int r = x / kParts, part = x - r * kParts, j = j0 + r;
         const long long at = j < n ? attn_row(a, b, h, off, j) : -1;
-        load_row_part<T, DP>(sm.k[r], at >= 0 ? static_cast<const T *>(a.k) + at : nullptr, a.d, part);
+        load_row_part<DP>(sm.k[r], at >= 0 ? static_cast<const float *>(a.k) + at : nullptr, a.d, part);
         if (part == 0) sm.present[r] = at >= 0;
     }
 }
-template <typename T, int DP, int ROWS>
+template <int DP, int ROWS>
 __device__ __forceinline__ void load_queries(const AttnArgs &a, float (&q)[ROWS][DP + 4], int b, int h, long long off, int row0, int rows)
 {
-    constexpr int kVec = 16 / sizeof(T), kParts = DP / kVec;
+    constexpr int kParts = DP / 4;
     for (int x = threadIdx.x; x < ROWS * kParts; x += kThreads) {
         const int r = x / kParts, part = x - r * kParts, row = row0 + r, i = row / a.G, g = row - i * a.G;
-        const T *p = row < rows ? static_cast<const T *>(a.q) + (off + i) * a.qt + b * a.qb + (long long)(h * a.G + g) * a.qh : nullptr;
-        load_row_part<T, DP>(q[r], p, a.d, part);
+        const float *p = row < rows ? static_cast<const float *>(a.q) + (off + i) * a.qt + b * a.qb + (long long)(h * a.G + g) * a.qh : nullptr;
+        load_row_part<DP>(q[r], p, a.d, part);
     }
 }
 // logits (base 2) of rows ty*RT.. against keys tx + 16 j
@@ -177,7 +163,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     }
     if (t0 < t1) fetch_keys(a, sm, 0, b, h, sq.q_off, sq.n, t0 * kKeys);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    load_queries<float, DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
+    load_queries<DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
     const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
     for (int t = t0; t < t1; ++t) {
         const int j0 = t * kKeys, st = NS == 2 ? (t - t0) & 1 : 0;
@@ -298,7 +284,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
 
 // Weights that the rows of the cache receive: one block per 64 rows of a unit sums exp2(logit - lse) over all of the unit's
 // queries.  The logits are computed once more, from the normalisers that the attention has written; sums in a fixed order.
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr int ROWS = 64, RT = ROWS / 16;
@@ -311,13 +297,13 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
     if (j0 >= sq.n) return;
     const int rows = sq.m * a.G, base = sq.n - sq.m + 1;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    load_keys<T, DP>(a, sm, b, h, sq.q_off, sq.n, j0);
+    load_keys<DP>(a, sm, b, h, sq.q_off, sq.n, j0);
     float got[4] = {0.f, 0.f, 0.f, 0.f};
     // queries in front of the tile's first key do not attend to any of it
     const long long first = base > j0 ? 0 : (long long)(j0 - base + 1) * a.G;
     for (int row0 = (int)(first / ROWS * ROWS); row0 < rows; row0 += ROWS) {
         __syncthreads();
-        load_queries<T, DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
+        load_queries<DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
         __syncthreads();
         float s[RT][4];
         logits<DP, ROWS>(sm.q, sm.k, ty, tx, a.scale_log2, s);
@@ -501,7 +487,6 @@ int launch_rows(const AttnArgs &a, cudaStream_t stream)
     if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
     return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel", cluster);
 }
-template <typename T>
 int launch_weights(const AttnArgs &a, cudaStream_t stream)
 {
     const long long blocks = ((long long)a.cap + kKeys - 1) / kKeys * a.batch * a.hkv;
@@ -510,9 +495,9 @@ int launch_weights(const AttnArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)blocks);
-    if (a.d <= 64) return launch(attn_weights_kernel<T, 64>, grid, sizeof(WeightsSmem<64>), a, stream, "attention weights kernel");
-    if (a.d <= 128) return launch(attn_weights_kernel<T, 128>, grid, sizeof(WeightsSmem<128>), a, stream, "attention weights kernel");
-    return launch(attn_weights_kernel<T, 256>, grid, sizeof(WeightsSmem<256>), a, stream, "attention weights kernel");
+    if (a.d <= 64) return launch(attn_weights_kernel<64>, grid, sizeof(WeightsSmem<64>), a, stream, "attention weights kernel");
+    if (a.d <= 128) return launch(attn_weights_kernel<128>, grid, sizeof(WeightsSmem<128>), a, stream, "attention weights kernel");
+    return launch(attn_weights_kernel<256>, grid, sizeof(WeightsSmem<256>), a, stream, "attention weights kernel");
 }
 
 }  // namespace
@@ -523,10 +508,7 @@ int launch_attn_simt(const AttnArgs &a, cudaStream_t stream)
     if (a.rows_max <= 16 || ((long long)a.rows_max + 31) / 32 * units < enough) return launch_rows<16>(a, stream);
     return ((long long)a.rows_max + 63) / 64 * units < enough ? launch_rows<32>(a, stream) : launch_rows<64>(a, stream);
 }
-int launch_attn_weights(const AttnArgs &a, int dtype, cudaStream_t stream)
-{
-    return dtype == WKV_F32 ? launch_weights<float>(a, stream) : launch_weights<__nv_bfloat16>(a, stream);
-}
+int launch_attn_weights(const AttnArgs &a, cudaStream_t stream) { return launch_weights(a, stream); }
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
 {
     const int units = a.batch * a.hkv;

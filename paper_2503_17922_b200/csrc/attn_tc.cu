@@ -1,4 +1,4 @@
-// Attention on the tensor cores (tcgen05, tensor memory, TMA): bf16, head dimension 64 or 128, whole prompts and chunks of new
+// Attention on the tensor cores (tcgen05, tensor memory, TMA): bf16, head dimensions up to 128, whole prompts and chunks of new
 // tokens over a paged cache.
 //
 // An item is two query tiles of up to 128 rows of one unit (row = position x query head of the group, so one key tile serves
@@ -329,11 +329,13 @@ __device__ __forceinline__ float largest(float top, const float (&v)[32])
     return fmaxf(t0, fmaxf(t1, v[31]));
 }
 
-template <int KB>
+// WHOLE: the head dimension is KB * 64.  Otherwise the columns from it on are zeros in shared memory, and the products leave out the
+// steps and columns of 16 that hold nothing else.
+template <int KB, bool WHOLE>
 __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, int x, uint32_t tmem)
 {
-    constexpr int D = KB * 64;
     const AttnArgs &a = t.a;
+    const int D = WHOLE ? KB * 64 : a.d;
     const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3, row = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
     const uint32_t s_addr = lanes + x * kTile, o_addr = lanes + 2 * kTile + x * kTile;
@@ -400,7 +402,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                 if (follow) m = grown;
                 l *= f;
 #pragma unroll 1
-                for (int y = 0; y < D / 16; ++y) {
+                for (int y = 0; y < (D + 15) / 16; ++y) {
                     float o[16];
                     tmem_ld16(o_addr + y * 16, o);
                     uint32_t w[16];
@@ -474,7 +476,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
         const bool poisoned = any && *static_cast<volatile int *>(&sh.poison[walk.seq % kMaskSlots]) == walk.seq + 1;
         const long long left = ((long long)im.piece * 2 * kTile + x * kTile + row);      // row of the pieces
 #pragma unroll 1
-        for (int y = 0; y < D / 32; ++y) {
+        for (int y = 0; y < (D + 31) / 32; ++y) {
             float o[32];
             if (any) {
                 tmem_ld32(o_addr + y * 32, o);
@@ -492,6 +494,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + at + y * 32;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
+                        if (!WHOLE && y * 32 + e >= D) break;
                         const float ve = __bfloat162float(v[e]);
                         if (!(fabsf(ve) < INFINITY)) o[e] += ve;
                     }
@@ -501,18 +504,19 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
             if (im.piece >= 0) {
                 float *to = t.piece_o + left * D + y * 32;
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) store32(to + j, o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
+                for (int j = 0; j < 32; j += 8)
+                    if (WHOLE || y * 32 + j < D) store32(to + j, o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]);
             } else if (t.wide_out) {
                 // (32 bytes a store are whole sectors: 16 take twice as many of L2's write cycles)
 #pragma unroll
                 for (int j = 0; j < 32; j += 16)
-                    store32(dst + y * 32 + j, pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]), pack_bf16(o[j + 4], o[j + 5]),
+                    if (WHOLE || y * 32 + j < D) store32(dst + y * 32 + j, pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]), pack_bf16(o[j + 4], o[j + 5]),
                             pack_bf16(o[j + 6], o[j + 7]), pack_bf16(o[j + 8], o[j + 9]), pack_bf16(o[j + 10], o[j + 11]),
                             pack_bf16(o[j + 12], o[j + 13]), pack_bf16(o[j + 14], o[j + 15]));
             } else {
 #pragma unroll
                 for (int j = 0; j < 32; j += 8)
-                    *reinterpret_cast<uint4 *>(dst + y * 32 + j) = make_uint4(pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]),
+                    if (WHOLE || y * 32 + j < D) *reinterpret_cast<uint4 *>(dst + y * 32 + j) = make_uint4(pack_bf16(o[j], o[j + 1]), pack_bf16(o[j + 2], o[j + 3]),
                                                                               pack_bf16(o[j + 4], o[j + 5]), pack_bf16(o[j + 6], o[j + 7]));
             }
         }
@@ -533,7 +537,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
 // ---- MMAs --------------------------------------------------------------------------------------
 // One warp issues for both query tiles in turn, which keeps them half a step apart: with a warp for each they fell into step, both
 // at their exponentials or both at their products (8,192 tokens of 32 heads: 683 us against 617).
-template <int KB>
+template <int KB, bool WHOLE>
 __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, uint32_t tmem)
 {
     constexpr int NS = stages_for(KB), kStage = KB * kRegion;
@@ -541,7 +545,9 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
     const uint32_t leader = elect_one();
     volatile int *const abort_flag = &sh.abort;
     const uint64_t q_desc0 = umma_desc_sw128(smem_u32(q_img)), k_desc0 = umma_desc_sw128(smem_u32(ring)), v_desc0 = value_desc(smem_u32(ring));
-    constexpr uint32_t s_idesc = umma_idesc_bf16(kTile, kTile), o_idesc = umma_idesc_bf16(kTile, KB * 64) | kBTransposed;
+    const int steps = WHOLE ? KB * 4 : (t.a.d + 15) / 16;        // of 16 columns
+    constexpr uint32_t s_idesc = umma_idesc_bf16(kTile, kTile);
+    const uint32_t o_idesc = umma_idesc_bf16(kTile, steps * 16) | kBTransposed;
     uint32_t entry = 0, clean_phase = 0;               // ring entries so far; parity per stage of the looked-through tiles
     uint32_t turn[2] = {0, 0}, outs[2] = {0, 0};       // tiles and items of each query tile so far
     Walk walk;
@@ -550,6 +556,7 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
         const uint64_t kd = k_desc0 + (uint64_t)((uint32_t)(stage * kStage) >> 4), qd = q_desc0 + (uint64_t)((uint32_t)(x * kStage) >> 4);
 #pragma unroll
         for (int ks = 0; ks < KB * 4; ++ks) {
+            if (!WHOLE && ks >= steps) break;
             const uint32_t at = (uint32_t)((ks >> 2) * kRegion + (ks & 3) * 32) >> 4;
             umma_bf16_if(leader, tmem + x * kTile, qd + at, kd + at, s_idesc, ks > 0);
         }
@@ -697,7 +704,7 @@ __device__ __forceinline__ void load_queries(const TcAttnArgs &t, const Item &im
     const int chunk = lane % kChunks;
     for (int r = which * (32 / kChunks) + lane / kChunks; r < 2 * kTile; r += 64 / kChunks) {
         const int x = r / kTile, row = r - x * kTile, place = row / a.G, head = row - place * a.G;
-        const bool there = place < t.ppt && place < (x ? im.rows[1] : im.rows[0]);
+        const bool there = place < t.ppt && place < (x ? im.rows[1] : im.rows[0]) && chunk * 8 < a.d;
         const __nv_bfloat16 *from = there ? q + (long long)(im.pos0 + x * t.ppt + place) * a.qt + head * a.qh + chunk * 8 : q;
         uint8_t *to = q_img + x * KB * kRegion + (chunk >> 3) * kRegion + swz128_offset(row, chunk & 7);
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -756,7 +763,7 @@ __device__ __forceinline__ void helper_warp(const TcAttnArgs &t, Shared &sh, uin
     }
 }
 
-template <int KB>
+template <int KB, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ TcAttnArgs t)
 {
@@ -795,9 +802,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
     if (warp < 8) {
-        softmax_warps<KB>(t, sh, warp >> 2, tmem);
+        softmax_warps<KB, WHOLE>(t, sh, warp >> 2, tmem);
     } else if (warp == 8) {
-        mma_warp<KB>(t, sh, q_img, ring, tmem);
+        mma_warp<KB, WHOLE>(t, sh, q_img, ring, tmem);
     } else if (warp == 9) {
         if (lane == 0) {
             tma_prefetch_desc(&k_map);
@@ -885,7 +892,7 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
     }
 }
 
-template <int KB>
+template <int KB, bool WHOLE>
 int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream)
 {
     constexpr size_t smem = 1024 + (size_t)(2 + stages_for(KB)) * KB * kRegion;
@@ -894,9 +901,9 @@ int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &
     int dev = 0, sms = 0;
     cudaError_t err = cudaGetDevice(&dev);
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (err == cudaSuccess) err = allow_smem(attn_tc_kernel<KB>, smem, asked);
+    if (err == cudaSuccess) err = allow_smem(attn_tc_kernel<KB, WHOLE>, smem, asked);
     const long long grid = t.by_work ? t.by_work : (t.items < sms ? t.items : sms);
-    if (err == cudaSuccess) err = launch_pdl(attn_tc_kernel<KB>, dim3((unsigned)grid), kThreads, smem, stream, 1, k_map, v_map, t);
+    if (err == cudaSuccess) err = launch_pdl(attn_tc_kernel<KB, WHOLE>, dim3((unsigned)grid), kThreads, smem, stream, 1, k_map, v_map, t);
     if (err == cudaSuccess) count_launches(1);
     if (err == cudaSuccess && t.by_work) {
         err = launch_pdl(attn_tc_join_kernel, dim3((unsigned)t.items, 2 * kTile / kJoinRows), 256, 0, stream, 1, t);
@@ -907,14 +914,18 @@ int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &
 
 }  // namespace
 
+// A tile's rows come in boxes that never cross a page's end: the largest power of two that a page is a multiple of, eight at
+// least, since the swizzle's pattern repeats every eight rows.  (Four sequences of 10-16 K rows, up to
+// 512 new tokens of 32 heads: 375 us in pages of 128 rows, 440 in pages of 24 and so boxes of eight; 2,260 on the warp-level kernel.)
+static int box_of_page(int page_size) { return std::min(page_size & -page_size, kTile); }
+
 // Shapes that the kernel takes; a layout that no tensor map describes is found out at launch (WKV_ERR_UNSUPPORTED).
 bool attn_tc_supported(const AttnArgs &a, int dtype)
 {
-    if (dtype != WKV_BF16 || (a.d != 64 && a.d != 128) || a.G > kTile) return false;
+    if (dtype != WKV_BF16 || a.d > 128 || a.G > kTile) return false;
     // a key tile is one box: tensors of fewer rows are left to the other kernels, which are as fast there
     if (!a.table && (a.cu_q ? a.total_q : a.max_q) < kTile) return false;
-    // a tile's rows come in boxes of whole pages or parts of one; the swizzle's pattern repeats every eight rows
-    if (a.table && !(a.page_size % kTile == 0 || (kTile % a.page_size == 0 && a.page_size >= 8))) return false;
+    if (a.table && box_of_page(a.page_size) < 8) return false;
     int dev = 0, major = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -939,8 +950,8 @@ int launch_attn_tc(const AttnArgs &a, float *piece_o, float2 *piece_ml, long lon
     const long long units = (long long)a.batch * a.hkv;
     t.max_pairs = (a.max_q + 2 * t.ppt - 1) / (2 * t.ppt);
     t.items = units * t.max_pairs;
-    t.box_rows = a.table && a.page_size < kTile ? a.page_size : kTile;
-    t.wide_out = (reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ot * 2) | (uintptr_t)(a.oh * 2) | (uintptr_t)(a.ob * 2)) % 32 == 0;
+    t.box_rows = a.table ? box_of_page(a.page_size) : kTile;
+    t.wide_out = a.d % 16 == 0 && (reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ot * 2) | (uintptr_t)(a.oh * 2) | (uintptr_t)(a.ob * 2)) % 32 == 0;
     int rows = 0, most = 0;
     t.by_work = piece_o && attn_tc_pieces(units, a.max_q, a.G, a.cap, &rows, &most) ? kWorkBlocks : 0;
     t.piece_o = piece_o;
@@ -954,7 +965,8 @@ int launch_attn_tc(const AttnArgs &a, float *piece_o, float2 *piece_ml, long lon
                               {a.table ? (unsigned long long)a.num_pages : batch, (unsigned long long)a.kb * 2, 1}};
     if (!make_row_tensor_map(a.k, a.d, k_dims, &k_map, t.k_slot) || !make_row_tensor_map(a.v, a.d, k_dims, &v_map, t.k_slot))
         return WKV_ERR_UNSUPPORTED;
-    return a.d == 128 ? launch_kb<2>(t, k_map, v_map, stream) : launch_kb<1>(t, k_map, v_map, stream);
+    if (a.d > 64) return a.d == 128 ? launch_kb<2, true>(t, k_map, v_map, stream) : launch_kb<2, false>(t, k_map, v_map, stream);
+    return a.d == 64 ? launch_kb<1, true>(t, k_map, v_map, stream) : launch_kb<1, false>(t, k_map, v_map, stream);
 }
 
 }  // namespace wkv

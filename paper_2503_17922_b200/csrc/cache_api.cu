@@ -173,7 +173,7 @@ PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
     off = w.ml_off;
     int rows = 0, items = 0;
     const int G = c->n_q_heads / c->n_kv_heads;
-    w.pieces = c->dtype == WKV_BF16 && p.rows_max > kFewRows && G <= 128 && (c->head_dim == 64 || c->head_dim == 128)
+    w.pieces = c->dtype == WKV_BF16 && p.rows_max > kFewRows && G <= 128 && c->head_dim <= 128
                    ? attn_tc_pieces(p.units, c->max_new, G, p.cap, &rows, &items) : 0;
     w.line_off = off;
     off = align_up(off + (w.pieces ? (size_t)(items + 1) * sizeof(long long) : 0), 256);
@@ -535,7 +535,7 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
         if (st == WKV_OK && !a.clustered && (a.splits > 1 || a.logits)) st = launch_attn_join(a, c->dtype, stream);
     }
     if (st != WKV_OK) return st;
-    if (weights_out && !a.logits) return launch_attn_weights(a, c->dtype, stream);
+    if (weights_out && !a.logits) return c->dtype == WKV_BF16 ? launch_attn_mma_weights(a, stream) : launch_attn_weights(a, stream);
     return WKV_OK;
 }
 

@@ -719,3 +719,71 @@ def test_attend_shared_work_with_infinities_and_missing_pages():
     a.c.table[0, 20:40] = -1
     a.run()
     a.check()
+
+
+@pytest.mark.parametrize("case", [
+    # head dimensions that are not a whole number of the tensor cores' steps, or of 64 columns
+    ("bf16", 4, 2, 8, [140], "bhnd", 4, 0),
+    ("bf16", 6, 3, 24, [333, 128], "packed", 4, 0),
+    ("bf16", 8, 2, 40, [129, 129], "bnhd", 8, 8),
+    ("bf16", 12, 2, 72, [513], "bhnd", 4, 0),
+    ("bf16", 8, 1, 80, [1, 400, 260], "packed", 16, 8),
+    ("bf16", 6, 2, 96, [257, 257], "bnhd", 8, 0),
+    ("bf16", 3, 3, 104, [300], "bhnd", 4, 0),
+    ("bf16", 5, 1, 120, [200, 31], "packed", 4, 8),
+], ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+def test_prompt_head_dimensions(case):
+    dtype, hq, hk, d, lens, layout, alpha, pad = case
+    p = Prompt(dtype, hq, hk, d, lens, layout, alpha, pad=pad)
+    p.run()
+    p.check()
+
+
+def test_head_dimension_80_does_not_see_what_follows():
+    p = Prompt("bf16", 4, 2, 80, [300, 200], "packed", 4)
+    p.run()
+    torch.cuda.synchronize()
+    clean = p.out.clone()
+    at = 170
+    p.v[at, 0, 3], p.v[at, 0, 70], p.v[at, 1, 79] = NAN, INF, -INF
+    p.k[260, 0, :] = NAN
+    p.v[300:, 0] = NAN
+    p.run()
+    torch.cuda.synchronize()
+    assert torch.equal(p.out[:at], clean[:at]) and torch.isnan(p.out[at:300, :2, 3]).all()
+    assert (p.out[at:260, :2, 70] == INF).all() and (p.out[at:300, 2:, 79] == -INF).all()
+    assert torch.equal(p.out[at:300, 2:, :79], clean[at:300, 2:, :79])
+
+
+@pytest.mark.parametrize("case", [
+    # pages that are no part of a key tile; shared work with such pages and head dimensions; weights over more than one block of keys
+    ("bf16", 8, 2, 128, 40, "phsd", [[1000, 998], [333, 330]], [200, 33], True),
+    ("bf16", 8, 2, 64, 48, "pshd", [[700, 650], [5, 5]], [150, 2], True),
+    ("bf16", 4, 1, 96, 192, "phsd", [[900]], [70], False),
+    ("bf16", 12, 2, 80, 24, "pshd", [[2600, 2500], [60, 61], [2333, 0]], [140, 60, 333], True),
+    ("bf16", 4, 2, 40, 8, "phsd", [[2900, 2890]], [300], False),
+    ("bf16", 9, 3, 128, 200, "phsd", [[513] * 3], [129], False),
+    ("bf16", 8, 1, 256, 16, "phsd", [[700]], [90], False),
+    ("bf16", 17, 1, 64, 12, "phsd", [[640], [63]], [2, 1], True),
+], ids=lambda c: "-".join(map(str, c)).replace(" ", "")[:70])
+def test_attend_pages_and_head_dimensions(case):
+    a = Attend(*case)
+    a.run()
+    a.check()
+    a.c.table[0, 1] = -1
+    a.run()
+    a.check()
+
+
+def test_weights_of_a_chunk_beside_keys_that_nobody_sees():
+    """Rows behind the last query's position (more rows than the chunk accounts for cannot be: the last query sees the last row), and
+    infinities in keys that only some queries see: the others' weights stay as they are."""
+    a = Attend("bf16", 8, 2, 128, 24, "phsd", [[600, 590]], [100], False)
+    a.run()
+    torch.cuda.synchronize()
+    clean = a.w_out.clone()
+    a.c.slot(a.c.k[0], 0, 0, 599)[:] = NAN                       # seen by the last query alone
+    a.run()
+    torch.cuda.synchronize()
+    assert torch.isnan(a.w_out[0, 0, :600]).all() and torch.equal(a.w_out[0, 1], clean[0, 1])
+    assert torch.isnan(a.out[0, :4, 99]).all() and torch.isfinite(a.out[0, :4, :99]).all()
