@@ -1,4 +1,4 @@
-// Joining the key splits of up to 16 rows inside one launch: the splits are the blocks of a cluster, and each reads the others'
+// Joining the key splits of a block's rows inside one launch: the splits are the blocks of a cluster, and each reads the others'
 // maxima, sums and outputs from their shared memory.  It takes the place of a kernel behind this one (one token over 992 rows:
 // 12.6 us with it), as far as a cluster reaches: eight blocks.
 #pragma once
@@ -41,8 +41,8 @@ __device__ __forceinline__ void store_four(__nv_bfloat16 *p, float a, float b, f
     *reinterpret_cast<uint2 *>(p) = r;
 }
 
-// By all threads of all blocks of the cluster (1 .. kClusterSplits blocks, whose rank is their split): `n` rows from row0 on, m, l [16] and
-// o [16][stride] in shared memory at the same places in all of them, m in base 2, o relative to m.  With a.logits the block also adds up
+// By all threads of all blocks of the cluster (1 .. kClusterSplits blocks, whose rank is their split): `n` rows from row0 on, m, l [n] and
+// o [n][stride] in shared memory at the same places in all of them, m in base 2, o relative to m.  With a.logits (16 rows at most) the block also adds up
 // the weights of the keys [key0, key1), whose logits it has written.  lse2 [16]: shared memory.
 template <typename T, int THREADS>
 __device__ __forceinline__ void cluster_join(const AttnArgs &a, const AttnSeq &sq, int unit, int b, int h, int row0, int n, int rank, const float *m,

@@ -1,14 +1,21 @@
 // Attention on the CUDA cores for fp32, its weights kernel, and the joining kernels of all types.  One block holds ROWS rows of one
 // unit in shared memory and walks over the unit's keys in tiles of 64 with a running maximum and sum per row; everything is
-// fp32, products in plain multiply-adds, which bound it (2 * 64 * d per row and tile).  A tile's keys and values come by asynchronous copies
-// while the one before is worked on.
+// fp32, products in plain multiply-adds of pairs.  A thread has ROWS / 16 rows x 4 keys, then as many rows x d / 16 columns.
 //
-// ROWS is the largest of 64, 32 and 16 that gives every SM a block (4 heads of 1,024 tokens, d = 64: 122 us with 64 rows in 64 blocks).
+// Bound by the reads of shared memory (80 % of their peak at 4,096 tokens): 16 bytes to every thread of a warp take four cycles whatever
+// the addresses, so that 64 products per thread cost 32 of them with 4 rows to a thread and 24 with 8.  32 heads on 8 of 4,096
+// tokens: d = 64 1,890 us (36 TFLOP/s; with 8 rows 2,110, a block per SM then instead of two), d = 128 3,400 us with 8 rows
+// (40 TFLOP/s; 4,650 with 4).
+//
+// ROWS is the largest of 128 (d above 64), 64, 32 and 16 that gives nearly every SM a block.  A prompt without enough of them has its keys split over
+// the blocks of a cluster; paged rows are split by the caller.
 //
 // With S key splits a block walks over one of S parts of the keys and leaves (maximum, sum, unnormalised output) per row for
-// the joining kernel.  A row's sums are taken in one order whatever else the launch holds, so results do not depend
-// on the other sequences of a batch.
+// the joining kernel.  A row's sums are taken in an order that the launch's sizes give, never in that of arrival.
 #include "attn_cluster.cuh"
+#include "score_math.cuh"
+
+#include <type_traits>
 
 namespace wkv {
 namespace {
@@ -19,6 +26,12 @@ constexpr int kKeys = 64;
 __device__ __forceinline__ void from_float(float &y, float x) { y = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16 &y, float x) { y = __float2bfloat16_rn(x); }
 
+__device__ __forceinline__ unsigned long long mul_pair(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 // four elements of a row of d into shared memory, zeros from d on; `p` null: zeros
 template <int DP>
 __device__ __forceinline__ void load_row_part(float *dst, const float *p, int d, int part)
@@ -27,16 +40,17 @@ __device__ __forceinline__ void load_row_part(float *dst, const float *p, int d,
     *reinterpret_cast<float4 *>(dst + c) = p && c < d ? *reinterpret_cast<const float4 *>(p + c) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
-// Stages of key tiles: two where they fit.
-__host__ __device__ constexpr int simt_stages(int dp) { return dp <= 128 ? 2 : 1; }
+// Stages of key tiles: with 16 rows the loads take as long as the arithmetic, and the next tile's come during this one's.  With more
+// rows a tile's values come during the product with its keys, and the next keys during that with the values, in half the memory.
 template <int DP, int ROWS>
 struct SimtSmem {
+    static constexpr int kStages = ROWS == 16 && DP <= 128 ? 2 : 1;
     float q[ROWS][DP + 4];
-    float k[simt_stages(DP)][kKeys][DP + 4];
-    float v[simt_stages(DP)][kKeys][DP];
+    float k[kStages][kKeys][DP + 4];
+    float v[kStages][kKeys][DP];
     float p[ROWS][kKeys + 4];
-    int present[simt_stages(DP)][kKeys];       // the key's page is one
-    float m[16], l[16], lse2[16];
+    int present[2][kKeys];                 // the key's page is one
+    float m[ROWS], l[ROWS], lse2[16];
 };
 template <int DP>
 struct WeightsSmem {
@@ -46,30 +60,46 @@ struct WeightsSmem {
     int present[kKeys];
 };
 
-// the keys and values of one tile, on their way; rows from n on and rows without a page are zeros
-template <int DP, int ROWS>
-__device__ __forceinline__ void fetch_keys(const AttnArgs &a, SimtSmem<DP, ROWS> &sm, int st, int b, int h, long long off, int n, int j0)
-{
-    // a row's vectors lie in neighbouring threads; the rows' places first, so that their looking up (a trip to memory where paged) overlaps
-    constexpr int kParts = DP / 4, kEach = kKeys * kParts / kThreads;
-    const int c = (int)(threadIdx.x % kParts) * 4, r0 = threadIdx.x / kParts;
-    long long at[kEach];
+// The keys or the values of a tile, on their way; rows from n on and rows without a page are zeros.  A row's vectors lie in neighbouring
+// threads, and a thread has EACH rows.  Their pages are looked up some work ahead, as that is a trip to memory.
+template <int DP>
+struct Fetch {
+    static constexpr int kParts = DP / 4, kEach = kKeys * kParts / kThreads, kStep = kThreads / kParts;
+    int page[kEach], slot[kEach];
+    long long at[kEach];                   // element offsets, -1: none
+    __device__ __forceinline__ void look_up(const AttnArgs &a, int b, int n, int j0)
+    {
+        if (!a.table) return;
 #pragma unroll
-    for (int x = 0; x < kEach; ++x) {
-        const int j = j0 + r0 + x * (kThreads / kParts);
-        at[x] = j < n ? attn_row(a, b, h, off, j) : -1;
+        for (int x = 0; x < kEach; ++x) {
+            const int j = j0 + (int)threadIdx.x / kParts + x * kStep, pg = j / a.page_size;
+            slot[x] = j - pg * a.page_size;
+            page[x] = j < n ? __ldg(a.table + (long long)b * a.max_pages + pg) : -1;
+        }
     }
+    __device__ __forceinline__ void place(const AttnArgs &a, int *present, int h, long long dense, int n, int j0)
+    {
 #pragma unroll
-    for (int x = 0; x < kEach; ++x) {
-        const int r = r0 + x * (kThreads / kParts);
-        const bool have = at[x] >= 0 && c < a.d;
-        const int size = have ? 16 : 0;
-        const float *kp = static_cast<const float *>(a.k) + (have ? at[x] + c : 0), *vp = static_cast<const float *>(a.v) + (have ? at[x] + c : 0);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&sm.k[st][r][c]))), "l"(kp), "r"(size) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(&sm.v[st][r][c]))), "l"(vp), "r"(size) : "memory");
-        if (c == 0) sm.present[st][r] = at[x] >= 0;
+        for (int x = 0; x < kEach; ++x) {
+            const int r = (int)threadIdx.x / kParts + x * kStep, j = j0 + r;
+            if (a.table) at[x] = (unsigned)page[x] < (unsigned)a.num_pages ? page[x] * a.kb + h * a.kh + slot[x] * a.kt : -1;
+            else at[x] = j < n ? dense + j * a.kt : -1;
+            if (threadIdx.x % kParts == 0) present[r] = at[x] >= 0;
+        }
     }
-}
+    __device__ __forceinline__ void issue(const AttnArgs &a, const void *from, float *to, int stride) const
+    {
+        const int c = (int)(threadIdx.x % kParts) * 4;
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) {
+            const int r = (int)threadIdx.x / kParts + x * kStep;
+            const bool have = at[x] >= 0 && c < a.d;
+            const float *p = static_cast<const float *>(from) + (have ? at[x] + c : 0);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + r * stride + c))), "l"(p), "r"(have ? 16 : 0) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+};
 template <int DP>
 __device__ __forceinline__ void load_keys(const AttnArgs &a, WeightsSmem<DP> &sm, int b, int h, long long off, int n, int j0)
 {
@@ -96,42 +126,41 @@ template <int DP, int ROWS>
 __device__ __forceinline__ void logits(const float (&q)[ROWS][DP + 4], const float (&k)[kKeys][DP + 4], int ty, int tx, float c, float (&s)[ROWS / 16][4])
 {
     constexpr int RT = ROWS / 16;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[r][j] = 0.f;
-#pragma unroll 4
+    // products of pairs: sums over the even and the odd elements apart
+    unsigned long long sum[RT][4] = {};
+#pragma unroll (ROWS >= 128 ? 2 : 4)
     for (int e = 0; e < DP; e += 4) {
-        float4 qv[RT], kv[4];
+        ulonglong2 qv[RT], kv[4];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) qv[r] = *reinterpret_cast<const float4 *>(&q[ty * RT + r][e]);
+        for (int r = 0; r < RT; ++r) qv[r] = *reinterpret_cast<const ulonglong2 *>(&q[ty * RT + r][e]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4 *>(&k[tx + 16 * j][e]);
+        for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const ulonglong2 *>(&k[tx + 16 * j][e]);
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                s[r][j] = fmaf(qv[r].x, kv[j].x, s[r][j]);
-                s[r][j] = fmaf(qv[r].y, kv[j].y, s[r][j]);
-                s[r][j] = fmaf(qv[r].z, kv[j].z, s[r][j]);
-                s[r][j] = fmaf(qv[r].w, kv[j].w, s[r][j]);
+                sum[r][j] = fma_pair(qv[r].x, kv[j].x, sum[r][j]);
+                sum[r][j] = fma_pair(qv[r].y, kv[j].y, sum[r][j]);
             }
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[r][j] *= c;
+        for (int j = 0; j < 4; ++j) {
+            const float2 x = halves_of(sum[r][j]);
+            s[r][j] = (x.x + x.y) * c;
+        }
 }
 
 template <int DP, int ROWS>
-__global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_constant__ AttnArgs a)
+__global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 64 && ROWS < 64 ? 3 : 1)) attn_simt_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
     SimtSmem<DP, ROWS> &sm = *reinterpret_cast<SimtSmem<DP, ROWS> *>(raw);
-    constexpr int RT = ROWS / 16, CT = DP / 64, NS = simt_stages(DP);
+    constexpr int RT = ROWS / 16, CT = DP / 64, NS = SimtSmem<DP, ROWS>::kStages;
     // The joining kernel may be placed now.  Another of this kind is not to be before this one ends: its blocks would crowd onto the
     // SMs that have room at that time.
-    const bool clustered = ROWS == 16 && a.clustered, parts = !clustered && (a.splits > 1 || a.logits);
+    const bool clustered = a.clustered, parts = !clustered && (a.splits > 1 || a.logits);
     if (parts) pdl_trigger();
     pdl_wait();
     const int units = a.batch * a.hkv;
@@ -152,35 +181,69 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
     const int t0 = (int)((long long)all_tiles * split / splits), t1 = (int)((long long)all_tiles * (split + 1) / splits);
     int limit[RT];
     float m[RT], l[RT];
-    float4 o[RT][CT];
+    unsigned long long o[RT][CT][2];                                     // pairs of columns
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         limit[r] = base + (row0 + ty * RT + r) / a.G;
         m[r] = -INFINITY;
         l[r] = 0.f;
 #pragma unroll
-        for (int x = 0; x < CT; ++x) o[r][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int x = 0; x < CT; ++x) o[r][x][0] = o[r][x][1] = 0ull;
     }
-    if (t0 < t1) fetch_keys(a, sm, 0, b, h, sq.q_off, sq.n, t0 * kKeys);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    const long long dense = sq.q_off * a.kt + b * a.kb + h * a.kh;
+    Fetch<DP> rows_of;
+    auto fetch_keys = [&](int t) {
+        rows_of.place(a, sm.present[t & 1], h, dense, sq.n, t * kKeys);
+        rows_of.issue(a, a.k, &sm.k[t % NS][0][0], DP + 4);
+    };
+    auto fetch_values = [&](int t) { rows_of.issue(a, a.v, &sm.v[t % NS][0][0], DP); };
+    if (t0 < t1) {
+        rows_of.look_up(a, b, sq.n, t0 * kKeys);
+        fetch_keys(t0);
+        fetch_values(t0);
+        if (NS == 2) rows_of.look_up(a, b, sq.n, (t0 + 1) * kKeys);
+    }
     load_queries<DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
+    if (NS == 1) {
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncthreads();
+    }
     const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
     for (int t = t0; t < t1; ++t) {
-        const int j0 = t * kKeys, st = NS == 2 ? (t - t0) & 1 : 0;
-        if (NS == 2 && t + 1 < t1) fetch_keys(a, sm, st ^ 1, b, h, sq.q_off, sq.n, j0 + kKeys);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        asm volatile("cp.async.wait_group %0;" ::"n"(NS - 1) : "memory");
-        __syncthreads();
+        const int j0 = t * kKeys, st = t % NS;
+        if (NS == 2) {
+            if (t + 1 < t1) {
+                fetch_keys(t + 1);
+                fetch_values(t + 1);
+                rows_of.look_up(a, b, sq.n, j0 + 2 * kKeys);
+                asm volatile("cp.async.wait_group 2;" ::: "memory");
+            } else {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            }
+            __syncthreads();
+        } else {
+            rows_of.look_up(a, b, sq.n, j0 + kKeys);
+        }
         float s[RT][4];
         logits<DP, ROWS>(sm.q, sm.k[st], ty, tx, a.scale_log2, s);
+        if (NS == 1) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();                                             // the values have landed for all, and nobody reads the keys any more
+            if (t + 1 < t1) fetch_keys(t + 1);
+        }
+        const bool guarded = j0 + kKeys > plain;
+        if (guarded || a.table) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j0 + tx + 16 * j >= limit[r] || !sm.present[t & 1][tx + 16 * j]) s[r][j] = -INFINITY;
+        }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             float top = m[r];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j0 + tx + 16 * j >= limit[r] || !sm.present[st][tx + 16 * j]) s[r][j] = -INFINITY;
-                top = fmaxf(top, s[r][j]);
-            }
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, s[r][j]);
             if (ROWS == 16 && a.logits && row0 + ty < rows) {
                 float *to = a.logits + ((long long)unit * a.rows_max + row0 + ty) * a.logit_stride + j0 + tx;
 #pragma unroll
@@ -202,56 +265,64 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
             for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
             l[r] = l[r] * keep + sum;
             m[r] = top;
+            const unsigned long long keep2 = pair_of(keep, keep);
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
-                o[r][x].x *= keep;
-                o[r][x].y *= keep;
-                o[r][x].z *= keep;
-                o[r][x].w *= keep;
+                o[r][x][0] = mul_pair(o[r][x][0], keep2);
+                o[r][x][1] = mul_pair(o[r][x][1], keep2);
             }
         }
         __syncwarp();                                                    // a row's 16 threads are in one warp
-        const bool guarded = j0 + kKeys > plain;
+        // what stands behind a row's position may be infinite or NaN: 0 times it is not 0
+        auto product = [&](auto skip_zeros) {
 #pragma unroll 2
-        for (int j = 0; j < kKeys; j += 4) {
-            float4 pp[RT];
+            for (int j = 0; j < kKeys; j += 4) {
+                float4 pp[RT];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) pp[r] = *reinterpret_cast<const float4 *>(&sm.p[ty * RT + r][j]);
+                for (int r = 0; r < RT; ++r) pp[r] = *reinterpret_cast<const float4 *>(&sm.p[ty * RT + r][j]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float4 vv[CT];
+                for (int e = 0; e < 4; ++e) {
+                    ulonglong2 v[CT];
 #pragma unroll
-                for (int x = 0; x < CT; ++x) vv[x] = *reinterpret_cast<const float4 *>(&sm.v[st][j + e][tx * 4 + 64 * x]);
+                    for (int x = 0; x < CT; ++x) v[x] = *reinterpret_cast<const ulonglong2 *>(&sm.v[st][j + e][tx * 4 + 64 * x]);
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const float p = e == 0 ? pp[r].x : (e == 1 ? pp[r].y : (e == 2 ? pp[r].z : pp[r].w));
-                    // what stands behind a row's position may be infinite or NaN: 0 times it is not 0
-                    if (guarded && p == 0.f) continue;
+                    for (int r = 0; r < RT; ++r) {
+                        const float p = e == 0 ? pp[r].x : (e == 1 ? pp[r].y : (e == 2 ? pp[r].z : pp[r].w));
+                        if (decltype(skip_zeros)::value && p == 0.f) continue;
+                        const unsigned long long p2 = pair_of(p, p);
 #pragma unroll
-                    for (int x = 0; x < CT; ++x) {
-                        o[r][x].x = fmaf(p, vv[x].x, o[r][x].x);
-                        o[r][x].y = fmaf(p, vv[x].y, o[r][x].y);
-                        o[r][x].z = fmaf(p, vv[x].z, o[r][x].z);
-                        o[r][x].w = fmaf(p, vv[x].w, o[r][x].w);
+                        for (int x = 0; x < CT; ++x) {
+                            o[r][x][0] = fma_pair(p2, v[x].x, o[r][x][0]);
+                            o[r][x][1] = fma_pair(p2, v[x].y, o[r][x][1]);
+                        }
                     }
                 }
             }
-        }
-        __syncthreads();
-        if (NS == 1 && t + 1 < t1) fetch_keys(a, sm, 0, b, h, sq.q_off, sq.n, j0 + kKeys);
+        };
+        if (guarded) product(std::true_type{});
+        else product(std::false_type{});
+        if (NS == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                                                 // the next keys have landed for all, and nobody reads the values any more
+        if (NS == 1 && t + 1 < t1) fetch_values(t + 1);
     }
+    auto columns = [&](int r, int x) {
+        const float2 lo = halves_of(o[r][x][0]), hi = halves_of(o[r][x][1]);
+        return make_float4(lo.x, lo.y, hi.x, hi.y);
+    };
     if (!parts) pdl_trigger();
     if (clustered) {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncthreads();
-        float *const all = &sm.k[0][0][0];                               // [16][DP + 4]
-        if (tx == 0) {
-            sm.m[ty] = m[0];
-            sm.l[ty] = l[0];
-        }
+        float *const all = &sm.q[0][0];                                  // [ROWS][DP + 4]: the queries are not needed any more
 #pragma unroll
-        for (int x = 0; x < CT; ++x) *reinterpret_cast<float4 *>(all + ty * (DP + 4) + tx * 4 + 64 * x) = o[0][x];
-        cluster_join<float, kThreads>(a, sq, unit, b, h, row0, min(16, rows - row0), split, sm.m, sm.l, all, DP + 4, sm.lse2, t0 * kKeys,
+        for (int r = 0; r < RT; ++r) {
+            if (tx == 0) {
+                sm.m[ty * RT + r] = m[r];
+                sm.l[ty * RT + r] = l[r];
+            }
+#pragma unroll
+            for (int x = 0; x < CT; ++x) *reinterpret_cast<float4 *>(all + (ty * RT + r) * (DP + 4) + tx * 4 + 64 * x) = columns(r, x);
+        }
+        cluster_join<float, kThreads>(a, sq, unit, b, h, row0, min(ROWS, rows - row0), split, sm.m, sm.l, all, DP + 4, sm.lse2, t0 * kKeys,
                                       min(t1 * kKeys, sq.n));
         return;
     }
@@ -267,7 +338,7 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
 #pragma unroll
             for (int x = 0; x < CT; ++x) {
                 const int c = tx * 4 + 64 * x;
-                if (c < a.d) *reinterpret_cast<float4 *>(a.part_o + at * a.d + c) = o[r][x];
+                if (c < a.d) *reinterpret_cast<float4 *>(a.part_o + at * a.d + c) = columns(r, x);
             }
             continue;
         }
@@ -277,7 +348,8 @@ __global__ void __launch_bounds__(kThreads) attn_simt_kernel(const __grid_consta
 #pragma unroll
         for (int x = 0; x < CT; ++x) {
             const int c = tx * 4 + 64 * x;
-            if (c < a.d) *reinterpret_cast<float4 *>(dst + c) = make_float4(o[r][x].x * inv, o[r][x].y * inv, o[r][x].z * inv, o[r][x].w * inv);
+            const float4 y = columns(r, x);
+            if (c < a.d) *reinterpret_cast<float4 *>(dst + c) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
         }
     }
 }
@@ -482,10 +554,14 @@ int launch_rows(const AttnArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)blocks);
-    const int cluster = ROWS == 16 && a.clustered ? a.splits : 1;
-    if (a.d <= 64) return launch(attn_simt_kernel<64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel", cluster);
-    if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
-    return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel", cluster);
+    const int cluster = a.clustered ? a.splits : 1;
+    if constexpr (ROWS == 128) {
+        return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
+    } else {
+        if (a.d <= 64) return launch(attn_simt_kernel<64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel", cluster);
+        if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
+        return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel", cluster);
+    }
 }
 int launch_weights(const AttnArgs &a, cudaStream_t stream)
 {
@@ -502,11 +578,23 @@ int launch_weights(const AttnArgs &a, cudaStream_t stream)
 
 }  // namespace
 
-int launch_attn_simt(const AttnArgs &a, cudaStream_t stream)
+int launch_attn_simt(const AttnArgs &args, cudaStream_t stream)
 {
-    const long long units = (long long)a.batch * a.hkv * a.splits, enough = 120;
-    if (a.rows_max <= 16 || ((long long)a.rows_max + 31) / 32 * units < enough) return launch_rows<16>(a, stream);
-    return ((long long)a.rows_max + 63) / 64 * units < enough ? launch_rows<32>(a, stream) : launch_rows<64>(a, stream);
+    AttnArgs a = args;
+    const long long units = (long long)a.batch * a.hkv;
+    const auto blocks = [&](int rows) { return ((long long)a.rows_max + rows - 1) / rows * units * a.splits; };
+    if (!a.table) {
+        // A prompt's keys are split over a cluster: until there are 200 blocks of 64 rows, and two for every SM as long as each keeps 1.5
+        // key tiles or more, of which the rows see half on average (4 heads on 2, d = 64, 1,024 tokens: 64 blocks x 2 51 us, x 4 37,
+        // x 8 44; 2,000 tokens at d = 128: x 2 271 us, x 4 178).
+        while (a.splits < kClusterSplits && (blocks(64) < 200 || (blocks(64) < 2 * 148 && a.cap >= 6 * kKeys * a.splits)) && a.splits * kKeys < a.cap)
+            a.splits *= 2;
+        a.clustered = a.splits > 1;
+    }
+    if (a.rows_max <= 16 || blocks(32) < 120) return launch_rows<16>(a, stream);
+    // (128 rows: a fragment of keys or values serves twice as many products, and shared memory bounds them)
+    if (a.d > 64 && a.d <= 128 && blocks(128) >= 120) return launch_rows<128>(a, stream);
+    return blocks(64) < 120 ? launch_rows<32>(a, stream) : launch_rows<64>(a, stream);
 }
 int launch_attn_weights(const AttnArgs &a, cudaStream_t stream) { return launch_weights(a, stream); }
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)

@@ -787,3 +787,32 @@ def test_weights_of_a_chunk_beside_keys_that_nobody_sees():
     torch.cuda.synchronize()
     assert torch.isnan(a.w_out[0, 0, :600]).all() and torch.equal(a.w_out[0, 1], clean[0, 1])
     assert torch.isnan(a.out[0, :4, 99]).all() and torch.isfinite(a.out[0, :4, :99]).all()
+
+
+@pytest.mark.parametrize("case", [
+    # fp32: keys split over two, four and eight blocks of a cluster, 16 to 128 rows a block, sequences shorter than the splits
+    ("f32", 4, 2, 64, [1024], "bhnd", 8, 0),
+    ("f32", 4, 2, 128, [1500], "bnhd", 8, 4),
+    ("f32", 2, 2, 80, [700, 3, 64, 1], "packed", 4, 0),
+    ("f32", 8, 1, 96, [2100], "bhnd", 4, 0),
+    ("f32", 16, 16, 128, [1100], "bnhd", 1, 0),
+    ("f32", 1, 1, 256, [500], "bhnd", 4, 0),
+    ("f32", 7, 1, 8, [333], "bhnd", 4, 0),
+], ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+def test_prompt_fp32_splits(case):
+    dtype, hq, hk, d, lens, layout, alpha, pad = case
+    p = Prompt(dtype, hq, hk, d, lens, layout, alpha, pad=pad)
+    p.run()
+    p.check(rows=None if max(lens) < 600 else [0, 1, 63, 64, 127, 128, 600, 699, 1023, 1024, 1099, 1499, 2098, 2099])
+
+
+def test_fp32_splits_do_not_see_what_follows():
+    p = Prompt("f32", 4, 2, 64, [900], "bhnd", 4)
+    p.run()
+    torch.cuda.synchronize()
+    clean = p.out.clone()
+    p.v[0, 0, 500, 3], p.v[0, 0, 500, 5], p.k[0, 1, 700] = NAN, INF, NAN
+    p.run()
+    torch.cuda.synchronize()
+    assert torch.equal(p.out[0, :2, :500], clean[0, :2, :500]) and torch.equal(p.out[0, 2:, :700], clean[0, 2:, :700])
+    assert torch.isnan(p.out[0, :2, 500:, 3]).all() and (p.out[0, :2, 500:, 5] == INF).all() and torch.isnan(p.out[0, 2:, 700:]).all()
