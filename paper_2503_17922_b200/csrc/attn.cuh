@@ -153,6 +153,7 @@ struct EvictArgs {
     int *positions_out, *lengths_out;
     int *counts;           // [units] rows that move
     int2 *moves;           // [units][cap / 2 + 1] (to, from)
+    longlong2 *places;     // the same rows' element offsets in the pools, -1: no page
     int moves_max;
 };
 struct PoolTable {

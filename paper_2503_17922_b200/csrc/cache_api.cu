@@ -120,7 +120,7 @@ int resolve_paged(const wkv_paged *c, Paged &p)
 struct PagedWorkspace {
     int splits;
     bool clustered;
-    size_t lse_off, ml_off, o_off, logits_off, counts_off, moves_off, total;
+    size_t lse_off, ml_off, o_off, logits_off, counts_off, moves_off, places_off, total;
     long long logit_stride;      // 0: the weights are computed from K once more
     int pieces;                  // of the tensor-core kernel
     size_t line_off, piece_o_off, piece_ml_off;
@@ -188,6 +188,8 @@ PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
     off = align_up(off + (size_t)p.units * sizeof(int), 256);
     w.moves_off = off;
     off = align_up(off + (size_t)p.units * w.moves_max * sizeof(int2), 256);
+    w.places_off = off;
+    off = align_up(off + (size_t)p.units * w.moves_max * sizeof(longlong2), 256);
     if (off > w.total) w.total = off;
     return w;
 }
@@ -599,6 +601,7 @@ int wkv_evict_kv_paged(const wkv_paged *c, int32_t n_layers, void *const *k_pool
     a.lengths_out = lengths_out;
     a.counts = reinterpret_cast<int *>(static_cast<char *>(workspace) + w.counts_off);
     a.moves = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + w.moves_off);
+    a.places = reinterpret_cast<longlong2 *>(static_cast<char *>(workspace) + w.places_off);
     a.moves_max = w.moves_max;
     return launch_evict(a, pools, static_cast<cudaStream_t>(cuda_stream));
 }

@@ -1,8 +1,8 @@
 // Eviction from the paged cache by accumulated attention weight, and the state that it goes by.
 //
 // First kernel, a block per unit: rows get 32-bit keys in the order of eviction, the key of the keep-th is found by a radix
-// select of 8 bits per pass, and one walk over the rows lists those that leave in front of row `keep` and those that stay
-// behind it, pairwise.  Ties go to the lower row.
+// select of 8 bits per pass, and the rows that leave in front of row `keep` and those that stay behind it are listed, pairwise.
+// Ties go to the lower row.  Bound by the latency of its steps, of which there are about 20 between barriers.
 // Second kernel: every listed row of every layer's K and V is copied over its counterpart.  Targets lie in front of row `keep`
 // and sources behind it, so the copies depend on nothing and a call repeated on the same lengths and weights does the same.
 #include "attn.cuh"
@@ -17,7 +17,7 @@ constexpr int kHeldKeys = 48 * 1024;        // keys that a block holds in shared
 
 struct SelectSmem {
     int hist[256];
-    int warp_sums[2][32];
+    int equal[32], holes[32], fills[32];
     int newest[32], recent[32];
     unsigned lowest[32], highest[32];
     unsigned prefix;
@@ -51,36 +51,52 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
         for (int j = tid; j < keep; j += kSelThreads) pos_out[j] = pos[j];
     int moved = 0;
     if (keep < n && keep > 0) {
+        const bool hold = n <= kHeldKeys;
         int newest = INT_MIN;
-        for (int j = tid; j < n; j += kSelThreads) newest = max(newest, pos[j]);
+        for (int j = tid; j < n; j += kSelThreads) {
+            newest = max(newest, pos[j]);
+            if (hold) held[j] = __float_as_uint(w[j]);
+        }
         newest = __reduce_max_sync(0xffffffffu, newest);
         if (lane == 0) sm.newest[warp] = newest;
         if (tid < 256) sm.hist[tid] = 0;
         __syncthreads();
         newest = __reduce_max_sync(0xffffffffu, sm.newest[lane]);
         const long long recent_from = (long long)newest - a.recent;
+        // The keys, for no more recent rows than stay; with more of them, once more.  lo and hi: of the rows that are chosen among.
+        unsigned lo = 0xffffffffu, hi = 0u;
+        auto range = [&](unsigned key) {
+            if (key == 0u || key == 0xffffffffu) return;
+            lo = min(lo, key);
+            hi = max(hi, key);
+        };
         int n_recent = 0;
-        for (int j = tid; j < n; j += kSelThreads) n_recent += (long long)pos[j] > recent_from;
+        for (int j = tid; j < n; j += kSelThreads) {
+            const bool is_recent = (long long)pos[j] > recent_from;
+            const unsigned key = evict_key(hold ? __uint_as_float(held[j]) : w[j], is_recent, false);
+            n_recent += is_recent;
+            if (hold) held[j] = key;
+            range(key);
+        }
         n_recent = __reduce_add_sync(0xffffffffu, n_recent);
         if (lane == 0) sm.recent[warp] = n_recent;
         __syncthreads();
         const int all_recent = __reduce_add_sync(0xffffffffu, sm.recent[lane]);
         const bool among_recent = all_recent > keep;
-        const bool hold = n <= kHeldKeys;
         auto fresh_key = [&](int j) { return evict_key(w[j], (long long)pos[j] > recent_from, among_recent); };
         auto key_at = [&](int j) { return hold ? held[j] : fresh_key(j); };
-        if (hold)
-            for (int j = tid; j < n; j += kSelThreads) held[j] = fresh_key(j);
+        if (among_recent) {
+            lo = 0xffffffffu;
+            hi = 0u;
+            for (int j = tid; j < n; j += kSelThreads) {
+                const unsigned key = fresh_key(j);
+                if (hold) held[j] = key;
+                range(key);
+            }
+        }
         // Radix select among the rows that are chosen among (keys that are neither lowest nor highest), 8 bits at a time over the bits in
         // which they differ: counted from the top of all 32, nearly all weights share the first eight, and with them
         // one counter (8,192 rows: 26 us).
-        unsigned lo = 0xffffffffu, hi = 0u;
-        for (int j = tid; j < n; j += kSelThreads) {
-            const unsigned key = key_at(j);
-            if (key == 0u || key == 0xffffffffu) continue;
-            lo = min(lo, key);
-            hi = max(hi, key);
-        }
         lo = __reduce_min_sync(0xffffffffu, lo);
         hi = __reduce_max_sync(0xffffffffu, hi);
         if (lane == 0) {
@@ -138,42 +154,57 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
         // the threshold, and how many of the rows that equal it stay (the lower ones)
         const unsigned threshold = none ? 0xffffffffu : prefix + lo;
         if (none) remaining = keep;
-        // rows in order, kSelThreads at a time: which stay, and the two lists
+        // The rows in order, a part for each warp: which stay, and the two lists.  Three walks, with the warps' counts between them.
         int2 *moves = a.moves + (long long)unit * a.moves_max;
-        int equal_before = 0, holes = 0, fills = 0;
-        for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-            const int j = j0 + tid;
-            const unsigned key = j < n ? key_at(j) : 0u;
-            const bool equal = j < n && key == threshold;
-            unsigned votes = __ballot_sync(0xffffffffu, equal);
-            if (lane == 0) sm.warp_sums[0][warp] = __popc(votes);
-            __syncthreads();
-            int sum = sm.warp_sums[0][lane];
-            const int before = equal_before + __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0) + __popc(votes & ((1u << lane) - 1u));
-            equal_before += __reduce_add_sync(0xffffffffu, sum);
-            const bool stays = j < n && (key > threshold || (equal && before < remaining));
-            const bool hole = j < keep && !stays, fill = j >= keep && stays;
-            // holes and fills in one count: low and high half of a word (at most 1,024 of each here)
-            const unsigned hv = __ballot_sync(0xffffffffu, hole), fv = __ballot_sync(0xffffffffu, fill);
-            if (lane == 0) sm.warp_sums[1][warp] = __popc(hv) | __popc(fv) << 16;
-            __syncthreads();
-            sum = sm.warp_sums[1][lane];
-            const int ahead = __reduce_add_sync(0xffffffffu, lane < warp ? sum : 0), total = __reduce_add_sync(0xffffffffu, sum);
-            if (hole) {
-                const int at = holes + (ahead & 0xffff) + __popc(hv & ((1u << lane) - 1u));
-                if (at < a.moves_max) moves[at].x = j;
+        const int per = ((n + 31) / 32 + 31) / 32 * 32, part0 = (int)min((long long)warp * per, (long long)n), part1 = (int)min((long long)part0 + per, (long long)n);
+        const unsigned lower = (1u << lane) - 1u;
+        int equal = 0, holes = 0, fills = 0;
+        for (int j0 = part0; j0 < part1; j0 += 32) equal += __popc(__ballot_sync(0xffffffffu, j0 + lane < part1 && key_at(j0 + lane) == threshold));
+        if (lane == 0) sm.equal[warp] = equal;
+        __syncthreads();
+        const int equal_before = __reduce_add_sync(0xffffffffu, lane < warp ? sm.equal[lane] : 0);
+        auto walk = [&](auto visit) {                  // visit(row, leaves in front of row `keep`, stays behind it)
+            int before = equal_before;
+            for (int j0 = part0; j0 < part1; j0 += 32) {
+                const int j = j0 + lane;
+                const unsigned key = j < part1 ? key_at(j) : 0u;
+                const bool same = j < part1 && key == threshold;
+                const unsigned votes = __ballot_sync(0xffffffffu, same);
+                const bool stays = j < part1 && (key > threshold || (same && before + __popc(votes & lower) < remaining));
+                before += __popc(votes);
+                visit(j, __ballot_sync(0xffffffffu, j < part1 && j < keep && !stays), __ballot_sync(0xffffffffu, j >= keep && stays));
             }
-            if (fill) {
-                const int at = fills + (ahead >> 16) + __popc(fv & ((1u << lane) - 1u));
-                if (at < a.moves_max) moves[at].y = j;
-            }
-            holes += total & 0xffff;
-            fills += total >> 16;
+        };
+        walk([&](int, unsigned out, unsigned in) {
+            holes += __popc(out);
+            fills += __popc(in);
+        });
+        if (lane == 0) {
+            sm.holes[warp] = holes;
+            sm.fills[warp] = fills;
         }
+        __syncthreads();
+        int hole = __reduce_add_sync(0xffffffffu, lane < warp ? sm.holes[lane] : 0), fill = __reduce_add_sync(0xffffffffu, lane < warp ? sm.fills[lane] : 0);
+        holes = __reduce_add_sync(0xffffffffu, sm.holes[lane]);
+        fills = __reduce_add_sync(0xffffffffu, sm.fills[lane]);
+        walk([&](int j, unsigned out, unsigned in) {
+            if (out >> lane & 1u && hole + __popc(out & lower) < a.moves_max) moves[hole + __popc(out & lower)].x = j;
+            if (in >> lane & 1u && fill + __popc(in & lower) < a.moves_max) moves[fill + __popc(in & lower)].y = j;
+            hole += __popc(out);
+            fill += __popc(in);
+        });
         moved = min(min(holes, fills), a.moves_max);
         __syncthreads();                               // the lists are complete (and the copies above)
+        // (where the rows are, for the second kernel: its blocks would each look that up for every tensor)
+        longlong2 *places = a.places + (long long)unit * a.moves_max;
+        auto place = [&](int row) -> long long {
+            const int pg = row / a.page_size, page = __ldg(a.table + (long long)b * a.max_pages + pg);
+            if ((unsigned)page >= (unsigned)a.num_pages) return -1;
+            return page * a.page_stride + (unit - b * a.hkv) * a.head_stride + (row - pg * a.page_size) * a.row_stride;
+        };
         for (int x = tid; x < moved; x += kSelThreads) {
             const int2 mv = moves[x];
+            places[x] = make_longlong2(place(mv.x), place(mv.y));
             w_out[mv.x] = w[mv.y];
             pos_out[mv.x] = pos[mv.y];
         }
@@ -185,48 +216,32 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
     }
 }
 
-// a quarter, half or whole warp per row (`lanes` of them), four vectors in flight each
+// A quarter, half or whole warp per row (`lanes` of them), two rows in flight each.  Bound by memory, in pieces of one row: 128 units of
+// 4-8 K rows of 256 bytes to 3,932, four layers: 0.68 GB read and written, 146 us with the selection.  Four rows in flight (40
+// registers) 148, one 154; with the rows' places looked up here, 204.
+constexpr int kAhead = 2;
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ PoolTable pools,
                                                                   int lanes_shift)
 {
     pdl_trigger();
     pdl_wait();
-    const int units = a.batch * a.hkv, unit = blockIdx.x % units, tensor = blockIdx.x / units, b = unit / a.hkv, h = unit - b * a.hkv;
+    const int units = a.batch * a.hkv, unit = blockIdx.x % units, tensor = blockIdx.x / units;
     const int moved = a.counts[unit], lanes = 1 << lanes_shift, lane = threadIdx.x & (lanes - 1);
     const int step = (int)gridDim.y * (kMoveThreads >> lanes_shift), vecs = a.d * a.elem_bytes / 16;
-    const int2 *moves = a.moves + (long long)unit * a.moves_max;
-    const int *table = a.table + (long long)b * a.max_pages;
-    int4 *pool = static_cast<int4 *>(pools.ptr[tensor]);
-    const long long page_vecs = a.page_stride * a.elem_bytes / 16, head_vecs = a.head_stride * a.elem_bytes / 16,
-                    row_vecs = a.row_stride * a.elem_bytes / 16;
-    auto place = [&](int row) -> int4 * {
-        const int pg = row / a.page_size, page = __ldg(table + pg);
-        if ((unsigned)page >= (unsigned)a.num_pages) return nullptr;
-        return pool + page * page_vecs + h * head_vecs + (long long)(row - pg * a.page_size) * row_vecs;
-    };
-    constexpr int kAhead = 4;
+    const longlong2 *places = a.places + (long long)unit * a.moves_max;
+    char *pool = static_cast<char *>(pools.ptr[tensor]);
     for (int x0 = (int)blockIdx.y * (kMoveThreads >> lanes_shift) + (threadIdx.x >> lanes_shift); x0 < moved; x0 += step * kAhead) {
-        int4 *to[kAhead];
-        const int4 *from[kAhead];
+        longlong2 at[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int x = x0 + u * step;
-            to[u] = nullptr;
-            from[u] = nullptr;
-            if (x < moved) {
-                const int2 mv = moves[x];
-                to[u] = place(mv.x);
-                from[u] = place(mv.y);
-            }
-        }
+        for (int u = 0; u < kAhead; ++u) at[u] = x0 + u * step < moved ? places[x0 + u * step] : make_longlong2(-1, -1);
         for (int v = lane; v < vecs; v += lanes) {
             int4 y[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (to[u] && from[u]) y[u] = from[u][v];
+                if (at[u].x >= 0 && at[u].y >= 0) y[u] = reinterpret_cast<const int4 *>(pool + at[u].y * a.elem_bytes)[v];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (to[u] && from[u]) to[u][v] = y[u];
+                if (at[u].x >= 0 && at[u].y >= 0) reinterpret_cast<int4 *>(pool + at[u].x * a.elem_bytes)[v] = y[u];
         }
     }
 }
@@ -273,13 +288,13 @@ int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream
     int lanes_shift = 5;
     const int vecs = a.d * a.elem_bytes / 16;
     while (lanes_shift > 2 && (1 << (lanes_shift - 1)) >= vecs) --lanes_shift;
-    // as many blocks as the GPU holds (eight of 256 threads per SM) and a few more, however many units there are
+    // several times as many blocks as the GPU holds (eight of 256 threads per SM), so that units of different lengths even out
     const long long pairs = (long long)units * a.n_tensors;
     if (pairs > 0x7fffffffLL) {
         set_error_detail("eviction: %lld (unit, tensor) pairs", pairs);
         return WKV_ERR_LIMIT;
     }
-    long long slices = (148 * 16 + pairs - 1) / pairs;
+    long long slices = (148 * 64 + pairs - 1) / pairs;
     const long long most = (a.moves_max + (kMoveThreads >> lanes_shift) - 1) / (kMoveThreads >> lanes_shift);
     if (slices > most) slices = most;
     if (slices < 1) slices = 1;
