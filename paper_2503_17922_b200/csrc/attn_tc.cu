@@ -17,6 +17,11 @@
 // does not see: P is 0 there, but 0 times an infinity or NaN is not.  Such elements are replaced by 0 in shared memory, and the rows that do see them
 // get them added at the end.
 //
+// Bound by the chain of one query tile, product - weights - product, of which two are in flight (tensor memory holds no third): 32 heads on 8 of 8,192
+// tokens, d = 128, 570 us = 0.96 PFLOP/s, tensor pipe 51 % of cycles, special functions 45 %; 32,768 tokens 8.1 ms = 1.08 PFLOP/s
+// and the power limit.  Of a chain's 4,000 cycles the weights take 2,500, the products 1,100.  Sixteen warps for the weights, two
+// to a row, were slower (600 us): they have to agree on the maximum.
+//
 // Blocks are persistent, one per SM; the items come in order of descending work and are dealt to the blocks back and forth.
 // Every wait is bounded; on expiry the block sets bit 0 of the status word, lets its loads land, frees its tensor memory and returns.
 #include "attn.cuh"
@@ -37,8 +42,9 @@ constexpr int kRegion = kTile * 128;          // bytes of 64 columns of a tile
 constexpr uint32_t kTmemCols = 512;           // all of it: S/P of the two query tiles (128 columns each), O of both (128 each)
 constexpr int kMaxStages = 8;
 constexpr int kMaskSlots = 8;
-constexpr int kFmaEvery = 8;                  // one pair of exponentials in so many on the FMA pipe (measured below)
+constexpr int kFmaEvery = 8;                  // one pair of exponentials in so many on the FMA pipe, see exp2_pair_fma()
 constexpr int kFirst = 2;                     // 32-key pieces of a tile whose product begins while the others' weights are computed
+                                              // (32 heads of 8,192 tokens: one 506 us, two 499, three 513)
 constexpr float kLazy = 8.f;                  // exponent by which the maximum may be outgrown
 __host__ __device__ constexpr int stages_for(int kb) { return kb == 2 ? 5 : 8; }
 struct TcAttnArgs {
@@ -49,7 +55,7 @@ struct TcAttnArgs {
     int k_slot[3];           // tensor-map coordinates of (token, head, batch) / (slot, head, page)
     int box_rows;            // rows of a key box
     bool wide_out;           // rows of the output begin on 32 bytes
-    int by_work;             // blocks that share the items' key tiles evenly (0: items are dealt out whole)
+    bool by_work;            // kWorkBlocks blocks share the items' key tiles evenly; otherwise items are dealt out whole
     float *piece_o;          // by_work: [2 * blocks][256][d] and
     float2 *piece_ml;        // [2 * blocks][256], what a block has of an item that it does not have all of
     long long *line;         // [items + 1]: where the items begin on the line of work, for the joining kernel
@@ -144,9 +150,9 @@ __device__ __forceinline__ void walk_line(const TcAttnArgs &t, int lane, F visit
     }
 }
 // what block c has of an item at `at` on a line of `total`: tiles begin .. end - 1
-__device__ __forceinline__ void piece_of(const TcAttnArgs &t, long long total, int c, long long at, int n_tiles, int &begin, int &end)
+__device__ __forceinline__ void piece_of(long long total, int c, long long at, int n_tiles, int &begin, int &end)
 {
-    const long long lo = total * c / t.by_work - at, hi = total * (c + 1) / t.by_work - at;
+    const long long lo = total * c / kWorkBlocks - at, hi = total * (c + 1) / kWorkBlocks - at;
     begin = (int)min(max(lo - kItemCost, 0ll), (long long)n_tiles);
     end = (int)min(max(hi - kItemCost, 0ll), (long long)n_tiles);
 }
@@ -173,7 +179,7 @@ struct Walk {
         if (total < 0) {
             const int lane = threadIdx.x & 31;
             total = line_length(t, lane);
-            const long long lo = total * blockIdx.x / t.by_work;
+            const long long lo = total * blockIdx.x / kWorkBlocks;
             long long k = t.items, from = 0;
             walk_line(t, lane, [&](int item, long long start, long long end) {
                 const unsigned there = __ballot_sync(0xffffffffu, end > lo);
@@ -185,7 +191,7 @@ struct Walk {
             k0 = k;
             at = from;
         }
-        const long long lo = total * blockIdx.x / t.by_work, hi = total * (blockIdx.x + 1) / t.by_work;
+        const long long lo = total * blockIdx.x / kWorkBlocks, hi = total * (blockIdx.x + 1) / kWorkBlocks;
         while (k0 < t.items && at < hi) {
             if (!get_item(t, k0, im)) {
                 ++k0;
@@ -195,7 +201,7 @@ struct Walk {
             ++k0;
             at += im.n_tiles + kItemCost;
             if (at <= lo) continue;
-            piece_of(t, total, blockIdx.x, here, im.n_tiles, im.begin, im.end);
+            piece_of(total, blockIdx.x, here, im.n_tiles, im.begin, im.end);
             if (im.n_tiles == 0) {
                 if (here >= lo) return true;              // nothing to see: its rows are written where it begins
                 continue;
@@ -295,7 +301,8 @@ __device__ __forceinline__ void hide(float (&v)[32], uint32_t seen)
     for (int j = 0; j < 32; ++j) v[j] = seen >> j & 1u ? v[j] : -INFINITY;
 }
 
-// 2^x of two values on the FMA pipe: 2^t * 2^f with t the nearest integer, 2^f by a polynomial of degree five (a Remez fit of the
+// 2^x of two values on the FMA pipe, which is half idle where the special functions are not (32 heads of 8,192 tokens: none 546 us, one
+// pair in eight 499, in four 507, in two 599): 2^t * 2^f with t the nearest integer, 2^f by a polynomial of degree five (a Remez fit of the
 // relative error on [-1/2, 1/2], 7.5e-8; evaluated in fp32 2.1e-7).  x is at most kLazy; below -126 it counts as -126, so
 // that a weight of 0 comes out as 1e-38 (rows that see nothing of a tile do not come here); a NaN stays one.
 __device__ __forceinline__ unsigned long long exp2_pair_fma(unsigned long long x2)
@@ -830,9 +837,12 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     if (warp == 8) tmem_dealloc(sh.tmem_base, kTmemCols);
 }
 
-// Joins the pieces of the items that lie across blocks: block (item, y) takes 64 of its 256 rows, a warp per row in turn.
-constexpr int kJoinRows = 64;
-__global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant__ TcAttnArgs t)
+// Joins the pieces of the items that lie across blocks: block (item, y) takes `join_rows` of its 256 rows, a warp per row in turn.  With few
+// items each is in many pieces, whose reading is trips to memory: a row per warp then (8 items of 32 rows over 16,384 keys: 44
+// us with the kernel in front, 66 with 32 rows per block).  With many there are two pieces or so, and fewer blocks look for them
+// more seldom (160 items: 101 us with 8 rows, 96 with 32).
+constexpr int kFewItems = 128;
+__global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant__ TcAttnArgs t, int join_rows)
 {
     pdl_trigger();
     pdl_wait();
@@ -842,14 +852,17 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Item im;
     if (!get_item(t, blockIdx.x, im) || im.n_tiles == 0) return;
+    const int first_row = (int)blockIdx.y * join_rows, x = first_row / kTile;
+    if ((first_row - x * kTile) / a.G >= (x ? im.rows[1] : im.rows[0])) return;                // (no row of this block's)
     const long long at = t.line[blockIdx.x], total = t.line[t.items];
     // the pieces, in order: 32 blocks at a time, by the first warp
     if (warp == 0) {
         int n = 0, whole = 0;
-        for (int c0 = 0; c0 < t.by_work; c0 += 32) {
+        const int from = (int)(at * kWorkBlocks / total), to = (int)min((at + im.n_tiles + kItemCost) * kWorkBlocks / total + 1, (long long)kWorkBlocks);
+        for (int c0 = from; c0 < to; c0 += 32) {
             const int c = c0 + lane;
             int begin = 0, end = 0;
-            if (c < t.by_work) piece_of(t, total, c, at, im.n_tiles, begin, end);
+            if (c < to) piece_of(total, c, at, im.n_tiles, begin, end);
             const unsigned some = __ballot_sync(0xffffffffu, begin < end);
             whole |= __any_sync(0xffffffffu, end - begin == im.n_tiles);
             if (begin < end) slots[n + __popc(some & ((1u << lane) - 1u))] = piece_slot(c, begin);
@@ -860,8 +873,8 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
     __syncthreads();
     const int n = n_slots;
     if (n == 0) return;
-    for (int r = blockIdx.y * kJoinRows + warp; r < (int)(blockIdx.y + 1) * kJoinRows; r += 8) {
-        const int x = r / kTile, row = r - x * kTile, place = row / a.G, head = row - place * a.G;
+    for (int r = first_row + warp; r < first_row + join_rows; r += 8) {
+        const int row = r - x * kTile, place = row / a.G, head = row - place * a.G;
         if (place >= t.ppt || place >= (x ? im.rows[1] : im.rows[0])) continue;
         float top = -INFINITY;
         for (int i = lane; i < n; i += 32) top = fmaxf(top, t.piece_ml[(long long)slots[i] * 2 * kTile + r].x);
@@ -870,7 +883,7 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
         const float ref = top == -INFINITY ? 0.f : top;
         float l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
         for (int i = 0; i < n; ++i) {
             const long long left = (long long)slots[i] * 2 * kTile + r;
             const float2 ml = t.piece_ml[left];
@@ -902,11 +915,12 @@ int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &
     cudaError_t err = cudaGetDevice(&dev);
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (err == cudaSuccess) err = allow_smem(attn_tc_kernel<KB, WHOLE>, smem, asked);
-    const long long grid = t.by_work ? t.by_work : (t.items < sms ? t.items : sms);
+    const long long grid = t.by_work ? kWorkBlocks : (t.items < sms ? t.items : sms);
     if (err == cudaSuccess) err = launch_pdl(attn_tc_kernel<KB, WHOLE>, dim3((unsigned)grid), kThreads, smem, stream, 1, k_map, v_map, t);
     if (err == cudaSuccess) count_launches(1);
     if (err == cudaSuccess && t.by_work) {
-        err = launch_pdl(attn_tc_join_kernel, dim3((unsigned)t.items, 2 * kTile / kJoinRows), 256, 0, stream, 1, t);
+        const int join_rows = t.items <= kFewItems ? 8 : 32;
+        err = launch_pdl(attn_tc_join_kernel, dim3((unsigned)t.items, 2 * kTile / join_rows), 256, 0, stream, 1, t, join_rows);
         if (err == cudaSuccess) count_launches(1);
     }
     return check_cuda(err, "tensor-core attention kernel");
@@ -953,7 +967,7 @@ int launch_attn_tc(const AttnArgs &a, float *piece_o, float2 *piece_ml, long lon
     t.box_rows = a.table ? box_of_page(a.page_size) : kTile;
     t.wide_out = a.d % 16 == 0 && (reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ot * 2) | (uintptr_t)(a.oh * 2) | (uintptr_t)(a.ob * 2)) % 32 == 0;
     int rows = 0, most = 0;
-    t.by_work = piece_o && attn_tc_pieces(units, a.max_q, a.G, a.cap, &rows, &most) ? kWorkBlocks : 0;
+    t.by_work = piece_o && attn_tc_pieces(units, a.max_q, a.G, a.cap, &rows, &most);
     t.piece_o = piece_o;
     t.piece_ml = piece_ml;
     t.line = line;

@@ -148,8 +148,9 @@ int plan_splits(const wkv_paged *c, const Paged &p, bool &clustered)
                 (s <= power || 2ll * p.cap * c->head_dim * p.eb / kClusterSplits <= kClusterBytes);
     return (int)(clustered ? power : s);
 }
-// More rows than this go to the tensor-core kernel where it takes the shape.
-constexpr int kFewRows = 32;
+// More rows than this go to the tensor-core kernel where it takes the shape (8 new tokens of 32 heads on 8, 32 rows: 4 sequences of 16,384
+// keys 171 us on the warp-level kernel, 88 here; one of 4,000 42 and 32).
+constexpr int kFewRows = 16;
 // Rows per unit whose logits are kept for the weights: 4 bytes for each beside the 2 * d * 2 of K and V, written and read.
 constexpr int kLogitRows = 16;
 PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
