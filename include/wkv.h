@@ -473,7 +473,9 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
  * element c of it at pool[page*page_stride + h*head_stride + slot*row_stride + c].  A table entry outside [0, num_pages) is no
  * page: its rows are neither read nor written, and nothing attends to them.  Lengths are per unit, as kept_len.
  * The chunk of new tokens: max_new for every sequence ([B, heads, max_new, d], strides given with each tensor), or packed
- * [T, heads, d] with cu_new (0 .. max_new tokens per sequence; HOST and DEVICE copies as for cu_seqlens).
+ * [T, heads, d] with cu_new (0 .. max_new tokens per sequence; HOST and DEVICE copies as for cu_seqlens).  Without any new token
+ * (T = 0) the chunk's tensors and strides may be NULL.  Sequences may share pages that are only read; a row that is appended or
+ * moves (eviction) is written in its page, for whoever shares that.
  */
 typedef struct {
     uint32_t struct_size;        /* sizeof(wkv_paged), checked */

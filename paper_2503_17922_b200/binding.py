@@ -671,8 +671,10 @@ def _check_same_layout(a, b, what: str) -> None:
 def _check_kv_layout(prob: "Problem", t, what: str) -> None:
     """Keys or values in the layout that the problem describes."""
     s = prob.shape
-    if t.dtype != prob.torch_dtype or t.shape[-1] != s.head_dim or t.stride(-1) != 1 and s.head_dim != 1:
-        raise ValueError(f"{what}: rows of {s.head_dim} {prob.torch_dtype} expected")
+    tokens = int(prob.cu_host[-1]) if prob.packed else s.batch * s.max_seqlen
+    if (t.dtype != prob.torch_dtype or t.shape[-1] != s.head_dim or t.stride(-1) != 1 and s.head_dim != 1
+            or t.numel() < tokens * s.n_kv_heads * s.head_dim):
+        raise ValueError(f"{what}: {tokens * s.n_kv_heads} rows of {s.head_dim} {prob.torch_dtype} expected, got {tuple(t.shape)} of {t.dtype}")
 
 
 def prepare_rotate_prompt(prob: Problem, rope: Rope, q, k, q_out, k_out, positions=None, stream=None) -> PreparedCall:
@@ -717,6 +719,16 @@ def wkv_attend_prompt(prob: Problem, q, k, v, out, lse=None, lse_obs=None, statu
     prepare_attend_prompt(prob, q, k, v, out, lse, lse_obs, status, stream).run()
 
 
+def _check_pool(cache: PagedCache, t, what: str) -> None:
+    """A pool's type, and that its last page's last row lies in its storage (tensors only: an address says neither)."""
+    s = cache.shape
+    if not hasattr(t, "untyped_storage"):
+        return
+    need = (s.num_pages - 1) * s.page_stride + (s.n_kv_heads - 1) * s.head_stride + (s.page_size - 1) * s.row_stride + s.head_dim
+    if t.dtype != cache.torch_dtype or t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < need:
+        raise ValueError(f"{what}: {cache.torch_dtype} with {need} elements expected, got {tuple(t.shape)} of {t.dtype}")
+
+
 def _chunk_tokens(cache: PagedCache) -> int:
     return int(cache.cu_host[-1]) if cache.packed else cache.shape.max_new
 
@@ -731,6 +743,8 @@ def prepare_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_
             _check_heads(t, heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
     _check_same_layout(k_new, v_new, "k_new and v_new")
     _check_same_layout(q, q_out, "q and q_out")
+    _check_pool(cache, k_pool, "k_pool")
+    _check_pool(cache, v_pool, "v_pool")
     units = (s.batch, s.n_kv_heads)
     _check_state(lengths, units, "int32", "lengths")
     _check_state(lengths_out, units, "int32", "lengths_out")
@@ -757,6 +771,8 @@ def prepare_attend_paged(cache: PagedCache, q, k_pool, v_pool, lengths, out, wor
     s, tokens = cache.shape, _chunk_tokens(cache)
     for t, what in ((q, "q"), (out, "out")):
         _check_heads(t, s.n_q_heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
+    _check_pool(cache, k_pool, "k_pool")
+    _check_pool(cache, v_pool, "v_pool")
     units = (s.batch, s.n_kv_heads)
     _check_state(lengths, units, "int32", "lengths")
     _check_state(lse, (s.batch, s.n_q_heads, s.max_new), "float32", "lse")
@@ -785,6 +801,11 @@ def prepare_evict_kv_paged(cache: PagedCache, k_pools, v_pools, weights, positio
     for t, what in ((lengths, "lengths"), (lengths_out, "lengths_out")):
         _check_state(t, units, "int32", what)
     _check_state(budgets, (s.batch,), "int32", "budgets")
+    for pools, what in ((k_pools, "k_pools"), (v_pools, "v_pools")):
+        if pools is not None and len(pools) != len(k_pools):
+            raise ValueError(f"{what}: one pool per layer")
+        for t in pools or ():
+            _check_pool(cache, t, what)
     arrs = (_ptr_array(k_pools), _ptr_array(v_pools))
     args = (ctypes.byref(s), len(k_pools), arrs[0], arrs[1], budget, _ptr(budgets), recent, _ptr(weights), _ptr(positions), _ptr(lengths),
             _ptr(weights_out), _ptr(positions_out), _ptr(lengths_out), _ptr(workspace), workspace.numel(), _stream(stream))

@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const __grid_consta
     const int n = min(16, sq.m * a.G - row0);
     if (n > 0) join_rows<T>(a, sm, sq, unit, b, h, row0, n, true);
 }
-// The same for up to 16 rows whose logits are in the workspace: block (unit, y) also adds up the weights of kJoinKeys keys.  Every
+// The same for up to 16 rows whose logits are in the workspace: block (y, unit) also adds up the weights of kJoinKeys keys.  Every
 // block of a unit needs the rows' normalisers and joins the few parts for itself; block 0 writes the rows.
 constexpr int kJoinKeys = 4 * kThreads;
 template <typename T>
@@ -498,14 +498,14 @@ __global__ void __launch_bounds__(kThreads) attn_join_weights_kernel(const __gri
     __shared__ JoinSmem sm;
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.x, b = unit / a.hkv, h = unit - b * a.hkv;
+    const int units = a.batch * a.hkv, unit = (int)blockIdx.x % units, part = (int)blockIdx.x / units - 1, b = unit / a.hkv, h = unit - b * a.hkv;
     const AttnSeq sq = attn_seq(a, b, h);
-    const int rows = sq.m * a.G, j = ((int)blockIdx.y - 1) * kJoinKeys + threadIdx.x * 4;
-    if (blockIdx.y == 0) {                                               // the first block writes the rows, the others weights
+    const int rows = sq.m * a.G, j = part * kJoinKeys + threadIdx.x * 4;
+    if (part < 0) {                                               // the first block writes the rows, the others weights
         join_rows<T>(a, sm, sq, unit, b, h, 0, rows, true);
         return;
     }
-    if (((int)blockIdx.y - 1) * kJoinKeys >= sq.n) return;
+    if (part * kJoinKeys >= sq.n) return;
     join_rows<T>(a, sm, sq, unit, b, h, 0, rows, false);
     if (j >= sq.n) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
@@ -601,12 +601,12 @@ int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
 {
     const int units = a.batch * a.hkv;
     if (a.logits) {
-        const int blocks = 1 + (a.cap + kJoinKeys - 1) / kJoinKeys;
-        if (blocks > 65535) {
-            set_error_detail("attention weights: %d rows of a unit", a.cap);
+        const long long blocks = (1ll + (a.cap + kJoinKeys - 1) / kJoinKeys) * units;
+        if (blocks > 0x7fffffffLL) {
+            set_error_detail("attention weights: %lld blocks", blocks);
             return WKV_ERR_LIMIT;
         }
-        const dim3 grid(units, blocks);
+        const dim3 grid((unsigned)blocks);
         return dtype == WKV_F32 ? launch(attn_join_weights_kernel<float>, grid, 0, a, stream, "attention joining kernel")
                                 : launch(attn_join_weights_kernel<__nv_bfloat16>, grid, 0, a, stream, "attention joining kernel");
     }

@@ -398,16 +398,17 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
     if (rope && (st = check_rope(rope, c->head_dim)) != WKV_OK) return st;
     const void *const ptrs[4] = {k_new, v_new, k_pool, v_pool};
     static const char *const names[4] = {"k_new", "v_new", "k_pool", "v_pool"};
-    for (int i = 0; i < 4; ++i)
+    const bool packed = c->cu_new_host != nullptr, none = packed && p.total_new == 0;      // no new tokens: their tensors may be null
+    for (int i = none ? 2 : 0; i < 4; ++i)
         if ((st = check_pointer(ptrs[i], names[i])) != WKV_OK) return st;
-    if ((st = check_strides(kv_strides, c->head_dim, p.eb, "kv_strides")) != WKV_OK) return st;
-    if ((q == nullptr) != (q_out == nullptr)) return missing(q ? "q_out" : "q");
-    if (q) {
+    if (!none && (st = check_strides(kv_strides, c->head_dim, p.eb, "kv_strides")) != WKV_OK) return st;
+    if (!none && (q == nullptr) != (q_out == nullptr)) return missing(q ? "q_out" : "q");
+    if (q && !none) {
         if ((st = check_pointer(q, "q")) != WKV_OK || (st = check_pointer(q_out, "q_out")) != WKV_OK) return st;
         if ((st = check_strides(q_strides, c->head_dim, p.eb, "q_strides")) != WKV_OK) return st;
     }
     if (!lengths) return missing("lengths");
-    if (!positions && (rope || row_positions)) return missing("positions");
+    if (!none && !positions && (rope || row_positions)) return missing("positions");
     if (lengths_out == lengths) {
         set_error_detail("lengths_out must not be lengths (other blocks still read them)");
         return WKV_ERR_SHAPE;
@@ -430,8 +431,7 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
     a.hkv = c->n_kv_heads;
     a.q = q;
     a.q_out = q_out;
-    const bool packed = c->cu_new_host != nullptr;
-    if (q) {
+    if (q && !none) {
         a.qb = packed ? 0 : q_strides[0];
         a.qh = q_strides[1];
         a.qt = q_strides[2];
@@ -440,9 +440,11 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
     a.v = v_new;
     a.k_out = k_pool;
     a.v_out = v_pool;
-    a.kb = packed ? 0 : kv_strides[0];
-    a.kh = kv_strides[1];
-    a.kt = kv_strides[2];
+    if (!none) {
+        a.kb = packed ? 0 : kv_strides[0];
+        a.kh = kv_strides[1];
+        a.kt = kv_strides[2];
+    }
     a.lengths = lengths;
     a.table = c->block_table;
     a.max_pages = c->max_pages;
@@ -468,21 +470,21 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
     if ((st = check_head_dim(c->head_dim)) != WKV_OK) return st;
     const void *const ptrs[4] = {q, k_pool, v_pool, out};
     static const char *const names[4] = {"q", "k_pool", "v_pool", "out"};
+    const bool packed = c->cu_new_host != nullptr, none = packed && p.total_new == 0;      // no new tokens: q and out may be null
     for (int i = 0; i < 4; ++i)
-        if ((st = check_pointer(ptrs[i], names[i])) != WKV_OK) return st;
-    if ((st = check_strides(q_strides, c->head_dim, p.eb, "q_strides")) != WKV_OK ||
-        (st = check_strides(out_strides, c->head_dim, p.eb, "out_strides")) != WKV_OK)
+        if (!(none && (i == 0 || i == 3)) && (st = check_pointer(ptrs[i], names[i])) != WKV_OK) return st;
+    if (!none && ((st = check_strides(q_strides, c->head_dim, p.eb, "q_strides")) != WKV_OK ||
+                  (st = check_strides(out_strides, c->head_dim, p.eb, "out_strides")) != WKV_OK))
         return st;
     if (!lengths) return missing("lengths");
     if (weights_in && !weights_out) return missing("weights_out");
-    if (out == q || out == k_pool || out == v_pool) {
+    if (!none && (out == q || out == k_pool || out == v_pool)) {
         set_error_detail("out must not be an input");
         return WKV_ERR_SHAPE;
     }
     const PagedWorkspace w = plan_paged(c, p);
     if ((st = check_workspace(w, workspace, workspace_bytes)) != WKV_OK) return st;
-    const bool packed = c->cu_new_host != nullptr;
-    if (packed && p.total_new == 0 && !weights_out) return WKV_OK;         // no new tokens at all
+    if (none && !weights_out) return WKV_OK;
     char *ws = static_cast<char *>(workspace);
     AttnArgs a;
     memset(&a, 0, sizeof a);
@@ -496,12 +498,14 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
     a.cu_q = c->cu_new_dev;
     a.q = q;
     a.out = out;
-    a.qb = packed ? 0 : q_strides[0];
-    a.qh = q_strides[1];
-    a.qt = q_strides[2];
-    a.ob = packed ? 0 : out_strides[0];
-    a.oh = out_strides[1];
-    a.ot = out_strides[2];
+    if (!none) {
+        a.qb = packed ? 0 : q_strides[0];
+        a.qh = q_strides[1];
+        a.qt = q_strides[2];
+        a.ob = packed ? 0 : out_strides[0];
+        a.oh = out_strides[1];
+        a.ot = out_strides[2];
+    }
     a.k = k_pool;
     a.v = v_pool;
     a.kb = c->page_stride;

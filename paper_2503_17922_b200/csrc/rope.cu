@@ -221,6 +221,10 @@ int launch(const RopeArgs &a, cudaStream_t stream)
         set_error_detail("rotary positions: %lld tokens", tokens);
         return WKV_ERR_LIMIT;
     }
+    if ((a.hq + 2ll * a.hkv) * per > 0x3fffffffLL) {
+        set_error_detail("rotary positions: %d query and %d KV heads", a.hq, a.hkv);
+        return WKV_ERR_LIMIT;
+    }
     const dim3 grid((unsigned)(blocks > 0 ? blocks : 1));
     // vectors must end where the turned part does, and in HALF order where its first half does
     const bool pairs = a.order == WKV_ROPE_INTERLEAVED;

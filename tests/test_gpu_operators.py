@@ -816,3 +816,36 @@ def test_fp32_splits_do_not_see_what_follows():
     torch.cuda.synchronize()
     assert torch.equal(p.out[0, :2, :500], clean[0, :2, :500]) and torch.equal(p.out[0, 2:, :700], clean[0, 2:, :700])
     assert torch.isnan(p.out[0, :2, 500:, 3]).all() and (p.out[0, :2, 500:, 5] == INF).all() and torch.isnan(p.out[0, 2:, 700:]).all()
+
+
+@pytest.mark.parametrize("case", [
+    # fp32 splits with 128 rows a block; 17 to 32 rows on the tensor cores, of few and many items, short and long, ending inside a page
+    ("f32", 8, 2, 128, 16, "phsd", [[3001, 2990], [2500, 2400]], [200, 200], False),
+    ("bf16", 8, 2, 128, 64, "pshd", [[2500, 2400], [17, 5], [130, 129]], [5, 8, 6], True),
+    ("bf16", 4, 1, 64, 16, "phsd", [[333], [90]], [8, 8], False),
+    ("bf16", 16, 1, 128, 128, "phsd", [[5000]], [2], False),
+    ("bf16", 16, 4, 128, 16, "pshd", [[2222] * 4] * 9, [6] * 9, False),
+], ids=lambda c: "-".join(map(str, c)).replace(" ", "")[:70])
+def test_attend_row_counts(case):
+    a = Attend(*case)
+    a.run()
+    a.check()
+
+
+@pytest.mark.parametrize("dtype,max_new", [("bf16", 2), ("bf16", 100), ("f32", 2), ("f32", 100)])
+def test_no_new_tokens_at_all(dtype, max_new):
+    """A packed chunk of nothing: tensors without elements, whose addresses are null."""
+    a = Attend(dtype, 8, 2, 64, 16, "phsd", [[100, 90], [40, 0]], [0, 0], True, max_new=max_new)
+    assert a.q.numel() == 0
+    a.run()
+    torch.cuda.synchronize()
+    there = torch.arange(a.c.cap, device="cuda") < a.lengths.cuda().unsqueeze(-1)
+    assert torch.equal(a.w_out, torch.where(there, a.w_in, torch.full_like(a.w_in, 77.0))) and (a.lse == 77.0).all()
+    a.run(weights=False)
+    lengths, out = a.lengths.cuda(), torch.zeros_like(a.lengths).cuda()
+    before = a.c.k[0].clone()
+    kv = a.q[:, :2]
+    positions = torch.zeros(0, dtype=torch.int32, device="cuda")
+    wkv.wkv_append_kv_paged(a.cache, kv, kv, lengths, a.c.k[0], a.c.v[0], q=a.q, q_out=a.q, positions=positions, rope=wkv.Rope(64), lengths_out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, lengths) and torch.equal(a.c.k[0].view(torch.uint8), before.view(torch.uint8)) and wkv.device_status(a.ws) == 0

@@ -224,3 +224,23 @@ def test_python_side_checks_shapes():
         binding._check_state(torch.zeros((2, 4), dtype=torch.int32)[:, ::2], (2, 2), "int32", "lengths")
     with pytest.raises(ValueError):
         binding._check_same_layout(t, t.transpose(1, 2), "q and q_out")
+
+
+def test_binding_refuses_pools_and_keys_that_are_too_small():
+    import torch
+    table = torch.zeros((2, 4), dtype=torch.int32)
+    cache = binding.PagedCache(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=16, num_pages=6, block_table=table)
+    q, n, ws = torch.zeros((2, 4, 1, 64), dtype=torch.bfloat16), torch.zeros((2, 2), dtype=torch.int32), torch.zeros(8, dtype=torch.uint8)
+    pool = torch.zeros((6, 2, 16, 64), dtype=torch.bfloat16)
+    for bad in (pool[:5].clone(), pool.float(), pool.view(-1)[64:]):
+        with pytest.raises(ValueError, match="pool"):
+            binding.prepare_attend_paged(cache, q, bad, pool, n, q.clone(), ws)
+        with pytest.raises(ValueError, match="pool"):
+            binding.prepare_attend_paged(cache, q, pool, bad, n, q.clone(), ws)
+        with pytest.raises(ValueError, match="pool"):
+            binding.prepare_append_kv_paged(cache, q[:, :2], q[:, :2], n, bad, pool)
+        w, pos = torch.zeros((2, 2, 64)), torch.zeros((2, 2, 64), dtype=torch.int32)
+        with pytest.raises(ValueError, match="pool"):
+            binding.prepare_evict_kv_paged(cache, [pool, bad], None, w, pos, n, 8, 2, w, pos, n, ws)
+    with pytest.raises(ValueError, match="per layer"):
+        binding.prepare_evict_kv_paged(cache, [pool, pool], [pool], w, pos, n, 8, 2, w, pos, n, ws)
