@@ -837,12 +837,13 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     if (warp == 8) tmem_dealloc(sh.tmem_base, kTmemCols);
 }
 
-// Joins the pieces of the items that lie across blocks: block (item, y) takes `join_rows` of its 256 rows, a warp per row in turn.  With few
+// Joins the pieces of the items that lie across blocks: block (item, y) takes 8 * RPW of its 256 rows, RPW to a warp.  With few
 // items each is in many pieces, whose reading is trips to memory: a row per warp then (8 items of 32 rows over 16,384 keys: 44
 // us with the kernel in front, 66 with 32 rows per block).  With many there are two pieces or so, and fewer blocks look for them
 // more seldom (160 items: 101 us with 8 rows, 96 with 32).
 constexpr int kFewItems = 128;
-__global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant__ TcAttnArgs t, int join_rows)
+template <int RPW>                      // rows of a warp, all in flight together
+__global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant__ TcAttnArgs t)
 {
     pdl_trigger();
     pdl_wait();
@@ -852,7 +853,7 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Item im;
     if (!get_item(t, blockIdx.x, im) || im.n_tiles == 0) return;
-    const int first_row = (int)blockIdx.y * join_rows, x = first_row / kTile;
+    const int first_row = (int)blockIdx.y * 8 * RPW, x = first_row / kTile;
     if ((first_row - x * kTile) / a.G >= (x ? im.rows[1] : im.rows[0])) return;                // (no row of this block's)
     const long long at = t.line[blockIdx.x], total = t.line[t.items];
     // the pieces, in order: 32 blocks at a time, by the first warp
@@ -873,35 +874,62 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
     __syncthreads();
     const int n = n_slots;
     if (n == 0) return;
-    for (int r = first_row + warp; r < first_row + join_rows; r += 8) {
-        const int row = r - x * kTile, place = row / a.G, head = row - place * a.G;
-        if (place >= t.ppt || place >= (x ? im.rows[1] : im.rows[0])) continue;
-        float top = -INFINITY;
-        for (int i = lane; i < n; i += 32) top = fmaxf(top, t.piece_ml[(long long)slots[i] * 2 * kTile + r].x);
+    int row[RPW];
+    bool there[RPW];
+    float top[RPW], l[RPW];
+    float4 o[RPW];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float ref = top == -INFINITY ? 0.f : top;
-        float l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) {
-            const long long left = (long long)slots[i] * 2 * kTile + r;
-            const float2 ml = t.piece_ml[left];
-            float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (lane * 4 < a.d) p = *reinterpret_cast<const float4 *>(t.piece_o + left * a.d + lane * 4);
-            const float f = ml.y == 0.f ? 0.f : exp2f(ml.x - ref);
-            if (f == 0.f) continue;
-            l += f * ml.y;
-            o.x = fmaf(f, p.x, o.x);
-            o.y = fmaf(f, p.y, o.y);
-            o.z = fmaf(f, p.z, o.z);
-            o.w = fmaf(f, p.w, o.w);
+    for (int k = 0; k < RPW; ++k) {
+        row[k] = first_row - x * kTile + warp + 8 * k;
+        const int place = row[k] / a.G;
+        there[k] = place < t.ppt && place < (x ? im.rows[1] : im.rows[0]);
+        top[k] = -INFINITY;
+        l[k] = 0.f;
+        o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int i = lane; i < n; i += 32) {
+        const float2 *from = t.piece_ml + (long long)slots[i] * 2 * kTile + x * kTile;
+#pragma unroll
+        for (int k = 0; k < RPW; ++k)
+            if (there[k]) top[k] = fmaxf(top[k], from[row[k]].x);
+    }
+#pragma unroll
+    for (int k = 0; k < RPW; ++k)
+#pragma unroll
+        for (int y = 16; y; y >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], y));
+#pragma unroll (RPW == 1 ? 8 : 2)
+    for (int i = 0; i < n; ++i) {
+        const long long from = (long long)slots[i] * 2 * kTile + x * kTile;
+        float2 ml[RPW];
+        float4 p[RPW];
+#pragma unroll
+        for (int k = 0; k < RPW; ++k) {
+            ml[k] = make_float2(0.f, 0.f);
+            p[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (!there[k]) continue;
+            ml[k] = t.piece_ml[from + row[k]];
+            if (lane * 4 < a.d) p[k] = *reinterpret_cast<const float4 *>(t.piece_o + (from + row[k]) * a.d + lane * 4);
         }
-        const int pos = im.pos0 + x * t.ppt + place, hq = im.h * a.G + head;
-        if (lane == 0) attn_store_lse(a, im.b, hq, pos, im.sq.m, l > 0.f || l != l ? top + log2f(l) : -INFINITY);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int k = 0; k < RPW; ++k) {
+            const float f = ml[k].y == 0.f ? 0.f : exp2f(ml[k].x - (top[k] == -INFINITY ? 0.f : top[k]));
+            if (f == 0.f) continue;
+            l[k] += f * ml[k].y;
+            o[k].x = fmaf(f, p[k].x, o[k].x);
+            o[k].y = fmaf(f, p[k].y, o[k].y);
+            o[k].z = fmaf(f, p[k].z, o[k].z);
+            o[k].w = fmaf(f, p[k].w, o[k].w);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < RPW; ++k) {
+        if (!there[k]) continue;
+        const int place = row[k] / a.G, pos = im.pos0 + x * t.ppt + place, hq = im.h * a.G + row[k] - place * a.G;
+        if (lane == 0) attn_store_lse(a, im.b, hq, pos, im.sq.m, l[k] > 0.f || l[k] != l[k] ? top[k] + log2f(l[k]) : -INFINITY);
+        const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (im.sq.q_off + pos) * a.ot + im.b * a.ob + (long long)hq * a.oh;
-        if (lane * 4 < a.d) *reinterpret_cast<uint2 *>(dst + lane * 4) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (lane * 4 < a.d)
+            *reinterpret_cast<uint2 *>(dst + lane * 4) = make_uint2(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv));
     }
 }
 
@@ -919,8 +947,8 @@ int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &
     if (err == cudaSuccess) err = launch_pdl(attn_tc_kernel<KB, WHOLE>, dim3((unsigned)grid), kThreads, smem, stream, 1, k_map, v_map, t);
     if (err == cudaSuccess) count_launches(1);
     if (err == cudaSuccess && t.by_work) {
-        const int join_rows = t.items <= kFewItems ? 8 : 32;
-        err = launch_pdl(attn_tc_join_kernel, dim3((unsigned)t.items, 2 * kTile / join_rows), 256, 0, stream, 1, t, join_rows);
+        const auto join = [&](auto kernel, int rows) { return launch_pdl(kernel, dim3((unsigned)t.items, 2 * kTile / rows), 256, 0, stream, 1, t); };
+        err = t.items <= kFewItems ? join(attn_tc_join_kernel<1>, 8) : join(attn_tc_join_kernel<4>, 32);
         if (err == cudaSuccess) count_launches(1);
     }
     return check_cuda(err, "tensor-core attention kernel");
