@@ -849,3 +849,104 @@ def test_no_new_tokens_at_all(dtype, max_new):
     wkv.wkv_append_kv_paged(a.cache, kv, kv, lengths, a.c.k[0], a.c.v[0], q=a.q, q_out=a.q, positions=positions, rope=wkv.Rope(64), lengths_out=out)
     torch.cuda.synchronize()
     assert torch.equal(out, lengths) and torch.equal(a.c.k[0].view(torch.uint8), before.view(torch.uint8)) and wkv.device_status(a.ws) == 0
+
+
+@pytest.mark.parametrize("dtype,d,stride,new", [("bf16", 128, 400_000_000, 1), ("bf16", 128, 400_000_000, 9), ("f32", 64, 200_000_000, 3)])
+def test_pools_beyond_32_bits(dtype, d, stride, new):
+    """Pages whose offsets pass 2^31 and 2^32: the same bits as in a small pool with the same table."""
+    g = gen(21)
+    small = Attend(dtype, 8, 2, d, 64, "phsd", [[600, 599]], [new], False, max_pages=10)
+    c = small.c
+    shape = tuple(c.k[0].shape)
+    assert shape[0] == 12 and int(c.table.max()) * stride > (2 ** 32 if dtype == "bf16" else 2 ** 31)
+    flat = [torch.empty(11 * stride + shape[1] * shape[2] * d, dtype=c.dtype, device="cuda") for _ in range(2)]
+    far = [f.as_strided(shape, (stride, shape[2] * d, d, 1)) for f in flat]
+    far_cache = wkv.PagedCache(dtype=dtype, batch=1, n_q_heads=8, n_kv_heads=2, head_dim=d, page_size=64, num_pages=12, block_table=c.table,
+                               max_new=new, layout=(stride, shape[2] * d, d))
+    for x, y in zip(far, (c.k[0], c.v[0])):
+        x.copy_(y)
+    k, v = (chunk_of(g, c.dtype, 2, d, [new], False) for _ in range(2))
+    pos = torch.arange(new, dtype=torch.int32, device="cuda").view(1, -1) + 700
+    rope = wkv.Rope(d)
+    results = []
+    for cache, pools in ((small.cache, (c.k[0], c.v[0])), (far_cache, far)):
+        w, p = small.w_in.clone(), torch.arange(c.cap, dtype=torch.int32, device="cuda").expand(1, 2, -1).contiguous()
+        n0, n1, n2 = small.lengths.cuda(), torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+        out, ws, q_out = torch.full_like(small.q, 77.0), cache.alloc_workspace(), torch.empty_like(small.q)
+        wkv.wkv_append_kv_paged(cache, k, v, n0, pools[0], pools[1], q=small.q, q_out=q_out, positions=pos, rope=rope, lengths_out=n1, row_positions=p,
+                                row_weights=w)
+        wkv.wkv_attend_paged(cache, q_out, pools[0], pools[1], n1, out, ws, weights_in=w, weights_out=w)
+        wkv.wkv_evict_kv_paged(cache, [pools[0]], [pools[1]], w, p, n1, 300, 20, w, p, n2, ws)
+        torch.cuda.synchronize()
+        assert wkv.device_status(ws) == 0 and (n2 == 300).all()
+        results.append([out, q_out, w, p, n1, pools[0], pools[1]])
+    for x, y in zip(*results):
+        assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 200), ("bf16", 90), ("f32", 150)])
+def test_prompt_queries_beyond_32_bits(dtype, n):
+    """Queries and outputs whose last tokens lie behind 2^31 elements."""
+    p = Prompt(dtype, 4, 2, 64, [n], "bhnd", 4)
+    p.run()
+    stride = 2 ** 31 // (n - 4) // 64 * 64
+    far = [torch.empty((n - 1) * stride + 4 * 64, dtype=p.q.dtype, device="cuda").as_strided((1, 4, n, 64), (0, 64, stride, 1)) for _ in range(2)]
+    far[0].copy_(p.q)
+    wkv.wkv_attend_prompt(p.prob, far[0], p.k, p.v, far[1])
+    torch.cuda.synchronize()
+    assert torch.equal(far[1].contiguous(), p.out)
+    rope, turned = wkv.Rope(64), torch.empty_like(p.q)
+    wkv.wkv_rotate_prompt(p.prob, rope, p.q, None, turned, None)
+    wkv.wkv_rotate_prompt(p.prob, rope, far[0], None, far[0], None)
+    torch.cuda.synchronize()
+    assert torch.equal(far[0].contiguous(), turned)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with a workspace of its own: the same bits as one after the other."""
+    calls = [Attend("bf16", 8, 2, 128, 64, "pshd", [[5000, 4990], [2100, 700]], [40, 300], True),
+             Attend("bf16", 32, 8, 128, 64, "pshd", [[2000] * 8, [1500] * 8], [1, 1], False),
+             Attend("f32", 8, 2, 64, 16, "phsd", [[900, 899]], [7], False)]
+    prompts = [Prompt("bf16", 8, 2, 128, [2500], "bhnd", 4), Prompt("f32", 4, 2, 64, [700], "bhnd", 4)]
+    for a in calls + prompts:
+        a.run()
+    torch.cuda.synchronize()
+    alone = [[x.clone() for x in (a.out, a.lse)] + ([a.w_out.clone()] if isinstance(a, Attend) else []) for a in calls + prompts]
+    streams = [torch.cuda.Stream() for _ in calls + prompts]
+    for a in calls + prompts:
+        a.out.fill_(77.0)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for a, s in zip(calls + prompts, streams):
+            with torch.cuda.stream(s):
+                a.run()
+    torch.cuda.synchronize()
+    for a, want in zip(calls + prompts, alone):
+        for x, y in zip([a.out, a.lse] + ([a.w_out] if isinstance(a, Attend) else []), want):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_prompt_and_rotation_captured_and_replayed():
+    p = Prompt("bf16", 8, 2, 96, [700, 333], "packed", 8)
+    f = Prompt("f32", 4, 2, 64, [600], "bhnd", 8)
+    rope, turned = wkv.Rope(64), torch.empty_like(p.q)
+
+    def step():
+        wkv.wkv_rotate_prompt(p.prob, rope, p.q, None, turned, None)
+        wkv.wkv_attend_prompt(p.prob, turned, p.k, p.v, p.out, p.lse, p.lse_obs, p.status)
+        f.run()
+    step()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (turned, p.out, p.lse, p.lse_obs, f.out)]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        for x in (turned, p.out, f.out):
+            x.fill_(77.0)
+        for _ in range(3):
+            graph.replay()
+    torch.cuda.synchronize()
+    for x, y in zip((turned, p.out, p.lse, p.lse_obs, f.out), want):
+        assert torch.equal(x, y)
+    assert int(p.status) == 0
