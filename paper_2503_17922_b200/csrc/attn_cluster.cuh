@@ -89,10 +89,17 @@ __device__ __forceinline__ void cluster_join(const AttnArgs &a, const AttnSeq &s
     if (a.logits) {
         if ((int)threadIdx.x < n) {
             const int r = threadIdx.x;
-            float top = -INFINITY, sum = 0.f;
-            for (int s = 0; s < S; ++s) top = fmaxf(top, remote_float(in_block(ms + r * 4, s)));
+            float mm[kClusterSplits], ll[kClusterSplits], top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int s = 0; s < kClusterSplits; ++s) {                   // (all trips to the other blocks at once)
+                mm[s] = s < S ? remote_float(in_block(ms + r * 4, s)) : -INFINITY;
+                ll[s] = s < S ? remote_float(in_block(ls + r * 4, s)) : 0.f;
+                top = fmaxf(top, mm[s]);
+            }
             const float ref = top == -INFINITY ? 0.f : top;
-            for (int s = 0; s < S; ++s) sum += exp2f(remote_float(in_block(ms + r * 4, s)) - ref) * remote_float(in_block(ls + r * 4, s));
+#pragma unroll
+            for (int s = 0; s < kClusterSplits; ++s)
+                if (s < S) sum += exp2f(mm[s] - ref) * ll[s];
             lse2[r] = sum > 0.f || sum != sum ? top + log2f(sum) : -INFINITY;
         }
         __syncthreads();

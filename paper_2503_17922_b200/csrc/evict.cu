@@ -8,11 +8,16 @@
 #include "attn.cuh"
 #include "topk_block.cuh"
 
+#include <algorithm>
+
 namespace wkv {
 namespace {
 
 constexpr int kSelThreads = 1024;
 constexpr int kMoveThreads = 256;
+// Few rows are moved by the first kernel itself: up to so many, and so many vectors of 16 bytes in all.  (8 units of 992 rows, 4 layers, 9
+// rows to move 10.1 us with a second kernel, 8.4 without; 25 rows 10.4 and 9.3; 92 rows, 11.8 K vectors, 10.5 and 13.4.)
+constexpr int kFewMoves = 256, kFewVecs = 4096;
 constexpr int kHeldKeys = 48 * 1024;        // keys that a block holds in shared memory (192 KB); longer lists are re-read
 
 struct SelectSmem {
@@ -33,10 +38,14 @@ __device__ __forceinline__ unsigned evict_key(float w, bool is_recent, bool amon
     return w != w ? 1u : topk_order_key(w);
 }
 
-__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs a)
+// MOVES: the rows are moved here as well, without a second kernel
+template <bool MOVES>
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ PoolTable pools)
 {
     extern __shared__ unsigned held[];
     __shared__ SelectSmem sm;
+    __shared__ int2 few[MOVES ? kFewMoves : 1];
+    __shared__ longlong2 few_places[MOVES ? kFewMoves : 1];
     pdl_trigger();
     pdl_wait();
     const int unit = blockIdx.x, b = unit / a.hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -155,7 +164,8 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
         const unsigned threshold = none ? 0xffffffffu : prefix + lo;
         if (none) remaining = keep;
         // The rows in order, a part for each warp: which stay, and the two lists.  Three walks, with the warps' counts between them.
-        int2 *moves = a.moves + (long long)unit * a.moves_max;
+        int2 *moves = MOVES ? few : a.moves + (long long)unit * a.moves_max;
+        const int moves_max = MOVES ? kFewMoves : a.moves_max;
         const int per = ((n + 31) / 32 + 31) / 32 * 32, part0 = (int)min((long long)warp * per, (long long)n), part1 = (int)min((long long)part0 + per, (long long)n);
         const unsigned lower = (1u << lane) - 1u;
         int equal = 0, holes = 0, fills = 0;
@@ -188,15 +198,15 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
         holes = __reduce_add_sync(0xffffffffu, sm.holes[lane]);
         fills = __reduce_add_sync(0xffffffffu, sm.fills[lane]);
         walk([&](int j, unsigned out, unsigned in) {
-            if (out >> lane & 1u && hole + __popc(out & lower) < a.moves_max) moves[hole + __popc(out & lower)].x = j;
-            if (in >> lane & 1u && fill + __popc(in & lower) < a.moves_max) moves[fill + __popc(in & lower)].y = j;
+            if (out >> lane & 1u && hole + __popc(out & lower) < moves_max) moves[hole + __popc(out & lower)].x = j;
+            if (in >> lane & 1u && fill + __popc(in & lower) < moves_max) moves[fill + __popc(in & lower)].y = j;
             hole += __popc(out);
             fill += __popc(in);
         });
-        moved = min(min(holes, fills), a.moves_max);
+        moved = min(min(holes, fills), moves_max);
         __syncthreads();                               // the lists are complete (and the copies above)
         // (where the rows are, for the second kernel: its blocks would each look that up for every tensor)
-        longlong2 *places = a.places + (long long)unit * a.moves_max;
+        longlong2 *places = MOVES ? few_places : a.places + (long long)unit * a.moves_max;
         auto place = [&](int row) -> long long {
             const int pg = row / a.page_size, page = __ldg(a.table + (long long)b * a.max_pages + pg);
             if ((unsigned)page >= (unsigned)a.num_pages) return -1;
@@ -209,7 +219,17 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
             pos_out[mv.x] = pos[mv.y];
         }
     }
-    __syncthreads();                                   // lengths_out may be lengths: all have read it
+    __syncthreads();                                   // lengths_out may be lengths: all have read it (and the places are there)
+    if (MOVES) {
+        const int vecs = a.d * a.elem_bytes / 16, each = moved * vecs;
+        for (int x = tid; x < each * a.n_tensors; x += kSelThreads) {
+            const int tensor = x / each, y = x - tensor * each, move = y / vecs, v = y - move * vecs;
+            const longlong2 at = few_places[move];
+            if (at.x < 0 || at.y < 0) continue;
+            char *pool = static_cast<char *>(pools.ptr[tensor]);
+            reinterpret_cast<int4 *>(pool + at.x * a.elem_bytes)[v] = reinterpret_cast<const int4 *>(pool + at.y * a.elem_bytes)[v];
+        }
+    }
     if (tid == 0) {
         a.counts[unit] = moved;
         a.lengths_out[unit] = keep;
@@ -281,12 +301,19 @@ int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream
 {
     const int units = a.batch * a.hkv;
     const size_t smem = (size_t)(a.cap < kHeldKeys ? a.cap : kHeldKeys) * sizeof(unsigned);
-    cudaError_t err = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldKeys * 4);
-    if (err == cudaSuccess) err = launch_pdl(evict_select_kernel, dim3(units), kSelThreads, smem, stream, 1, a);
+    const int vecs = a.d * a.elem_bytes / 16;
+    // Rows that a unit can have to move: what the budget leaves over, as far as the host knows it.
+    long long most_moves = a.moves_max;
+    if (!a.budgets) most_moves = std::min(most_moves, (long long)std::min(a.budget, std::max(a.cap - a.budget, 0)));
+    const bool here = most_moves <= kFewMoves && most_moves * vecs * a.n_tensors <= kFewVecs;
+    static SmemAsked asked[2];
+    cudaError_t err = here ? allow_smem(evict_select_kernel<true>, kHeldKeys * 4, asked[1]) : allow_smem(evict_select_kernel<false>, kHeldKeys * 4, asked[0]);
+    if (err == cudaSuccess) err = here ? launch_pdl(evict_select_kernel<true>, dim3(units), kSelThreads, smem, stream, 1, a, pools)
+                                       : launch_pdl(evict_select_kernel<false>, dim3(units), kSelThreads, smem, stream, 1, a, pools);
     if (err != cudaSuccess) return check_cuda(err, "eviction kernel");
     count_launches(1);
+    if (here) return WKV_OK;
     int lanes_shift = 5;
-    const int vecs = a.d * a.elem_bytes / 16;
     while (lanes_shift > 2 && (1 << (lanes_shift - 1)) >= vecs) --lanes_shift;
     // several times as many blocks as the GPU holds (eight of 256 threads per SM), so that units of different lengths even out
     const long long pairs = (long long)units * a.n_tensors;
@@ -295,7 +322,7 @@ int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream
         return WKV_ERR_LIMIT;
     }
     long long slices = (148 * 64 + pairs - 1) / pairs;
-    const long long most = (a.moves_max + (kMoveThreads >> lanes_shift) - 1) / (kMoveThreads >> lanes_shift);
+    const long long rows = kAhead * (kMoveThreads >> lanes_shift), most = (most_moves + rows - 1) / rows;
     if (slices > most) slices = most;
     if (slices < 1) slices = 1;
     err = launch_pdl(evict_move_kernel, dim3((unsigned)pairs, (unsigned)slices), kMoveThreads, 0, stream, 1, a, pools, lanes_shift);

@@ -950,3 +950,32 @@ def test_prompt_and_rotation_captured_and_replayed():
     for x, y in zip((turned, p.out, p.lse, p.lse_obs, f.out), want):
         assert torch.equal(x, y)
     assert int(p.status) == 0
+
+
+@pytest.mark.parametrize("budget,layers,n", [(300, 1, 303), (290, 4, 320), (0, 2, 9), (1, 2, 9), (310, 8, 320), (250, 32, 255), (63, 1, 320)])
+def test_evict_few_rows(budget, layers, n):
+    """With few rows to move, by the budget and the table's size, they are moved without a second kernel: the same as by one of its own.
+    With a budget per sequence, whose numbers the host does not see, only the table's size counts."""
+    g = gen(31)
+    c = ou.Cache(g, torch.bfloat16, 2, 2, 64, 16, 20, "phsd", layers=layers)
+    lengths = [[n, max(n - 3, 0)], [min(budget, n), n // 2]]
+    c.fill(g, lengths)
+    c.table[1, 0] = -1
+    cache = paged(c, 4, 1)
+    ws = cache.alloc_workspace()
+    w = torch.rand((2, 2, c.cap), generator=g).cuda()
+    p = torch.randperm(c.cap, generator=g).to(torch.int32).cuda().expand(2, 2, -1).contiguous()
+    lens = torch.tensor(lengths, dtype=torch.int32).cuda()
+    results, launches = [], []
+    for budgets in (None, torch.full((2,), budget, dtype=torch.int32, device="cuda")):
+        k, v = [x.clone() for x in c.k], [x.clone() for x in c.v]
+        w1, p1, n1 = w.clone(), p.clone(), lens.clone()
+        before = wkv.lib().wkv_launch_count()
+        wkv.wkv_evict_kv_paged(cache, k, v, w1, p1, n1, budget if budgets is None else 0, 5, w1, p1, n1, ws, budgets=budgets)
+        launches.append(wkv.lib().wkv_launch_count() - before)
+        torch.cuda.synchronize()
+        results.append(k + v + [w1, p1, n1])
+    for x, y in zip(*results):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    most = [min(budget, c.cap - budget), c.cap // 2 + 1]
+    assert launches == [1 if x <= 256 and x * 8 * 2 * layers <= 4096 else 2 for x in most]
