@@ -18,7 +18,7 @@
 // get them added at the end.
 //
 // Bound by the chain of one query tile, product - weights - product, of which two are in flight (tensor memory holds no third): 32 heads on 8 of 8,192
-// tokens, d = 128, 570 us = 0.96 PFLOP/s, tensor pipe 51 % of cycles, special functions 45 %; 32,768 tokens 8.1 ms = 1.08 PFLOP/s
+// tokens, d = 128, 550 us = 1.0 PFLOP/s, tensor pipe 51 % of cycles, special functions 45 %; 32,768 tokens 8.2 ms = 1.07 PFLOP/s
 // and the power limit.  Of a chain's 4,000 cycles the weights take 2,500, the products 1,100.  Sixteen warps for the weights, two
 // to a row, were slower (600 us): they have to agree on the maximum.
 //
