@@ -3,8 +3,10 @@
 // pages of sizes that eight does not divide).
 //
 // A block of four warps walks over the keys of one unit (or a split of them) in tiles of 64, which come through a ring of
-// asynchronous 16-byte copies: two or three tiles are in flight while one is worked on.  Rows (position x head of the group) sit
-// on the M side of the instruction:
+// asynchronous 16-byte copies: one tile is in flight while another is worked on (three for d up to 64).  What keeps memory busy
+// is three blocks per SM: 32 sequences of 4-8 K rows, one token of 32 heads on 8, with weights, 155 us with two tiles in the ring
+// and 187 with a deeper one and two blocks; the kernel itself reads 5.6 TB/s.  Rows (position x head of the group) sit on the M
+// side of the instruction:
 //   FEW    up to 16 rows, all in every warp; a warp takes 16 of the tile's keys and keeps a maximum and a sum of its own, joined
 //          once at the end
 //   else   64 rows, 16 per warp, every warp takes all keys

@@ -16,7 +16,7 @@ namespace {
 constexpr int kSelThreads = 1024;
 constexpr int kMoveThreads = 256;
 // Few rows are moved by the first kernel itself: up to so many, and so many vectors of 16 bytes in all.  (8 units of 992 rows, 4 layers, 9
-// rows to move 10.1 us with a second kernel, 8.4 without; 25 rows 10.4 and 9.3; 92 rows, 11.8 K vectors, 10.5 and 13.4.)
+// rows to move 10.1 us with a second kernel, 8.7 without; 25 rows 10.4 and 9.5; 92 rows, 11.8 K vectors, 10.5 and 13.4.)
 constexpr int kFewMoves = 256, kFewVecs = 4096;
 constexpr int kHeldKeys = 48 * 1024;        // keys that a block holds in shared memory (192 KB); longer lists are re-read
 
