@@ -7,7 +7,7 @@
 // Each thread reads what it writes, so an output may be its input.
 //
 // Bound by memory: 32,768 tokens of 40 rows of 128 in bf16, 64 of each turned, take 114 us, 5.9 TB/s read and written, and 118 us
-// with all 128 turned in HALF order.  Two rows in flight per thread leave room for seven or eight blocks per SM; four rows (half as
+// with all 128 turned in HALF order; 8,192 tokens 32 us, with 62 turned 34, and in HALF order, element by element, 59.  Two rows in flight per thread leave room for seven or eight blocks per SM; four rows (half as
 // many blocks) took 128 us, one 122; four tokens per block: eight took 117.  When each thread worked out its own addresses,
 // piece by piece, the divisions and strides took as long as the memory (186 us).
 #include "attn.cuh"
@@ -16,7 +16,6 @@ namespace wkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 2;                // rows that a thread has in flight
 constexpr int kMaxPairs = 2048;          // rot/2 at most, per block: cosines and sines in shared memory (16 KB)
 
 __device__ __forceinline__ float to_float(float x) { return x; }
@@ -77,13 +76,14 @@ struct Row {
 
 // The rows of a block's tokens are listed in shared memory, one per thread and kThreads at a time: the divisions, the strides
 // and the look-up of the page are done once for a row, not once for each of its pieces.  A thread keeps to one piece of the rows and
-// takes them kBatch at a time, loads first.  Pieces of a row: HALF order: half / VEC pairs of vectors; INTERLEAVED: rot / VEC
-// vectors of pairs (rot / 2 pairs of elements if VEC = 1); then the rest, copied.  VEC is the largest of which the two halves, or
-// the turned part, are whole multiples.
-// PAIRS: vectors of whole pairs, one to a piece
-template <typename T, int VEC, bool PAIRS>
+// takes a few at a time, loads first.  Pieces of a row:
+//   PAIRS (INTERLEAVED order)  16-byte vectors, whose pairs from rot on stay as they are
+//   else (HALF order)          half / VEC pairs of vectors, VEC the largest of which a half is a multiple; from rot on single vectors of
+//                              VEC as far as the next 16 bytes, then 16-byte vectors
+template <typename T, int VEC, bool PAIRS, bool TAIL = false>      // TAIL: the turned part ends inside a vector of pairs
 __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a, int tokens_per_block, long long tokens)
 {
+    constexpr int kWide = 16 / sizeof(T), kBatch = VEC > 1 ? 2 : 4;       // rows in flight
     __shared__ __align__(16) float2 turn[kMaxPairs];
     __shared__ Row list[kThreads];
     __shared__ int list_token[kThreads];
@@ -116,8 +116,9 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         sincospif((float)(int)(angle >> 32) * (1.f / 2147483648.f), &sine, &cosine);      // angle in half turns, -1 .. 1
         turn[x] = make_float2(cosine * a.scale, sine * a.scale);
     }
-    const bool inter = a.order == WKV_ROPE_INTERLEAVED;
-    const int turned = PAIRS ? rot / VEC : half / VEC, pieces = turned + (a.d - rot) / VEC;
+    const int turned = PAIRS ? (rot + VEC - 1) / VEC : half / VEC, wide_from = (rot + kWide - 1) / kWide * kWide;
+    const int single = PAIRS ? 0 : (wide_from - rot) / VEC;                       // vectors of VEC behind the turned part
+    const int pieces = PAIRS ? a.d / VEC : turned + single + (a.d - wide_from) / kWide;
     const int hq = a.q ? a.hq : 0, hk = a.k ? a.hkv : 0, hv = a.v ? a.hkv : 0, rows = hq + hk + hv;
     const int width = min(pieces, kThreads), step = kThreads / width, slot = threadIdx.x / width;
     for (int y0 = 0; y0 < n * rows; y0 += kThreads) {
@@ -163,11 +164,14 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
         if (slot < step)
             for (int piece = threadIdx.x - slot * width; piece < pieces; piece += width) {
                 const bool turns = piece < turned;
-                const int j = !turns ? rot + (piece - turned) * VEC : (PAIRS || !inter ? piece * VEC : 2 * piece);
-                const int k = inter ? j + 1 : j + half;                       // the second vector of a pair
+                const bool wide = !PAIRS && piece >= turned + single;
+                const int j = PAIRS || turns ? piece * VEC : (wide ? wide_from + (piece - turned - single) * kWide : rot + (piece - turned) * VEC);
+                const int k = j + half;                                          // the second vector of a pair
                 const float2 *tr = turn + (PAIRS ? piece * (VEC / 2) : piece * VEC);
                 for (int x0 = slot; x0 < listed; x0 += step * kBatch) {
                     Vec<T, VEC> first[kBatch], second[PAIRS ? 1 : kBatch];
+                    Vec<T, kWide> whole[PAIRS || VEC == kWide ? 1 : kBatch];
+                    constexpr bool kOther = !PAIRS && VEC != kWide;              // wide vectors are of another size
                     T *dst[kBatch];
                     int w[kBatch];
 #pragma unroll
@@ -180,18 +184,27 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
                         dst[u] = static_cast<T *>(list[x].dst);
                         w[u] = list_token[x];
                         if (!dst[u]) continue;
+                        if (kOther && wide) {
+                            whole[kOther ? u : 0].load(src + j);
+                            continue;
+                        }
                         first[u].load(src + j);
                         if (!PAIRS && turns) second[PAIRS ? 0 : u].load(src + k);
                     }
 #pragma unroll
                     for (int u = 0; u < kBatch; ++u) {
                         if (!dst[u]) continue;
+                        if (kOther && wide) {
+                            whole[kOther ? u : 0].store(dst[u] + j);
+                            continue;
+                        }
                         if (turns && w[u] >= 0) {
                             const float2 *cs = tr + w[u] * half;
 #pragma unroll
                             for (int e = 0; e < VEC; e += PAIRS ? 2 : 1) {
                                 Vec<T, VEC> &to = PAIRS ? first[u] : second[PAIRS ? 0 : u];
                                 constexpr int kNext = PAIRS ? 1 : 0;
+                                if (PAIRS && TAIL && piece * VEC + e >= rot) break;
                                 const float2 t = cs[PAIRS ? e / 2 : e];
                                 const float p = first[u].get(e), q = to.get(e + kNext);
                                 first[u].set(e, p * t.x - q * t.y);
@@ -226,14 +239,12 @@ int launch(const RopeArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)(blocks > 0 ? blocks : 1));
-    // vectors must end where the turned part does, and in HALF order where its first half does
-    const bool pairs = a.order == WKV_ROPE_INTERLEAVED;
-    const int part = pairs ? 2 * half : half;
     auto go = [&](auto kernel) { return launch_pdl(kernel, grid, kThreads, 0, stream, 1, a, (int)per, tokens); };
     cudaError_t err;
-    if (part % kVec == 0) err = pairs ? go(rope_kernel<T, kVec, true>) : go(rope_kernel<T, kVec, false>);
-    else if (part % (kVec / 2) == 0) err = pairs ? go(rope_kernel<T, kVec / 2, true>) : go(rope_kernel<T, kVec / 2, false>);
-    else if (part % 2 == 0) err = pairs ? go(rope_kernel<T, 2, true>) : go(rope_kernel<T, 2, false>);
+    if (a.order == WKV_ROPE_INTERLEAVED) err = (2 * half) % kVec ? go(rope_kernel<T, kVec, true, true>) : go(rope_kernel<T, kVec, true>);
+    else if (half % kVec == 0) err = go(rope_kernel<T, kVec, false>);
+    else if (half % (kVec / 2) == 0) err = go(rope_kernel<T, kVec / 2, false>);
+    else if (half % 2 == 0) err = go(rope_kernel<T, 2, false>);
     else err = go(rope_kernel<T, 1, false>);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "rotary positions kernel");

@@ -979,3 +979,34 @@ def test_evict_few_rows(budget, layers, n):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
     most = [min(budget, c.cap - budget), c.cap // 2 + 1]
     assert launches == [1 if x <= 256 and x * 8 * 2 * layers <= 4096 else 2 for x in most]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("order", ["half", "interleaved"])
+@pytest.mark.parametrize("d,rot", [(72, 2), (72, 62), (72, 66), (72, 70), (72, 72), (40, 36), (128, 120), (128, 126), (8, 6)])
+def test_rotate_odd_parts_leave_the_rest_alone(dtype, order, d, rot):
+    """Turned parts that end inside 16 bytes: infinities and NaN in the rest and beside it come out as they are, and the turned
+    part is, in bits, what it is in a head that ends with it."""
+    p = Prompt(dtype, 3, 1, d, [37], "bhnd", 4)
+    p.q[..., rot:] = INF
+    if rot + 1 < d:
+        p.q[..., rot + 1] = NAN
+    rope = wkv.Rope(rot, 10000.0, order=order)
+    turned = torch.full_like(p.q, 77.0)
+    wkv.wkv_rotate_prompt(p.prob, rope, p.q, None, turned, None)
+    torch.cuda.synchronize()
+    if rot < d:
+        assert torch.equal(turned[..., rot:].contiguous().view(torch.uint8), p.q[..., rot:].contiguous().view(torch.uint8))
+    angle = torch.arange(37, dtype=torch.float64).view(-1, 1) * torch.tensor(ou.frequencies(rot, 10000.0, "none", 1.0, 0.0), dtype=torch.float64)
+    cos, sin = torch.cos(angle).cuda(), torch.sin(angle).cuda()
+    x = p.q[..., :rot].double()
+    a, b = (x[..., : rot // 2], x[..., rot // 2:]) if order == "half" else (x[..., 0::2], x[..., 1::2])
+    u, v = a * cos - b * sin, b * cos + a * sin
+    want = torch.cat([u, v], -1) if order == "half" else torch.stack([u, v], -1).flatten(-2)
+    size = torch.cat([a.abs() + b.abs()] * 2, -1) if order == "half" else torch.stack([a.abs() + b.abs()] * 2, -1).flatten(-2)
+    # sine and cosine from an angle of 32 bits (2^-31 of half a turn, times pi) and their own rounding (2 units), the products' and the sum's
+    bound = size * (2.0 ** -29 + 4 * 2.0 ** -24) + (want.abs() * 2.0 ** -8 if dtype == "bf16" else 0)
+    ou.assert_close(turned[..., :rot], want, bound, "turned part")
+    wkv.wkv_rotate_prompt(p.prob, rope, p.q, None, p.q, None)
+    torch.cuda.synchronize()
+    assert torch.equal(p.q.view(torch.uint8), turned.view(torch.uint8))
