@@ -7,9 +7,10 @@
 // Each thread reads what it writes, so an output may be its input.
 //
 // Bound by memory: 32,768 tokens of 40 rows of 128 in bf16, 64 of each turned, take 114 us, 5.9 TB/s read and written, and 118 us
-// with all 128 turned in HALF order; 8,192 tokens 32 us, with 62 turned 34, and in HALF order, element by element, 59.  Two rows in flight per thread leave room for seven or eight blocks per SM; four rows (half as
-// many blocks) took 128 us, one 122; four tokens per block: eight took 117.  When each thread worked out its own addresses,
-// piece by piece, the divisions and strides took as long as the memory (186 us).
+// with all 128 turned in HALF order; 8,192 tokens 32 us, with 62 turned 34, and in HALF order, element by element, 59.  Two rows
+// in flight per thread leave room for seven or eight blocks per SM; four rows (half as many blocks) took 128 us, one 122; four
+// tokens per block: eight took 117.  When each thread worked out its own addresses, piece by piece, the divisions and strides took
+// as long as the memory (186 us).
 #include "attn.cuh"
 
 namespace wkv {
