@@ -929,8 +929,9 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
         }
 #pragma unroll
         for (int k = 0; k < RPW; ++k) {
-            const float f = ml[k].y == 0.f ? 0.f : exp2f(ml[k].x - (top[k] == -INFINITY ? 0.f : top[k]));
-            if (f == 0.f) continue;
+            // (only a piece without weight is left out: with a factor of 0, NaN in its sum and infinities in its output still count)
+            if (ml[k].y == 0.f) continue;
+            const float f = exp2f(ml[k].x - (top[k] == -INFINITY ? 0.f : top[k]));
             l[k] += f * ml[k].y;
             o[k].x = fmaf(f, p[k].x, o[k].x);
             o[k].y = fmaf(f, p[k].y, o[k].y);

@@ -1,0 +1,84 @@
+"""GPU tests of what infinities, NaN and rows without weight do in the attention kernels: the same in every one of them, whichever the
+sizes lead to."""
+import pytest
+import torch
+
+import operators_util as ou
+from test_gpu_operators import Attend, INF, NAN, Prompt, tokens_of
+
+pytestmark = pytest.mark.gpu
+
+# A call over the paged cache for each kernel and each way of joining key splits
+PAGED = {
+    "tcgen05-shared-items": ("bf16", 8, 2, 128, 64, "phsd", [[4000, 3990]], [40], False),
+    "tcgen05-shared-items-160": ("bf16", 32, 8, 128, 64, "phsd", [[2200] * 8] * 20, [9] * 20, False),
+    "tcgen05": ("bf16", 8, 2, 128, 64, "phsd", [[1500, 1490]], [40], False),
+    "warps-cluster": ("bf16", 8, 2, 128, 16, "phsd", [[992, 990]], [3], False),
+    "warps-splits": ("bf16", 8, 2, 128, 64, "phsd", [[16000, 15990]], [3], False),
+    "warps-many-rows": ("bf16", 8, 2, 128, 13, "phsd", [[1500, 1490]], [40], False),
+    "fp32-cluster": ("f32", 4, 2, 64, 16, "phsd", [[700, 690]], [3], False),
+    "fp32-splits": ("f32", 4, 2, 64, 16, "phsd", [[9000, 8990]], [3], False),
+    "fp32-many-rows": ("f32", 4, 2, 64, 16, "phsd", [[1500, 1490]], [40], False),
+}
+# ... and a prompt (n tokens)
+PROMPTS = {
+    "tcgen05": ("bf16", 8, 2, 128, [700]),
+    "tcgen05-64": ("bf16", 4, 2, 64, [700]),
+    "warps": ("bf16", 4, 2, 128, [100]),
+    "fp32-one-tile": ("f32", 4, 2, 64, [40]),
+    "fp32-cluster": ("f32", 4, 2, 64, [300]),
+}
+paged_calls = pytest.mark.parametrize("name", PAGED)
+prompts = pytest.mark.parametrize("name", PROMPTS)
+
+
+def unit_rows(a, h=0):
+    return min(int(a.lengths[0, h]), a.c.cap)
+
+
+def set_rows(a, pool, h, rows, value, column=slice(None)):
+    """Elements of rows of unit (0, h)."""
+    pages, slots = a.c.table[0].long()[rows // a.c.page], (rows % a.c.page).cuda()
+    pool[pages, h, slots, column] = value
+
+
+def same_bits(x, y):
+    kind = {2: torch.int16, 4: torch.int32}[x.element_size()]
+    return torch.equal(x.contiguous().view(kind), y.contiguous().view(kind))
+
+
+# ---- NaN among the queries and the keys ------------------------------------------------------
+@paged_calls
+def test_a_nan_query_gives_nan(name):
+    """Its own row alone, and not the 0 and -infinity of a query that has nothing to attend to."""
+    a = Attend(*PAGED[name])
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    out, lse = a.out.clone(), a.lse.clone()
+    i = a.max_new // 2
+    a.q[0, 1, i, 5] = NAN
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    assert torch.isnan(a.out[0, 1, i]).all() and torch.isnan(a.lse[0, 1, i])
+    a.out[0, 1, i], a.lse[0, 1, i] = out[0, 1, i], lse[0, 1, i]
+    assert same_bits(a.out, out) and same_bits(a.lse, lse)
+
+
+@paged_calls
+@pytest.mark.parametrize("part", ["first", "middle"])
+def test_a_stretch_of_nan_keys_gives_nan(name, part):
+    """NaN in all keys of a stretch of whole key tiles, all that some blocks have: every query that sees them is NaN."""
+    a = Attend(*PAGED[name])
+    n = unit_rows(a)
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    out, lse = a.out.clone(), a.lse.clone()
+    first = 0 if part == "first" else n // 4 // 128 * 128
+    rows = torch.arange(first, first + n // 3 // 128 * 128)
+    set_rows(a, a.c.k[0], 0, rows, NAN)
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    G = a.hq // a.hk
+    assert torch.isnan(a.out[0, :G]).all() and torch.isnan(a.lse[0, :G]).all()
+    a.out[0, :G], a.lse[0, :G] = out[0, :G], lse[0, :G]
+    assert same_bits(a.out, out) and same_bits(a.lse, lse)
