@@ -463,7 +463,8 @@ int wkv_rotate_prompt(const wkv_shape *s, const wkv_rope *rope, const void *q, v
  *   lse_obs    DEVICE out or NULL, float [B, H_q, alpha]: the same of the observation rows, as wkv_score_windows_lse and the
  *              others take it; -infinity where the sequence has fewer than alpha tokens and the row does not exist
  *   status     DEVICE int32 or NULL, OR-ed with 1 if a bounded wait inside the kernel expired (the outputs are invalid then)
- * What stands in K or V behind a row's position (infinities and NaN included) does not reach the row.  head_dim up to 256.
+ * What stands in K or V behind a row's position (infinities and NaN included) does not reach the row.  An infinity or NaN in a value
+ * that it does attend to leaves one in its output, however small the weight.  head_dim up to 256.
  */
 int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_strides, const void *k, const void *v, void *out,
                       const int64_t *out_strides, float *lse, float *lse_obs, int32_t *status, void *cuda_stream);
@@ -522,7 +523,8 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
  *   weights_out    DEVICE out or NULL, float [same]: weights_in plus the weight that the row has received from the new tokens of all
  *                  query heads of its group (the sum of the softmax entries of its column); may be weights_in; entries from
  *                  the unit's length on are not written
- * What stands in rows that a query does not attend to does not reach it.  head_dim up to 256.
+ * What stands in rows that a query does not attend to does not reach it.  An infinity or NaN in a value that it does attend to leaves one
+ * in its output, however small the weight.  head_dim up to 256.
  */
 int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides, const void *k_pool, const void *v_pool,
                      const int32_t *lengths, void *out, const int64_t *out_strides, float *lse, const float *weights_in,

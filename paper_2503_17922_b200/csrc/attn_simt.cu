@@ -447,7 +447,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs &a, JoinSmem &sm, const
             for (int y = threadIdx.x; y < n * parts; y += kThreads) {
                 const int fr = y / parts, fs = y - fr * parts;
                 const float2 ml = a.part_ml[((long long)unit * a.rows_max + row0 + fr) * a.splits + s0 + fs];
-                sm.factor[fr][fs] = ml.y == 0.f ? 0.f : exp2f(ml.x - sm.top[fr]);       // (a part without a key of the row has no output)
+                sm.factor[fr][fs] = ml.y == 0.f ? -1.f : exp2f(ml.x - sm.top[fr]);      // -1: a part without weight, which has no output
             }
             __syncthreads();
             if (x >= n * cols) continue;
@@ -456,7 +456,8 @@ __device__ __forceinline__ void join_rows(const AttnArgs &a, JoinSmem &sm, const
             for (int s = 0; s < parts; ++s) {
                 const float f = sm.factor[r][s];
                 float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (f != 0.f) p = *reinterpret_cast<const float4 *>(from + (long long)s * a.d);
+                // (a factor of 0 does not leave a part out: an infinity or NaN in its output counts)
+                if (!(f < 0.f)) p = *reinterpret_cast<const float4 *>(from + (long long)s * a.d);
                 o.x = fmaf(f, p.x, o.x);
                 o.y = fmaf(f, p.y, o.y);
                 o.z = fmaf(f, p.z, o.z);

@@ -82,3 +82,27 @@ def test_a_stretch_of_nan_keys_gives_nan(name, part):
     assert torch.isnan(a.out[0, :G]).all() and torch.isnan(a.lse[0, :G]).all()
     a.out[0, :G], a.lse[0, :G] = out[0, :G], lse[0, :G]
     assert same_bits(a.out, out) and same_bits(a.lse, lse)
+
+
+# ---- infinities among values that are seen --------------------------------------------------------
+@paged_calls
+def test_an_infinity_in_a_row_of_tiny_weight_counts(name):
+    """The first half's logits are so low that their weights are 0 in fp32: an infinity or NaN among their values still leaves one (0 times it
+    is NaN), wherever the keys are split."""
+    a = Attend(*PAGED[name])
+    n, G, d = unit_rows(a), a.hq // a.hk, a.c.d
+    a.q[:] = a.q.sign() * 0.5 + 1.0                                  # 0.5 or 1.5
+    set_rows(a, a.c.k[0], 0, torch.arange(0, n // 2), -32.0)         # logits of -16 sqrt(d) and below, those of the others of the order of 1
+    a.run()
+    torch.cuda.synchronize()
+    out, lse, w = a.out.clone(), a.lse.clone(), a.w_out.clone()
+    assert torch.isfinite(out).all()
+    set_rows(a, a.c.v[0], 0, torch.tensor([5]), INF, 3)
+    set_rows(a, a.c.v[0], 0, torch.tensor([n // 4]), -INF, 4)
+    set_rows(a, a.c.v[0], 0, torch.tensor([n // 2 - 1]), NAN, 6)
+    a.run()
+    torch.cuda.synchronize()
+    assert not torch.isfinite(a.out[0, :G][..., [3, 4]]).any() and torch.isnan(a.out[0, :G, :, 6]).all()
+    for c in (3, 4, 6):
+        a.out[0, :G, :, c] = out[0, :G, :, c]
+    assert same_bits(a.out, out) and same_bits(a.lse, lse) and same_bits(a.w_out, w)
