@@ -273,8 +273,8 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
             }
         }
         __syncwarp();                                                    // a row's 16 threads are in one warp
-        // what stands behind a row's position may be infinite or NaN: 0 times it is not 0
-        auto product = [&](auto skip_zeros) {
+        // what stands behind a row's position may be infinite or NaN: 0 times it is not 0 (rows without a page are zeros)
+        auto product = [&](auto skip_unseen) {
 #pragma unroll 2
             for (int j = 0; j < kKeys; j += 4) {
                 float4 pp[RT];
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
                         const float p = e == 0 ? pp[r].x : (e == 1 ? pp[r].y : (e == 2 ? pp[r].z : pp[r].w));
-                        if (decltype(skip_zeros)::value && p == 0.f) continue;
+                        if (decltype(skip_unseen)::value && j0 + j + e >= limit[r]) continue;
                         const unsigned long long p2 = pair_of(p, p);
 #pragma unroll
                         for (int x = 0; x < CT; ++x) {

@@ -106,3 +106,23 @@ def test_an_infinity_in_a_row_of_tiny_weight_counts(name):
     for c in (3, 4, 6):
         a.out[0, :G, :, c] = out[0, :G, :, c]
     assert same_bits(a.out, out) and same_bits(a.lse, lse) and same_bits(a.w_out, w)
+
+
+@prompts
+def test_an_infinity_in_a_prompt_row_of_tiny_weight_counts(name):
+    p = Prompt(*PROMPTS[name])
+    n = p.lens[0]
+    p.q[:] = p.q.sign() * 0.5 + 1.0
+    for row in (5, 17):
+        p.k[0, 0, row] = -32.0
+    p.run()
+    torch.cuda.synchronize()
+    out, G = p.out.clone(), p.hq // p.hk
+    assert torch.isfinite(out).all()
+    p.v[0, 0, 5, 3], p.v[0, 0, 17, 4] = INF, NAN
+    p.run()
+    torch.cuda.synchronize()
+    assert not torch.isfinite(p.out[0, :G, 5:, 3]).any() and torch.isnan(p.out[0, :G, 17:, 4]).all()
+    assert same_bits(p.out[0, :G, :5], out[0, :G, :5]) and same_bits(p.out[0, :G, :17, 4], out[0, :G, :17, 4])
+    rest = [c for c in range(p.d) if c not in (3, 4)]
+    assert same_bits(p.out[0, :G][..., rest], out[0, :G][..., rest]) and same_bits(p.out[0, G:], out[0, G:])
