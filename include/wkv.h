@@ -464,7 +464,8 @@ int wkv_rotate_prompt(const wkv_shape *s, const wkv_rope *rope, const void *q, v
  *              others take it; -infinity where the sequence has fewer than alpha tokens and the row does not exist
  *   status     DEVICE int32 or NULL, OR-ed with 1 if a bounded wait inside the kernel expired (the outputs are invalid then)
  * What stands in K or V behind a row's position (infinities and NaN included) does not reach the row.  An infinity or NaN in a value
- * that it does attend to leaves one in its output, however small the weight.  head_dim up to 256.
+ * that it does attend to leaves one in its output, however small the weight.  A row of logits of -infinity gives 0 and -infinity.
+ * head_dim up to 256.
  */
 int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_strides, const void *k, const void *v, void *out,
                       const int64_t *out_strides, float *lse, float *lse_obs, int32_t *status, void *cuda_stream);
@@ -515,7 +516,8 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
 
 /*
  * Attention of the new tokens over the cache, their own rows (the last ones) included: with n = lengths[b][h] rows and m new tokens,
- * query i attends to rows 0 .. n - m + i of its unit.  A query that has no row to attend to gives 0 and -infinity.
+ * query i attends to rows 0 .. n - m + i of its unit.  A query that has no row to attend to, or only logits of -infinity, gives 0 and
+ * -infinity.
  *   q, out         DEVICE  [B, H_q, max_new, d] or packed [T, H_q, d], strides as for q above
  *   lengths        DEVICE int32 [B, H_kv]: rows of every unit, new tokens included
  *   lse            DEVICE out or NULL, float [B, H_q, max_new]; entries behind a sequence's new tokens are not written

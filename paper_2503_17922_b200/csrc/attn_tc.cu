@@ -303,13 +303,13 @@ __device__ __forceinline__ void hide(float (&v)[32], uint32_t seen)
 
 // 2^x of two values on the FMA pipe, which is half idle where the special functions are not (32 heads of 8,192 tokens: none 546 us, one
 // pair in eight 499, in four 507, in two 599): 2^t * 2^f with t the nearest integer, 2^f by a polynomial of degree five (a Remez fit of the
-// relative error on [-1/2, 1/2], 7.5e-8; evaluated in fp32 2.1e-7).  x is at most kLazy; below -126 it counts as -126, so
-// that a weight of 0 comes out as 1e-38 (rows that see nothing of a tile do not come here); a NaN stays one.
+// relative error on [-1/2, 1/2], 7.5e-8; evaluated in fp32 2.1e-7).  x is at most kLazy; below -127 it counts as -127,
+// whose factor 2^t is 0, so that the weight is 0 below -126.5, as with the special functions; a NaN stays one.
 __device__ __forceinline__ unsigned long long exp2_pair_fma(unsigned long long x2)
 {
     float2 x = halves_of(x2);
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(x.x));      // -126
-    asm("max.NaN.f32 %0, %0, 0fC2FC0000;" : "+f"(x.y));
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.x));      // -127
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.y));
     auto both = [](float v) { return pair_of(v, v); };
     x2 = pair_of(x.x, x.y);
     const unsigned long long shifted = add_pair(x2, both(12582912.f));            // 1.5 * 2^23: the integer is in the low bits

@@ -126,3 +126,47 @@ def test_an_infinity_in_a_prompt_row_of_tiny_weight_counts(name):
     assert same_bits(p.out[0, :G, :5], out[0, :G, :5]) and same_bits(p.out[0, :G, :17, 4], out[0, :G, :17, 4])
     rest = [c for c in range(p.d) if c not in (3, 4)]
     assert same_bits(p.out[0, :G][..., rest], out[0, :G][..., rest]) and same_bits(p.out[0, G:], out[0, G:])
+
+
+# ---- rows whose logits are all -infinity --------------------------------------------------------------
+BELOW = 3.0e38               # times 3e4: beyond fp32, in whatever order the products are summed
+
+
+@prompts
+def test_a_prompt_row_of_logits_minus_infinity_is_zero(name):
+    """No weight anywhere: 0 and -infinity, as for a row that has nothing to attend to."""
+    p = Prompt(*PROMPTS[name])
+    n, G = p.lens[0], p.hq // p.hk
+    p.k[0, 0, :, 0], p.q[0, :G, :, 0] = -BELOW, 0.0
+    p.run()
+    torch.cuda.synchronize()
+    out, lse = p.out.clone(), p.lse.clone()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    rows = [0, n // 2, n - 1]
+    for i in rows:
+        p.q[0, 0, i, 0] = 3.0e4
+    p.run()
+    torch.cuda.synchronize()
+    for i in rows:
+        assert (p.out[0, 0, i] == 0).all() and p.lse[0, 0, i] == -INF
+        p.out[0, 0, i], p.lse[0, 0, i] = out[0, 0, i], lse[0, 0, i]
+    assert same_bits(p.out, out) and same_bits(p.lse, lse)
+
+
+@paged_calls
+def test_a_query_of_logits_minus_infinity_is_zero(name):
+    a = Attend(*PAGED[name])
+    n, G = unit_rows(a), a.hq // a.hk
+    set_rows(a, a.c.k[0], 0, torch.arange(n), -BELOW, 0)
+    a.q[0, :G, :, 0] = 0.0
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    out, lse = a.out.clone(), a.lse.clone()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    i = a.max_new // 2
+    a.q[0, 1, i, 0] = 3.0e4
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    assert (a.out[0, 1, i] == 0).all() and a.lse[0, 1, i] == -INF
+    a.out[0, 1, i], a.lse[0, 1, i] = out[0, 1, i], lse[0, 1, i]
+    assert same_bits(a.out, out) and same_bits(a.lse, lse)
