@@ -487,7 +487,8 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) attn_mma_weights_kerne
             for (int y = 0; y < 2; ++y) {
                 const int r = g + y * 8 + ql * 2;
                 const float2 lse = *reinterpret_cast<const float2 *>(&sm.lse[st][r]);
-                const float ref[2] = {lse.x * 1.44269504088896341f, lse.y * 1.44269504088896341f};
+                // (a row of logits of -infinity has no weight: infinity in the place of its normaliser)
+                const float ref[2] = {lse.x == -INFINITY ? INFINITY : lse.x * 1.44269504088896341f, lse.y == -INFINITY ? INFINITY : lse.y * 1.44269504088896341f};
                 const int2 limit = masked ? *reinterpret_cast<const int2 *>(&sm.limit[st][r]) : make_int2(INT_MAX, INT_MAX);
 #pragma unroll
                 for (int f = 0; f < F; ++f)

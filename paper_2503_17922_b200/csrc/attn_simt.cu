@@ -384,6 +384,7 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
             const int row = row0 + ty * RT + r, i = row / a.G, hq = h * a.G + row - i * a.G;
             if (row >= rows) continue;
             const float lse2 = a.lse[((long long)b * a.hq + hq) * a.max_q + i] * 1.44269504088896341f;
+            if (lse2 == -INFINITY) continue;                             // nothing to attend to, or logits of -infinity alone
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (j0 + tx + 16 * j < base + i && sm.present[tx + 16 * j]) got[j] += exp2f(s[r][j] - lse2);

@@ -170,3 +170,25 @@ def test_a_query_of_logits_minus_infinity_is_zero(name):
     assert (a.out[0, 1, i] == 0).all() and a.lse[0, 1, i] == -INF
     a.out[0, 1, i], a.lse[0, 1, i] = out[0, 1, i], lse[0, 1, i]
     assert same_bits(a.out, out) and same_bits(a.lse, lse)
+
+
+@paged_calls
+def test_a_query_of_logits_minus_infinity_leaves_no_weight(name):
+    """The weights are those of the other queries."""
+    a = Attend(*PAGED[name])
+    n, G, m = unit_rows(a), a.hq // a.hk, a.max_new
+    set_rows(a, a.c.k[0], 0, torch.arange(n), -BELOW, 0)
+    a.q[0, :G, :, 0] = 0.0
+    i = m // 2
+    k, ok = a.c.rows(a.c.k[0], 0, 0, n)
+    v, _ = a.c.rows(a.c.v[0], 0, 0, n)
+    others = torch.tensor([g * m + j for g in range(G) for j in range(m) if (g, j) != (1, i)], device="cuda")
+    qs = tokens_of(a.q, 0, a.news, a.packed)[:, :G].transpose(0, 1).reshape(G * m, -1)[others]
+    _, _, p, bd = ou.attention(qs, k, v, torch.arange(n - m + 1, n + 1, device="cuda").repeat(G)[others], ok)
+    a.q[0, 1, i, 0] = 3.0e4
+    a.run()
+    torch.cuda.synchronize()
+    assert (a.out[0, 1, i] == 0).all() and a.lse[0, 1, i] == -INF
+    want = a.w_in[0, 0, :n].double() + p.sum(0)
+    bound = (bd["factor"][:, None] * p).sum(0) + G * m * ou.U * p.sum(0) + 2 * ou.U * want + 1e-37        # as in Attend.check
+    ou.assert_close(a.w_out[0, 0, :n], want, bound, "weights")
