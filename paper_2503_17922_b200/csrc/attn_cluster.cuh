@@ -111,8 +111,9 @@ __device__ __forceinline__ void cluster_join(const AttnArgs &a, const AttnSeq &s
                 const float ref = lse2[r];
                 const float2 s = *reinterpret_cast<const float2 *>(x + r * a.logit_stride + j);
                 if (ref == -INFINITY) continue;                          // the row attends to nothing
-                w0 += exp2f(s.x - ref);
-                w1 += exp2f(s.y - ref);
+                // (a row that is NaN has no weight for keys that it does not see)
+                w0 += s.x == -INFINITY ? 0.f : exp2f(s.x - ref);
+                w1 += s.y == -INFINITY ? 0.f : exp2f(s.y - ref);
             }
             const long long at = (long long)unit * a.cap + j;
             a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + w0;

@@ -517,10 +517,11 @@ __global__ void __launch_bounds__(kThreads) attn_join_weights_kernel(const __gri
         const float ref = sm.lse2[row];
         if (ref == -INFINITY) continue;                                  // the row attends to nothing
         const float4 s = *reinterpret_cast<const float4 *>(x + row * a.logit_stride);
-        w[0] += exp2f(s.x - ref);
-        w[1] += exp2f(s.y - ref);
-        w[2] += exp2f(s.z - ref);
-        w[3] += exp2f(s.w - ref);
+        // (a row that is NaN has no weight for keys that it does not see)
+        w[0] += s.x == -INFINITY ? 0.f : exp2f(s.x - ref);
+        w[1] += s.y == -INFINITY ? 0.f : exp2f(s.y - ref);
+        w[2] += s.z == -INFINITY ? 0.f : exp2f(s.z - ref);
+        w[3] += s.w == -INFINITY ? 0.f : exp2f(s.w - ref);
     }
     const long long at = (long long)unit * a.cap + j;
 #pragma unroll

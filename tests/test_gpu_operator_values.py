@@ -192,3 +192,25 @@ def test_a_query_of_logits_minus_infinity_leaves_no_weight(name):
     want = a.w_in[0, 0, :n].double() + p.sum(0)
     bound = (bd["factor"][:, None] * p).sum(0) + G * m * ou.U * p.sum(0) + 2 * ou.U * want + 1e-37        # as in Attend.check
     ou.assert_close(a.w_out[0, 0, :n], want, bound, "weights")
+
+
+@paged_calls
+def test_a_nan_query_leaves_weights_alone_that_it_does_not_see(name):
+    """Rows behind a query, and rows without a page, get nothing from it, NaN or not."""
+    a = Attend(*PAGED[name])
+    n, m = unit_rows(a), a.max_new
+    a.c.table[0, 2] = -1
+    a.run()
+    torch.cuda.synchronize()
+    clean = a.w_out.clone()
+    missing = slice(2 * a.c.page, 3 * a.c.page)
+    assert torch.isfinite(clean).all() and same_bits(clean[0, 0, missing], a.w_in[0, 0, missing])
+    i = m // 2
+    a.q[0, 1, i, 5] = NAN
+    a.run()
+    torch.cuda.synchronize()
+    seen = n - m + i + 1
+    assert same_bits(a.w_out[0, 0, seen:], clean[0, 0, seen:]) and same_bits(a.w_out[0, 0, missing], clean[0, 0, missing])
+    rows = torch.arange(seen, device="cuda")
+    assert torch.isnan(a.w_out[0, 0, :seen][(rows < missing.start) | (rows >= missing.stop)]).all()
+    assert same_bits(a.w_out[0, 1:], clean[0, 1:])
