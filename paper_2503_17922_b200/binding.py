@@ -669,12 +669,25 @@ def _check_same_layout(a, b, what: str) -> None:
 
 
 def _check_kv_layout(prob: "Problem", t, what: str) -> None:
-    """Keys or values in the layout that the problem describes."""
+    """Keys or values as the problem's strides find them: [B, H_kv, N, d] or [B, N, H_kv, d] (packed [T, H_kv, d]) of those strides, or a
+    contiguous tensor of another shape that holds them all.  (Strides of dimensions of one do not matter; a larger tensor will do.)"""
     s = prob.shape
-    tokens = int(prob.cu_host[-1]) if prob.packed else s.batch * s.max_seqlen
-    if (t.dtype != prob.torch_dtype or t.shape[-1] != s.head_dim or t.stride(-1) != 1 and s.head_dim != 1
-            or t.numel() < tokens * s.n_kv_heads * s.head_dim):
-        raise ValueError(f"{what}: {tokens * s.n_kv_heads} rows of {s.head_dim} {prob.torch_dtype} expected, got {tuple(t.shape)} of {t.dtype}")
+    dims = [(int(prob.cu_host[-1]) if prob.packed else s.max_seqlen, s.stride_t), (s.n_kv_heads, s.stride_h)]
+    if not prob.packed:
+        dims.append((s.batch, s.stride_b))
+    last = sum((n - 1) * stride for n, stride in dims) + s.head_dim
+
+    def laid_out(order):
+        return all(have >= n and (n == 1 or got == stride) for (n, stride), have, got in zip(order, t.shape, t.stride()))
+    ok = t.dtype == prob.torch_dtype and t.dim() > 0 and t.shape[-1] == s.head_dim and (t.stride(-1) == 1 or s.head_dim == 1)
+    if ok and t.dim() == len(dims) + 1:
+        orders = [dims, dims[::-1]] if prob.packed else [[dims[2], dims[1], dims[0]], [dims[2], dims[0], dims[1]]]
+        ok = any(laid_out(order) for order in orders)
+    elif ok:
+        ok = t.is_contiguous() and t.numel() >= last
+    if not ok:
+        raise ValueError(f"{what}: {prob.torch_dtype} rows of {s.head_dim} in the problem's layout expected (tokens, heads, batch x strides: {dims}), "
+                         f"got {tuple(t.shape)} of {t.dtype} with strides {t.stride()}")
 
 
 def prepare_rotate_prompt(prob: Problem, rope: Rope, q, k, q_out, k_out, positions=None, stream=None) -> PreparedCall:

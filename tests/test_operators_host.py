@@ -244,3 +244,42 @@ def test_binding_refuses_pools_and_keys_that_are_too_small():
             binding.prepare_evict_kv_paged(cache, [pool, bad], None, w, pos, n, 8, 2, w, pos, n, ws)
     with pytest.raises(ValueError, match="per layer"):
         binding.prepare_evict_kv_paged(cache, [pool, pool], [pool], w, pos, n, 8, 2, w, pos, n, ws)
+
+
+def problem(**kw):
+    import torch
+    args = dict(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, l_obs=4, window=8, task=0, top_p=0, max_seqlen=30, budgets=[30] * 2,
+                device=torch.device("cpu"))
+    args.update(kw)
+    return binding.Problem(**args)
+
+
+def test_keys_and_values_in_another_layout_are_refused():
+    """The C side goes by the problem's strides: a tensor that has others would be read, or written, in the wrong places."""
+    import torch
+    new = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)
+    packed = dict(batch=3, budgets=[30] * 3, max_seqlen=12, cu_seqlens=[0, 5, 9, 20])
+    q, kv = new(2, 4, 30, 64), new(2, 2, 30, 64)
+    good = [(problem(), kv), (problem(), kv.view(-1, 64)), (problem(), new(3, 2, 30, 64)), (problem(), kv.transpose(1, 2)),
+            (problem(kv_layout="bnhd"), new(2, 30, 2, 64)), (problem(kv_layout="bnhd"), new(2, 30, 2, 64).transpose(1, 2)),
+            (problem(kv_layout="bnhd", batch=1, budgets=[30]), new(1, 31, 2, 64)),
+            (problem(n_kv_heads=1), new(2, 1, 30, 64)), (problem(n_kv_heads=1, kv_layout="bnhd"), new(2, 1, 30, 64)),
+            (problem(**packed), new(20, 2, 64)), (problem(**packed), new(25, 2, 64)), (problem(**packed), new(20, 2, 64).transpose(0, 1))]
+    bad = [(problem(), new(2, 30, 2, 64)), (problem(kv_layout="bnhd"), kv), (problem(), new(1, 2, 30, 64).expand(2, 2, 30, 64)),
+           (problem(), new(2, 1, 30, 64).expand(2, 2, 30, 64)), (problem(), new(2, 2, 30, 72)[..., :64]), (problem(), new(2, 2, 31, 64)),
+           (problem(), new(2, 2, 31, 64)[:, :, :30]), (problem(), new(2, 2, 29, 64)), (problem(), kv.view(-1, 64)[1:]), (problem(), kv.float()),
+           (problem(), new(2, 2, 30, 128)[..., ::2]), (problem(), new(2, 2, 30, 32)),
+           (problem(**packed), new(20, 2, 72)[..., :64]), (problem(**packed), new(2, 20, 64)), (problem(**packed), new(19, 2, 64)),
+           (problem(**packed), new(1, 2, 64).expand(20, 2, 64)), (problem(**packed), new(20, 1, 64).expand(20, 2, 64))]
+    rope = binding.Rope(64, device=torch.device("cpu"))
+    for prob, t in good:
+        binding.prepare_rotate_prompt(prob, rope, None, t, None, t, stream=0)
+    for prob, t in bad:
+        ok = next(g for p, g in good if (p.packed, p.shape.stride_h, p.shape.stride_b) == (prob.packed, prob.shape.stride_h, prob.shape.stride_b))
+        for k, k_out in ((t, ok), (ok, t)):
+            with pytest.raises(ValueError, match="layout expected"):
+                binding.prepare_rotate_prompt(prob, rope, None, k, None, k_out, stream=0)
+        x = new(20, 4, 64) if prob.packed else q
+        for k, v in ((t, ok), (ok, t)):
+            with pytest.raises(ValueError, match="layout expected"):
+                binding.prepare_attend_prompt(prob, x, k, v, x.clone(), stream=0)
