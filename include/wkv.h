@@ -429,9 +429,10 @@ typedef enum { WKV_ROPE_HALF = 0, WKV_ROPE_INTERLEAVED = 1 } wkv_rope_order;
  * (LINEAR); base times factor^(rot_dim/(rot_dim-2)) (BASE); by bands (BANDS): with t = (original_length * f_i / 2 pi - low) /
  * (high - low) limited to 0..1, f_i (t + (1 - t)/factor), so that pairs which turn often keep their angle. */
 typedef enum { WKV_ROPE_NONE = 0, WKV_ROPE_LINEAR = 1, WKV_ROPE_BASE = 2, WKV_ROPE_BANDS = 3 } wkv_rope_scaling;
+#define WKV_MAX_ROT_DIM 4096
 typedef struct {
     uint32_t struct_size;      /* sizeof(wkv_rope), checked */
-    int32_t rot_dim;           /* even, 2 .. head_dim */
+    int32_t rot_dim;           /* even, 2 .. head_dim, at most WKV_MAX_ROT_DIM (WKV_ERR_LIMIT) */
     int32_t order;             /* wkv_rope_order */
     float scale;               /* factor of the turned dimensions, finite (1 where the model has none) */
     const uint64_t *turns;     /* DEVICE [rot_dim/2], as wkv_rope_frequencies writes them on the host */

@@ -213,11 +213,14 @@ int check_rope(const wkv_rope *r, int head_dim)
         set_error_detail("rope: struct_size %u != %zu", r->struct_size, sizeof(wkv_rope));
         return WKV_ERR_SHAPE;
     }
-    if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > head_dim || r->rot_dim > 4096 ||
-        (r->order != WKV_ROPE_HALF && r->order != WKV_ROPE_INTERLEAVED) || !isfinite(r->scale)) {
-        set_error_detail("rope: rot_dim %d (even, 2 .. head_dim %d, at most 4,096), order %d or scale invalid", r->rot_dim, head_dim,
-                         r->order);
+    if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > head_dim || (r->order != WKV_ROPE_HALF && r->order != WKV_ROPE_INTERLEAVED) ||
+        !isfinite(r->scale)) {
+        set_error_detail("rope: rot_dim %d (even, 2 .. head_dim %d), order %d or scale invalid", r->rot_dim, head_dim, r->order);
         return WKV_ERR_SHAPE;
+    }
+    if (r->rot_dim > WKV_MAX_ROT_DIM) {
+        set_error_detail("rope: rot_dim %d beyond %d", r->rot_dim, WKV_MAX_ROT_DIM);
+        return WKV_ERR_LIMIT;
     }
     return r->turns ? WKV_OK : missing("rope: turns");
 }

@@ -17,7 +17,7 @@ namespace wkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxPairs = 2048;          // rot/2 at most, per block: cosines and sines in shared memory (16 KB)
+constexpr int kMaxPairs = WKV_MAX_ROT_DIM / 2;          // per block: cosines and sines in shared memory (16 KB)
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }

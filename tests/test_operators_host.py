@@ -283,3 +283,14 @@ def test_keys_and_values_in_another_layout_are_refused():
         for k, v in ((t, ok), (ok, t)):
             with pytest.raises(ValueError, match="layout expected"):
                 binding.prepare_attend_prompt(prob, x, k, v, x.clone(), stream=0)
+
+
+def test_rotated_dimensions_have_a_limit_of_their_own(L):
+    """More pairs than a block holds angles for, in heads that have them: a limit, not a wrong shape."""
+    c = paged(head_dim=8192, page_stride=2 * 16 * 8192, head_stride=16 * 8192, row_stride=8192)
+    st = strides(2 * 3 * 8192, 3 * 8192, 8192)
+    s = shape(head_dim=8192, stride_b=2 * 1024 * 8192, stride_h=1024 * 8192, stride_t=8192, q_stride_t=8192)
+    for rot, status in ((4098, 9), (8192, 9), (8194, 2), (4097, 2)):
+        r = rope(rot_dim=rot)
+        assert L.wkv_append_kv_paged(ctypes.byref(c), ctypes.byref(r), P, P, st, None, None, None, P, P, P, 2 * P, None, None, None, None) == status
+        assert L.wkv_rotate_prompt(ctypes.byref(s), ctypes.byref(r), None, None, None, P, P, None, None) == status
