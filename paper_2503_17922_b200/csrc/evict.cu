@@ -267,11 +267,11 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
 }
 
 __global__ void __launch_bounds__(256) seed_rows_kernel(const __grid_constant__ KShape s, const int *window_idx, const float *token_scores,
-                                                        int row_capacity, int *positions, float *weights)
+                                                        int row_capacity, int *positions, float *weights, int blocks)
 {
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.y, b = unit / s.hkv;
+    const int unit = (int)blockIdx.x / blocks, part = (int)blockIdx.x - unit * blocks, b = unit / s.hkv;
     const SeqInfo si = seq_info(s, b);
     const int n_r = si.n > s.alpha ? si.n - s.alpha : 0, kw = num_windows(si.n, s.alpha, s.omega);
     const int k = num_selected_capped(si.n, s.alpha, s.omega, si.budget, s.k_max);
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(256) seed_rows_kernel(const __grid_constant__ 
     int review = k * s.omega;
     if (k > 0 && idx[k - 1] == kw - 1) review -= kw * s.omega - n_r;      // the sequence's short last window
     review = min(review, n_r);
-    for (int r = blockIdx.x * blockDim.x + threadIdx.x; r < review + si.n - n_r && r < row_capacity; r += gridDim.x * blockDim.x) {
+    for (int r = part * (int)blockDim.x + (int)threadIdx.x; r < review + si.n - n_r && r < row_capacity; r += blocks * (int)blockDim.x) {
         int at;
         float w = 0.f;
         if (r < review) {
@@ -333,14 +333,15 @@ int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream
 int launch_seed_rows(const KShape &ks, const int *window_idx, const float *token_scores, int row_capacity, int *positions,
                      float *weights, cudaStream_t stream)
 {
-    const int units = ks.batch * ks.hkv;
-    if (units > 65535) {
-        set_error_detail("%d (sequence, KV head) pairs", units);
+    const long long units = (long long)ks.batch * ks.hkv;
+    int blocks = row_capacity > 256 * 16 ? 16 : (row_capacity + 255) / 256;
+    if (blocks < 1 || units * blocks > 0x7fffffffLL) blocks = 1;
+    if (units > 0x7fffffffLL) {
+        set_error_detail("%lld (sequence, KV head) pairs", units);
         return WKV_ERR_LIMIT;
     }
-    const int blocks = row_capacity > 256 * 16 ? 16 : (row_capacity + 255) / 256;
-    const cudaError_t err = launch_pdl(seed_rows_kernel, dim3(blocks < 1 ? 1 : blocks, units), 256, 0, stream, 1, ks, window_idx, token_scores,
-                                       row_capacity, positions, weights);
+    const cudaError_t err = launch_pdl(seed_rows_kernel, dim3((unsigned)(units * blocks)), 256, 0, stream, 1, ks, window_idx, token_scores,
+                                       row_capacity, positions, weights, blocks);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "row state kernel");
 }

@@ -214,3 +214,21 @@ def test_a_nan_query_leaves_weights_alone_that_it_does_not_see(name):
     rows = torch.arange(seen, device="cuda")
     assert torch.isnan(a.w_out[0, 0, :seen][(rows < missing.start) | (rows >= missing.stop)]).all()
     assert same_bits(a.w_out[0, 1:], clean[0, 1:])
+
+
+# ---- many sequences --------------------------------------------------------------------------------
+def test_row_state_of_many_sequences():
+    """More (sequence, KV head) pairs than a grid's second dimension has room for."""
+    from paper_2503_17922_b200 import binding as wkv
+    B, H, n, alpha, window = 35000, 2, 12, 4, 4
+    prob = wkv.Problem(dtype="bf16", batch=B, n_q_heads=2, n_kv_heads=H, head_dim=64, l_obs=alpha, window=window, task=0, top_p=0, max_seqlen=n,
+                       budgets=[8] * B)
+    idx = torch.randint(0, 2, (B, H, 1), generator=torch.Generator().manual_seed(2)).to(torch.int32).cuda()
+    scores = torch.rand((B, H, n - alpha), device="cuda")
+    positions = torch.full((B, H, 10), -1, dtype=torch.int32, device="cuda")
+    weights = torch.full((B, H, 10), -1.0, device="cuda")
+    wkv.wkv_seed_rows(prob, idx, scores, positions, weights)
+    torch.cuda.synchronize()
+    review = idx * window + torch.arange(window, dtype=torch.int32, device="cuda")
+    assert torch.equal(positions[..., :4], review) and (positions[..., 4:8] == torch.arange(8, 12, device="cuda")).all() and (positions[..., 8:] == -1).all()
+    assert torch.equal(weights[..., :4], scores.gather(-1, review.long())) and (weights[..., 4:8] == 0).all() and (weights[..., 8:] == -1).all()
