@@ -24,11 +24,11 @@ int check_pointer(const void *p, const char *what)
     set_error_detail("%s is not 16-byte aligned", what);
     return WKV_ERR_ALIGN;
 }
-// strides of a [B, heads, tokens, d] or packed [T, heads, d] tensor (batch stride 0 then)
-int check_strides(const int64_t *st, int head_dim, int eb, const char *what)
+// strides of a [B, heads, tokens, d] or packed [T, heads, d] tensor (whose batch stride is not looked at)
+int check_strides(const int64_t *st, bool packed, int head_dim, int eb, const char *what)
 {
     if (!st) return missing(what);
-    for (int i = 0; i < 3; ++i)
+    for (int i = packed ? 1 : 0; i < 3; ++i)
         if (st[i] < 0 || (st[i] * eb) % 16) {
             set_error_detail("%s: stride #%d = %lld is negative or not 16-byte aligned", what, i, (long long)st[i]);
             return WKV_ERR_ALIGN;
@@ -290,7 +290,7 @@ int wkv_rotate_prompt(const wkv_shape *s, const wkv_rope *rope, const void *q, v
     const int eb = elem_bytes(s->dtype);
     if (q) {
         if ((st = check_pointer(q, "q")) != WKV_OK || (st = check_pointer(q_out, "q_out")) != WKV_OK) return st;
-        if ((st = check_strides(q_strides, s->head_dim, eb, "q_strides")) != WKV_OK) return st;
+        if ((st = check_strides(q_strides, ks.cu != nullptr, s->head_dim, eb, "q_strides")) != WKV_OK) return st;
     }
     if (k && ((st = check_pointer(k, "k")) != WKV_OK || (st = check_pointer(k_out, "k_out")) != WKV_OK)) return st;
     RopeArgs a;
@@ -331,8 +331,8 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
     if ((st = check_pointer(q, "q")) != WKV_OK || (st = check_pointer(k, "k")) != WKV_OK || (st = check_pointer(v, "v")) != WKV_OK ||
         (st = check_pointer(out, "out")) != WKV_OK)
         return st;
-    if ((st = check_strides(q_strides, s->head_dim, eb, "q_strides")) != WKV_OK ||
-        (st = check_strides(out_strides, s->head_dim, eb, "out_strides")) != WKV_OK)
+    if ((st = check_strides(q_strides, ks.cu != nullptr, s->head_dim, eb, "q_strides")) != WKV_OK ||
+        (st = check_strides(out_strides, ks.cu != nullptr, s->head_dim, eb, "out_strides")) != WKV_OK)
         return st;
     if (out == q || out == k || out == v) {
         set_error_detail("out must not be an input");
@@ -404,11 +404,11 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
     const bool packed = c->cu_new_host != nullptr, none = packed && p.total_new == 0;      // no new tokens: their tensors may be null
     for (int i = none ? 2 : 0; i < 4; ++i)
         if ((st = check_pointer(ptrs[i], names[i])) != WKV_OK) return st;
-    if (!none && (st = check_strides(kv_strides, c->head_dim, p.eb, "kv_strides")) != WKV_OK) return st;
+    if (!none && (st = check_strides(kv_strides, packed, c->head_dim, p.eb, "kv_strides")) != WKV_OK) return st;
     if (!none && (q == nullptr) != (q_out == nullptr)) return missing(q ? "q_out" : "q");
     if (q && !none) {
         if ((st = check_pointer(q, "q")) != WKV_OK || (st = check_pointer(q_out, "q_out")) != WKV_OK) return st;
-        if ((st = check_strides(q_strides, c->head_dim, p.eb, "q_strides")) != WKV_OK) return st;
+        if ((st = check_strides(q_strides, packed, c->head_dim, p.eb, "q_strides")) != WKV_OK) return st;
     }
     if (!lengths) return missing("lengths");
     if (!none && !positions && (rope || row_positions)) return missing("positions");
@@ -476,8 +476,8 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
     const bool packed = c->cu_new_host != nullptr, none = packed && p.total_new == 0;      // no new tokens: q and out may be null
     for (int i = 0; i < 4; ++i)
         if (!(none && (i == 0 || i == 3)) && (st = check_pointer(ptrs[i], names[i])) != WKV_OK) return st;
-    if (!none && ((st = check_strides(q_strides, c->head_dim, p.eb, "q_strides")) != WKV_OK ||
-                  (st = check_strides(out_strides, c->head_dim, p.eb, "out_strides")) != WKV_OK))
+    if (!none && ((st = check_strides(q_strides, packed, c->head_dim, p.eb, "q_strides")) != WKV_OK ||
+                  (st = check_strides(out_strides, packed, c->head_dim, p.eb, "out_strides")) != WKV_OK))
         return st;
     if (!lengths) return missing("lengths");
     if (weights_in && !weights_out) return missing("weights_out");

@@ -232,3 +232,47 @@ def test_row_state_of_many_sequences():
     review = idx * window + torch.arange(window, dtype=torch.int32, device="cuda")
     assert torch.equal(positions[..., :4], review) and (positions[..., 4:8] == torch.arange(8, 12, device="cuda")).all() and (positions[..., 8:] == -1).all()
     assert torch.equal(weights[..., :4], scores.gather(-1, review.long())) and (weights[..., 4:8] == 0).all() and (weights[..., 8:] == -1).all()
+
+
+# ---- strides that are not looked at -------------------------------------------------------------------
+def test_the_batch_stride_of_packed_tensors_is_not_used():
+    import ctypes
+    from paper_2503_17922_b200 import binding as wkv
+    L, stream = wkv.lib(), torch.cuda.current_stream().cuda_stream
+
+    def st(t):
+        return (ctypes.c_int64 * 3)(-5, t.stride(1), t.stride(0))
+    p = Prompt("bf16", 4, 2, 64, [130, 70], "packed", 4)
+    p.run()
+    rope, turned, want_turned = wkv.Rope(64), torch.empty_like(p.q), torch.empty_like(p.q)
+    wkv.wkv_rotate_prompt(p.prob, rope, p.q, None, want_turned, None)
+    torch.cuda.synchronize()
+    want = p.out.clone()
+    p.out.fill_(77.0)
+    s = ctypes.byref(p.prob.shape)
+    assert L.wkv_attend_prompt(s, p.q.data_ptr(), st(p.q), p.k.data_ptr(), p.v.data_ptr(), p.out.data_ptr(), st(p.out), None, None, None, stream) == 0
+    assert L.wkv_rotate_prompt(s, ctypes.byref(rope.struct), p.q.data_ptr(), turned.data_ptr(), st(p.q), None, None, None, stream) == 0
+    torch.cuda.synchronize()
+    assert same_bits(p.out, want) and same_bits(turned, want_turned)
+
+    a = Attend("bf16", 4, 2, 64, 16, "phsd", [[80, 80], [60, 60]], [3, 4], True)
+    a.run(weights=False)
+    torch.cuda.synchronize()
+    want, n = a.out.clone(), a.lengths.cuda()
+    a.out.fill_(77.0)
+    assert L.wkv_attend_paged(ctypes.byref(a.cache.shape), a.q.data_ptr(), st(a.q), a.c.k[0].data_ptr(), a.c.v[0].data_ptr(), n.data_ptr(),
+                              a.out.data_ptr(), st(a.out), None, None, None, a.ws.data_ptr(), a.ws.numel(), stream) == 0
+    torch.cuda.synchronize()
+    assert same_bits(a.out, want)
+    k, v = a.q[:, :2].contiguous(), a.q[:, 2:].contiguous()
+    pools = []
+    for strides in (None, st(k)):
+        kp, vp, n1 = torch.zeros_like(a.c.k[0]), torch.zeros_like(a.c.k[0]), torch.zeros_like(n)
+        if strides is None:
+            wkv.wkv_append_kv_paged(a.cache, k, v, n, kp, vp, lengths_out=n1)
+        else:
+            assert L.wkv_append_kv_paged(ctypes.byref(a.cache.shape), None, k.data_ptr(), v.data_ptr(), strides, None, None, None, None, n.data_ptr(),
+                                         kp.data_ptr(), vp.data_ptr(), n1.data_ptr(), None, None, stream) == 0
+        torch.cuda.synchronize()
+        pools.append((kp, vp, n1))
+    assert all(same_bits(x, y) for x, y in zip(*pools))
