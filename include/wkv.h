@@ -417,6 +417,8 @@ int wkv_compress_group_host_rows(const wkv_shape *s, int32_t n_layers,
  * observation rows is what the _lse calls take) and after it (new tokens appended to the paged compact cache of section
  * 2.1's decode phase and attending over it, rows leaving the cache by the attention weight they have received).
  * The general conventions at the head of this file hold.  Scores are scaled by 1/sqrt(head_dim) as in Eq. 1.
+ * Strides of an output (and of pools that are written) keep its rows apart: of the dimensions larger than one, in order of increasing stride,
+ * each steps over what the ones before it reach (WKV_ERR_SHAPE otherwise).  Strides of inputs may be 0, or overlap.
  */
 
 /* Rotary positions: of each head's first rot_dim dimensions, pairs (x_j, x_k) are turned by position * f_i,

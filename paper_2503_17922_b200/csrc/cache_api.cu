@@ -2,6 +2,8 @@
 // (append, attend, evict, row state).  Validation, workspace carve-up and kernel choice; no device memory is allocated here.
 #include "attn_cluster.cuh"
 
+#include <algorithm>
+
 #include <math.h>
 #include <string.h>
 
@@ -38,6 +40,36 @@ int check_strides(const int64_t *st, bool packed, int head_dim, int eb, const ch
         return WKV_ERR_SHAPE;
     }
     return WKV_OK;
+}
+
+// The rows of an output lie apart: each dimension, in order of increasing stride, steps over all that the ones before it reach.  (Rows in
+// one place are written by several threads, and rotated in place once for each of them.)
+struct Dim {
+    long long size, stride;
+};
+int check_apart(Dim x, Dim y, Dim z, int head_dim, const char *what)
+{
+    Dim dims[3] = {x, y, z};
+    std::sort(dims, dims + 3, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    unsigned __int128 reach = (unsigned)head_dim;
+    for (const Dim &a : dims) {
+        if (a.size <= 1) continue;
+        if ((unsigned __int128)a.stride < reach) {
+            set_error_detail("%s: a stride of %lld puts rows of an output into one place", what, a.stride);
+            return WKV_ERR_SHAPE;
+        }
+        reach += (unsigned __int128)a.stride * (unsigned long long)(a.size - 1);
+    }
+    return WKV_OK;
+}
+// ... of a tensor whose strides check_strides has seen
+int check_apart(const int64_t *st, int batch, int heads, long long tokens, bool packed, int head_dim, const char *what)
+{
+    return check_apart({packed ? 1 : batch, st[0]}, {heads, st[1]}, {tokens, st[2]}, head_dim, what);
+}
+int check_pools_apart(const wkv_paged *c)
+{
+    return check_apart({c->num_pages, c->page_stride}, {c->n_kv_heads, c->head_stride}, {c->page_size, c->row_stride}, c->head_dim, "paged cache");
 }
 
 // what a call knows about its paged cache
@@ -293,6 +325,10 @@ int wkv_rotate_prompt(const wkv_shape *s, const wkv_rope *rope, const void *q, v
         if ((st = check_strides(q_strides, ks.cu != nullptr, s->head_dim, eb, "q_strides")) != WKV_OK) return st;
     }
     if (k && ((st = check_pointer(k, "k")) != WKV_OK || (st = check_pointer(k_out, "k_out")) != WKV_OK)) return st;
+    const bool packed = ks.cu != nullptr;
+    const long long tokens = packed ? ks.total_rows : ks.max_seqlen;
+    if (q && (st = check_apart(q_strides, ks.batch, ks.hq, tokens, packed, ks.d, "q_strides")) != WKV_OK) return st;
+    if (k && (st = check_apart({packed ? 1 : ks.batch, ks.sb}, {ks.hkv, ks.sh}, {tokens, ks.st}, ks.d, "k_out")) != WKV_OK) return st;
     RopeArgs a;
     memset(&a, 0, sizeof a);
     a.batch = ks.batch;
@@ -338,6 +374,7 @@ int wkv_attend_prompt(const wkv_shape *s, const void *q, const int64_t *q_stride
         set_error_detail("out must not be an input");
         return WKV_ERR_SHAPE;
     }
+    if ((st = check_apart(out_strides, ks.batch, ks.hq, ks.cu ? ks.total_rows : ks.max_seqlen, ks.cu != nullptr, ks.d, "out_strides")) != WKV_OK) return st;
     if ((long long)ks.max_seqlen * ks.G > 0x3fffffffLL || (long long)ks.batch * ks.hkv > 0xffffffLL) {
         set_error_detail("attention: %d tokens of %d query heads per KV head, %d sequences", ks.max_seqlen, ks.G, ks.batch);
         return WKV_ERR_LIMIT;
@@ -420,6 +457,9 @@ int wkv_append_kv_paged(const wkv_paged *c, const wkv_rope *rope, const void *k_
         set_error_detail("k_pool and v_pool are the same");
         return WKV_ERR_SHAPE;
     }
+    if ((st = check_pools_apart(c)) != WKV_OK) return st;
+    if (q && !none && (st = check_apart(q_strides, c->batch, c->n_q_heads, packed ? p.total_new : c->max_new, packed, c->head_dim, "q_strides")) != WKV_OK)
+        return st;
     RopeArgs a;
     memset(&a, 0, sizeof a);
     a.batch = c->batch;
@@ -485,6 +525,8 @@ int wkv_attend_paged(const wkv_paged *c, const void *q, const int64_t *q_strides
         set_error_detail("out must not be an input");
         return WKV_ERR_SHAPE;
     }
+    if (!none && (st = check_apart(out_strides, c->batch, c->n_q_heads, packed ? p.total_new : c->max_new, packed, c->head_dim, "out_strides")) != WKV_OK)
+        return st;
     const PagedWorkspace w = plan_paged(c, p);
     if ((st = check_workspace(w, workspace, workspace_bytes)) != WKV_OK) return st;
     if (none && !weights_out) return WKV_OK;
@@ -581,6 +623,7 @@ int wkv_evict_kv_paged(const wkv_paged *c, int32_t n_layers, void *const *k_pool
         if ((st = check_pointer(v_pools[l], "a layer's V pool")) != WKV_OK) return st;
         pools.ptr[n_tensors++] = v_pools[l];
     }
+    if ((st = check_pools_apart(c)) != WKV_OK) return st;
     const PagedWorkspace w = plan_paged(c, p);
     if ((st = check_workspace(w, workspace, workspace_bytes)) != WKV_OK) return st;
     EvictArgs a;

@@ -294,3 +294,38 @@ def test_rotated_dimensions_have_a_limit_of_their_own(L):
         r = rope(rot_dim=rot)
         assert L.wkv_append_kv_paged(ctypes.byref(c), ctypes.byref(r), P, P, st, None, None, None, P, P, P, 2 * P, None, None, None, None) == status
         assert L.wkv_rotate_prompt(ctypes.byref(s), ctypes.byref(r), None, None, None, P, P, None, None) == status
+
+
+def test_outputs_whose_rows_share_a_place_are_refused(L):
+    """An expanded or overlapping output would be written by several blocks at once."""
+    tight = [(3 * 64, 3 * 64, 64), (0, 3 * 64, 64), (4 * 3 * 64, 0, 64), (4 * 3 * 64, 64, 64), (4 * 3 * 64, 3 * 64 - 8, 64), (2 * 3 * 64, 3 * 64, 64)]
+    fine = strides(4 * 3 * 64, 3 * 64, 64)
+    need = L.wkv_paged_workspace_bytes(ctypes.byref(paged()))
+    c, s, r = paged(), shape(max_seqlen=3, l_obs=1, budget=3), rope()
+    s2 = shape(max_seqlen=3, l_obs=1, budget=3, batch=2)
+    for t in tight:
+        assert L.wkv_attend_paged(ctypes.byref(c), P, fine, P, P, P, 2 * P, strides(*t), None, None, None, P, need, None) == 2, t
+        assert L.wkv_append_kv_paged(ctypes.byref(c), None, P, P, fine, P, P, strides(*t), None, P, P, 2 * P, None, None, None, None) == 2, t
+        assert L.wkv_attend_prompt(ctypes.byref(s2), P, fine, P, P, 2 * P, strides(*t), None, None, None, None) == 2, t
+        assert L.wkv_rotate_prompt(ctypes.byref(s2), ctypes.byref(r), P, P, strides(*t), None, None, None, None) == 2, t
+    for kw in (dict(stride_b=0), dict(stride_h=0), dict(stride_b=64, stride_h=64), dict(stride_h=64)):
+        bad = shape(max_seqlen=3, l_obs=1, budget=3, batch=2, stride_b=2 * 3 * 64, stride_h=3 * 64)
+        for name, x in kw.items():
+            setattr(bad, name, x)
+        assert L.wkv_rotate_prompt(ctypes.byref(bad), ctypes.byref(r), None, None, None, P, P, None, None) == 2, kw
+    ptrs = (ctypes.c_void_p * 1)(P)
+    for kw in (dict(page_stride=0), dict(head_stride=0), dict(page_stride=16 * 64), dict(head_stride=64), dict(head_stride=2 * 64)):
+        bad = paged(**kw)
+        assert L.wkv_append_kv_paged(ctypes.byref(bad), None, P, P, fine, None, None, None, None, P, P, 2 * P, None, None, None, None) == 2, kw
+        assert L.wkv_evict_kv_paged(ctypes.byref(bad), 1, ptrs, None, 4, None, 0, P, P, P, P, P, P, P, need, None) == 2, kw
+    # what lies apart in another order, or has one element, gets as far as the next check
+    cu = np.array([0, 1, 3], dtype=np.int32)
+    for t in ((64, 3 * 2 * 64, 2 * 64), (3 * 4 * 64, 64, 4 * 64), (4 * 3 * 72, 3 * 72, 72)):
+        assert L.wkv_attend_paged(ctypes.byref(c), P, fine, P, P, P, 2 * P, strides(*t), None, None, None, P, need - 1, None) == 5, t
+    packed = paged(cu_new_host=cu.ctypes.data, cu_new_dev=P)
+    assert L.wkv_attend_paged(ctypes.byref(packed), P, fine, P, P, P, 2 * P, strides(0, 64, 4 * 64), None, None, None, P, 0, None) == 5
+    one = paged(batch=1, n_kv_heads=1, n_q_heads=1, max_new=1)
+    assert L.wkv_attend_paged(ctypes.byref(one), P, fine, P, P, P, 2 * P, strides(0, 0, 64), None, None, None, P, 0, None) == 5
+    # pools that are only read may share rows
+    for kw in (dict(page_stride=0), dict(head_stride=0)):
+        assert L.wkv_attend_paged(ctypes.byref(paged(**kw)), P, fine, P, P, P, 2 * P, fine, None, None, None, P, 0, None) == 5
