@@ -657,6 +657,19 @@ def _check_state(t, shape, dtype: str, what: str) -> None:
         raise ValueError(f"{what}: contiguous {tuple(shape)} of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
 
 
+def _check_devices(device, what: str, *tensors) -> None:
+    """All tensors of a call (or lists of them, addresses, None) are on the device of its description, which is the current one: kernels are
+    launched there, and another device's memory, or the host's, is none of theirs."""
+    import torch
+    if device.type == "cuda" and device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: described on {device}, but the current device is cuda:{torch.cuda.current_device()}")
+    for t in tensors:
+        if isinstance(t, (list, tuple)):
+            _check_devices(device, what, *t)
+        elif hasattr(t, "device") and t.device != device:
+            raise ValueError(f"{what}: all tensors on {device} expected, got one on {t.device}")
+
+
 def _check_positions(t, shape) -> None:
     """Positions of the expected shape, or the same number of them in one dimension."""
     flat = (int(np.prod(shape)),)
@@ -694,6 +707,7 @@ def prepare_rotate_prompt(prob: Problem, rope: Rope, q, k, q_out, k_out, positio
     """Rotary positions of a prompt: q, q_out [B, H_q, N, d] (any strides) or packed [T, H_q, d]; k, k_out in the problem's layout.
     Either pair may be None; an output may be its input."""
     s = prob.shape
+    _check_devices(prob.budgets_dev.device, "rotary positions", rope.turns, q, k, q_out, k_out, positions)
     tokens = int(prob.cu_host[-1]) if prob.packed else s.max_seqlen
     for t, what in ((q, "q"), (q_out, "q_out")):
         if t is not None:
@@ -716,6 +730,7 @@ def prepare_attend_prompt(prob: Problem, q, k, v, out, lse=None, lse_obs=None, s
     """Causal attention of whole prompts: q, out [B, H_q, N, d] (any strides) or packed [T, H_q, d]; k, v in the problem's layout;
     lse float [B, H_q, max_seqlen], lse_obs float [B, H_q, alpha] as the _lse calls take it; status int32 [1]."""
     s = prob.shape
+    _check_devices(prob.budgets_dev.device, "prompt attention", q, k, v, out, lse, lse_obs, status)
     tokens = int(prob.cu_host[-1]) if prob.packed else s.max_seqlen
     for t, what in ((q, "q"), (out, "out")):
         _check_heads(t, s.n_q_heads, prob.torch_dtype, s.head_dim, prob.packed, s.batch, tokens, what)
@@ -751,6 +766,8 @@ def prepare_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_
     """New tokens into the cache, behind lengths[b, h] rows: k_new, v_new [B, H_kv, max_new, d] or packed [T, H_kv, d] (same strides);
     q likewise, turned into q_out; positions int32 [B, max_new] or [T]."""
     s, tokens = cache.shape, _chunk_tokens(cache)
+    _check_devices(cache.device, "append", rope.turns if rope is not None else None, k_new, v_new, lengths, k_pool, v_pool, q, q_out, positions,
+                   lengths_out, row_positions, row_weights)
     for t, heads, what in ((k_new, s.n_kv_heads, "k_new"), (v_new, s.n_kv_heads, "v_new"), (q, s.n_q_heads, "q"), (q_out, s.n_q_heads, "q_out")):
         if t is not None:
             _check_heads(t, heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
@@ -782,6 +799,7 @@ def prepare_attend_paged(cache: PagedCache, q, k_pool, v_pool, lengths, out, wor
     """Attention of the new tokens over the cache (their own rows, the last of lengths[b, h], included): q, out [B, H_q, max_new, d]
     or packed [T, H_q, d]; lse float [B, H_q, max_new]; weights float [B, H_kv, capacity], weights_out may be weights_in."""
     s, tokens = cache.shape, _chunk_tokens(cache)
+    _check_devices(cache.device, "paged attention", q, k_pool, v_pool, lengths, out, workspace, lse, weights_in, weights_out)
     for t, what in ((q, "q"), (out, "out")):
         _check_heads(t, s.n_q_heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
     _check_pool(cache, k_pool, "k_pool")
@@ -806,6 +824,8 @@ def prepare_evict_kv_paged(cache: PagedCache, k_pools, v_pools, weights, positio
                            positions_out, lengths_out, workspace, budgets=None, stream=None) -> PreparedCall:
     """Rows of least weight leave the cache, for all layers given; outputs may be their inputs.  budgets: int32 [B] on the device."""
     s = cache.shape
+    _check_devices(cache.device, "eviction", k_pools, v_pools, weights, positions, lengths, weights_out, positions_out, lengths_out, workspace,
+                   budgets)
     units = (s.batch, s.n_kv_heads)
     for t, what in ((weights, "weights"), (weights_out, "weights_out")):
         _check_state(t, units + (cache.capacity,), "float32", what)
@@ -835,6 +855,7 @@ def wkv_evict_kv_paged(cache: PagedCache, k_pools, v_pools, weights, positions, 
 
 def wkv_seed_rows(prob: Problem, window_idx, token_scores, positions, weights, stream=None) -> None:
     """The rows' state behind a gather: positions int32 and weights float [B, H_kv, row_capacity] (either may be None)."""
+    _check_devices(prob.budgets_dev.device, "row state", window_idx, token_scores, positions, weights)
     capacity = (positions if positions is not None else weights).shape[-1]
     units = (prob.shape.batch, prob.shape.n_kv_heads)
     _check_state(positions, units + (capacity,), "int32", "positions")

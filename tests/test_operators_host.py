@@ -329,3 +329,48 @@ def test_outputs_whose_rows_share_a_place_are_refused(L):
     # pools that are only read may share rows
     for kw in (dict(page_stride=0), dict(head_stride=0)):
         assert L.wkv_attend_paged(ctypes.byref(paged(**kw)), P, fine, P, P, P, 2 * P, fine, None, None, None, P, 0, None) == 5
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """A kernel that is given another device's memory, or the host's, faults: every tensor of a call is looked at."""
+    import torch
+    bf, i32, f32 = torch.bfloat16, torch.int32, torch.float32
+    prob, rope = problem(), binding.Rope(64, device=torch.device("cpu"))
+    cache = binding.PagedCache(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=16, num_pages=6,
+                               block_table=torch.zeros((2, 3), dtype=i32))
+    units, rows = (2, 2), (2, 2, 48)
+    zeros = lambda shape, dtype: torch.zeros(shape, dtype=dtype)
+    q, kv, pool = (lambda: zeros((2, 4, 30, 64), bf)), (lambda: zeros((2, 2, 30, 64), bf)), (lambda: zeros((6, 2, 16, 64), bf))
+    new, newkv, ws = (lambda: zeros((2, 4, 1, 64), bf)), (lambda: zeros((2, 2, 1, 64), bf)), lambda: torch.zeros(cache.workspace_bytes, dtype=torch.uint8)
+    calls = [
+        (binding.prepare_rotate_prompt, dict(prob=prob, rope=rope), dict(q=q(), k=kv(), q_out=q(), k_out=kv(), positions=zeros((2, 30), i32))),
+        (binding.prepare_attend_prompt, dict(prob=prob), dict(q=q(), k=kv(), v=kv(), out=q(), lse=zeros((2, 4, 30), f32), lse_obs=zeros((2, 4, 4), f32),
+                                                              status=zeros((1,), i32))),
+        (binding.prepare_append_kv_paged, dict(cache=cache, rope=rope),
+         dict(k_new=newkv(), v_new=newkv(), lengths=zeros(units, i32), k_pool=pool(), v_pool=pool(), q=new(), q_out=new(), positions=zeros((2, 1), i32),
+              lengths_out=zeros(units, i32), row_positions=zeros(rows, i32), row_weights=zeros(rows, f32))),
+        (binding.prepare_attend_paged, dict(cache=cache),
+         dict(q=new(), k_pool=pool(), v_pool=pool(), lengths=zeros(units, i32), out=new(), workspace=ws(), lse=zeros((2, 4, 1), f32),
+              weights_in=zeros(rows, f32), weights_out=zeros(rows, f32))),
+        (binding.prepare_evict_kv_paged, dict(cache=cache, budget=3, recent=1),
+         dict(k_pools=[pool()], v_pools=[pool()], weights=zeros(rows, f32), positions=zeros(rows, i32), lengths=zeros(units, i32),
+              weights_out=zeros(rows, f32), positions_out=zeros(rows, i32), lengths_out=zeros(units, i32), workspace=ws(), budgets=zeros((2,), i32))),
+    ]
+    away = lambda t: [x.to("meta") for x in t] if isinstance(t, list) else t.to("meta")
+    for fn, fixed, tensors in calls:
+        fn(**fixed, **tensors, stream=0)
+        for name in tensors:
+            with pytest.raises(ValueError, match="expected, got one on meta"):
+                fn(**fixed, **{**tensors, name: away(tensors[name])}, stream=0)
+    with pytest.raises(ValueError, match="on cpu expected, got one on meta"):
+        far = binding.Rope(64, device=torch.device("cpu"))
+        far.turns = far.turns.to("meta")
+        binding.prepare_rotate_prompt(prob, far, q(), None, q(), None, stream=0)
+    seed = dict(window_idx=zeros((2, 2, prob.k_max), i32), token_scores=zeros((2, 2, 26), f32), positions=zeros((2, 2, 30), i32), weights=zeros((2, 2, 30), f32))
+    for name in seed:
+        with pytest.raises(ValueError, match="got one on meta"):
+            binding.wkv_seed_rows(prob, **{**seed, name: seed[name].to("meta")}, stream=0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    binding._check_devices(torch.device("cuda", 0), "call", None, 12)
+    with pytest.raises(ValueError, match="current device is cuda:0"):
+        binding._check_devices(torch.device("cuda", 1), "call")
