@@ -738,6 +738,8 @@ def prepare_attend_prompt(prob: Problem, q, k, v, out, lse=None, lse_obs=None, s
         _check_kv_layout(prob, t, what)
     _check_state(lse, (s.batch, s.n_q_heads, s.max_seqlen), "float32", "lse")
     _check_state(lse_obs, (s.batch, s.n_q_heads, s.l_obs), "float32", "lse_obs")
+    if hasattr(status, "numel") and (str(status.dtype) != "torch.int32" or status.numel() < 1):
+        raise ValueError(f"status: int32 expected, got {tuple(status.shape)} of {status.dtype}")
     qs, os_ = _head_strides(q, prob.packed, "q"), _head_strides(out, prob.packed, "out")
     args = (ctypes.byref(s), _ptr(q), qs, _ptr(k), _ptr(v), _ptr(out), os_, _ptr(lse), _ptr(lse_obs), _ptr(status), _stream(stream))
     return PreparedCall(lib().wkv_attend_prompt, "wkv_attend_prompt", args, (prob, q, qs, k, v, out, os_, lse, lse_obs, status))
@@ -856,8 +858,11 @@ def wkv_evict_kv_paged(cache: PagedCache, k_pools, v_pools, weights, positions, 
 def wkv_seed_rows(prob: Problem, window_idx, token_scores, positions, weights, stream=None) -> None:
     """The rows' state behind a gather: positions int32 and weights float [B, H_kv, row_capacity] (either may be None)."""
     _check_devices(prob.budgets_dev.device, "row state", window_idx, token_scores, positions, weights)
+    if positions is None and weights is None:
+        raise ValueError("row state: positions, weights or both")
     capacity = (positions if positions is not None else weights).shape[-1]
     units = (prob.shape.batch, prob.shape.n_kv_heads)
+    _check_state(window_idx, units + (prob.k_max,), "int32", "window_idx")
     _check_state(positions, units + (capacity,), "int32", "positions")
     _check_state(weights, units + (capacity,), "float32", "weights")
     _check_state(token_scores, units + (prob.nr_max,), "float32", "token_scores")

@@ -374,3 +374,20 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     binding._check_devices(torch.device("cuda", 0), "call", None, 12)
     with pytest.raises(ValueError, match="current device is cuda:0"):
         binding._check_devices(torch.device("cuda", 1), "call")
+
+
+def test_binding_refuses_status_and_indices_of_other_types():
+    import torch
+    prob = problem()
+    q, kv = torch.zeros((2, 4, 30, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 30, 64), dtype=torch.bfloat16)
+    for bad in (torch.zeros(1, dtype=torch.uint8), torch.zeros(1), torch.zeros(0, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="status"):
+            binding.prepare_attend_prompt(prob, q, kv, kv, q.clone(), status=bad, stream=0)
+    binding.prepare_attend_prompt(prob, q, kv, kv, q.clone(), status=torch.zeros(3, dtype=torch.int32)[1:], stream=0)
+    positions = torch.zeros((2, 2, 30), dtype=torch.int32)
+    idx = torch.zeros((2, 2, prob.k_max), dtype=torch.int32)
+    for bad in (idx.long(), idx[..., :-1].contiguous(), idx.float()):
+        with pytest.raises(ValueError, match="window_idx"):
+            binding.wkv_seed_rows(prob, bad, None, positions, None, stream=0)
+    with pytest.raises(ValueError, match="positions, weights"):
+        binding.wkv_seed_rows(prob, idx, None, None, None, stream=0)
