@@ -647,6 +647,8 @@ def _head_strides(t, packed: bool, what: str):
 def _check_heads(t, heads: int, prob_dtype, head_dim: int, packed: bool, batch: int, tokens: int, what: str) -> None:
     """Shape and type of a [B, heads, tokens, d] or packed [T, heads, d] tensor: the C side sees an address and strides only."""
     want = (tokens, heads, head_dim) if packed else (batch, heads, tokens, head_dim)
+    if t is None:
+        raise ValueError(f"{what}: {want} of {prob_dtype} expected, got None")
     if tuple(t.shape) != want or t.dtype != prob_dtype:
         raise ValueError(f"{what}: {want} of {prob_dtype} expected, got {tuple(t.shape)} of {t.dtype}")
 
@@ -799,11 +801,12 @@ def wkv_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_pool
 def prepare_attend_paged(cache: PagedCache, q, k_pool, v_pool, lengths, out, workspace, lse=None, weights_in=None, weights_out=None,
                          stream=None) -> PreparedCall:
     """Attention of the new tokens over the cache (their own rows, the last of lengths[b, h], included): q, out [B, H_q, max_new, d]
-    or packed [T, H_q, d]; lse float [B, H_q, max_new]; weights float [B, H_kv, capacity], weights_out may be weights_in."""
+    or packed [T, H_q, d] (None where T = 0); lse float [B, H_q, max_new]; weights float [B, H_kv, capacity], weights_out may be weights_in."""
     s, tokens = cache.shape, _chunk_tokens(cache)
     _check_devices(cache.device, "paged attention", q, k_pool, v_pool, lengths, out, workspace, lse, weights_in, weights_out)
     for t, what in ((q, "q"), (out, "out")):
-        _check_heads(t, s.n_q_heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
+        if t is not None or not cache.packed or tokens > 0:
+            _check_heads(t, s.n_q_heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
     _check_pool(cache, k_pool, "k_pool")
     _check_pool(cache, v_pool, "v_pool")
     units = (s.batch, s.n_kv_heads)

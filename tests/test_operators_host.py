@@ -384,6 +384,8 @@ def test_binding_refuses_status_and_indices_of_other_types():
         with pytest.raises(ValueError, match="status"):
             binding.prepare_attend_prompt(prob, q, kv, kv, q.clone(), status=bad, stream=0)
     binding.prepare_attend_prompt(prob, q, kv, kv, q.clone(), status=torch.zeros(3, dtype=torch.int32)[1:], stream=0)
+    with pytest.raises(ValueError, match="None"):
+        binding.prepare_attend_prompt(prob, None, kv, kv, q.clone(), stream=0)
     positions = torch.zeros((2, 2, 30), dtype=torch.int32)
     idx = torch.zeros((2, 2, prob.k_max), dtype=torch.int32)
     for bad in (idx.long(), idx[..., :-1].contiguous(), idx.float()):
@@ -391,3 +393,18 @@ def test_binding_refuses_status_and_indices_of_other_types():
             binding.wkv_seed_rows(prob, bad, None, positions, None, stream=0)
     with pytest.raises(ValueError, match="positions, weights"):
         binding.wkv_seed_rows(prob, idx, None, None, None, stream=0)
+
+
+def test_binding_takes_a_chunk_of_nothing_without_tensors():
+    import torch
+    table, n = torch.zeros((2, 4), dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32)
+    pool, q = torch.zeros((6, 2, 16, 64), dtype=torch.bfloat16), torch.zeros((2, 4, 1, 64), dtype=torch.bfloat16)
+    args = dict(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=16, num_pages=6, block_table=table)
+    empty, some, dense = (binding.PagedCache(**args, **kw) for kw in (dict(cu_new=[0, 0, 0]), dict(cu_new=[0, 0, 1]), {}))
+    ws = empty.alloc_workspace()
+    binding.prepare_attend_paged(empty, None, pool, pool, n, None, ws, stream=0)
+    binding.prepare_append_kv_paged(empty, None, None, n, pool, pool.clone(), stream=0)
+    for cache in (some, dense):
+        for q_, out in ((None, q), (q, None)):
+            with pytest.raises(ValueError, match="expected, got"):
+                binding.prepare_attend_paged(cache, q_, pool, pool, n, out, ws, stream=0)
