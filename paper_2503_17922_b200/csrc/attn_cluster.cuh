@@ -42,9 +42,9 @@ __device__ __forceinline__ void store_four(__nv_bfloat16 *p, float a, float b, f
 }
 
 // By all threads of all blocks of the cluster (1 .. kClusterSplits blocks, whose rank is their split): `n` rows from row0 on, m, l [n] and
-// o [n][stride] in shared memory at the same places in all of them, m in base 2, o relative to m.  With a.logits (16 rows at most) the block also adds up
+// o [n][stride] in shared memory at the same places in all of them, m in base 2, o relative to m.  With WEIGHTS and a.logits (16 rows at most) the block also adds up
 // the weights of the keys [key0, key1), whose logits it has written.  lse2 [16]: shared memory.
-template <typename T, int THREADS>
+template <typename T, int THREADS, bool WEIGHTS>
 __device__ __forceinline__ void cluster_join(const AttnArgs &a, const AttnSeq &sq, int unit, int b, int h, int row0, int n, int rank, const float *m,
                                              const float *l, const float *o, int stride, float *lse2, int key0, int key1)
 {
@@ -86,7 +86,7 @@ __device__ __forceinline__ void cluster_join(const AttnArgs &a, const AttnSeq &s
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         store_four(static_cast<T *>(a.out) + (sq.q_off + i) * a.ot + b * a.ob + (long long)hq * a.oh + c, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
     }
-    if (a.logits) {
+    if (WEIGHTS && a.logits) {
         if ((int)threadIdx.x < n) {
             const int r = threadIdx.x;
             float mm[kClusterSplits], ll[kClusterSplits], top = -INFINITY, sum = 0.f;
@@ -106,15 +106,24 @@ __device__ __forceinline__ void cluster_join(const AttnArgs &a, const AttnSeq &s
         const float *x = a.logits + ((long long)unit * a.rows_max + row0) * a.logit_stride;
         for (int j = key0 + (int)threadIdx.x * 2; j < key1; j += THREADS * 2) {
             float w0 = 0.f, w1 = 0.f;
+            bool nan = false;
 #pragma unroll 4
             for (int r = 0; r < n; ++r) {
                 const float ref = lse2[r];
                 const float2 s = *reinterpret_cast<const float2 *>(x + r * a.logit_stride + j);
-                if (ref == -INFINITY) continue;                          // the row attends to nothing
-                // (a row that is NaN has no weight for keys that it does not see)
-                w0 += s.x == -INFINITY ? 0.f : exp2f(s.x - ref);
-                w1 += s.y == -INFINITY ? 0.f : exp2f(s.y - ref);
+                nan |= ref != ref;
+                if (!(fabsf(ref) < INFINITY)) continue;                  // the row has no weight, or is NaN
+                w0 += exp2f(s.x - ref);
+                w1 += exp2f(s.y - ref);
             }
+            if (nan)                                                     // a NaN for the keys that such a row sees: the others' logits are -infinity
+                for (int r = 0; r < n; ++r) {
+                    const float ref = lse2[r];
+                    if (ref == ref) continue;
+                    const float2 s = *reinterpret_cast<const float2 *>(x + r * a.logit_stride + j);
+                    if (s.x != -INFINITY) w0 = ref;
+                    if (s.y != -INFINITY) w1 = ref;
+                }
             const long long at = (long long)unit * a.cap + j;
             a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + w0;
             if (j + 1 < key1) a.weights_out[at + 1] = (a.weights_in ? a.weights_in[at + 1] : 0.f) + w1;

@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
                 sm.m[0][tid] = top;
                 sm.l[0][tid] = sum;
             }
-            cluster_join<__nv_bfloat16, kThreads>(a, sq, unit, b, h, row0, live, split, sm.m[0], sm.l[0], all, kPad, sm.lse2, t0 * kKeys,
+            cluster_join<__nv_bfloat16, kThreads, true>(a, sq, unit, b, h, row0, live, split, sm.m[0], sm.l[0], all, kPad, sm.lse2, t0 * kKeys,
                                                   min(t1 * kKeys, sq.n));
         }
     } else {

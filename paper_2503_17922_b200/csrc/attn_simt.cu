@@ -4,8 +4,8 @@
 //
 // Bound by the reads of shared memory (80 % of their peak at 4,096 tokens): 16 bytes to every thread of a warp take four cycles whatever
 // the addresses, so that 64 products per thread cost 32 of them with 4 rows to a thread and 24 with 8.  32 heads on 8 of 4,096
-// tokens: d = 64 1,890 us (36 TFLOP/s; with 8 rows 2,110, a block per SM then instead of two), d = 128 3,400 us with 8 rows
-// (40 TFLOP/s; 4,650 with 4).
+// tokens: d = 64 1,815 us (38 TFLOP/s; with 8 rows about an eighth more, a block per SM then instead of two), d = 128 3,440 us with 8 rows
+// (40 TFLOP/s; about 4,700 with 4).
 //
 // ROWS is the largest of 128 (d above 64), 64, 32 and 16 that gives nearly every SM a block.  A prompt without enough of them has its keys split over
 // the blocks of a cluster; paged rows are split by the caller.
@@ -273,10 +273,12 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
             }
         }
         __syncwarp();                                                    // a row's 16 threads are in one warp
-        // what stands behind a row's position may be infinite or NaN: 0 times it is not 0 (rows without a page are zeros)
+        // What stands behind a row's position may be infinite or NaN, and 0 times that is not 0: tiles with such rows go by the rows' limits
+        // (a weight of 0 would leave out a seen infinity too; rows without a page are zeros), as far as any row sees them.
         auto product = [&](auto skip_unseen) {
-#pragma unroll 2
-            for (int j = 0; j < kKeys; j += 4) {
+            const int end = decltype(skip_unseen)::value ? min(kKeys, most - j0) : kKeys;
+#pragma unroll (decltype(skip_unseen)::value ? 1 : 2)
+            for (int j = 0; j < end; j += 4) {
                 float4 pp[RT];
 #pragma unroll
                 for (int r = 0; r < RT; ++r) pp[r] = *reinterpret_cast<const float4 *>(&sm.p[ty * RT + r][j]);
@@ -322,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
 #pragma unroll
             for (int x = 0; x < CT; ++x) *reinterpret_cast<float4 *>(all + (ty * RT + r) * (DP + 4) + tx * 4 + 64 * x) = columns(r, x);
         }
-        cluster_join<float, kThreads>(a, sq, unit, b, h, row0, min(ROWS, rows - row0), split, sm.m, sm.l, all, DP + 4, sm.lse2, t0 * kKeys,
+        cluster_join<float, kThreads, ROWS == 16>(a, sq, unit, b, h, row0, min(ROWS, rows - row0), split, sm.m, sm.l, all, DP + 4, sm.lse2, t0 * kKeys,
                                       min(t1 * kKeys, sq.n));
         return;
     }
@@ -511,18 +513,27 @@ __global__ void __launch_bounds__(kThreads) attn_join_weights_kernel(const __gri
     join_rows<T>(a, sm, sq, unit, b, h, 0, rows, false);
     if (j >= sq.n) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
+    bool nan = false;
     const float *x = a.logits + (long long)unit * a.rows_max * a.logit_stride + j;
 #pragma unroll 4
     for (int row = 0; row < rows; ++row) {
         const float ref = sm.lse2[row];
-        if (ref == -INFINITY) continue;                                  // the row attends to nothing
+        nan |= ref != ref;
+        if (!(fabsf(ref) < INFINITY)) continue;                          // the row has no weight, or is NaN
         const float4 s = *reinterpret_cast<const float4 *>(x + row * a.logit_stride);
-        // (a row that is NaN has no weight for keys that it does not see)
-        w[0] += s.x == -INFINITY ? 0.f : exp2f(s.x - ref);
-        w[1] += s.y == -INFINITY ? 0.f : exp2f(s.y - ref);
-        w[2] += s.z == -INFINITY ? 0.f : exp2f(s.z - ref);
-        w[3] += s.w == -INFINITY ? 0.f : exp2f(s.w - ref);
+        w[0] += exp2f(s.x - ref);
+        w[1] += exp2f(s.y - ref);
+        w[2] += exp2f(s.z - ref);
+        w[3] += exp2f(s.w - ref);
     }
+    if (nan)                                                             // a NaN for the keys that such a row sees: the others' logits are -infinity
+        for (int row = 0; row < rows; ++row) {
+            const float ref = sm.lse2[row];
+            if (ref == ref) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (x[row * a.logit_stride + e] != -INFINITY) w[e] = ref;
+        }
     const long long at = (long long)unit * a.cap + j;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
