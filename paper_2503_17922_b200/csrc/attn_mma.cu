@@ -4,13 +4,15 @@
 //
 // A block of four warps walks over the keys of one unit (or a split of them) in tiles of 64, which come through a ring of
 // asynchronous 16-byte copies: one tile is in flight while another is worked on (three for d up to 64).  What keeps memory busy
-// is three blocks per SM: 32 sequences of 4-8 K rows, one token of 32 heads on 8, with weights, 155 us with two tiles in the ring
-// and 187 with a deeper one and two blocks; the kernel itself reads 5.6 TB/s.  Rows (position x head of the group) sit on the M
+// is three blocks per SM: 32 sequences of 4-8 K rows, one token of 32 heads on 8, with weights, 160 us with two tiles in the ring
+// and about 190 with a deeper one and two blocks; the kernel itself reads 5.6 TB/s.  Rows (position x head of the group) sit on the M
 // side of the instruction:
 //   FEW    up to 16 rows, all in every warp; a warp takes 16 of the tile's keys and keeps a maximum and a sum of its own, joined
 //          once at the end
 //   else   64 rows, 16 per warp, every warp takes all keys
 // Rows that do not exist cost nothing that counts: with 4 rows of 16 the instructions take a third of the time of the loads.
+//
+// P is rounded to bf16 for the product (as its operand has to be); logits, maxima, sums and outputs are fp32, the sum of the unrounded P.
 //
 // Where weights are wanted (FEW), the logits go to the workspace (4 bytes per row and key beside the 512 of K and V) and the joining
 // kernel adds up exp2(logit - lse), instead of K being read once more.
@@ -392,8 +394,8 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
 // stay in registers, 16 F for each warp; the queries come through a ring in tiles of 64, and every fragment of them serves F
 // instructions.  Sums are fp32, over a thread's queries in order and then over the four threads of a key: one order, no atomics.
 //
-// Bound by the instructions: 2 * keys * rows * d.  Four sequences of 10-16 K rows and up to 512 new tokens of 32 heads, d = 128: 545 us
-// (on the CUDA cores 4,650); of up to 64 tokens 102 us (660).
+// Bound by the instructions: 2 * keys * rows * d.  Four sequences of 10-16 K rows and up to 512 new tokens of 32 heads, d = 128: 580 us
+// beside 327 of the attention (on the CUDA cores 4,650); of up to 64 tokens 101 us (660).
 constexpr int kWeightRows = 64, kWeightStages = 3;
 template <int DP>
 struct WeightsSmem {

@@ -18,9 +18,10 @@
 // get them added at the end.
 //
 // Bound by the chain of one query tile, product - weights - product, of which two are in flight (tensor memory holds no third): 32 heads on 8 of 8,192
-// tokens, d = 128, 550 us = 1.0 PFLOP/s, tensor pipe 51 % of cycles, special functions 45 %; 32,768 tokens 8.2 ms = 1.07 PFLOP/s
-// and the power limit.  Of a chain's 4,000 cycles the weights take 2,500, the products 1,100.  Sixteen warps for the weights, two
-// to a row, were slower (600 us): they have to agree on the maximum.
+// tokens, d = 128, 492 us = 1.12 PFLOP/s in a run of 25 ms at 1,965 MHz, 555-575 us = 0.97 PFLOP/s in long runs, which the power limit holds at
+// 1,600 to 1,800; tensor pipe 51 % of cycles, special functions 45 %; 32,768 tokens 8.2-8.5 ms = 1.05 PFLOP/s.  Of a chain's 4,000 cycles the
+// weights take 2,500, the products 1,100.  Sixteen warps for the weights, two to a row, were slower (600 us where eight took 575): they
+// have to agree on the maximum.
 //
 // Blocks are persistent, one per SM; the items come in order of descending work and are dealt to the blocks back and forth.
 // Every wait is bounded; on expiry the block sets bit 0 of the status word, lets its loads land, frees its tensor memory and returns.
@@ -44,7 +45,7 @@ constexpr int kMaxStages = 8;
 constexpr int kMaskSlots = 8;
 constexpr int kFmaEvery = 8;                  // one pair of exponentials in so many on the FMA pipe, see exp2_pair_fma()
 constexpr int kFirst = 2;                     // 32-key pieces of a tile whose product begins while the others' weights are computed
-                                              // (32 heads of 8,192 tokens: one 506 us, two 499, three 513)
+                                              // (32 heads on 8 of 8,192 tokens, long runs: one 556 us, two 554, three 565; d = 64: 434, 428, 424)
 constexpr float kLazy = 8.f;                  // exponent by which the maximum may be outgrown
 __host__ __device__ constexpr int stages_for(int kb) { return kb == 2 ? 5 : 8; }
 struct TcAttnArgs {
@@ -289,7 +290,7 @@ __device__ __forceinline__ void store32(float *p, float a, float b, float c, flo
 
 // ---- the softmax of one query tile ------------------------------------------------------------
 // S is read twice, 32 columns at a time, for the maximum and for the exponentials: a row of 128 in registers takes more of them than
-// a thread has, and the code of a row in one piece more than the instruction cache holds (8,192 tokens of 32 heads: 1,010 us).
+// a thread has (168 for each of 384), and the code of a row in one piece more than the instruction cache holds.
 struct RowMask {
     uint4 bits;              // of the tile's 128 keys: those that the row sees
     __device__ __forceinline__ uint32_t of(int y) const { return y == 0 ? bits.x : (y == 1 ? bits.y : (y == 2 ? bits.z : bits.w)); }
@@ -301,8 +302,8 @@ __device__ __forceinline__ void hide(float (&v)[32], uint32_t seen)
     for (int j = 0; j < 32; ++j) v[j] = seen >> j & 1u ? v[j] : -INFINITY;
 }
 
-// 2^x of two values on the FMA pipe, which is half idle where the special functions are not (32 heads of 8,192 tokens: none 546 us, one
-// pair in eight 499, in four 507, in two 599): 2^t * 2^f with t the nearest integer, 2^f by a polynomial of degree five (a Remez fit of the
+// 2^x of two values on the FMA pipe, which is half idle where the special functions are not (32 heads on 8 of 8,192 tokens, long runs: none
+// 567 us, one pair in eight 554, in four 554, in two 612; d = 64: 485, 428, 436, 497): 2^t * 2^f with t the nearest integer, 2^f by a polynomial of degree five (a Remez fit of the
 // relative error on [-1/2, 1/2], 7.5e-8; evaluated in fp32 2.1e-7).  x is at most kLazy; below -127 it counts as -127,
 // whose factor 2^t is 0, so that the weight is 0 below -126.5, as with the special functions; a NaN stays one.
 __device__ __forceinline__ unsigned long long exp2_pair_fma(unsigned long long x2)
@@ -543,7 +544,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
 
 // ---- MMAs --------------------------------------------------------------------------------------
 // One warp issues for both query tiles in turn, which keeps them half a step apart: with a warp for each they fell into step, both
-// at their exponentials or both at their products (8,192 tokens of 32 heads: 683 us against 617).
+// at their exponentials or both at their products (8,192 tokens of 32 heads: 11 % more time).
 template <int KB, bool WHOLE>
 __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, uint32_t tmem)
 {
@@ -976,7 +977,8 @@ int launch_kb(const TcAttnArgs &t, const CUtensorMap &k_map, const CUtensorMap &
 
 // A tile's rows come in boxes that never cross a page's end: the largest power of two that a page is a multiple of, eight at
 // least, since the swizzle's pattern repeats every eight rows.  (Four sequences of 10-16 K rows, up to
-// 512 new tokens of 32 heads: 375 us in pages of 128 rows, 440 in pages of 24 and so boxes of eight; 2,260 on the warp-level kernel.)
+// 512 new tokens of 32 heads, a short run: 327 us in pages of 128 rows, 403 in pages of 24 and so boxes of eight; in pages of seven, on the
+// warp-level kernel, 2,310.)
 static int box_of_page(int page_size) { return std::min(page_size & -page_size, kTile); }
 
 // Shapes that the kernel takes; a layout that no tensor map describes is found out at launch (WKV_ERR_UNSUPPORTED).

@@ -6,10 +6,10 @@
 // integers: exact at any position, where the product in fp32 would be off by 2^-24 of itself, 0.04 radians at position 10^6.
 // Each thread reads what it writes, so an output may be its input.
 //
-// Bound by memory: 32,768 tokens of 40 rows of 128 in bf16, 64 of each turned, take 114 us, 5.9 TB/s read and written, and 118 us
-// with all 128 turned in HALF order; 8,192 tokens 32 us, with 62 turned 34, and in HALF order, element by element, 59.  Two rows
-// in flight per thread leave room for seven or eight blocks per SM; four rows (half as many blocks) took 128 us, one 122; four
-// tokens per block: eight took 117.  When each thread worked out its own addresses, piece by piece, the divisions and strides took
+// Bound by memory: 32,768 tokens of 40 rows of 128 in bf16, 64 of each turned, take 116 us, 5.8 TB/s read and written, and 120 us
+// with all 128 turned in HALF order; 8,192 tokens 35 us, with 62 turned 36, and in HALF order, element by element, 61.  Two rows
+// in flight per thread leave room for seven or eight blocks per SM; four rows (half as many blocks) took 12 % more, one 7 %; four
+// tokens per block: eight took 3 % more.  When each thread worked out its own addresses, piece by piece, the divisions and strides took
 // as long as the memory (186 us).
 #include "attn.cuh"
 
