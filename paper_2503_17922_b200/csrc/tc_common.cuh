@@ -90,6 +90,31 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     }
 }
 
+// A whole warp waits.  The phase is looked at without suspending the thread: a suspended one came back as much as 2,000 cycles
+// after the phase had completed, and the MMA warp waits five times per key tile.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    const uint32_t addr = smem_u32(bar);
+    unsigned long long t0 = 0;
+    for (uint32_t it = 1;; ++it) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                     "selp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok)
+                     : "r"(addr), "r"(parity)
+                     : "memory");
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if ((it & 1023u) == 0u) {
+            const unsigned long long now = global_timer_ns();
+            const bool over = t0 != 0 && now - t0 > kWaitLimitNs;
+            if (t0 == 0) t0 = now;
+            if (over) *abort_flag = 1;
+            if (__any_sync(0xffffffffu, over || *abort_flag)) return false;
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------
 // TMA (tiled, no multicast) and proxy fences
 // ---------------------------------------------------------------------------------

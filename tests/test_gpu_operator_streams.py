@@ -106,3 +106,24 @@ def test_two_graphs_that_share_a_workspace_in_turn():
     torch.cuda.synchronize()
     for x, w in zip((a, b), want):
         assert all(same(s, t) for s, t in zip(outputs(x), w))
+
+
+def test_the_attention_kernels_wait_ends(tmp_path):
+    """For a barrier that nobody arrives at, after its limit, in all warps of the block, and the context goes on."""
+    import ctypes
+    import os
+    import subprocess
+    from paper_2503_17922_b200 import build
+    so = str(tmp_path / "libwaits.so")
+    subprocess.check_call([build._nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-Xcompiler", "-fPIC", "-shared", "-I", build.CSRC,
+                           "-o", so, os.path.join(os.path.dirname(os.path.abspath(__file__)), "warp_wait.cu")])
+    result, ns = torch.full((128,), -1, dtype=torch.int32, device="cuda"), torch.zeros(128, dtype=torch.int64, device="cuda")
+    abort = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    ptr = lambda t: ctypes.c_void_p(t.data_ptr())
+    assert ctypes.CDLL(so).run_waits(ptr(result), ptr(ns), ptr(abort), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+    torch.cuda.synchronize()
+    assert (result == 1).all() and int(abort) == 1                        # the complete barrier is seen, the other is not
+    assert 0.5e9 < int(ns.min()) and int(ns.max()) < 3e9                  # the limit is one second
+    a = Attend("bf16", 8, 2, 128, 16, "phsd", [[300, 299]], [20], False)
+    a.run()
+    a.check()
