@@ -364,7 +364,7 @@ def _handles(c, s):
                  cu_new=s["cu"] if c["op"] != "fill" else None, layout=c["layout"], **shape)
     if c["cache"] == "plain":
         cache = wkv.PagedCache(**paged)
-        return [wkv.prepare_attend_tree_paged(cache, s["masks"], s["q"], s["k_pool"], s["v_pool"], s["lengths"], s["q_out"],
+        return [wkv.prepare_attend_draft_paged(cache, s["masks"], s["q"], s["k_pool"], s["v_pool"], s["lengths"], s["q_out"],
                                               cache.alloc_workspace(), lse=s["lse"])]
     cache = wkv.PagedCache8(kind=c["cache"], **paged)
     layers = [wkv.Layer8(cache, k, v, k_scales, v_scales) for (k, v), (k_scales, v_scales) in zip(s["codes"], s["scales"])]
@@ -376,7 +376,7 @@ def _handles(c, s):
                                              lengths_out=s["lengths_out"], **more),
                 wkv.prepare_read_kv_paged8(cache, layers[0], s["lengths_out"], s["rows"][0], s["rows"][1], first=s["lengths"])]
     return [wkv.prepare_attend_paged8(cache, layers[0], s["q"], s["lengths"], s["q_out"], cache.alloc_workspace(), lse=s["lse"],
-                                      weights_in=s.get("weights"), weights_out=s.get("weights_out"), tree=s.get("masks"))]
+                                      weights_in=s.get("weights"), weights_out=s.get("weights_out"), draft=s.get("masks"))]
 
 
 # ---- one pass ----------------------------------------------------------------------------------
