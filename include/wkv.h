@@ -565,6 +565,137 @@ int wkv_seed_rows(const wkv_shape *s, const int32_t *window_idx, const float *to
                   int32_t *positions, float *weights, void *cuda_stream);
 
 /*
+ * ---- norms with rotary positions, a cache of 8-bit rows, drafted tokens ----
+ *
+ * Per-head norms of queries and keys and rotary positions in one pass: each row x of d = head_dim elements becomes
+ *   y = x / sqrt(mean(x^2) + eps) * (weight + offset)        (not with a norm of NULL)
+ * and then its first rot_dim dimensions are turned (not with a rope of NULL); in fp32 throughout, rounded once at the end.
+ */
+typedef struct {
+    uint32_t struct_size;      /* sizeof(wkv_head_norm), checked */
+    float eps;                 /* finite, >= 0; a row of zeros with eps 0 gives NaN */
+    float offset;              /* added to the weights (1 where they are kept as what they differ from 1 by), finite */
+    int32_t reserved;          /* must be 0 */
+    const void *q_weight;      /* DEVICE [head_dim] of the tensors' type, or NULL: ones (and no offset) */
+    const void *k_weight;
+} wkv_head_norm;
+/* Positions with several axes (time, height, width): pair i turns by the position along axis[i].  Positions of axis x stand
+ * position_stride elements behind those of axis x - 1.  An entry of `axis` outside 0 .. n_axes - 1 turns its pair by nothing. */
+typedef struct {
+    uint32_t struct_size;      /* sizeof(wkv_rope_axes), checked */
+    int32_t n_axes;            /* >= 1 */
+    const int32_t *axis;       /* DEVICE [rot_dim/2] */
+    int64_t position_stride;   /* >= the positions of one axis */
+} wkv_rope_axes;
+
+/*
+ * The prompt's queries and keys: as wkv_rotate_prompt, with norms and axes.  norm, rope and axes may each be NULL, but not both norm
+ * and rope; axes only with rope, and then with positions.  head_dim up to 256.
+ */
+int wkv_norm_rotate_prompt(const wkv_shape *s, const wkv_head_norm *norm, const wkv_rope *rope, const wkv_rope_axes *axes,
+                           const void *q, void *q_out, const int64_t *q_strides, const void *k, void *k_out,
+                           const int32_t *positions, void *cuda_stream);
+/* New tokens into the cache: as wkv_append_kv_paged, with norms (of queries and keys) and axes; row_positions takes those of axis 0. */
+int wkv_norm_append_kv_paged(const wkv_paged *c, const wkv_head_norm *norm, const wkv_rope *rope, const wkv_rope_axes *axes,
+                             const void *k_new, const void *v_new, const int64_t *kv_strides, const void *q, void *q_out,
+                             const int64_t *q_strides, const int32_t *positions, const int32_t *lengths, void *k_pool, void *v_pool,
+                             int32_t *lengths_out, int32_t *row_positions, float *row_weights, void *cuda_stream);
+
+/*
+ * A paged cache of 8-bit rows.  A row of head_dim elements is head_dim codes and one scale 2^e, kept as the byte e + 127:
+ *   element = code * 2^e,   e the least number >= -100 with max |x| <= M 2^e,   code = x / 2^e rounded to nearest, ties to even
+ * with M = 448 (WKV_CACHE_E4M3: 8-bit floats of four exponent and three mantissa bits) or 127 (WKV_CACHE_I8: integers).  So what
+ * a row stands for is exact in bf16 and fp32.  e stops at 100 (codes of larger rows at M).  A row with an infinity or NaN gets
+ * the scale byte 255, which reads as NaN whatever the codes; an E4M3 code of 0x7f or 0xff, which no call writes, is NaN too.
+ * wkv_paged describes the cache as before; its strides are those of the pools of codes, in bytes, and `dtype` is the type of queries,
+ * new keys and values, and outputs.  Scales: [num_pages, n_kv_heads, page_size], contiguous.  head_dim is a multiple of 16, up to 256.
+ */
+typedef enum { WKV_CACHE_E4M3 = 0, WKV_CACHE_I8 = 1 } wkv_cache8_type;
+typedef struct {
+    uint32_t struct_size;      /* sizeof(wkv_cache8), checked */
+    int32_t type;              /* wkv_cache8_type */
+    void *k_codes, *v_codes;   /* DEVICE pools of codes of one layer */
+    uint8_t *k_scales, *v_scales;   /* DEVICE */
+} wkv_cache8;
+/* As wkv_paged_workspace_bytes, for the calls on an 8-bit cache. */
+size_t wkv_paged8_workspace_bytes(const wkv_paged *c);
+
+/* New tokens into the cache, quantised as they are written: as wkv_norm_append_kv_paged; norm, rope and axes may be NULL. */
+int wkv_append_kv_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_head_norm *norm, const wkv_rope *rope,
+                         const wkv_rope_axes *axes, const void *k_new, const void *v_new, const int64_t *kv_strides, const void *q,
+                         void *q_out, const int64_t *q_strides, const int32_t *positions, const int32_t *lengths,
+                         int32_t *lengths_out, int32_t *row_positions, float *row_weights, void *cuda_stream);
+/*
+ * The gather behind the selection (wkv_gather_kv_paged) into an 8-bit cache: `c` describes it (its max_new and cu_new are not used; batch,
+ * n_kv_heads, head_dim and dtype as in `s`), layers: HOST array [n_layers], all of one type.  v_layers may be NULL (then v_codes and
+ * v_scales are not used).  max_pages * page_size must cover wkv_keep_max().
+ */
+int wkv_gather_kv_paged8(const wkv_shape *s, const wkv_paged *c, int32_t n_layers, const void *const *k_layers,
+                         const void *const *v_layers, const int32_t *window_idx, const wkv_cache8 *layers, void *cuda_stream);
+/*
+ * Rows of the cache read back as what they stand for: row r of k_out and v_out of unit (b, h), r < lengths[b][h] - first[b][h], is the
+ * cache's row first[b][h] + r; rows behind those, and rows without a page, are left as they are.
+ *   first          DEVICE int32 [B, H_kv] or NULL (zeros); negative entries count as 0
+ *   k_out, v_out   DEVICE [B, H_kv, row_capacity, d], contiguous, of out_dtype (wkv_dtype); either may be NULL.  Rows from row_capacity on
+ *                  are not written.
+ */
+int wkv_read_kv_paged8(const wkv_paged *c, const wkv_cache8 *layer, const int32_t *first, const int32_t *lengths, int32_t out_dtype,
+                       int32_t row_capacity, void *k_out, void *v_out, void *cuda_stream);
+/* Rows leave the cache by weight: as wkv_evict_kv_paged, codes and scales of all layers given (HOST array [n_layers], all of one type).
+ * Workspace of wkv_paged8_workspace_bytes(). */
+int wkv_evict_kv_paged8(const wkv_paged *c, int32_t n_layers, const wkv_cache8 *layers, int32_t budget, const int32_t *budgets,
+                        int32_t recent, const float *weights, const int32_t *positions, const int32_t *lengths, float *weights_out,
+                        int32_t *positions_out, int32_t *lengths_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Drafted tokens.  The new tokens of a sequence are a draft whose i-th token attends to all rows in front of the draft and to those of its
+ * tokens that its mask names (its ancestors and itself): bit j % 32 of word j / 32 for token j; bits from the sequence's number of
+ * tokens on do not count.  Any mask will do, also one that names later tokens, or none.
+ */
+#define WKV_MAX_DRAFT 1024
+typedef struct {
+    uint32_t struct_size;      /* sizeof(wkv_draft), checked */
+    int32_t words;             /* of a mask, >= max_new / 32 rounded up; max_new is at most WKV_MAX_DRAFT (WKV_ERR_LIMIT) */
+    const uint32_t *masks;     /* DEVICE [B, max_new, words] or packed [T, words] */
+} wkv_draft;
+/*
+ * Masks of a draft that is a tree: token i hangs on token parents[i] of its sequence, or, where that is not in 0 .. i - 1, on the last
+ * token in front of the draft.
+ *   parents     DEVICE int32 [B, max_new] or [T]
+ *   masks       DEVICE out or NULL, [.., words] as above: ancestors and the token itself; words beyond are zeros
+ *   first       DEVICE int32 [B] or NULL (zeros): position of a sequence's tokens that hang on the last token in front of the draft
+ *   positions   DEVICE out or NULL, int32 as parents: first plus the number of ancestors
+ */
+int wkv_draft_masks(const wkv_paged *c, const int32_t *parents, int32_t words, uint32_t *masks, const int32_t *first,
+                    int32_t *positions, void *cuda_stream);
+/* Attention of drafted tokens over the cache: as wkv_attend_paged, without weights (tokens that are not kept would count). */
+int wkv_attend_draft_paged(const wkv_paged *c, const wkv_draft *draft, const void *q, const int64_t *q_strides, const void *k_pool,
+                           const void *v_pool, const int32_t *lengths, void *out, const int64_t *out_strides, float *lse,
+                           void *workspace, size_t workspace_bytes, void *cuda_stream);
+/* Attention of new tokens over an 8-bit cache: as wkv_attend_paged; with a draft as wkv_attend_draft_paged (weights_in and weights_out
+ * NULL then, WKV_ERR_UNSUPPORTED otherwise).  Workspace of wkv_paged8_workspace_bytes(). */
+int wkv_attend_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_draft *draft, const void *q, const int64_t *q_strides,
+                      const int32_t *lengths, void *out, const int64_t *out_strides, float *lse, const float *weights_in,
+                      float *weights_out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+/*
+ * What is kept of a draft: the tokens that the mask of token last[b] names (its path, itself included), in their order, take the rows
+ * behind those in front of the draft; the others' rows are given up.  With a last[b] that is no token of the sequence none is kept.
+ *   k_pools, v_pools    HOST arrays [n_layers] of DEVICE pool pointers, read and written; v_pools may be NULL
+ *   last                DEVICE int32 [B]
+ *   lengths             DEVICE int32 [B, H_kv]: rows of every unit, the draft's included
+ *   lengths_out         DEVICE out, int32 [B, H_kv]; not `lengths` itself
+ *   row_positions, row_weights   DEVICE or NULL, [B, H_kv, max_pages*page_size]: the rows' state, which moves with them
+ * Rows whose page, or the one they would move to, is none are not moved.
+ */
+int wkv_keep_draft_paged(const wkv_paged *c, const wkv_draft *draft, int32_t n_layers, void *const *k_pools, void *const *v_pools,
+                         const int32_t *last, const int32_t *lengths, int32_t *lengths_out, int32_t *row_positions,
+                         float *row_weights, void *cuda_stream);
+/* The same in an 8-bit cache, codes and scales (layers: HOST array [n_layers], all of one type). */
+int wkv_keep_draft_paged8(const wkv_paged *c, const wkv_draft *draft, int32_t n_layers, const wkv_cache8 *layers, const int32_t *last,
+                          const int32_t *lengths, int32_t *lengths_out, int32_t *row_positions, float *row_weights,
+                          void *cuda_stream);
+
+/*
  * Measurement aid (no counterpart in the paper): launches a kernel that does nothing but evaluate
  * ex2.approx.ftz.f32 (the exponential of Eq. 1 in base 2, the instruction that bounds the score
  * stage) in eight independent chains per thread, `iters` times.  Timing the launch with CUDA events

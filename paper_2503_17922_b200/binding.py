@@ -28,7 +28,9 @@ EXPORTED_SYMBOLS = [
     "wkv_compress_group", "wkv_compress_group_host", "wkv_compress_group_host_rows", "wkv_score_windows_lse", "wkv_compress_group_lse",
     "wkv_select_leader_windows", "wkv_probe_ex2_rate", "wkv_probe_colsum_rate", "wkv_probe_published_select", "wkv_probe_impatient_select", "wkv_group_plan_create", "wkv_group_plan_launch", "wkv_group_plan_destroy", "wkv_status_string", "wkv_last_error_detail",
     "wkv_launch_count", "wkv_rope_frequencies", "wkv_rotate_prompt", "wkv_attend_prompt", "wkv_paged_workspace_bytes", "wkv_append_kv_paged",
-    "wkv_attend_paged", "wkv_evict_kv_paged", "wkv_seed_rows",
+    "wkv_attend_paged", "wkv_evict_kv_paged", "wkv_seed_rows", "wkv_norm_rotate_prompt", "wkv_norm_append_kv_paged",
+    "wkv_paged8_workspace_bytes", "wkv_append_kv_paged8", "wkv_gather_kv_paged8", "wkv_read_kv_paged8", "wkv_evict_kv_paged8",
+    "wkv_draft_masks", "wkv_attend_draft_paged", "wkv_attend_paged8", "wkv_keep_draft_paged", "wkv_keep_draft_paged8",
 ]
 
 
@@ -93,6 +95,49 @@ class WkvPaged(ctypes.Structure):
         ("page_stride", ctypes.c_int64),
         ("head_stride", ctypes.c_int64),
         ("row_stride", ctypes.c_int64),
+    ]
+
+
+class WkvHeadNorm(ctypes.Structure):
+    """Mirror of `wkv_head_norm`."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("eps", ctypes.c_float),
+        ("offset", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+    ]
+
+
+class WkvRopeAxes(ctypes.Structure):
+    """Mirror of `wkv_rope_axes`."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("n_axes", ctypes.c_int32),
+        ("axis", ctypes.c_void_p),
+        ("position_stride", ctypes.c_int64),
+    ]
+
+
+class WkvCache8(ctypes.Structure):
+    """Mirror of `wkv_cache8`."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("type", ctypes.c_int32),
+        ("k_codes", ctypes.c_void_p),
+        ("v_codes", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
+    ]
+
+
+class WkvDraft(ctypes.Structure):
+    """Mirror of `wkv_draft`."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("words", ctypes.c_int32),
+        ("masks", ctypes.c_void_p),
     ]
 
 
@@ -196,6 +241,31 @@ def lib() -> ctypes.CDLL:
     L.wkv_evict_kv_paged.argtypes = [pp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.wkv_seed_rows.restype = ctypes.c_int
     L.wkv_seed_rows.argtypes = [sp, vp, vp, i32, vp, vp, vp]
+    np_, xp, c8, dp = (ctypes.POINTER(x) for x in (WkvHeadNorm, WkvRopeAxes, WkvCache8, WkvDraft))
+    L.wkv_norm_rotate_prompt.restype = ctypes.c_int
+    L.wkv_norm_rotate_prompt.argtypes = [sp, np_, rp, xp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_norm_append_kv_paged.restype = ctypes.c_int
+    L.wkv_norm_append_kv_paged.argtypes = [pp, np_, rp, xp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_paged8_workspace_bytes.restype = sz
+    L.wkv_paged8_workspace_bytes.argtypes = [pp]
+    L.wkv_append_kv_paged8.restype = ctypes.c_int
+    L.wkv_append_kv_paged8.argtypes = [pp, c8, np_, rp, xp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_gather_kv_paged8.restype = ctypes.c_int
+    L.wkv_gather_kv_paged8.argtypes = [sp, pp, i32, vp, vp, vp, c8, vp]
+    L.wkv_read_kv_paged8.restype = ctypes.c_int
+    L.wkv_read_kv_paged8.argtypes = [pp, c8, vp, vp, i32, i32, vp, vp, vp]
+    L.wkv_evict_kv_paged8.restype = ctypes.c_int
+    L.wkv_evict_kv_paged8.argtypes = [pp, i32, c8, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.wkv_draft_masks.restype = ctypes.c_int
+    L.wkv_draft_masks.argtypes = [pp, vp, i32, vp, vp, vp, vp]
+    L.wkv_attend_draft_paged.restype = ctypes.c_int
+    L.wkv_attend_draft_paged.argtypes = [pp, dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.wkv_attend_paged8.restype = ctypes.c_int
+    L.wkv_attend_paged8.argtypes = [pp, c8, dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.wkv_keep_draft_paged.restype = ctypes.c_int
+    L.wkv_keep_draft_paged.argtypes = [pp, dp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.wkv_keep_draft_paged8.restype = ctypes.c_int
+    L.wkv_keep_draft_paged8.argtypes = [pp, dp, i32, c8, vp, vp, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -622,9 +692,12 @@ class PagedCache:
             s.cu_new_host, s.cu_new_dev = self.cu_host.ctypes.data, self.cu_dev.data_ptr()
         self.shape = s
         self.capacity = page_size * block_table.shape[1]
-        self.workspace_bytes = lib().wkv_paged_workspace_bytes(ctypes.byref(s))
+        self.workspace_bytes = self._workspace_bytes()
         if self.workspace_bytes == 0:
             raise WkvError(-1, "wkv_paged", lib().wkv_last_error_detail().decode())
+
+    def _workspace_bytes(self) -> int:
+        return lib().wkv_paged_workspace_bytes(ctypes.byref(self.shape))
 
     def alloc_workspace(self):
         """Scratch; its first int32 is the device status word (see `device_status`)."""
@@ -871,6 +944,342 @@ def wkv_seed_rows(prob: Problem, window_idx, token_scores, positions, weights, s
     _check_state(token_scores, units + (prob.nr_max,), "float32", "token_scores")
     _check(lib().wkv_seed_rows(ctypes.byref(prob.shape), _ptr(window_idx), _ptr(token_scores), capacity, _ptr(positions), _ptr(weights),
                                _stream(stream)), "wkv_seed_rows")
+
+
+# ---- norms with rotary positions, the 8-bit cache, drafted tokens ----
+WKV_CACHE_E4M3, WKV_CACHE_I8 = 0, 1
+WKV_MAX_DRAFT = 1024
+_CACHE8_TYPES = {"e4m3": WKV_CACHE_E4M3, "i8": WKV_CACHE_I8}
+
+
+class HeadNorm:
+    """A `wkv_head_norm`: weights [head_dim] of the tensors' type on the device (kept alive here), or None for ones; `offset` is added to them."""
+
+    def __init__(self, q_weight=None, k_weight=None, *, eps: float = 1e-6, offset: float = 0.0):
+        for t in (q_weight, k_weight):
+            if t is not None and (t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError("norm: contiguous weights [head_dim] expected")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.struct = WkvHeadNorm(ctypes.sizeof(WkvHeadNorm), eps, offset, 0, _ptr(q_weight), _ptr(k_weight))
+
+    def check(self, dtype, head_dim: int) -> None:
+        for t, what in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
+            if t is not None and (t.dtype != dtype or t.shape[0] != head_dim):
+                raise ValueError(f"{what}: [{head_dim}] of {dtype} expected, got {tuple(t.shape)} of {t.dtype}")
+
+
+class RopeAxes:
+    """Which of `n_axes` position axes turns each rotated pair: a list of rot_dim / 2 numbers, kept on the device."""
+
+    def __init__(self, axis: Sequence[int], n_axes: int, device=None):
+        import torch
+        if n_axes < 1 or any(not 0 <= int(a) < n_axes for a in axis):
+            raise ValueError(f"axes: numbers in 0 .. {n_axes - 1} expected")
+        self.n_axes = n_axes
+        self.device = device if device is not None else torch.device("cuda", torch.cuda.current_device())
+        self.axis = torch.tensor([int(a) for a in axis], dtype=torch.int32, device=self.device)
+
+    def at(self, stride: int) -> WkvRopeAxes:
+        return WkvRopeAxes(ctypes.sizeof(WkvRopeAxes), self.n_axes, self.axis.data_ptr(), stride)
+
+
+def _turn_args(norm, rope, axes, positions, shape, dtype, head_dim: int):
+    """The three structs (or None) of a norm with rotary positions, checked; `shape`: that of one axis' positions."""
+    if norm is not None:
+        norm.check(dtype, head_dim)
+    one = int(np.prod(shape))
+    if axes is None:
+        _check_positions(positions, shape)
+        return norm and ctypes.byref(norm.struct), rope and ctypes.byref(rope.struct), None
+    if rope is None:
+        raise ValueError("axes: only with rotary positions")
+    if axes.axis.numel() != rope.struct.rot_dim // 2:
+        raise ValueError(f"axes: one number for each of the {rope.struct.rot_dim // 2} pairs expected, got {axes.axis.numel()}")
+    flat = (axes.n_axes, one)
+    _check_state(positions, flat if positions is not None and positions.dim() == 2 else (axes.n_axes,) + tuple(shape), "int32", "positions")
+    return norm and ctypes.byref(norm.struct), ctypes.byref(rope.struct), ctypes.byref(axes.at(one))
+
+
+def _turn_tensors(norm, rope, axes):
+    return [norm.q_weight if norm is not None else None, norm.k_weight if norm is not None else None, rope.turns if rope is not None else None,
+            axes.axis if axes is not None else None]
+
+
+def prepare_norm_rotate_prompt(prob: Problem, q, k, q_out, k_out, norm: Optional[HeadNorm] = None, rope: Optional[Rope] = None,
+                               axes: Optional[RopeAxes] = None, positions=None, stream=None) -> PreparedCall:
+    """Per-head norms and rotary positions of a prompt in one pass; tensors as in prepare_rotate_prompt.  positions: int32 [T] or [B, N]; with
+    axes [n_axes, T] or [n_axes, B, N]."""
+    s = prob.shape
+    _check_devices(prob.budgets_dev.device, "norms and rotary positions", _turn_tensors(norm, rope, axes), q, k, q_out, k_out, positions)
+    tokens = int(prob.cu_host[-1]) if prob.packed else s.max_seqlen
+    for t, what in ((q, "q"), (q_out, "q_out")):
+        if t is not None:
+            _check_heads(t, s.n_q_heads, prob.torch_dtype, s.head_dim, prob.packed, s.batch, tokens, what)
+    _check_same_layout(q, q_out, "q and q_out")
+    for t, what in ((k, "k"), (k_out, "k_out")):
+        if t is not None:
+            _check_kv_layout(prob, t, what)
+    turn = _turn_args(norm, rope, axes, positions, (tokens,) if prob.packed else (s.batch, s.max_seqlen), prob.torch_dtype, s.head_dim)
+    qs = _head_strides(q, prob.packed, "q")
+    args = (ctypes.byref(s), *turn, _ptr(q), _ptr(q_out), qs, _ptr(k), _ptr(k_out), _ptr(positions), _stream(stream))
+    return PreparedCall(lib().wkv_norm_rotate_prompt, "wkv_norm_rotate_prompt", args, (prob, norm, rope, axes, turn, q, q_out, qs, k, k_out, positions))
+
+
+def wkv_norm_rotate_prompt(prob: Problem, q, k, q_out, k_out, **kw) -> None:
+    prepare_norm_rotate_prompt(prob, q, k, q_out, k_out, **kw).run()
+
+
+class PagedCache8(PagedCache):
+    """A `wkv_paged` whose pools hold codes of 8 bits (`kind`: "e4m3" or "i8"), one scale byte to a row: pools uint8 of the shapes that PagedCache
+    has, strides in bytes; `dtype` is the type of queries, new keys and values, and outputs."""
+
+    def __init__(self, *, kind: str, **kw):
+        self.kind = kind
+        self.type = _CACHE8_TYPES[kind]
+        super().__init__(**kw)
+
+    def _workspace_bytes(self) -> int:
+        return lib().wkv_paged8_workspace_bytes(ctypes.byref(self.shape))
+
+    def alloc_scales(self):
+        """Scales of one pool: uint8 [pages, H_kv, page_size]."""
+        import torch
+        s = self.shape
+        return torch.zeros((s.num_pages, s.n_kv_heads, s.page_size), dtype=torch.uint8, device=self.device)
+
+
+class Layer8:
+    """A `wkv_cache8`: one layer's pools of codes (uint8, or the type that the codes are of) and their scales (uint8 [pages, H_kv, page_size]),
+    kept alive here."""
+
+    def __init__(self, cache: PagedCache8, k_codes, v_codes, k_scales, v_scales):
+        s = cache.shape
+        need = (s.num_pages - 1) * s.page_stride + (s.n_kv_heads - 1) * s.head_stride + (s.page_size - 1) * s.row_stride + s.head_dim
+        for t, what in ((k_codes, "k_codes"), (v_codes, "v_codes")):
+            if t is not None and hasattr(t, "untyped_storage") and (t.element_size() != 1 or t.untyped_storage().nbytes() - t.storage_offset() < need):
+                raise ValueError(f"{what}: {need} bytes of codes expected, got {tuple(t.shape)} of {t.dtype}")
+        for t, what in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+            _check_state(t, (s.num_pages, s.n_kv_heads, s.page_size), "uint8", what)
+        self.tensors = (k_codes, v_codes, k_scales, v_scales)
+        self.type = cache.type
+        self.struct = WkvCache8(ctypes.sizeof(WkvCache8), cache.type, _ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales))
+
+
+def _layers8(layers: Sequence[Layer8]):
+    return (WkvCache8 * len(layers))(*[x.struct for x in layers])
+
+
+def _prepare_append(cache, layer, name, call_pools, k_new, v_new, lengths, q, q_out, positions, norm, rope, axes, lengths_out, row_positions,
+                    row_weights, stream) -> PreparedCall:
+    s, tokens = cache.shape, _chunk_tokens(cache)
+    _check_devices(cache.device, "append", _turn_tensors(norm, rope, axes), layer.tensors if layer is not None else call_pools, k_new, v_new, lengths, q,
+                   q_out, positions, lengths_out, row_positions, row_weights)
+    for t, heads, what in ((k_new, s.n_kv_heads, "k_new"), (v_new, s.n_kv_heads, "v_new"), (q, s.n_q_heads, "q"), (q_out, s.n_q_heads, "q_out")):
+        if t is not None:
+            _check_heads(t, heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
+    _check_same_layout(k_new, v_new, "k_new and v_new")
+    _check_same_layout(q, q_out, "q and q_out")
+    units = (s.batch, s.n_kv_heads)
+    _check_state(lengths, units, "int32", "lengths")
+    _check_state(lengths_out, units, "int32", "lengths_out")
+    _check_state(row_positions, units + (cache.capacity,), "int32", "row_positions")
+    _check_state(row_weights, units + (cache.capacity,), "float32", "row_weights")
+    turn = _turn_args(norm, rope, axes, positions, (tokens,) if cache.packed else (s.batch, s.max_new), cache.torch_dtype, s.head_dim)
+    ks, qs = _head_strides(k_new, cache.packed, "k_new"), _head_strides(q, cache.packed, "q")
+    state = (_ptr(lengths_out), _ptr(row_positions), _ptr(row_weights), _stream(stream))
+    rows = (_ptr(k_new), _ptr(v_new), ks, _ptr(q), _ptr(q_out), qs, _ptr(positions), _ptr(lengths))
+    if layer is not None:
+        args = (ctypes.byref(s), ctypes.byref(layer.struct), *turn, *rows, *state)
+    else:
+        args = (ctypes.byref(s), *turn, *rows, _ptr(call_pools[0]), _ptr(call_pools[1]), *state)
+    return PreparedCall(getattr(lib(), name), name, args, (cache, layer, call_pools, norm, rope, axes, turn, k_new, v_new, ks, q, q_out, qs, positions, lengths,
+                                                           lengths_out, row_positions, row_weights))
+
+
+def prepare_norm_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_pool, q=None, q_out=None, positions=None, norm=None, rope=None,
+                                 axes=None, lengths_out=None, row_positions=None, row_weights=None, stream=None) -> PreparedCall:
+    """New tokens into the cache with norms and axes: tensors as in prepare_append_kv_paged, positions as there or with an axis in front."""
+    _check_pool(cache, k_pool, "k_pool")
+    _check_pool(cache, v_pool, "v_pool")
+    return _prepare_append(cache, None, "wkv_norm_append_kv_paged", (k_pool, v_pool), k_new, v_new, lengths, q, q_out, positions, norm, rope, axes,
+                           lengths_out, row_positions, row_weights, stream)
+
+
+def wkv_norm_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v_pool, **kw) -> None:
+    prepare_norm_append_kv_paged(cache, k_new, v_new, lengths, k_pool, v_pool, **kw).run()
+
+
+def prepare_append_kv_paged8(cache: PagedCache8, layer: Layer8, k_new, v_new, lengths, q=None, q_out=None, positions=None, norm=None, rope=None,
+                             axes=None, lengths_out=None, row_positions=None, row_weights=None, stream=None) -> PreparedCall:
+    """New tokens into the 8-bit cache, quantised as they are written; tensors as in prepare_norm_append_kv_paged."""
+    return _prepare_append(cache, layer, "wkv_append_kv_paged8", None, k_new, v_new, lengths, q, q_out, positions, norm, rope, axes, lengths_out,
+                           row_positions, row_weights, stream)
+
+
+def wkv_append_kv_paged8(cache: PagedCache8, layer: Layer8, k_new, v_new, lengths, **kw) -> None:
+    prepare_append_kv_paged8(cache, layer, k_new, v_new, lengths, **kw).run()
+
+
+def prepare_gather_kv_paged8(prob: Problem, cache: PagedCache8, layers: Sequence[Layer8], k_layers, v_layers, window_idx, stream=None) -> PreparedCall:
+    """The selected windows and the observation rows of every layer into the 8-bit cache; v_layers may be None."""
+    s = prob.shape
+    _check_devices(cache.device, "gather into the 8-bit cache", [x.tensors for x in layers], k_layers, v_layers, window_idx, prob.budgets_dev)
+    for tensors, what in ((k_layers, "k_layers"), (v_layers, "v_layers")):
+        if tensors is not None and len(tensors) != len(layers):
+            raise ValueError(f"{what}: one tensor per layer")
+        for t in tensors or ():
+            _check_kv_layout(prob, t, what)
+    _check_state(window_idx, (s.batch, s.n_kv_heads, prob.k_max), "int32", "window_idx")
+    arrs = (_ptr_array(k_layers), _ptr_array(v_layers), _layers8(layers))
+    args = (ctypes.byref(s), ctypes.byref(cache.shape), len(layers), arrs[0], arrs[1], _ptr(window_idx), arrs[2], _stream(stream))
+    return PreparedCall(lib().wkv_gather_kv_paged8, "wkv_gather_kv_paged8", args, (prob, cache, layers, k_layers, v_layers, window_idx, arrs))
+
+
+def wkv_gather_kv_paged8(prob: Problem, cache: PagedCache8, layers: Sequence[Layer8], k_layers, v_layers, window_idx, stream=None) -> None:
+    prepare_gather_kv_paged8(prob, cache, layers, k_layers, v_layers, window_idx, stream).run()
+
+
+def prepare_read_kv_paged8(cache: PagedCache8, layer: Layer8, lengths, k_out, v_out, first=None, stream=None) -> PreparedCall:
+    """Rows first[b, h] .. lengths[b, h] - 1 of the 8-bit cache as what they stand for: k_out, v_out [B, H_kv, rows, d] of bf16 or fp32 (either may be
+    None); first int32 [B, H_kv] or None."""
+    s = cache.shape
+    _check_devices(cache.device, "rows of the 8-bit cache", layer.tensors, lengths, k_out, v_out, first)
+    some = k_out if k_out is not None else v_out
+    if some is None or some.dim() != 4 or str(some.dtype) not in ("torch.float32", "torch.bfloat16"):
+        raise ValueError("k_out, v_out: [B, H_kv, rows, d] of bf16 or fp32 expected")
+    want = (s.batch, s.n_kv_heads, some.shape[2], s.head_dim)
+    for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+        _check_state(t, want, str(some.dtype)[6:], what)
+    for t, what in ((lengths, "lengths"), (first, "first")):
+        _check_state(t, want[:2], "int32", what)
+    args = (ctypes.byref(s), ctypes.byref(layer.struct), _ptr(first), _ptr(lengths), WKV_F32 if str(some.dtype) == "torch.float32" else WKV_BF16,
+            some.shape[2], _ptr(k_out), _ptr(v_out), _stream(stream))
+    return PreparedCall(lib().wkv_read_kv_paged8, "wkv_read_kv_paged8", args, (cache, layer, lengths, k_out, v_out, first))
+
+
+def wkv_read_kv_paged8(cache: PagedCache8, layer: Layer8, lengths, k_out, v_out, first=None, stream=None) -> None:
+    prepare_read_kv_paged8(cache, layer, lengths, k_out, v_out, first, stream).run()
+
+
+def _check_draft(cache: PagedCache, masks) -> WkvDraft:
+    """Masks of drafted tokens, int32 [B, max_new, words] or packed [T, words], as a struct."""
+    s, tokens = cache.shape, _chunk_tokens(cache)
+    if masks is None or masks.dim() != (2 if cache.packed else 3):
+        raise ValueError("masks: int32 [B, max_new, words] or packed [T, words] expected")
+    _check_state(masks, ((tokens,) if cache.packed else (s.batch, s.max_new)) + (masks.shape[-1],), "int32", "masks")
+    return WkvDraft(ctypes.sizeof(WkvDraft), masks.shape[-1], _ptr(masks))
+
+
+def wkv_draft_masks(cache: PagedCache, parents, masks=None, first=None, positions=None, stream=None) -> None:
+    """Masks (int32 [B, max_new, words] or [T, words]) and positions of a draft that is a tree, from every token's parent in it (int32 [B, max_new] or
+    [T]; anything but an earlier token: the last token in front of the draft, whose next position is first[b])."""
+    s, tokens = cache.shape, _chunk_tokens(cache)
+    _check_devices(cache.device, "draft masks", parents, masks, first, positions)
+    shape = (tokens,) if cache.packed else (s.batch, s.max_new)
+    _check_state(parents, shape, "int32", "parents")
+    _check_state(positions, shape, "int32", "positions")
+    _check_state(first, (s.batch,), "int32", "first")
+    words = _check_draft(cache, masks).words if masks is not None else (s.max_new + 31) // 32
+    _check(lib().wkv_draft_masks(ctypes.byref(s), _ptr(parents), words, _ptr(masks), _ptr(first), _ptr(positions), _stream(stream)), "wkv_draft_masks")
+
+
+def _check_attend(cache: PagedCache, q, lengths, out, lse, weights_in=None, weights_out=None):
+    s, tokens = cache.shape, _chunk_tokens(cache)
+    for t, what in ((q, "q"), (out, "out")):
+        if t is not None or not cache.packed or tokens > 0:
+            _check_heads(t, s.n_q_heads, cache.torch_dtype, s.head_dim, cache.packed, s.batch, tokens, what)
+    _check_state(lengths, (s.batch, s.n_kv_heads), "int32", "lengths")
+    _check_state(lse, (s.batch, s.n_q_heads, s.max_new), "float32", "lse")
+    for t, what in ((weights_in, "weights_in"), (weights_out, "weights_out")):
+        _check_state(t, (s.batch, s.n_kv_heads, cache.capacity), "float32", what)
+    return _head_strides(q, cache.packed, "q"), _head_strides(out, cache.packed, "out")
+
+
+def prepare_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, lse=None, stream=None) -> PreparedCall:
+    """Attention of drafted tokens: as prepare_attend_paged, each new token to the rows in front of the draft and to the tokens that its mask names."""
+    _check_devices(cache.device, "draft attention", masks, q, k_pool, v_pool, lengths, out, workspace, lse)
+    _check_pool(cache, k_pool, "k_pool")
+    _check_pool(cache, v_pool, "v_pool")
+    qs, os_ = _check_attend(cache, q, lengths, out, lse)
+    draft = _check_draft(cache, masks)
+    args = (ctypes.byref(cache.shape), ctypes.byref(draft), _ptr(q), qs, _ptr(k_pool), _ptr(v_pool), _ptr(lengths), _ptr(out), os_, _ptr(lse),
+            _ptr(workspace), workspace.numel(), _stream(stream))
+    return PreparedCall(lib().wkv_attend_draft_paged, "wkv_attend_draft_paged", args,
+                        (cache, draft, masks, q, qs, k_pool, v_pool, lengths, out, os_, lse, workspace))
+
+
+def wkv_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, **kw) -> None:
+    prepare_attend_draft_paged(cache, masks, q, k_pool, v_pool, lengths, out, workspace, **kw).run()
+
+
+def prepare_attend_paged8(cache: PagedCache8, layer: Layer8, q, lengths, out, workspace, lse=None, weights_in=None, weights_out=None, draft=None,
+                          stream=None) -> PreparedCall:
+    """Attention of the new tokens over the 8-bit cache: as prepare_attend_paged; `draft`: masks as in prepare_attend_draft_paged (without weights)."""
+    _check_devices(cache.device, "attention over the 8-bit cache", layer.tensors, q, lengths, out, workspace, lse, weights_in, weights_out, draft)
+    qs, os_ = _check_attend(cache, q, lengths, out, lse, weights_in, weights_out)
+    masks = _check_draft(cache, draft) if draft is not None else None
+    args = (ctypes.byref(cache.shape), ctypes.byref(layer.struct), ctypes.byref(masks) if masks is not None else None, _ptr(q), qs, _ptr(lengths),
+            _ptr(out), os_, _ptr(lse), _ptr(weights_in), _ptr(weights_out), _ptr(workspace), workspace.numel(), _stream(stream))
+    return PreparedCall(lib().wkv_attend_paged8, "wkv_attend_paged8", args,
+                        (cache, layer, masks, draft, q, qs, lengths, out, os_, lse, weights_in, weights_out, workspace))
+
+
+def wkv_attend_paged8(cache: PagedCache8, layer: Layer8, q, lengths, out, workspace, **kw) -> None:
+    prepare_attend_paged8(cache, layer, q, lengths, out, workspace, **kw).run()
+
+
+def _check_eviction(cache, weights, positions, lengths, weights_out, positions_out, lengths_out, budgets) -> None:
+    units = (cache.shape.batch, cache.shape.n_kv_heads)
+    for t, what in ((weights, "weights"), (weights_out, "weights_out")):
+        _check_state(t, units + (cache.capacity,), "float32", what)
+    for t, what in ((positions, "positions"), (positions_out, "positions_out")):
+        _check_state(t, units + (cache.capacity,), "int32", what)
+    for t, what in ((lengths, "lengths"), (lengths_out, "lengths_out")):
+        _check_state(t, units, "int32", what)
+    _check_state(budgets, units[:1], "int32", "budgets")
+
+
+def wkv_evict_kv_paged8(cache: PagedCache8, layers: Sequence[Layer8], weights, positions, lengths, budget: int, recent: int, weights_out,
+                        positions_out, lengths_out, workspace, budgets=None, stream=None) -> None:
+    """Rows of least weight leave the 8-bit cache, for all layers given; as wkv_evict_kv_paged."""
+    _check_devices(cache.device, "eviction", [x.tensors for x in layers], weights, positions, lengths, weights_out, positions_out, lengths_out, workspace,
+                   budgets)
+    _check_eviction(cache, weights, positions, lengths, weights_out, positions_out, lengths_out, budgets)
+    _check(lib().wkv_evict_kv_paged8(ctypes.byref(cache.shape), len(layers), _layers8(layers), budget, _ptr(budgets), recent, _ptr(weights),
+                                     _ptr(positions), _ptr(lengths), _ptr(weights_out), _ptr(positions_out), _ptr(lengths_out), _ptr(workspace),
+                                     workspace.numel(), _stream(stream)), "wkv_evict_kv_paged8")
+
+
+def _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, *pools) -> WkvDraft:
+    _check_devices(cache.device, "draft", masks, last, lengths, lengths_out, row_positions, row_weights, *pools)
+    units = (cache.shape.batch, cache.shape.n_kv_heads)
+    _check_state(last, units[:1], "int32", "last")
+    _check_state(lengths, units, "int32", "lengths")
+    _check_state(lengths_out, units, "int32", "lengths_out")
+    _check_state(row_positions, units + (cache.capacity,), "int32", "row_positions")
+    _check_state(row_weights, units + (cache.capacity,), "float32", "row_weights")
+    return _check_draft(cache, masks)
+
+
+def wkv_keep_draft_paged(cache: PagedCache, masks, k_pools, v_pools, last, lengths, lengths_out, row_positions=None, row_weights=None,
+                         stream=None) -> None:
+    """Of every sequence's draft the path of token last[b] (int32 [B]; -1: nothing) stays, directly behind the rows in front of the draft."""
+    draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, k_pools, v_pools)
+    for pools, what in ((k_pools, "k_pools"), (v_pools, "v_pools")):
+        if pools is not None and len(pools) != len(k_pools):
+            raise ValueError(f"{what}: one pool per layer")
+        for t in pools or ():
+            _check_pool(cache, t, what)
+    _check(lib().wkv_keep_draft_paged(ctypes.byref(cache.shape), ctypes.byref(draft), len(k_pools), _ptr_array(k_pools), _ptr_array(v_pools), _ptr(last),
+                                      _ptr(lengths), _ptr(lengths_out), _ptr(row_positions), _ptr(row_weights), _stream(stream)), "wkv_keep_draft_paged")
+
+
+def wkv_keep_draft_paged8(cache: PagedCache8, masks, layers: Sequence[Layer8], last, lengths, lengths_out, row_positions=None, row_weights=None,
+                          stream=None) -> None:
+    """The same in an 8-bit cache."""
+    draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, [x.tensors for x in layers])
+    _check(lib().wkv_keep_draft_paged8(ctypes.byref(cache.shape), ctypes.byref(draft), len(layers), _layers8(layers), _ptr(last), _ptr(lengths),
+                                       _ptr(lengths_out), _ptr(row_positions), _ptr(row_weights), _stream(stream)), "wkv_keep_draft_paged8")
 
 
 def wkv_keep_len(n: int, alpha: int, omega: int, budget: int):

@@ -42,7 +42,14 @@ struct AttnArgs {
     long long logit_stride;      // cap, rounded up to a multiple of four
     const float *weights_in;     // [units][cap] or null
     float *weights_out;          // [units][cap] or null
+    // K and V of 8 bits: strides in bytes, scales [page][head][slot]
+    int kind;                    // kPlain, or a wkv_cache8_type + 1
+    const unsigned char *k_scales, *v_scales;
+    // drafted tokens: query i attends to the rows in front of the new ones and to those of them that its mask names
+    const unsigned *masks;       // [batch][max_q][words] or packed [total_q][words], or null
+    int mask_words;
 };
+constexpr int kPlain = 0, kE4m3 = 1 + WKV_CACHE_E4M3, kI8 = 1 + WKV_CACHE_I8;
 
 struct AttnSeq {
     int m;            // queries
@@ -74,6 +81,17 @@ __device__ __forceinline__ long long attn_row(const AttnArgs &a, int b, int h, l
         return page * a.kb + h * a.kh + (long long)(j - pg * a.page_size) * a.kt;
     }
     return (q_off + j) * a.kt + b * a.kb + h * a.kh;
+}
+// index of row j of unit (b, h) in the scales of an 8-bit cache, of which attn_row() has said that its page is one
+__device__ __forceinline__ long long attn_scale(const AttnArgs &a, int b, int h, int j)
+{
+    const int pg = j / a.page_size, page = __ldg(a.table + (long long)b * a.max_pages + pg);
+    return ((long long)page * a.hkv + h) * a.page_size + (j - pg * a.page_size);
+}
+// the mask of query i of sequence b
+__device__ __forceinline__ const unsigned *attn_mask(const AttnArgs &a, const AttnSeq &s, int b, int i)
+{
+    return a.masks + ((a.cu_q ? s.q_off : (long long)b * a.max_q) + i) * a.mask_words;
 }
 // log-sum-exp of a row, where it is asked for; lse2 in base 2
 __device__ __forceinline__ void attn_store_lse(const AttnArgs &a, int b, int hq, int i, int m, float lse2)
@@ -108,6 +126,7 @@ bool attn_tc_supported(const AttnArgs &a, int dtype);
 int launch_attn_tc(const AttnArgs &a, float *piece_o, float2 *piece_ml, long long *line, cudaStream_t stream);
 int attn_tc_pieces(long long units, int max_q, int G, int cap, int *rows, int *items);
 int launch_attn_mma(const AttnArgs &a, cudaStream_t stream);         // bf16
+int launch_attn8(const AttnArgs &a, cudaStream_t stream);             // bf16 over the 8-bit cache
 int launch_attn_simt(const AttnArgs &a, cudaStream_t stream);         // fp32
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream);       // with a.logits: and the weights
 int launch_attn_weights(const AttnArgs &a, cudaStream_t stream);      // fp32; reads a.lse
@@ -139,6 +158,20 @@ struct RopeArgs {
 };
 int launch_rope(const RopeArgs &a, cudaStream_t stream);
 
+// The same with norms and several axes, into a cache of plain rows or of 8 bits.
+struct TurnArgs {
+    RopeArgs r;
+    bool norm;
+    float eps, offset;
+    const void *q_weight, *k_weight;         // or null: ones
+    int n_axes;
+    const int *axis;                         // null: one axis
+    long long position_stride;
+    int kind;                                // of the pools
+    unsigned char *k_scales, *v_scales;
+};
+int launch_turn(const TurnArgs &a, int dtype, cudaStream_t stream);
+
 struct EvictArgs {
     int batch, hkv, d, elem_bytes;
     const int *table;
@@ -155,11 +188,46 @@ struct EvictArgs {
     int2 *moves;           // [units][cap / 2 + 1] (to, from)
     longlong2 *places;     // the same rows' element offsets in the pools, -1: no page
     int moves_max;
+    bool scaled;           // 8-bit rows: each pool's scales move with them
 };
 struct PoolTable {
     void *ptr[2 * WKV_MAX_GROUP_LAYERS];
 };
-int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream);
+struct ScaleTable {
+    unsigned char *ptr[2 * WKV_MAX_GROUP_LAYERS];
+};
+int launch_evict(const EvictArgs &a, const PoolTable &pools, const ScaleTable &scales, cudaStream_t stream);
+// 8-bit cache: the gather into it, and rows read back
+struct Cache8Pages {
+    const int *table;
+    int max_pages, page_size, num_pages;
+    long long page_stride, head_stride, row_stride;       // bytes
+};
+struct LayerTable;
+int launch_gather8(const KShape &ks, int dtype, int n_tensors, const LayerTable &src, const PoolTable &codes, const ScaleTable &scales,
+                   int kind, const Cache8Pages &pages, const int *window_idx, cudaStream_t stream);
+int launch_read8(int batch, int hkv, int d, const Cache8Pages &pages, int kind, const void *const (&codes)[2],
+                 const unsigned char *const (&scales)[2], const int *first, const int *lengths, int out_dtype, int row_capacity,
+                 void *const (&out)[2], cudaStream_t stream);
+
+// drafted tokens
+struct DraftArgs {
+    int batch, hkv, d, elem_bytes;           // elem_bytes of the pools
+    int max_q, total_q;
+    const int *cu_q;
+    const unsigned *masks;
+    int words;
+    Cache8Pages pages;                       // strides in elements
+    int cap;
+    int n_tensors;
+    bool scaled;
+    const int *last, *lengths;
+    int *lengths_out, *row_positions;
+    float *row_weights;
+};
+int launch_draft_masks(int batch, int max_q, int total_q, const int *cu_q, const int *parents, int words, unsigned *masks, const int *first,
+                       int *positions, cudaStream_t stream);
+int launch_keep_draft(const DraftArgs &a, const PoolTable &pools, const ScaleTable &scales, cudaStream_t stream);
 int launch_seed_rows(const KShape &ks, const int *window_idx, const float *token_scores, int row_capacity, int *positions,
                      float *weights, cudaStream_t stream);
 

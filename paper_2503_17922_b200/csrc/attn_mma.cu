@@ -17,6 +17,7 @@
 // Where weights are wanted (FEW), the logits go to the workspace (4 bytes per row and key beside the 512 of K and V) and the joining
 // kernel adds up exp2(logit - lse), instead of K being read once more.
 #include "attn_cluster.cuh"
+#include "cache8.cuh"
 
 namespace wkv {
 namespace {
@@ -68,7 +69,8 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-template <int DP, bool FEW>
+// DRAFT: the rows go by their masks, as far as the new tokens' rows are concerned
+template <int DP, bool FEW, bool DRAFT>
 __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(128) unsigned char raw[];
@@ -92,19 +94,21 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
     }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane >> 2, ql = lane & 3;
     const int base = sq.n - sq.m + 1;                                    // keys that query 0 attends to (may be negative)
-    const int most = min(base + (min(row0 + kRows, rows) - 1) / a.G, sq.n);
+    const int most = DRAFT ? sq.n : min(base + (min(row0 + kRows, rows) - 1) / a.G, sq.n);
     const int all_tiles = (max(most, 0) + kKeys - 1) / kKeys;
     const int t0 = (int)((long long)all_tiles * split / splits), t1 = (int)((long long)all_tiles * (split + 1) / splits);
-    const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
+    const int plain = DRAFT ? base - 1 : base + row0 / a.G;              // every row attends to the keys before this one
 
     // rows of this thread: `quad` and quad + 8 of the warp's sixteen
     const int my_row[2] = {row0 + (FEW ? 0 : warp * 16) + quad, row0 + (FEW ? 0 : warp * 16) + quad + 8};
     int limit[2];
+    const unsigned *mask[2];
     uint32_t q[kSteps][4];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int row = my_row[x], i = row / a.G, g = row - i * a.G;
-        limit[x] = row < rows ? base + i : 0;
+        limit[x] = row < rows ? (DRAFT ? base - 1 : base + i) : 0;
+        mask[x] = DRAFT && row < rows ? attn_mask(a, sq, b, i) : nullptr;
         const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(a.q) + (sq.q_off + i) * a.qt + b * a.qb + (long long)(h * a.G + g) * a.qh;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
@@ -114,6 +118,12 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
                 q[s][2 * y + x] = row < rows && c < a.d ? *reinterpret_cast<const uint32_t *>(p + c) : 0u;
             }
     }
+    auto sees = [&](int x, int j) {                                      // row x and key j < n
+        if (j < limit[x]) return true;
+        if (!DRAFT || !mask[x]) return false;
+        const int at = j - (base - 1);                                   // token of the draft (limit is base - 1)
+        return (__ldg(mask[x] + (at >> 5)) >> (at & 31) & 1u) != 0u;
+    };
     float o[DP / 8][4];
 #pragma unroll
     for (int x = 0; x < DP / 8; ++x)
@@ -200,9 +210,9 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
                         if (there && a.table && (sm.missing[t % (NS + 1)][0] | sm.missing[t % (NS + 1)][1])) there = attn_row(a, b, h, sq.q_off, j) >= 0;
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
-                            const bool sees = there && j < limit[x];
-                            unseen |= there && !sees;
-                            if (!sees) s[y][2 * x + e] = -INFINITY;
+                            const bool seen = there && sees(x, j);
+                            unseen |= there && !seen;
+                            if (!seen) s[y][2 * x + e] = -INFINITY;
                         }
                     }
             }
@@ -273,6 +283,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
             if (!plain_product) {
                 for (int kk = 0; kk < 16; ++kk) {
                     const int row = key0 + kk;
+                    if (DRAFT && j0 + row >= sq.n) break;
 #pragma unroll
                     for (int d = 0; d < DP / 8; ++d) {
                         const __nv_bfloat162 w = *reinterpret_cast<const __nv_bfloat162 *>(
@@ -280,7 +291,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
                         const float w0 = __low2float(w), w1 = __high2float(w);
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
-                            if (j0 + row >= limit[x]) continue;
+                            if (!sees(x, j0 + row)) continue;
                             if (!(fabsf(w0) < INFINITY)) o[d][2 * x] += w0;
                             if (!(fabsf(w1) < INFINITY)) o[d][2 * x + 1] += w1;
                         }
@@ -403,7 +414,7 @@ struct WeightsSmem {
     __align__(16) float lse[kWeightStages][kWeightRows];
     __align__(16) int limit[kWeightStages][kWeightRows];           // keys that the row sees; 0: there is no such row
 };
-template <int DP, int WARPS>
+template <int DP, int WARPS, bool EIGHT>
 __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) attn_mma_weights_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(128) unsigned char raw[];
@@ -455,14 +466,27 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) attn_mma_weights_kerne
             const int j = key0 + 16 * f + 8 * x;
             const long long at = j < sq.n ? attn_row(a, b, h, sq.q_off, j) : -1;
             there[f][x] = at >= 0;
-            const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(a.k) + (at >= 0 ? at : 0);
+            if constexpr (EIGHT) {
+                const unsigned char *p = static_cast<const unsigned char *>(a.k) + (at >= 0 ? at : 0);
+                const float by = at >= 0 ? scale_value(a.k_scales[attn_scale(a, b, h, j)]) : 0.f;
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
+                for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int c = s * 16 + y * 8 + ql * 2;
-                    k[f][s][2 * y + x] = at >= 0 && c < a.d ? __ldg(reinterpret_cast<const uint32_t *>(p + c)) : 0u;
-                }
+                    for (int y = 0; y < 2; ++y) {
+                        const int c = s * 16 + y * 8 + ql * 2;
+                        const float4 v = codes_to_float(at >= 0 && c < a.d ? __ldg(reinterpret_cast<const unsigned short *>(p + c)) : 0u, a.kind);
+                        k[f][s][2 * y + x] = pack(v.x * by, v.y * by);       // (exact)
+                    }
+            } else {
+                const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(a.k) + (at >= 0 ? at : 0);
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int c = s * 16 + y * 8 + ql * 2;
+                        k[f][s][2 * y + x] = at >= 0 && c < a.d ? __ldg(reinterpret_cast<const uint32_t *>(p + c)) : 0u;
+                    }
+            }
         }
     float sum[F][2] = {};
     for (int t = 0; t < tiles; ++t) {
@@ -519,7 +543,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) attn_mma_weights_kerne
         }
 }
 
-template <int DP, bool FEW>
+template <int DP, bool FEW, bool DRAFT>
 int launch_dp(const AttnArgs &a, cudaStream_t stream)
 {
     static SmemAsked asked;
@@ -529,27 +553,27 @@ int launch_dp(const AttnArgs &a, cudaStream_t stream)
         set_error_detail("attention: %lld blocks", blocks);
         return WKV_ERR_LIMIT;
     }
-    cudaError_t err = allow_smem(attn_mma_kernel<DP, FEW>, sizeof(MmaSmem<DP>), asked);
-    if (err == cudaSuccess) err = launch_pdl(attn_mma_kernel<DP, FEW>, dim3((unsigned)blocks), kThreads, sizeof(MmaSmem<DP>), stream,
+    cudaError_t err = allow_smem(attn_mma_kernel<DP, FEW, DRAFT>, sizeof(MmaSmem<DP>), asked);
+    if (err == cudaSuccess) err = launch_pdl(attn_mma_kernel<DP, FEW, DRAFT>, dim3((unsigned)blocks), kThreads, sizeof(MmaSmem<DP>), stream,
                                              FEW && a.clustered ? a.splits : 1, a);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "attention kernel");
 }
 
-template <int DP, int WARPS>
+template <int DP, int WARPS, bool EIGHT>
 int launch_weights(const AttnArgs &a, cudaStream_t stream)
 {
     static SmemAsked asked;
     constexpr int kBlockKeys = WARPS * 16 * (DP == 256 ? 1 : 2);
     const long long blocks = ((long long)a.cap + kBlockKeys - 1) / kBlockKeys * a.batch * a.hkv;
     // (half as many keys to a block where that leaves SMs without one)
-    if (WARPS > 4 && blocks < 2 * 148) return launch_weights<DP, 4>(a, stream);
+    if (WARPS > 4 && blocks < 2 * 148) return launch_weights<DP, 4, EIGHT>(a, stream);
     if (blocks > 0x7fffffffLL) {
         set_error_detail("attention weights: %lld blocks", blocks);
         return WKV_ERR_LIMIT;
     }
-    cudaError_t err = allow_smem(attn_mma_weights_kernel<DP, WARPS>, sizeof(WeightsSmem<DP>), asked);
-    if (err == cudaSuccess) err = launch_pdl(attn_mma_weights_kernel<DP, WARPS>, dim3((unsigned)blocks), WARPS * 32, sizeof(WeightsSmem<DP>), stream, 1, a);
+    cudaError_t err = allow_smem(attn_mma_weights_kernel<DP, WARPS, EIGHT>, sizeof(WeightsSmem<DP>), asked);
+    if (err == cudaSuccess) err = launch_pdl(attn_mma_weights_kernel<DP, WARPS, EIGHT>, dim3((unsigned)blocks), WARPS * 32, sizeof(WeightsSmem<DP>), stream, 1, a);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "attention weights kernel");
 }
@@ -558,12 +582,19 @@ int launch_weights(const AttnArgs &a, cudaStream_t stream)
 
 int launch_attn_mma_weights(const AttnArgs &a, cudaStream_t stream)
 {
-    return a.d <= 64 ? launch_weights<64, 8>(a, stream) : a.d <= 128 ? launch_weights<128, 8>(a, stream) : launch_weights<256, 8>(a, stream);
+    if (a.kind != kPlain)
+        return a.d <= 64 ? launch_weights<64, 8, true>(a, stream) : a.d <= 128 ? launch_weights<128, 8, true>(a, stream) : launch_weights<256, 8, true>(a, stream);
+    return a.d <= 64 ? launch_weights<64, 8, false>(a, stream) : a.d <= 128 ? launch_weights<128, 8, false>(a, stream) : launch_weights<256, 8, false>(a, stream);
+}
+template <bool FEW, bool DRAFT>
+static int launch_any(const AttnArgs &a, cudaStream_t stream)
+{
+    return a.d <= 64 ? launch_dp<64, FEW, DRAFT>(a, stream) : a.d <= 128 ? launch_dp<128, FEW, DRAFT>(a, stream) : launch_dp<256, FEW, DRAFT>(a, stream);
 }
 int launch_attn_mma(const AttnArgs &a, cudaStream_t stream)
 {
-    if (a.rows_max <= 16) return a.d <= 64 ? launch_dp<64, true>(a, stream) : a.d <= 128 ? launch_dp<128, true>(a, stream) : launch_dp<256, true>(a, stream);
-    return a.d <= 64 ? launch_dp<64, false>(a, stream) : a.d <= 128 ? launch_dp<128, false>(a, stream) : launch_dp<256, false>(a, stream);
+    if (a.masks) return a.rows_max <= 16 ? launch_any<true, true>(a, stream) : launch_any<false, true>(a, stream);
+    return a.rows_max <= 16 ? launch_any<true, false>(a, stream) : launch_any<false, false>(a, stream);
 }
 
 }  // namespace wkv

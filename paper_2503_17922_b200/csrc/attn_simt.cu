@@ -13,6 +13,7 @@
 // With S key splits a block walks over one of S parts of the keys and leaves (maximum, sum, unnormalised output) per row for
 // the joining kernel.  A row's sums are taken in an order that the launch's sizes give, never in that of arrival.
 #include "attn_cluster.cuh"
+#include "cache8.cuh"
 #include "score_math.cuh"
 
 #include <type_traits>
@@ -62,11 +63,13 @@ struct WeightsSmem {
 
 // The keys or the values of a tile, on their way; rows from n on and rows without a page are zeros.  A row's vectors lie in neighbouring
 // threads, and a thread has EACH rows.  Their pages are looked up some work ahead, as that is a trip to memory.
-template <int DP>
+// EIGHT: the rows are codes, which become numbers on their way.
+template <int DP, bool EIGHT>
 struct Fetch {
     static constexpr int kParts = DP / 4, kEach = kKeys * kParts / kThreads, kStep = kThreads / kParts;
     int page[kEach], slot[kEach];
     long long at[kEach];                   // element offsets, -1: none
+    long long scale_at[EIGHT ? kEach : 1];
     __device__ __forceinline__ void look_up(const AttnArgs &a, int b, int n, int j0)
     {
         if (!a.table) return;
@@ -84,30 +87,64 @@ struct Fetch {
             const int r = (int)threadIdx.x / kParts + x * kStep, j = j0 + r;
             if (a.table) at[x] = (unsigned)page[x] < (unsigned)a.num_pages ? page[x] * a.kb + h * a.kh + slot[x] * a.kt : -1;
             else at[x] = j < n ? dense + j * a.kt : -1;
+            if (EIGHT) scale_at[EIGHT ? x : 0] = at[x] >= 0 ? ((long long)page[x] * a.hkv + h) * a.page_size + slot[x] : 0;
             if (threadIdx.x % kParts == 0) present[r] = at[x] >= 0;
         }
     }
-    __device__ __forceinline__ void issue(const AttnArgs &a, const void *from, float *to, int stride) const
+    __device__ __forceinline__ void issue(const AttnArgs &a, bool values, float *to, int stride) const
     {
         const int c = (int)(threadIdx.x % kParts) * 4;
+        const void *from = values ? a.v : a.k;
+        if constexpr (EIGHT) {
+            constexpr int kBatch = kEach < 8 ? kEach : 8;                // (loads first, a few at a time)
 #pragma unroll
-        for (int x = 0; x < kEach; ++x) {
-            const int r = (int)threadIdx.x / kParts + x * kStep;
-            const bool have = at[x] >= 0 && c < a.d;
-            const float *p = static_cast<const float *>(from) + (have ? at[x] + c : 0);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + r * stride + c))), "l"(p), "r"(have ? 16 : 0) : "memory");
+            for (int x0 = 0; x0 < kEach; x0 += kBatch) {
+                unsigned w[kBatch];
+                float by[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const bool have = at[x0 + u] >= 0 && c < a.d;
+                    w[u] = have ? *reinterpret_cast<const unsigned *>(static_cast<const unsigned char *>(from) + at[x0 + u] + c) : 0u;
+                    by[u] = have ? scale_value((values ? a.v_scales : a.k_scales)[scale_at[x0 + u]]) : 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const float4 v = codes_to_float(w[u], a.kind);
+                    *reinterpret_cast<float4 *>(to + ((int)threadIdx.x / kParts + (x0 + u) * kStep) * stride + c) =
+                        make_float4(v.x * by[u], v.y * by[u], v.z * by[u], v.w * by[u]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) {
+                const int r = (int)threadIdx.x / kParts + x * kStep;
+                const bool have = at[x] >= 0 && c < a.d;
+                const float *p = static_cast<const float *>(from) + (have ? at[x] + c : 0);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + r * stride + c))), "l"(p), "r"(have ? 16 : 0) : "memory");
+            }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");             // (an empty group with EIGHT: the waits count them)
     }
 };
-template <int DP>
+template <int DP, bool EIGHT>
 __device__ __forceinline__ void load_keys(const AttnArgs &a, WeightsSmem<DP> &sm, int b, int h, long long off, int n, int j0)
 {
     constexpr int kParts = DP / 4;
     for (int x = threadIdx.x; x < kKeys * kParts; x += kThreads) {
         const int r = x / kParts, part = x - r * kParts, j = j0 + r;
         const long long at = j < n ? attn_row(a, b, h, off, j) : -1;
-        load_row_part<DP>(sm.k[r], at >= 0 ? static_cast<const float *>(a.k) + at : nullptr, a.d, part);
+        if constexpr (EIGHT) {
+            const int c = part * 4;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (at >= 0 && c < a.d) {
+                const float by = scale_value(a.k_scales[attn_scale(a, b, h, j)]);
+                v = codes_to_float(*reinterpret_cast<const unsigned *>(static_cast<const unsigned char *>(a.k) + at + c), a.kind);
+                v = make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
+            }
+            *reinterpret_cast<float4 *>(&sm.k[r][c]) = v;
+        } else {
+            load_row_part<DP>(sm.k[r], at >= 0 ? static_cast<const float *>(a.k) + at : nullptr, a.d, part);
+        }
         if (part == 0) sm.present[r] = at >= 0;
     }
 }
@@ -152,7 +189,8 @@ __device__ __forceinline__ void logits(const float (&q)[ROWS][DP + 4], const flo
         }
 }
 
-template <int DP, int ROWS>
+// EIGHT: keys and values of 8 bits.  DRAFT: the rows go by their masks, as far as the new tokens' rows are concerned.
+template <int DP, int ROWS, bool EIGHT, bool DRAFT>
 __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 64 && ROWS < 64 ? 3 : 1)) attn_simt_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
@@ -176,27 +214,35 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
     }
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
     const int base = sq.n - sq.m + 1;                                    // keys that query 0 attends to (may be negative)
-    const int most = min(base + (min(row0 + ROWS, rows) - 1) / a.G, sq.n);
+    const int most = DRAFT ? sq.n : min(base + (min(row0 + ROWS, rows) - 1) / a.G, sq.n);
     const int all_tiles = (max(most, 0) + kKeys - 1) / kKeys;
     const int t0 = (int)((long long)all_tiles * split / splits), t1 = (int)((long long)all_tiles * (split + 1) / splits);
     int limit[RT];
+    const unsigned *mask[DRAFT ? RT : 1];
     float m[RT], l[RT];
     unsigned long long o[RT][CT][2];                                     // pairs of columns
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        limit[r] = base + (row0 + ty * RT + r) / a.G;
+        limit[r] = DRAFT ? base - 1 : base + (row0 + ty * RT + r) / a.G;
+        if (DRAFT) mask[DRAFT ? r : 0] = row0 + ty * RT + r < rows ? attn_mask(a, sq, b, (row0 + ty * RT + r) / a.G) : nullptr;
         m[r] = -INFINITY;
         l[r] = 0.f;
 #pragma unroll
         for (int x = 0; x < CT; ++x) o[r][x][0] = o[r][x][1] = 0ull;
     }
+    auto sees = [&](int r, int j) {                                      // row r and key j
+        if (j < limit[r]) return true;
+        if (!DRAFT || !mask[DRAFT ? r : 0] || j >= sq.n) return false;
+        const int at = j - (base - 1);                                   // token of the draft (limit is base - 1)
+        return (__ldg(mask[DRAFT ? r : 0] + (at >> 5)) >> (at & 31) & 1u) != 0u;
+    };
     const long long dense = sq.q_off * a.kt + b * a.kb + h * a.kh;
-    Fetch<DP> rows_of;
+    Fetch<DP, EIGHT> rows_of;
     auto fetch_keys = [&](int t) {
         rows_of.place(a, sm.present[t & 1], h, dense, sq.n, t * kKeys);
-        rows_of.issue(a, a.k, &sm.k[t % NS][0][0], DP + 4);
+        rows_of.issue(a, false, &sm.k[t % NS][0][0], DP + 4);
     };
-    auto fetch_values = [&](int t) { rows_of.issue(a, a.v, &sm.v[t % NS][0][0], DP); };
+    auto fetch_values = [&](int t) { rows_of.issue(a, true, &sm.v[t % NS][0][0], DP); };
     if (t0 < t1) {
         rows_of.look_up(a, b, sq.n, t0 * kKeys);
         fetch_keys(t0);
@@ -208,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncthreads();
     }
-    const int plain = base + row0 / a.G;                                 // every row attends to the keys before this one
+    const int plain = DRAFT ? base - 1 : base + row0 / a.G;              // every row attends to the keys before this one
     for (int t = t0; t < t1; ++t) {
         const int j0 = t * kKeys, st = t % NS;
         if (NS == 2) {
@@ -237,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (j0 + tx + 16 * j >= limit[r] || !sm.present[t & 1][tx + 16 * j]) s[r][j] = -INFINITY;
+                    if (!sees(r, j0 + tx + 16 * j) || !sm.present[t & 1][tx + 16 * j]) s[r][j] = -INFINITY;
         }
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -290,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
                         const float p = e == 0 ? pp[r].x : (e == 1 ? pp[r].y : (e == 2 ? pp[r].z : pp[r].w));
-                        if (decltype(skip_unseen)::value && j0 + j + e >= limit[r]) continue;
+                        if (decltype(skip_unseen)::value && !sees(r, j0 + j + e)) continue;
                         const unsigned long long p2 = pair_of(p, p);
 #pragma unroll
                         for (int x = 0; x < CT; ++x) {
@@ -358,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
 
 // Weights that the rows of the cache receive: one block per 64 rows of a unit sums exp2(logit - lse) over all of the unit's
 // queries.  The logits are computed once more, from the normalisers that the attention has written; sums in a fixed order.
-template <int DP>
+template <int DP, bool EIGHT>
 __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr int ROWS = 64, RT = ROWS / 16;
@@ -371,7 +417,7 @@ __global__ void __launch_bounds__(kThreads) attn_weights_kernel(const __grid_con
     if (j0 >= sq.n) return;
     const int rows = sq.m * a.G, base = sq.n - sq.m + 1;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-    load_keys<DP>(a, sm, b, h, sq.q_off, sq.n, j0);
+    load_keys<DP, EIGHT>(a, sm, b, h, sq.q_off, sq.n, j0);
     float got[4] = {0.f, 0.f, 0.f, 0.f};
     // queries in front of the tile's first key do not attend to any of it
     const long long first = base > j0 ? 0 : (long long)(j0 - base + 1) * a.G;
@@ -559,6 +605,17 @@ int launch(K kernel, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t str
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, what);
 }
+template <int DP, int ROWS>
+int launch_dp(const AttnArgs &a, dim3 grid, cudaStream_t stream)
+{
+    constexpr size_t smem = sizeof(SimtSmem<DP, ROWS>);
+    const int cluster = a.clustered ? a.splits : 1;
+    if (a.kind != kPlain)
+        return a.masks ? launch(attn_simt_kernel<DP, ROWS, true, true>, grid, smem, a, stream, "attention kernel (8-bit cache)", cluster)
+                       : launch(attn_simt_kernel<DP, ROWS, true, false>, grid, smem, a, stream, "attention kernel (8-bit cache)", cluster);
+    return a.masks ? launch(attn_simt_kernel<DP, ROWS, false, true>, grid, smem, a, stream, "attention kernel (draft)", cluster)
+                   : launch(attn_simt_kernel<DP, ROWS, false, false>, grid, smem, a, stream, "attention kernel", cluster);
+}
 template <int ROWS>
 int launch_rows(const AttnArgs &a, cudaStream_t stream)
 {
@@ -568,15 +625,14 @@ int launch_rows(const AttnArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)blocks);
-    const int cluster = a.clustered ? a.splits : 1;
     if constexpr (ROWS == 128) {
-        return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
+        return launch_dp<128, ROWS>(a, grid, stream);
     } else {
-        if (a.d <= 64) return launch(attn_simt_kernel<64, ROWS>, grid, sizeof(SimtSmem<64, ROWS>), a, stream, "attention kernel", cluster);
-        if (a.d <= 128) return launch(attn_simt_kernel<128, ROWS>, grid, sizeof(SimtSmem<128, ROWS>), a, stream, "attention kernel", cluster);
-        return launch(attn_simt_kernel<256, ROWS>, grid, sizeof(SimtSmem<256, ROWS>), a, stream, "attention kernel", cluster);
+        if (a.d <= 64) return launch_dp<64, ROWS>(a, grid, stream);
+        return a.d <= 128 ? launch_dp<128, ROWS>(a, grid, stream) : launch_dp<256, ROWS>(a, grid, stream);
     }
 }
+template <bool EIGHT>
 int launch_weights(const AttnArgs &a, cudaStream_t stream)
 {
     const long long blocks = ((long long)a.cap + kKeys - 1) / kKeys * a.batch * a.hkv;
@@ -585,9 +641,9 @@ int launch_weights(const AttnArgs &a, cudaStream_t stream)
         return WKV_ERR_LIMIT;
     }
     const dim3 grid((unsigned)blocks);
-    if (a.d <= 64) return launch(attn_weights_kernel<64>, grid, sizeof(WeightsSmem<64>), a, stream, "attention weights kernel");
-    if (a.d <= 128) return launch(attn_weights_kernel<128>, grid, sizeof(WeightsSmem<128>), a, stream, "attention weights kernel");
-    return launch(attn_weights_kernel<256>, grid, sizeof(WeightsSmem<256>), a, stream, "attention weights kernel");
+    if (a.d <= 64) return launch(attn_weights_kernel<64, EIGHT>, grid, sizeof(WeightsSmem<64>), a, stream, "attention weights kernel");
+    if (a.d <= 128) return launch(attn_weights_kernel<128, EIGHT>, grid, sizeof(WeightsSmem<128>), a, stream, "attention weights kernel");
+    return launch(attn_weights_kernel<256, EIGHT>, grid, sizeof(WeightsSmem<256>), a, stream, "attention weights kernel");
 }
 
 }  // namespace
@@ -610,7 +666,10 @@ int launch_attn_simt(const AttnArgs &args, cudaStream_t stream)
     if (a.d > 64 && a.d <= 128 && blocks(128) >= 120) return launch_rows<128>(a, stream);
     return blocks(64) < 120 ? launch_rows<32>(a, stream) : launch_rows<64>(a, stream);
 }
-int launch_attn_weights(const AttnArgs &a, cudaStream_t stream) { return launch_weights(a, stream); }
+int launch_attn_weights(const AttnArgs &a, cudaStream_t stream)
+{
+    return a.kind != kPlain ? launch_weights<true>(a, stream) : launch_weights<false>(a, stream);
+}
 int launch_attn_join(const AttnArgs &a, int dtype, cudaStream_t stream)
 {
     const int units = a.batch * a.hkv;

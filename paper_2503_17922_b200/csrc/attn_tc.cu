@@ -959,7 +959,7 @@ static int box_of_page(int page_size) { return std::min(page_size & -page_size, 
 // Shapes that the kernel takes; a layout that no tensor map describes is found out at launch (WKV_ERR_UNSUPPORTED).
 bool attn_tc_supported(const AttnArgs &a, int dtype)
 {
-    if (dtype != WKV_BF16 || a.d > 128 || a.G > kTile) return false;
+    if (dtype != WKV_BF16 || a.d > 128 || a.G > kTile || a.kind != kPlain || a.masks) return false;
     // a key tile is one box: tensors of fewer rows are left to the other kernels, which are as fast there
     if (!a.table && (a.cu_q ? a.total_q : a.max_q) < kTile) return false;
     if (a.table && box_of_page(a.page_size) < 8) return false;

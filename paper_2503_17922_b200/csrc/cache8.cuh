@@ -1,0 +1,69 @@
+// Rows of the 8-bit cache: a row's scale and codes, and what they stand for.
+//
+//   element = code * 2^e,  e the least number >= -100 with max |x| <= M 2^e (M = 448 or 127), at most 100
+//
+// The power of two makes x / 2^e and code * 2^e exact, so that the code's own rounding is the only one: what a row stands for is a bf16 number, the
+// operand of the attention's products, and reading a row back and quantising it again gives the same row.  A scale of 32
+// bits with max |x| on the largest code would leave integer codes half a bit more on average, nothing to 8-bit floats.
+#pragma once
+
+#include "attn.cuh"
+
+#include <cuda_fp16.h>
+
+namespace wkv {
+
+constexpr int kLeastExponent = -100, kMostExponent = 100;
+constexpr int kScaleBias = 127, kScaleNan = 255;
+
+// |x| as bits: of these the largest is the row's largest, infinity beyond all numbers and NaN beyond that
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// the scale byte of a row whose largest magnitude has these bits
+__device__ __forceinline__ int scale_byte(unsigned most, int kind)
+{
+    if (most >= 0x7f800000u) return kScaleNan;
+    // M = 1.75 * 2^8 or 1.984375 * 2^6: a mantissa above M's takes the next power
+    const unsigned frac = kind == kE4m3 ? 0x600000u : 0x7e0000u;
+    const int top = kind == kE4m3 ? 8 : 6, e = (int)((most + (0x7fffffu - frac)) >> 23) - 127 - top;
+    return min(max(e, kLeastExponent), kMostExponent) + kScaleBias;
+}
+// 2^e and 2^-e of a scale byte that a call has written (27 .. 227); 0 for a NaN row's codes
+__device__ __forceinline__ float scale_inverse(int byte) { return byte == kScaleNan ? 0.f : __uint_as_float((unsigned)(254 - byte) << 23); }
+// 2^(byte - 127) of any byte, NaN of 255
+__device__ __forceinline__ float scale_value(int byte)
+{
+    return byte == kScaleNan ? __uint_as_float(0x7fffffffu) : (byte == 0 ? __uint_as_float(0x400000u) : __uint_as_float((unsigned)byte << 23));
+}
+
+// codes of four elements, inverse = 2^-e; a NaN row's are zeros
+__device__ __forceinline__ unsigned quantise4(float a, float b, float c, float d, float inverse, int kind)
+{
+    if (inverse == 0.f) return 0u;
+    a *= inverse;
+    b *= inverse;
+    c *= inverse;
+    d *= inverse;
+    if (kind == kE4m3) {
+        unsigned short lo, hi;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+        return (unsigned)lo | (unsigned)hi << 16;
+    }
+    auto whole = [](float x) { return (unsigned)(__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 255); };
+    return whole(a) | whole(b) << 8 | whole(c) << 16 | whole(d) << 24;
+}
+__device__ __forceinline__ unsigned quantise1(float a, float inverse, int kind) { return quantise4(a, 0.f, 0.f, 0.f, inverse, kind) & 255u; }
+
+// four codes as they stand, without their scale
+__device__ __forceinline__ float4 codes_to_float(unsigned w, int kind)
+{
+    if (kind == kI8) return make_float4((float)(signed char)(w & 255u), (float)(signed char)(w >> 8 & 255u), (float)(signed char)(w >> 16 & 255u), (float)(signed char)(w >> 24));
+    unsigned lo, hi;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((unsigned short)w));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), y = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
+    return make_float4(x.x, x.y, y.x, y.y);
+}
+
+}  // namespace wkv

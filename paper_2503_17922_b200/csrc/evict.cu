@@ -38,9 +38,17 @@ __device__ __forceinline__ unsigned evict_key(float w, bool is_recent, bool amon
     return w != w ? 1u : topk_order_key(w);
 }
 
+// where a row's scale stands, whose page is one
+__device__ __forceinline__ long long scale_place(const EvictArgs &a, int unit, int row)
+{
+    const int b = unit / a.hkv, pg = row / a.page_size, page = __ldg(a.table + (long long)b * a.max_pages + pg);
+    return ((long long)page * a.hkv + (unit - b * a.hkv)) * a.page_size + (row - pg * a.page_size);
+}
+
 // MOVES: the rows are moved here as well, without a second kernel
 template <bool MOVES>
-__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ PoolTable pools)
+__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ PoolTable pools,
+                                                                   const __grid_constant__ ScaleTable scales)
 {
     extern __shared__ unsigned held[];
     __shared__ SelectSmem sm;
@@ -229,6 +237,13 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
             char *pool = static_cast<char *>(pools.ptr[tensor]);
             reinterpret_cast<int4 *>(pool + at.x * a.elem_bytes)[v] = reinterpret_cast<const int4 *>(pool + at.y * a.elem_bytes)[v];
         }
+        if (a.scaled)
+            for (int x = tid; x < moved * a.n_tensors; x += kSelThreads) {
+                const int tensor = x / moved, move = x - tensor * moved;
+                const longlong2 at = few_places[move];
+                if (at.x < 0 || at.y < 0) continue;
+                scales.ptr[tensor][scale_place(a, unit, few[move].x)] = scales.ptr[tensor][scale_place(a, unit, few[move].y)];
+            }
     }
     if (tid == 0) {
         a.counts[unit] = moved;
@@ -241,7 +256,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const __grid_
 // registers) 148, one 154; with the rows' places looked up here, 204.
 constexpr int kAhead = 2;
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ PoolTable pools,
-                                                                  int lanes_shift)
+                                                                  const __grid_constant__ ScaleTable scales, int lanes_shift)
 {
     pdl_trigger();
     pdl_wait();
@@ -262,6 +277,14 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
                 if (at[u].x >= 0 && at[u].y >= 0) reinterpret_cast<int4 *>(pool + at[u].x * a.elem_bytes)[v] = y[u];
+        }
+        if (a.scaled && lane == 0) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (at[u].x < 0 || at[u].y < 0) continue;
+                const int2 mv = a.moves[(long long)unit * a.moves_max + x0 + u * step];
+                scales.ptr[tensor][scale_place(a, unit, mv.x)] = scales.ptr[tensor][scale_place(a, unit, mv.y)];
+            }
         }
     }
 }
@@ -297,7 +320,7 @@ __global__ void __launch_bounds__(256) seed_rows_kernel(const __grid_constant__ 
 
 }  // namespace
 
-int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream)
+int launch_evict(const EvictArgs &a, const PoolTable &pools, const ScaleTable &scales, cudaStream_t stream)
 {
     const int units = a.batch * a.hkv;
     const size_t smem = (size_t)(a.cap < kHeldKeys ? a.cap : kHeldKeys) * sizeof(unsigned);
@@ -308,8 +331,8 @@ int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream
     const bool here = most_moves <= kFewMoves && most_moves * vecs * a.n_tensors <= kFewVecs;
     static SmemAsked asked[2];
     cudaError_t err = here ? allow_smem(evict_select_kernel<true>, kHeldKeys * 4, asked[1]) : allow_smem(evict_select_kernel<false>, kHeldKeys * 4, asked[0]);
-    if (err == cudaSuccess) err = here ? launch_pdl(evict_select_kernel<true>, dim3(units), kSelThreads, smem, stream, 1, a, pools)
-                                       : launch_pdl(evict_select_kernel<false>, dim3(units), kSelThreads, smem, stream, 1, a, pools);
+    if (err == cudaSuccess) err = here ? launch_pdl(evict_select_kernel<true>, dim3(units), kSelThreads, smem, stream, 1, a, pools, scales)
+                                       : launch_pdl(evict_select_kernel<false>, dim3(units), kSelThreads, smem, stream, 1, a, pools, scales);
     if (err != cudaSuccess) return check_cuda(err, "eviction kernel");
     count_launches(1);
     if (here) return WKV_OK;
@@ -325,7 +348,7 @@ int launch_evict(const EvictArgs &a, const PoolTable &pools, cudaStream_t stream
     const long long rows = kAhead * (kMoveThreads >> lanes_shift), most = (most_moves + rows - 1) / rows;
     if (slices > most) slices = most;
     if (slices < 1) slices = 1;
-    err = launch_pdl(evict_move_kernel, dim3((unsigned)pairs, (unsigned)slices), kMoveThreads, 0, stream, 1, a, pools, lanes_shift);
+    err = launch_pdl(evict_move_kernel, dim3((unsigned)pairs, (unsigned)slices), kMoveThreads, 0, stream, 1, a, pools, scales, lanes_shift);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "eviction kernel (rows)");
 }
