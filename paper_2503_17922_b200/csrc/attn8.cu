@@ -74,22 +74,6 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Codes of four elements as two pairs of f16.  Integers: with the sign bit flipped they count from 0 to 255, as the low byte of an f16 in
-// 1024 .. 1279, from which 1152 is taken.
-template <int KIND>
-__device__ __forceinline__ void to_f16(uint32_t w, uint32_t &lo, uint32_t &hi)
-{
-    if (KIND == kE4m3) {
-        asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
-    } else {
-        w ^= 0x80808080u;
-        lo = __byte_perm(w, 0x64646464u, 0x4140);
-        hi = __byte_perm(w, 0x64646464u, 0x4342);
-        const uint32_t by = 0x64806480u;
-        asm("sub.f16x2 %0, %0, %1;" : "+r"(lo) : "r"(by));
-        asm("sub.f16x2 %0, %0, %1;" : "+r"(hi) : "r"(by));
-    }
-}
 // codes that are NaN, as bytes of ones
 template <int KIND>
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w)
@@ -268,8 +252,8 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uint32_t f[4];
-                    to_f16<KIND>(w0[i], f[0], f[2]);
-                    to_f16<KIND>(w1[i], f[1], f[3]);
+                    codes_to_f16<KIND>(w0[i], f[0], f[2]);
+                    codes_to_f16<KIND>(w1[i], f[1], f[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma_f16(part[i & 1][n], f, q[n][c][2 * i], q[n][c][2 * i + 1]);
                 }
@@ -389,10 +373,10 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
                 uint32_t f[2][4];             // columns 4 i, 4 i + 1 and 4 i + 2, 4 i + 3
-                to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x5140), f[0][0], f[0][1]);
-                to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x5140), f[0][2], f[0][3]);
-                to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x7362), f[1][0], f[1][1]);
-                to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x7362), f[1][2], f[1][3]);
+                codes_to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x5140), f[0][0], f[0][1]);
+                codes_to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x5140), f[0][2], f[0][3]);
+                codes_to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x7362), f[1][0], f[1][1]);
+                codes_to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x7362), f[1][2], f[1][3]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     mma_f16(o[n][(c * kWords + i) * 2], f[0], p[n][0], p[n][1]);

@@ -55,15 +55,41 @@ __device__ __forceinline__ unsigned quantise4(float a, float b, float c, float d
 }
 __device__ __forceinline__ unsigned quantise1(float a, float inverse, int kind) { return quantise4(a, 0.f, 0.f, 0.f, inverse, kind) & 255u; }
 
-// four codes as they stand, without their scale
-__device__ __forceinline__ float4 codes_to_float(unsigned w, int kind)
+// Codes of four elements as two pairs of f16, exactly.  Integers: with the sign bit flipped they count from 0 to 255, as the low byte of an f16
+// in 1024 .. 1279, from which 1152 is taken.
+template <int KIND>
+__device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t &lo, uint32_t &hi)
 {
-    if (kind == kI8) return make_float4((float)(signed char)(w & 255u), (float)(signed char)(w >> 8 & 255u), (float)(signed char)(w >> 16 & 255u), (float)(signed char)(w >> 24));
-    unsigned lo, hi;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((unsigned short)w));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((unsigned short)(w >> 16)));
+    if (KIND == kE4m3) {
+        asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+    } else {
+        w ^= 0x80808080u;
+        lo = __byte_perm(w, 0x64646464u, 0x4140);
+        hi = __byte_perm(w, 0x64646464u, 0x4342);
+        const uint32_t by = 0x64806480u;
+        asm("sub.f16x2 %0, %0, %1;" : "+r"(lo) : "r"(by));
+        asm("sub.f16x2 %0, %0, %1;" : "+r"(hi) : "r"(by));
+    }
+}
+// four codes as they stand, without their scale
+template <int KIND>
+__device__ __forceinline__ float4 codes_to_float(unsigned w)
+{
+    uint32_t lo, hi;
+    codes_to_f16<KIND>(w, lo, hi);
     const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), y = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
     return make_float4(x.x, x.y, y.x, y.y);
+}
+__device__ __forceinline__ float4 codes_to_float(unsigned w, int kind) { return kind == kE4m3 ? codes_to_float<kE4m3>(w) : codes_to_float<kI8>(w); }
+// two pairs of bf16: four codes times their scale, exactly
+template <int KIND>
+__device__ __forceinline__ uint2 codes_to_bf16(unsigned w, float by)
+{
+    const float4 x = codes_to_float<KIND>(w);
+    uint2 r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x.y * by), "f"(x.x * by));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.y) : "f"(x.w * by), "f"(x.z * by));
+    return r;
 }
 
 }  // namespace wkv
