@@ -1,8 +1,8 @@
 // Attention over the 8-bit cache on warp-level matrix instructions (m16n8k16, f16): single tokens, short chunks and drafts, and the
 // shapes that the tcgen05 kernel does not take.
 //
-// A block of four warps walks over the keys of one unit (or a split of them) in tiles of 64, which come through a ring of asynchronous
-// 16-byte copies, codes as they are; a warp takes 16 of a tile's keys and keeps a maximum and a sum of its own, joined once at the end.
+// A block of four warps walks over the keys of one unit (or a split of them) in tiles of 128, which come through a ring of asynchronous
+// 16-byte copies, codes as they are; a warp takes 32 of a tile's keys and keeps a maximum and a sum of its own, joined once at the end.
 //   S^T = K Q^T     16 keys x 8 rows (position x head of the group) per instruction, K's codes as operand A
 //   O^T += V^T P^T  16 columns x 8 rows, V's codes as operand A
 // Keys and columns are on the M side, so that the few rows that share them fill N = 8 and not a quarter of M = 16; the accumulator of the
@@ -24,8 +24,9 @@ namespace wkv {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kKeys = 64;
-__host__ __device__ constexpr int stages_for(int dp) { return dp == 64 ? 5 : 3; }
+constexpr int kKeys = 128;
+constexpr int kGroups = 2;                     // of 16 keys, of a warp
+__host__ __device__ constexpr int stages_for(int dp) { return dp == 64 ? 3 : 2; }
 
 template <int DP>
 struct Smem8 {
@@ -33,7 +34,7 @@ struct Smem8 {
     __align__(128) unsigned char v[stages_for(DP)][kKeys * DP];
     long long at[2][kKeys];                    // byte offsets of a tile's rows, -1: none
     float scale[stages_for(DP)][2][kKeys];     // of K and V; 0: the row has no page
-    int missing[stages_for(DP) + 1][2];        // of a tile's two halves: some row has no page
+    __align__(16) int missing[stages_for(DP) + 1][4];        // of a tile's four quarters: some row has no page
     float m[4][16], l[4][16], lse2[16];
 };
 
@@ -83,7 +84,7 @@ __device__ __forceinline__ uint32_t nan_codes(uint32_t w)
 
 // NT: tiles of eight rows.  DRAFT: the rows go by their masks.
 template <int DP, int KIND, int NT, bool DRAFT>
-__global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) attn8_kernel(const __grid_constant__ AttnArgs a)
+__global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1 ? 4 : 3)) attn8_kernel(const __grid_constant__ AttnArgs a, int page_shift)
 {
     extern __shared__ __align__(128) unsigned char raw[];
     Smem8<DP> &sm = *reinterpret_cast<Smem8<DP> *>(raw);
@@ -181,69 +182,93 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
     float v_ref = __uint_as_float((unsigned)(kScaleBias + kLeastExponent) << 23);      // O is in units of v_ref / 2^15
 
     // ---- the ring of key tiles -----------------------------------------------------------------
-    // A row's place is looked up a tile ahead of its load, its scale a tile behind that: a trip to memory each.  The first 64 threads have the
-    // tile's rows for K's scales, the others for V's.
-    const int mine = tid & (kKeys - 1), kv = tid >> 6;
-    const unsigned char *const scales = kv ? a.v_scales : a.k_scales;
-    long long place, scale_place;
+    // A thread has a row of the tile: its place is looked up a tile ahead of its load, its scales a tile behind that: a trip to memory each.
+    const int *const table = a.table + (long long)b * a.max_pages;
+    auto page_of = [&](int j, int &slot) {
+        const int pg = page_shift >= 0 ? j >> page_shift : j / a.page_size;
+        slot = j - pg * a.page_size;
+        return __ldg(table + pg);
+    };
+    int page = -1, slot = 0;
     auto look_up = [&](int t) {
-        const int j = t * kKeys + mine;
-        place = t < t1 && j < sq.n ? attn_row(a, b, h, sq.q_off, j) : -1;
-        scale_place = place >= 0 ? attn_scale(a, b, h, j) : -1;
+        const int j = t * kKeys + tid;
+        page = -1;
+        if (t < t1 && j < sq.n) page = page_of(j, slot);
     };
+    int byte[2] = {-1, -1};                   // scales of the row whose place was kept last
     auto keep_place = [&](int t) {
-        if (kv) return;
-        sm.at[t & 1][mine] = place;
-        const unsigned there = __ballot_sync(0xffffffffu, place >= 0);
+        const bool have = (unsigned)page < (unsigned)a.num_pages;
+        sm.at[t & 1][tid] = have ? page * a.kb + h * a.kh + (long long)slot * a.kt : -1;
+        const unsigned there = __ballot_sync(0xffffffffu, have);
         if (lane == 0) sm.missing[t % (NS + 1)][warp] = there != 0xffffffffu;
+        byte[0] = byte[1] = -1;
+        if (have) {
+            const long long at = ((long long)page * a.hkv + h) * a.page_size + slot;
+            byte[0] = a.k_scales[at];
+            byte[1] = a.v_scales[at];
+        }
     };
-    auto fetch_scale = [&]() { return scale_place >= 0 ? (int)scales[scale_place] : -1; };
-    auto keep_scale = [&](int t, int byte) { sm.scale[t % NS][kv][mine] = byte < 0 ? 0.f : scale_value(byte); };
+    auto keep_scales = [&](int t) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) sm.scale[t % NS][x][tid] = byte[x] < 0 ? 0.f : scale_value(byte[x]);
+    };
     constexpr int kChunks = DP / 16, kRowsAtOnce = kThreads / kChunks;
-    const int chunk = tid % kChunks;
+    const int chunk = tid % kChunks, row_of = tid / kChunks;
     const bool real = chunk * 16 < a.d;
+    const unsigned char *const k_from = static_cast<const unsigned char *>(a.k) + chunk * 16, *const v_from = static_cast<const unsigned char *>(a.v) + chunk * 16;
+    // (the permutations of a line's chunks repeat every eight rows, and kRowsAtOnce rows on is the same place in them, or the same but for known bits)
     auto load = [&](int t) {
         if (t < t1) {
             const int st = t % NS;
             const uint32_t ks = smem_addr(&sm.k[st][0]), vs = smem_addr(&sm.v[st][0]);
 #pragma unroll
-            for (int r = tid / kChunks; r < kKeys; r += kRowsAtOnce) {
-                const long long at = sm.at[t & 1][r];
+            for (int r = 0; r < kKeys; r += kRowsAtOnce) {
+                const long long at = sm.at[t & 1][row_of + r];
                 const bool have = at >= 0 && real;
-                const unsigned char *kp = static_cast<const unsigned char *>(a.k) + (have ? at + chunk * 16 : 0);
-                const unsigned char *vp = static_cast<const unsigned char *>(a.v) + (have ? at + chunk * 16 : 0);
+                const long long off = have ? at : 0;
                 const int size = have ? 16 : 0;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + chunk_at<DP, false>(r, chunk)), "l"(kp), "r"(size) : "memory");
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + chunk_at<DP, true>(r, chunk)), "l"(vp), "r"(size) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ks + chunk_at<DP, false>(row_of + r, chunk)), "l"(k_from + off), "r"(size) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vs + chunk_at<DP, true>(row_of + r, chunk)), "l"(v_from + off), "r"(size) : "memory");
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     look_up(t0);
     keep_place(t0);
-    int byte = fetch_scale();                                            // of the tile whose place was kept last
     for (int x = 0; x < NS - 1; ++x) {
         look_up(t0 + x + 1);
         __syncthreads();
         load(t0 + x);
-        keep_scale(t0 + x, byte);
+        keep_scales(t0 + x);
         keep_place(t0 + x + 1);
-        byte = fetch_scale();
     }
+    // where this row's logits go, less the keys of the block's first tile
+    float *logits[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = row0 + n * 8 + 2 * ql + e;
+            logits[n][e] = a.logits && row < rows ? a.logits + ((long long)unit * a.rows_max + row) * a.logit_stride + warp * 32 + quad : nullptr;
+        }
     for (int t = t0; t < t1; ++t) {
         const int st = t % NS;
         look_up(t + NS);
         asm volatile("cp.async.wait_group %0;" ::"n"(NS - 2) : "memory");
         __syncthreads();                      // tile t has landed for all; the stage of tile t - 1 is free; places of t + NS - 1 are there
         load(t + NS - 1);
-        const int j0 = t * kKeys, key0 = warp * 16;
-        const bool holes = sm.missing[t % (NS + 1)][0] | sm.missing[t % (NS + 1)][1], masked = j0 + kKeys > plain || holes;
-        const float k_scale[2] = {sm.scale[st][0][key0 + quad], sm.scale[st][0][key0 + quad + 8]};
-        const float v_scale[2] = {sm.scale[st][1][key0 + quad], sm.scale[st][1][key0 + quad + 8]};
-        // ---- logits: keys quad and quad + 8 ----------------------------------------------------------
-        float s[NT][4];
-        {
-            float part[2][NT][4] = {};
+        const int j0 = t * kKeys + warp * 32;                            // the warp's first key
+        const int4 gaps = *reinterpret_cast<const int4 *>(&sm.missing[t % (NS + 1)][0]);
+        const bool holes = gaps.x | gaps.y | gaps.z | gaps.w, masked = (t + 1) * kKeys > plain || holes;
+        // ---- logits: keys quad and quad + 8 of each group ----------------------------------------------
+        float s[kGroups][NT][4] = {};
+        float v_scale[kGroups][2];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int key0 = warp * 32 + g * 16;
+            const float k_scale[2] = {sm.scale[st][0][key0 + quad], sm.scale[st][0][key0 + quad + 8]};
+            v_scale[g][0] = sm.scale[st][1][key0 + quad];
+            v_scale[g][1] = sm.scale[st][1][key0 + quad + 8];
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) {
                 const uint4 k0 = *reinterpret_cast<const uint4 *>(&sm.k[st][chunk_at<DP, false>(key0 + quad, c * 4 + ql)]);
@@ -255,44 +280,49 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
                     codes_to_f16<KIND>(w0[i], f[0], f[2]);
                     codes_to_f16<KIND>(w1[i], f[1], f[3]);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_f16(part[i & 1][n], f, q[n][c][2 * i], q[n][c][2 * i + 1]);
+                    for (int n = 0; n < NT; ++n) mma_f16(s[g][n], f, q[n][c][2 * i], q[n][c][2 * i + 1]);
                 }
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) s[n][y] = (part[0][n][y] + part[1][n][y]) * (scale_of[n][y & 1] * k_scale[y >> 1]);
+                for (int y = 0; y < 4; ++y) s[g][n][y] *= scale_of[n][y & 1] * k_scale[y >> 1];
         }
-        unsigned hidden = 0u;                 // bit 4 n + y: the row does not see the key
+        unsigned hidden = 0u;                 // bit (g NT + n) 4 + y: the row does not see the key
         bool unseen = false;                  // ... and there are such a key and such a row
         if (masked) {
 #pragma unroll
-            for (int y = 0; y < 4; y += 2) {
-                const int j = j0 + key0 + quad + 4 * y;
-                bool there = j < sq.n;
-                if (there && holes) there = attn_row(a, b, h, sq.q_off, j) >= 0;
+            for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        if (there && sees(n, e, j)) continue;
-                        s[n][y + e] = -INFINITY;
-                        hidden |= 1u << (4 * n + y + e);
-                        unseen |= there;
+                for (int y = 0; y < 4; y += 2) {
+                    const int j = j0 + g * 16 + quad + 4 * y;
+                    bool there = j < sq.n;
+                    if (there && holes) {
+                        int unused;
+                        there = (unsigned)page_of(j, unused) < (unsigned)a.num_pages;
                     }
-            }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (there && sees(n, e, j)) continue;
+                            s[g][n][y + e] = -INFINITY;
+                            hidden |= 1u << ((g * NT + n) * 4 + y + e);
+                            unseen |= there;
+                        }
+                }
         }
         if (a.logits) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int row = row0 + n * 8 + 2 * ql + (y & 1), j = j0 + key0 + quad + 8 * (y >> 1);
-                    if (row < rows && j < sq.n) a.logits[((long long)unit * a.rows_max + row) * a.logit_stride + j] = s[n][y];
-                }
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (logits[n][y & 1] && j0 + g * 16 + quad + 8 * (y >> 1) < sq.n) logits[n][y & 1][t * kKeys + g * 16 + 8 * (y >> 1)] = s[g][n][y];
         }
         // ---- weights ---------------------------------------------------------------------------------
-        float v_top = fmaxf(v_scale[0], v_scale[1]);
+        float v_top = fmaxf(fmaxf(v_scale[0][0], v_scale[0][1]), fmaxf(v_scale[1][0], v_scale[1][1]));
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, x));
         float grow = 1.f;
@@ -300,33 +330,45 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
             grow = v_ref / v_top;
             v_ref = v_top;
         }
-        const float unit_of = 32768.f / v_ref, v_by[2] = {v_scale[0] * unit_of, v_scale[1] * unit_of};
-        uint32_t p[NT][2];
+        // 2^15 / v_ref, a power of two by its bits
+        const float unit_of = __uint_as_float((269u << 23) - __float_as_uint(v_ref));
+        uint32_t p[kGroups][NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float w[4], keep[2];
+            float w[kGroups][4], keep[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float top = fmaxf(s[n][e], s[n][2 + e]);
+                float top = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
                 top = fmaxf(m[n][e], top);
                 const float ref = top == -INFINITY ? 0.f : top;
                 keep[e] = ex2(m[n][e] - ref);
                 m[n][e] = top;
-                const float p0 = ex2(s[n][e] - ref), p1 = ex2(s[n][2 + e] - ref);
-                l[n][e] = l[n][e] * keep[e] + (p0 + p1);                 // this thread's keys; joined over the quads at the end
-                w[e] = p0 * v_by[0];
-                w[2 + e] = p1 * v_by[1];
+                float sum = 0.f;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float x = ex2(s[g][n][2 * y + e] - ref);
+                        sum += x;
+                        w[g][2 * y + e] = x * (v_scale[g][y] * unit_of);
+                    }
+                l[n][e] = l[n][e] * keep[e] + sum;                       // this thread's keys; joined over the quads at the end
                 keep[e] *= grow;
             }
             if (masked) {
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    if (hidden >> (4 * n + y) & 1u) w[y] = 0.f;          // (0 times a NaN scale is not 0)
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (hidden >> ((g * NT + n) * 4 + y) & 1u) w[g][y] = 0.f;          // (0 times a NaN scale is not 0)
             }
-            p[n][0] = transposed(pack_f16(w[0], w[1]));
-            p[n][1] = transposed(pack_f16(w[2], w[3]));
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                p[g][n][0] = transposed(pack_f16(w[g][0], w[g][1]));
+                p[g][n][1] = transposed(pack_f16(w[g][2], w[g][3]));
+            }
             if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
 #pragma unroll
                 for (int x = 0; x < kTiles; ++x) {
@@ -343,50 +385,52 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
         const bool look = KIND == kE4m3 && masked && __any_sync(0xffffffffu, unseen);
         constexpr int kWords = DP == 64 ? 2 : 4;
 #pragma unroll
-        for (int c = 0; c < kCols / (4 * kWords); ++c) {
-            uint32_t w[4][kWords];
+        for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int row = key0 + 2 * ql + (x & 1) + (x >> 1) * 8;
-                if constexpr (DP == 64) {
-                    const uint2 y = *reinterpret_cast<const uint2 *>(&sm.v[st][chunk_at<DP, true>(row, quad >> 1) + (quad & 1) * 8]);
-                    w[x][0] = y.x;
-                    w[x][1] = y.y;
-                } else {
-                    const uint4 y = *reinterpret_cast<const uint4 *>(&sm.v[st][chunk_at<DP, true>(row, c * 8 + quad)]);
-                    w[x][0] = y.x;
-                    w[x][1] = y.y;
-                    w[x][2] = y.z;
-                    w[x][3] = y.w;
-                }
-            }
-            if (look) {
+            for (int c = 0; c < kCols / (4 * kWords); ++c) {
+                uint32_t w[4][kWords];
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int i = 0; i < kWords; ++i) {
-                        const uint32_t bad = nan_codes<KIND>(w[x][i]);
-                        poisoned |= bad != 0u;
-                        w[x][i] &= ~bad;
+                for (int x = 0; x < 4; ++x) {
+                    const int row = warp * 32 + g * 16 + 2 * ql + (x & 1) + (x >> 1) * 8;
+                    if constexpr (DP == 64) {
+                        const uint2 y = *reinterpret_cast<const uint2 *>(&sm.v[st][chunk_at<DP, true>(row, quad >> 1) + (quad & 1) * 8]);
+                        w[x][0] = y.x;
+                        w[x][1] = y.y;
+                    } else {
+                        const uint4 y = *reinterpret_cast<const uint4 *>(&sm.v[st][chunk_at<DP, true>(row, c * 8 + quad)]);
+                        w[x][0] = y.x;
+                        w[x][1] = y.y;
+                        w[x][2] = y.z;
+                        w[x][3] = y.w;
                     }
-            }
+                }
+                if (look) {
 #pragma unroll
-            for (int i = 0; i < kWords; ++i) {
-                uint32_t f[2][4];             // columns 4 i, 4 i + 1 and 4 i + 2, 4 i + 3
-                codes_to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x5140), f[0][0], f[0][1]);
-                codes_to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x5140), f[0][2], f[0][3]);
-                codes_to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x7362), f[1][0], f[1][1]);
-                codes_to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x7362), f[1][2], f[1][3]);
+                    for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    mma_f16(o[n][(c * kWords + i) * 2], f[0], p[n][0], p[n][1]);
-                    mma_f16(o[n][(c * kWords + i) * 2 + 1], f[1], p[n][0], p[n][1]);
+                        for (int i = 0; i < kWords; ++i) {
+                            const uint32_t bad = nan_codes<KIND>(w[x][i]);
+                            poisoned |= bad != 0u;
+                            w[x][i] &= ~bad;
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) {
+                    uint32_t f[2][4];             // columns 4 i, 4 i + 1 and 4 i + 2, 4 i + 3
+                    codes_to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x5140), f[0][0], f[0][1]);
+                    codes_to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x5140), f[0][2], f[0][3]);
+                    codes_to_f16<KIND>(__byte_perm(w[0][i], w[1][i], 0x7362), f[1][0], f[1][1]);
+                    codes_to_f16<KIND>(__byte_perm(w[2][i], w[3][i], 0x7362), f[1][2], f[1][3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma_f16(o[n][(c * kWords + i) * 2], f[0], p[g][n][0], p[g][n][1]);
+                        mma_f16(o[n][(c * kWords + i) * 2 + 1], f[1], p[g][n][0], p[g][n][1]);
+                    }
                 }
             }
-        }
         if (look && __any_sync(0xffffffffu, poisoned)) {
-            for (int kk = 0; kk < 16; ++kk) {
-                const int row = key0 + kk, j = j0 + row;
+            for (int kk = 0; kk < 32; ++kk) {
+                const int row = warp * 32 + kk, j = j0 + kk;
                 if (j >= sq.n) break;
 #pragma unroll
                 for (int x = 0; x < kTiles; ++x)
@@ -403,9 +447,8 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (NT == 1 ? 4 : 3)) a
                     }
             }
         }
-        keep_scale(t + NS - 1, byte);
+        keep_scales(t + NS - 1);
         keep_place(t + NS);
-        byte = fetch_scale();
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -496,9 +539,10 @@ int launch8(const AttnArgs &a, cudaStream_t stream)
         set_error_detail("attention: %lld blocks", blocks);
         return WKV_ERR_LIMIT;
     }
+    const int page_shift = (a.page_size & (a.page_size - 1)) == 0 ? __builtin_ctz(a.page_size) : -1;
     cudaError_t err = allow_smem(attn8_kernel<DP, KIND, NT, DRAFT>, sizeof(Smem8<DP>), asked);
     if (err == cudaSuccess) err = launch_pdl(attn8_kernel<DP, KIND, NT, DRAFT>, dim3((unsigned)blocks), kThreads, sizeof(Smem8<DP>), stream,
-                                             a.clustered ? a.splits : 1, a);
+                                             a.clustered ? a.splits : 1, a, page_shift);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "attention kernel (8-bit cache)");
 }

@@ -81,15 +81,47 @@ __device__ __forceinline__ float4 codes_to_float(unsigned w)
     return make_float4(x.x, x.y, y.x, y.y);
 }
 __device__ __forceinline__ float4 codes_to_float(unsigned w, int kind) { return kind == kE4m3 ? codes_to_float<kE4m3>(w) : codes_to_float<kI8>(w); }
-// two pairs of bf16: four codes times their scale, exactly
+// Two pairs of bf16: four codes times 2^e, exactly.  Where 2^e is an f16 (kLeastF16 .. kMostF16), by a multiply-add of f16 into fp32 per element: integers
+// keep the 1152 that they are too large by (codes_to_f16) until then.
+constexpr int kLeastF16 = kScaleBias - 24, kMostF16 = kScaleBias + 15;
+__device__ __forceinline__ uint32_t pack_pair_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 template <int KIND>
 __device__ __forceinline__ uint2 codes_to_bf16(unsigned w, float by)
 {
     const float4 x = codes_to_float<KIND>(w);
-    uint2 r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x.y * by), "f"(x.x * by));
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.y) : "f"(x.w * by), "f"(x.z * by));
-    return r;
+    return make_uint2(pack_pair_bf16(x.x * by, x.y * by), pack_pair_bf16(x.z * by, x.w * by));
 }
+template <int KIND>
+struct F16Scale {
+    unsigned short by;
+    float more;
+    __device__ __forceinline__ explicit F16Scale(float s)
+    {
+        asm("cvt.rn.f16.f32 %0, %1;" : "=h"(by) : "f"(s));
+        more = KIND == kI8 ? -1152.f * s : 0.f;
+    }
+    __device__ __forceinline__ uint32_t pair(uint32_t x) const
+    {
+        float lo, hi;
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tfma.rn.f32.f16 %0, a, %3, %4;\n\tfma.rn.f32.f16 %1, b, %3, %4;\n\t}"
+            : "=f"(lo), "=f"(hi) : "r"(x), "h"(by), "f"(more));
+        return pack_pair_bf16(lo, hi);
+    }
+    __device__ __forceinline__ uint2 four(uint32_t w) const
+    {
+        if (KIND == kI8) {
+            w ^= 0x80808080u;
+            return make_uint2(pair(__byte_perm(w, 0x64646464u, 0x4140)), pair(__byte_perm(w, 0x64646464u, 0x4342)));
+        }
+        uint32_t lo, hi;
+        codes_to_f16<KIND>(w, lo, hi);
+        return make_uint2(pair(lo), pair(hi));
+    }
+};
 
 }  // namespace wkv
