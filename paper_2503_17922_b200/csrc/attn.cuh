@@ -34,6 +34,7 @@ struct AttnArgs {
     int *status;                 // or null
     // key splits: `splits` > 1 leaves partial results for the joining kernel
     int splits;
+    bool few;                    // bf16: row tiles of 16 whatever their number
     bool clustered;              // the splits are the blocks of a cluster, which join them: no partial results in memory
     float *part_o;               // [units][rows_max][splits][d]: not yet normalised
     float2 *part_ml;             // [units][rows_max][splits]: (maximum in base 2, sum)

@@ -96,7 +96,8 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
     pdl_wait();
     const int units = a.batch * a.hkv;
     const int splits = a.splits, place_of = (int)blockIdx.x / splits, split = (int)blockIdx.x - place_of * splits;
-    const int unit = place_of % units, tile = place_of / units;
+    // (a unit's row tiles are neighbours: they read the same keys at about the same time, from L2)
+    const int tiles = (int)gridDim.x / splits / units, unit = place_of / tiles, tile = place_of - unit * tiles;
     const int b = unit / a.hkv, h = unit - b * a.hkv;
     const AttnSeq sq = attn_seq(a, b, h);
     const int rows = sq.m * a.G, row0 = tile * kRows;

@@ -593,7 +593,7 @@ static int launch_any(const AttnArgs &a, cudaStream_t stream)
 }
 int launch_attn_mma(const AttnArgs &a, cudaStream_t stream)
 {
-    if (a.masks) return a.rows_max <= 16 ? launch_any<true, true>(a, stream) : launch_any<false, true>(a, stream);
+    if (a.masks) return a.rows_max <= 16 || a.few ? launch_any<true, true>(a, stream) : launch_any<false, true>(a, stream);
     return a.rows_max <= 16 ? launch_any<true, false>(a, stream) : launch_any<false, false>(a, stream);
 }
 

@@ -106,6 +106,7 @@ Cache8Pages pages_of(const wkv_paged *c)
     return {c->block_table, c->max_pages, c->page_size, c->num_pages, c->page_stride, c->head_stride, c->row_stride};
 }
 
+constexpr int kFewDraftRows = 64;
 int check_draft(const wkv_paged *c, const wkv_draft *d)
 {
     if (d->struct_size != sizeof(wkv_draft)) {
@@ -352,6 +353,14 @@ int wkv_attend_draft_paged(const wkv_paged *c, const wkv_draft *draft, const voi
         return st;
     a.masks = draft->masks;
     a.mask_words = draft->words;
+    // A small draft over a short cache: every 16 rows read the keys for themselves, split over the blocks of a cluster, where all of those
+    // run at once.
+    bool clustered = false;
+    const int splits = c->dtype == WKV_BF16 && p.rows_max > 16 && p.rows_max <= kFewDraftRows ? plan_splits(c, p, 16, clustered) : 0;
+    if (clustered && splits > 1) {
+        a.few = a.clustered = true;
+        a.splits = splits;
+    }
     return launch_attend(c, p, w, a, static_cast<char *>(workspace), static_cast<cudaStream_t>(cuda_stream));
 }
 

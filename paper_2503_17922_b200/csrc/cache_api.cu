@@ -8,7 +8,7 @@ int launch_attend(const wkv_paged *c, const Paged &p, const PagedWorkspace &w, c
 {
     // Up to 16 rows are one tile of the warp-level kernel, whose time is that of the loads.
     int st = WKV_ERR_UNSUPPORTED;
-    if (p.rows_max > kFewRows && attn_tc_supported(a, c->dtype))
+    if (p.rows_max > (a.kind != kPlain ? kFewRows8 : kFewRows) && !a.few && attn_tc_supported(a, c->dtype))
         st = launch_attn_tc(a, w.pieces ? reinterpret_cast<float *>(ws + w.piece_o_off) : nullptr, reinterpret_cast<float2 *>(ws + w.piece_ml_off),
                             reinterpret_cast<long long *>(ws + w.line_off), stream);
     if (st == WKV_ERR_UNSUPPORTED) {

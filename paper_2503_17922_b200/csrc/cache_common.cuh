@@ -169,9 +169,8 @@ struct PagedWorkspace {
 // kernel; one sequence of 8 heads x 992 rows 8.8 and 12.6) and a block has no more than kClusterBytes of keys and values to read.
 constexpr int kSplitBlocks = 2 * 148, kSplitKeys = 64, kSplitEven = 1024;
 constexpr long long kClusterBytes = 512 << 10;
-inline int plan_splits(const wkv_paged *c, const Paged &p, bool &clustered)
+inline int plan_splits(const wkv_paged *c, const Paged &p, int tile, bool &clustered)
 {
-    const int tile = p.rows_max <= 16 || (p.pool_eb == 1 && p.eb == 2) ? 16 : 64;
     const long long blocks = ((long long)p.rows_max + tile - 1) / tile * p.units;
     long long s = (kSplitBlocks + blocks - 1) / blocks;
     if (s > (p.cap + kSplitKeys - 1) / kSplitKeys) s = (p.cap + kSplitKeys - 1) / kSplitKeys;
@@ -179,19 +178,23 @@ inline int plan_splits(const wkv_paged *c, const Paged &p, bool &clustered)
     if (s < 1) s = 1;
     long long power = 1;
     while (power < s && power < kClusterSplits) power *= 2;
-    clustered = p.rows_max <= 16 && blocks * power <= kSplitBlocks &&
+    clustered = tile == 16 && blocks * power <= kSplitBlocks &&
                 (s <= power || 2ll * p.cap * c->head_dim * p.pool_eb / kClusterSplits <= kClusterBytes);
     return (int)(clustered ? power : s);
 }
 // More rows than this go to the tensor-core kernel where it takes the shape (8 new tokens of 32 heads on 8, 32 rows: 4 sequences of 16,384
 // keys 171 us on the warp-level kernel, 88 here; one of 4,000 42 and 32).
 constexpr int kFewRows = 16;
+// Over the 8-bit cache the tensor-core kernel has the codes to convert, for one query tile as for two: more rows are left to the warp-level one, which reads the
+// keys once more for every 16 of them (16 drafts over 4-8 K rows of 8 heads, d = 128, 20 rows at most 82 us there and 166 on the tensor cores, 48
+// rows 117 and 172, 64 rows 135 and 175, 96 rows 176 and 178, 128 rows 221 and 179; one draft of 64 rows over 8 K 42 and 40).
+constexpr int kFewRows8 = 64;
 // Rows per unit whose logits are kept for the weights: 4 bytes for each beside the 2 * d * 2 of K and V, written and read.
 constexpr int kLogitRows = 16;
 inline PagedWorkspace plan_paged(const wkv_paged *c, const Paged &p)
 {
     PagedWorkspace w;
-    w.splits = plan_splits(c, p, w.clustered);
+    w.splits = plan_splits(c, p, p.rows_max <= 16 || (p.pool_eb == 1 && p.eb == 2) ? 16 : 64, w.clustered);
     size_t off = 256;
     w.lse_off = off;
     off = align_up(off + (size_t)c->batch * c->n_q_heads * c->max_new * sizeof(float), 256);
