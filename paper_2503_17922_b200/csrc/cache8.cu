@@ -6,6 +6,7 @@
 #include "cache8.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace wkv {
 namespace {
@@ -38,7 +39,9 @@ struct Gather8Args {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) gather8_kernel(const __grid_constant__ Gather8Args a)
 {
-    constexpr int kVec = 16 / sizeof(T), kEach = kAttnMaxHeadDim / kVec / 32, kAhead = kEach == 1 ? 4 : 2;
+    // two vectors to a lane: half as many lanes share a row's largest magnitude, scale and place
+    constexpr int kVec = 16 / sizeof(T), kEach = 2, kAhead = 2;
+    static_assert(kAttnMaxHeadDim / kVec <= 32 * kEach, "a row in the lanes of a warp");
     __shared__ long long from[kRows], to[kRows], to_scale[kRows];
     const KShape &s = a.s;
     pdl_trigger();
@@ -88,27 +91,28 @@ __global__ void __launch_bounds__(kThreads) gather8_kernel(const __grid_constant
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            unsigned most = 0u;
+            float top = 0.f;
 #pragma unroll
             for (int e = 0; e < kEach; ++e)
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) most = max(most, magnitude(to_float(reinterpret_cast<const T *>(&raw[u][e])[i])));
+                for (int i = 0; i < kVec; ++i) top = largest_nan(top, to_float(reinterpret_cast<const T *>(&raw[u][e])[i]));
+            unsigned most = magnitude(top);
             for (int o = 1; o < lanes; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
             const int x = x0 + u * groups + group, byte = scale_byte(most, a.kind);
             if (x >= rows || from[x] < 0) continue;
             if (lane == 0) scales[to_scale[x]] = (unsigned char)byte;
-            const float inverse = scale_inverse(byte);
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 const int piece = lane + e * lanes;
                 if (piece >= pieces) continue;
-                const T *v = reinterpret_cast<const T *>(&raw[u][e]);
-                unsigned char *dst = codes + to[x] + piece * kVec;
-                const unsigned lo = quantise4(to_float(v[0]), to_float(v[1]), to_float(v[2]), to_float(v[3]), inverse, a.kind);
-                if constexpr (kVec == 8)
-                    *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, quantise4(to_float(v[4]), to_float(v[5]), to_float(v[6]), to_float(v[7]), inverse, a.kind));
-                else
-                    *reinterpret_cast<unsigned *>(dst) = lo;
+                float v[kVec];
+                __align__(8) unsigned c[kVec / 4];
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) v[i] = to_float(reinterpret_cast<const T *>(&raw[u][e])[i]);
+                quantise<kVec>(v, c, byte, a.kind);
+                typename std::conditional<kVec == 8, uint2, unsigned>::type out;
+                out = *reinterpret_cast<const decltype(out) *>(c);
+                *reinterpret_cast<decltype(out) *>(codes + to[x] + piece * kVec) = out;
             }
         }
     }
@@ -121,14 +125,18 @@ struct Read8Args {
     void *out[2];
     const int *first, *lengths;
 };
-__device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
-__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x)
+// eight codes as what they stand for
+__device__ __forceinline__ void store8(float *p, uint2 w, float by, int kind)
+{
+    const float4 x = codes_to_float(w.x, kind), y = codes_to_float(w.y, kind);
+    reinterpret_cast<float4 *>(p)[0] = make_float4(x.x * by, x.y * by, x.z * by, x.w * by);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(y.x * by, y.y * by, y.z * by, y.w * by);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, uint2 w, float by, int kind)
 {
     // (exact: eight bits of a code at most, and a power of two)
-    uint2 r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x.y), "f"(x.x));
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.y) : "f"(x.w), "f"(x.z));
-    *reinterpret_cast<uint2 *>(p) = r;
+    const uint2 x = kind == kE4m3 ? codes_to_bf16<kE4m3>(w.x, by) : codes_to_bf16<kI8>(w.x, by), y = kind == kE4m3 ? codes_to_bf16<kE4m3>(w.y, by) : codes_to_bf16<kI8>(w.y, by);
+    *reinterpret_cast<uint4 *>(p) = make_uint4(x.x, x.y, y.x, y.y);
 }
 template <typename T>
 __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ Read8Args a)
@@ -166,14 +174,8 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
             byte[u] = scales[from_scale[x]];
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (byte[u] < 0) continue;
-            const float by = scale_value(byte[u]);
-            float4 lo = codes_to_float(raw[u].x, a.kind), hi = codes_to_float(raw[u].y, a.kind);
-            T *dst = out + (long long)(x0 + u * groups) * a.d;
-            store4(dst, make_float4(lo.x * by, lo.y * by, lo.z * by, lo.w * by));
-            store4(dst + 4, make_float4(hi.x * by, hi.y * by, hi.z * by, hi.w * by));
-        }
+        for (int u = 0; u < kAhead; ++u)
+            if (byte[u] >= 0) store8(out + (long long)(x0 + u * groups) * a.d, raw[u], scale_value(byte[u]), a.kind);
     }
 }
 
@@ -204,7 +206,7 @@ int launch_gather8(const KShape &ks, int dtype, int n_tensors, const LayerTable 
     a.window_idx = window_idx;
     a.kind = kind;
     a.units = ks.batch * ks.hkv;
-    a.lanes_shift = shift_for(ks.d * (dtype == WKV_F32 ? 4 : 2) / 16);
+    a.lanes_shift = shift_for((ks.d * (dtype == WKV_F32 ? 4 : 2) / 16 + 1) / 2);
     const long long most = (long long)ks.k_max * ks.omega + ks.alpha, parts = (std::min(most, (long long)ks.max_seqlen) + kRows - 1) / kRows;
     const long long blocks = (long long)a.units * n_tensors;
     if (const int st = check_grid(blocks, parts, "gather into the 8-bit cache")) return st;

@@ -36,24 +36,45 @@ __device__ __forceinline__ float scale_value(int byte)
     return byte == kScaleNan ? __uint_as_float(0x7fffffffu) : (byte == 0 ? __uint_as_float(0x400000u) : __uint_as_float((unsigned)byte << 23));
 }
 
-// codes of four elements, inverse = 2^-e; a NaN row's are zeros
-__device__ __forceinline__ unsigned quantise4(float a, float b, float c, float d, float inverse, int kind)
+// the larger of two magnitudes, NaN where one is (the instruction takes |x| as it stands)
+__device__ __forceinline__ float largest_nan(float top, float x)
 {
-    if (inverse == 0.f) return 0u;
-    a *= inverse;
-    b *= inverse;
-    c *= inverse;
-    d *= inverse;
-    if (kind == kE4m3) {
-        unsigned short lo, hi;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-        return (unsigned)lo | (unsigned)hi << 16;
-    }
-    auto whole = [](float x) { return (unsigned)(__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 255); };
-    return whole(a) | whole(b) << 8 | whole(c) << 16 | whole(d) << 24;
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(x)));
+    return r;
 }
-__device__ __forceinline__ unsigned quantise1(float a, float inverse, int kind) { return quantise4(a, 0.f, 0.f, 0.f, inverse, kind) & 255u; }
+
+// Codes of N elements, N a power of two, four to a word; byte: the row's scale.  Integers: in 1.5 * 2^23 + x / 2^e, rounded once, the low byte is the
+// code.  Only rows at the largest exponent can pass the largest code, and a NaN row's codes are zeros: those come first.
+__device__ __forceinline__ unsigned two_floats(float lo, float hi)
+{
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void quantise(const float *from, unsigned *to, int byte, int kind)
+{
+    const float inverse = scale_inverse(byte);
+    float v[N < 4 ? 4 : N];
+#pragma unroll
+    for (int i = 0; i < (N < 4 ? 4 : N); ++i) v[i] = i < N ? from[i] : 0.f;
+    if (byte >= kScaleBias + kMostExponent) {
+        const float most = byte == kScaleNan ? 0.f : (kind == kE4m3 ? 448.f : 127.f) * scale_value(byte);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = byte == kScaleNan ? 0.f : fminf(fmaxf(v[i], -most), most);
+    }
+    if (kind == kE4m3) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            to[i / 4] = two_floats(v[i] * inverse, v[i + 1] * inverse) | two_floats(v[i + 2] * inverse, v[i + 3] * inverse) << 16;
+    } else {
+        auto whole = [&](float x) { return __float_as_uint(fmaf(x, inverse, 12582912.f)); };
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            to[i / 4] = __byte_perm(__byte_perm(whole(v[i]), whole(v[i + 1]), 0x0040), __byte_perm(whole(v[i + 2]), whole(v[i + 3]), 0x0040), 0x5410);
+    }
+}
 
 // Codes of four elements as two pairs of f16, exactly.  Integers: with the sign bit flipped they count from 0 to 255, as the low byte of an f16
 // in 1024 .. 1279, from which 1152 is taken.

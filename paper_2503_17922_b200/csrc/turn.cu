@@ -17,7 +17,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxDim = kAttnMaxHeadDim;
 constexpr int kMaxTokens = 4;                // of a block
-constexpr int kAhead = 2;                    // rows of a group in flight
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -126,11 +125,12 @@ __device__ __forceinline__ void read(float *to, const float *from, int piece, in
 
 // EIGHT: keys and values go into an 8-bit cache
 template <typename T, int VEC, bool PAIRS, bool EIGHT>
-__global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __grid_constant__ TurnArgs p, int tokens_per_block, long long tokens, int lanes_shift)
+__global__ void __launch_bounds__(kThreads, EIGHT ? 3 : (sizeof(T) == 4 ? 4 : 5)) turn_kernel(const __grid_constant__ TurnArgs p, int tokens_per_block, long long tokens, int lanes_shift)
 {
     typedef typename Bits<VEC * sizeof(T)>::type Raw;
     typedef typename Bits<VEC>::type Codes;
     constexpr int kEach = VEC >= 8 ? 1 : 8 / VEC, kSides = PAIRS ? 1 : 2;       // pieces of a lane at most; vectors of a piece
+    constexpr int kAhead = 2;                                                  // rows of a group in flight
     const RopeArgs &a = p.r;
     constexpr int kPairsOf = PAIRS ? VEC / 2 : VEC;                            // pairs of a piece
     __shared__ __align__(16) float turn[kMaxTokens][kMaxDim + 8];              // cosines and sines, spread()
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
     pdl_trigger();
     pdl_wait();
     const int half = a.turns ? a.rot / 2 : 0, rot = 2 * half;
-    const int turned = PAIRS ? (rot + VEC - 1) / VEC : half / VEC, pieces = PAIRS ? a.d / VEC : turned + (a.d - rot) / VEC;
+    const int turned = PAIRS ? (rot + VEC - 1) / VEC : half / VEC, pieces = PAIRS ? a.d / VEC : turned + (a.d - rot + 2 * VEC - 1) / (2 * VEC);
     const long long t0 = (long long)blockIdx.x * tokens_per_block;
     const int n = (int)min((long long)tokens_per_block, tokens - t0);
     if (a.lengths_out)
@@ -156,8 +156,9 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
         for (int x = threadIdx.x; x < 2 * a.d; x += kThreads) {
             const int which = x >= a.d, c = x - which * a.d;
             const T *w = static_cast<const T *>(which ? p.k_weight : p.q_weight);
-            const int side = !PAIRS && c >= half && c < rot, first = PAIRS ? c : (c < rot ? c - side * half : turned * VEC + c - rot);       // of the side's pieces
-            weight[which][side ? kSides - 1 : 0][spread<VEC>(first / VEC, first % VEC, side ? turned : pieces)] = w ? to_float(w[c]) + p.offset : 1.f;
+            const int behind = c - rot, side = PAIRS ? 0 : (behind < 0 ? c >= half : behind / VEC & 1);
+            const int piece = PAIRS ? c / VEC : (behind < 0 ? (c - side * half) / VEC : turned + behind / (2 * VEC)), e = PAIRS || behind >= 0 ? c % VEC : (c - side * half) % VEC;
+            weight[which][side ? kSides - 1 : 0][spread<VEC>(piece, e, pieces)] = w ? to_float(w[c]) + p.offset : 1.f;
         }
     __syncthreads();
     const int hq = a.q ? a.hq : 0, hk = a.k ? a.hkv : 0, hv = a.v ? a.hkv : 0, rows = hq + hk + hv;
@@ -165,7 +166,10 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
     const int lanes = 1 << lanes_shift, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> lanes_shift, groups = kThreads >> lanes_shift;
     const int of_token = groups / tokens_per_block, mine = group / of_token, sub = group - mine * of_token, at_once = kThreads / tokens_per_block;
     const float inverse_d = 1.f / (float)a.d;
-    auto place = [&](int piece) { return PAIRS || piece < turned ? piece * VEC : rot + (piece - turned) * VEC; };
+    // where a piece's vectors begin: two of a turned piece, a half apart; behind the turned dimensions two neighbours, of which the last may be alone
+    auto place = [&](int piece) { return PAIRS || piece < turned ? piece * VEC : rot + (piece - turned) * 2 * VEC; };
+    auto other = [&](int piece) { return piece < turned ? half : VEC; };
+    auto two = [&](int piece) { return !PAIRS && (piece < turned || rot + (piece - turned) * 2 * VEC + VEC < a.d); };
     auto angles = [&]() {
         for (int x = threadIdx.x; x < n * half; x += kThreads) {
             const int w = x / half, pair = x - w * half;
@@ -233,10 +237,11 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
                 const T *src = static_cast<const T *>(list[at[u]].src);
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) {
+                    if (k * lanes >= pieces) break;
                     const int piece = lane + k * lanes, j = place(piece);
                     if (piece >= pieces) continue;
                     raw[u][k][0] = *reinterpret_cast<const Raw *>(src + j);
-                    if (!PAIRS && piece < turned) raw[u][k][kSides - 1] = *reinterpret_cast<const Raw *>(src + j + half);
+                    if (two(piece)) raw[u][k][kSides - 1] = *reinterpret_cast<const Raw *>(src + j + other(piece));
                 }
             }
         };
@@ -256,15 +261,18 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
                 if (p.norm) {
                     float squares = 0.f;
 #pragma unroll
-                    for (int k = 0; k < kEach; ++k)
+                    for (int k = 0; k < kEach; ++k) {
+                        if (k * lanes >= pieces) break;
 #pragma unroll
                         for (int s = 0; s < kSides; ++s) {
-                            if (!turns || lane + k * lanes >= (s == 0 ? pieces : turned)) continue;
+                            const int piece = lane + k * lanes;
+                            if (!turns || piece >= pieces || (s == 1 && !two(piece))) continue;
                             float x[VEC];
                             unpack<VEC>(reinterpret_cast<const T *>(&raw[u][k][s]), x);
 #pragma unroll
                             for (int i = 0; i < VEC; ++i) squares = fmaf(x[i], x[i], squares);
                         }
+                    }
                     for (int o = 1; o < lanes; o <<= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
                     by = rsqrtf(fmaf(squares, inverse_d, p.eps));
                 }
@@ -273,9 +281,10 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
                 constexpr int kStep = VEC < 4 ? VEC : 4;
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) {
+                    if (k * lanes >= pieces) break;
                     const int piece = lane + k * lanes, j = place(piece);
                     if (at[u] < 0 || piece >= pieces || (!EIGHT && !turns)) continue;
-                    const bool both = !PAIRS && piece < turned;
+                    const bool both = two(piece);
                     T *e[2] = {reinterpret_cast<T *>(&raw[u][k][0]), reinterpret_cast<T *>(&raw[u][k][kSides - 1])};
 #pragma unroll
                     for (int i0 = 0; i0 < VEC; i0 += kStep) {
@@ -289,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
 #pragma unroll
                                 for (int i = 0; i < kStep; ++i) x[0][i] = x[0][i] * by * w[i];
                                 if (both) {
-                                    read<VEC, kStep>(w, weight[kind][kSides - 1], piece, i0, turned);
+                                    read<VEC, kStep>(w, weight[kind][kSides - 1], piece, i0, pieces);
 #pragma unroll
                                     for (int i = 0; i < kStep; ++i) x[1][i] = x[1][i] * by * w[i];
                                 }
@@ -322,42 +331,40 @@ __global__ void __launch_bounds__(kThreads, EIGHT ? 3 : 5) turn_kernel(const __g
                         }
                     }
                 }
-                float inverse = 0.f;
+                int byte = 0;
                 if constexpr (EIGHT) {
                     if (__any_sync(0xffffffffu, codes)) {
-                        unsigned most = 0u;
+                        float top = 0.f;
 #pragma unroll
                         for (int k = 0; k < kEach; ++k)
 #pragma unroll
                             for (int s = 0; s < kSides; ++s)
 #pragma unroll
-                                for (int i = 0; i < VEC; ++i) most = max(most, magnitude(v[k][s][i]));
+                                for (int i = 0; i < VEC; ++i) top = largest_nan(top, v[k][s][i]);
+                        unsigned most = magnitude(top);
                         for (int o = 1; o < lanes; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-                        const int byte = scale_byte(most, p.kind);
-                        inverse = scale_inverse(byte);
+                        byte = scale_byte(most, p.kind);
                         if (codes && lane == 0) *row.scale = (unsigned char)byte;
                     }
                 }
                 if (at[u] < 0) continue;
 #pragma unroll
                 for (int k = 0; k < kEach; ++k) {
-                    const int piece = lane + k * lanes, j = place(piece);
+                    if (k * lanes >= pieces) break;
+                    const int piece = lane + k * lanes, j = place(piece), second = other(piece);
                     if (piece >= pieces) continue;
 #pragma unroll
                     for (int s = 0; s < kSides; ++s) {
-                        if (s == 1 && piece >= turned) continue;
+                        if (s == 1 && !two(piece)) continue;
                         if (codes) {
                             if constexpr (EIGHT) {
-                                unsigned char *dst = static_cast<unsigned char *>(row.dst) + j + s * half;
+                                unsigned char *dst = static_cast<unsigned char *>(row.dst) + j + s * second;
                                 __align__(8) unsigned c[(VEC + 3) / 4];
-#pragma unroll
-                                for (int i = 0; i < VEC; i += 4)
-                                    c[i / 4] = quantise4(v[k][s][i], VEC > 1 ? v[k][s][(i + 1) % VEC] : 0.f, VEC > 2 ? v[k][s][(i + 2) % VEC] : 0.f,
-                                                         VEC > 2 ? v[k][s][(i + 3) % VEC] : 0.f, inverse, p.kind);
+                                quantise<VEC>(v[k][s], c, byte, p.kind);
                                 *reinterpret_cast<Codes *>(dst) = *reinterpret_cast<const Codes *>(c);
                             }
                         } else {
-                            *reinterpret_cast<Raw *>(static_cast<T *>(row.dst) + j + s * half) = raw[u][k][s];
+                            *reinterpret_cast<Raw *>(static_cast<T *>(row.dst) + j + s * second) = raw[u][k][s];
                         }
                     }
                 }
@@ -390,7 +397,7 @@ int launch(const TurnArgs &p, cudaStream_t stream)
     const bool eight = p.kind != kPlain;
     auto go = [&](auto plain, auto codes, int vec, bool pairs) {
         const auto kernel = eight ? codes : plain;
-        const int pieces = pairs ? a.d / vec : half / vec + (a.d - 2 * half) / vec;
+        const int pieces = pairs ? a.d / vec : half / vec + (a.d - 2 * half + 2 * vec - 1) / (2 * vec);
         int shift = 0;
         while (shift < 5 && (1 << shift) < pieces) ++shift;
         return launch_pdl(kernel, grid, kThreads, 0, stream, 1, p, (int)per, tokens, shift);
