@@ -9,7 +9,7 @@ namespace {
 // us with the kernel in front, 66 with 32 rows per block).  With many there are two pieces or so, and fewer blocks look for them
 // more seldom (160 items: 101 us with 8 rows, 96 with 32).
 constexpr int kFewItems = 128;
-template <int RPW>                      // rows of a warp, all in flight together
+template <int RPW, bool DRAFT>          // rows of a warp, all in flight together
 __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant__ TcAttnArgs t)
 {
     pdl_trigger();
@@ -19,7 +19,7 @@ __global__ void __launch_bounds__(256) attn_tc_join_kernel(const __grid_constant
     const AttnArgs &a = t.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Item im;
-    if (!get_item(t, blockIdx.x, im) || im.n_tiles == 0) return;
+    if (!get_item<DRAFT>(t, blockIdx.x, im) || im.n_tiles == 0) return;
     const int first_row = (int)blockIdx.y * 8 * RPW, x = first_row / kTile;
     if ((first_row - x * kTile) / a.G >= (x ? im.rows[1] : im.rows[0])) return;                // (no row of this block's)
     const long long at = t.line[blockIdx.x], total = t.line[t.items];
@@ -140,7 +140,8 @@ static int launch_forms(const TcAttnArgs &t, const CUtensorMap &k_map, const CUt
     if (err == cudaSuccess) count_launches(1);
     if (err == cudaSuccess && t.by_work) {
         const auto join = [&](auto kernel, int rows) { return launch_pdl(kernel, dim3((unsigned)t.items, 2 * kTile / rows), 256, 0, stream, 1, t); };
-        err = t.items <= kFewItems ? join(attn_tc_join_kernel<1>, 8) : join(attn_tc_join_kernel<4>, 32);
+        if (t.a.masks) err = t.items <= kFewItems ? join(attn_tc_join_kernel<1, true>, 8) : join(attn_tc_join_kernel<4, true>, 32);
+        else err = t.items <= kFewItems ? join(attn_tc_join_kernel<1, false>, 8) : join(attn_tc_join_kernel<4, false>, 32);
         if (err == cudaSuccess) count_launches(1);
     }
     return check_cuda(err, "tensor-core attention kernel");

@@ -77,12 +77,12 @@ __host__ __device__ constexpr int raw_bytes(int kb) { return kTile * kb * 64; }
 struct Shared {
     uint64_t q_full, q_empty;
     uint64_t full[kMaxStages], empty[kMaxStages], look[kMaxStages], clean[kMaxStages];
-    uint64_t raw_full[kRawStages], raw_empty[kRawStages];
     uint64_t s_full[2], p_part[2], p_full[2], pv_done[2], o_free[2];
     uint32_t tmem_base;
     int abort;
     int poison[kMaskSlots];                        // item whose values held an infinity or NaN in a tile that was looked through
     uint4 present[kMaskSlots];                     // of the tiles' 128 rows: those with a page
+    uint64_t raw_full[kRawStages], raw_empty[kRawStages];          // EIGHT
 };
 
 struct Item {
@@ -97,6 +97,7 @@ struct Item {
     int begin, end;          // key tiles that this block takes
     int piece;               // where it leaves what it has of the item, -1: it has all of it
 };
+template <bool DRAFT>
 __device__ __forceinline__ bool get_item(const TcAttnArgs &t, long long k, Item &im)
 {
     const AttnArgs &a = t.a;
@@ -114,10 +115,10 @@ __device__ __forceinline__ bool get_item(const TcAttnArgs &t, long long k, Item 
     for (int x = 0; x < 2; ++x) {
         const int first = im.pos0 + x * t.ppt;
         im.rows[x] = min(max(im.sq.m - first, 0), t.ppt);
-        const int most = im.rows[x] > 0 ? (a.masks ? im.sq.n : min(im.base + first + im.rows[x] - 1, im.sq.n)) : 0;
+        const int most = im.rows[x] > 0 ? (DRAFT ? im.sq.n : min(im.base + first + im.rows[x] - 1, im.sq.n)) : 0;
         im.tiles[x] = (max(most, 0) + kTile - 1) / kTile;
     }
-    im.looked = max(a.masks ? im.base - 1 : im.base + im.pos0, 0) / kTile;       // every row sees all of the tiles in front of this one
+    im.looked = max(DRAFT ? im.base - 1 : im.base + im.pos0, 0) / kTile;       // every row sees all of the tiles in front of this one
     im.n_tiles = max(im.tiles[0], im.tiles[1]);
     im.begin = 0;
     im.end = im.n_tiles;
@@ -132,26 +133,28 @@ constexpr int kItemCost = 4;            // what an item costs beside its key til
 constexpr int kWorkItems = 4 * 148;     // with more items than this they are dealt out whole
 constexpr int kWorkKeys = 2048;         // ... and where a unit has fewer keys at most
 constexpr int kWorkBlocks = 148;
+template <bool DRAFT>
 __device__ __forceinline__ long long item_cost(const TcAttnArgs &t, long long k)
 {
     Item im;
-    return k < t.items && get_item(t, k, im) ? im.n_tiles + kItemCost : 0;
+    return k < t.items && get_item<DRAFT>(t, k, im) ? im.n_tiles + kItemCost : 0;
 }
 // By a whole warp, 32 items at a time: the length of the line; and, at a place on it, the item there and where that begins.
+template <bool DRAFT>
 __device__ __forceinline__ long long line_length(const TcAttnArgs &t, int lane)
 {
     long long sum = 0;
-    for (int x = lane; x < t.items; x += 32) sum += item_cost(t, x);
+    for (int x = lane; x < t.items; x += 32) sum += item_cost<DRAFT>(t, x);
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     return sum;
 }
-template <typename F>
+template <bool DRAFT, typename F>
 __device__ __forceinline__ void walk_line(const TcAttnArgs &t, int lane, F visit)      // visit(item, where it begins, where it ends): enough?
 {
     long long before = 0;
     for (int x0 = 0; x0 < t.items; x0 += 32) {
-        const long long c = item_cost(t, x0 + lane);
+        const long long c = item_cost<DRAFT>(t, x0 + lane);
         long long end = c;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -173,6 +176,7 @@ __device__ __forceinline__ void piece_of(long long total, int c, long long at, i
 __device__ __forceinline__ int piece_slot(int c, int begin) { return 2 * c + (begin == 0); }
 
 // a block's items: back and forth over the list, or its share of the line
+template <bool DRAFT>
 struct Walk {
     long long k0 = 0;
     int round = 0, seq = 0;       // seq: items with key tiles so far
@@ -184,7 +188,7 @@ struct Walk {
             const long long k = k0 + (round & 1 ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
             k0 += gridDim.x;
             ++round;
-            if (k < t.items && get_item(t, k, im)) return true;
+            if (k < t.items && get_item<DRAFT>(t, k, im)) return true;
         }
         return false;
     }
@@ -192,10 +196,10 @@ struct Walk {
     {
         if (total < 0) {
             const int lane = threadIdx.x & 31;
-            total = line_length(t, lane);
+            total = line_length<DRAFT>(t, lane);
             const long long lo = total * blockIdx.x / kWorkBlocks;
             long long k = t.items, from = 0;
-            walk_line(t, lane, [&](int item, long long start, long long end) {
+            walk_line<DRAFT>(t, lane, [&](int item, long long start, long long end) {
                 const unsigned there = __ballot_sync(0xffffffffu, end > lo);
                 if (!there) return false;
                 k = __shfl_sync(0xffffffffu, item, __ffs(there) - 1);
@@ -207,7 +211,7 @@ struct Walk {
         }
         const long long lo = total * blockIdx.x / kWorkBlocks, hi = total * (blockIdx.x + 1) / kWorkBlocks;
         while (k0 < t.items && at < hi) {
-            if (!get_item(t, k0, im)) {
+            if (!get_item<DRAFT>(t, k0, im)) {
                 ++k0;
                 continue;
             }
@@ -335,14 +339,6 @@ __device__ __forceinline__ uint32_t mask_window(const unsigned *mask, int words,
     const uint32_t lo = w >= 0 && w < words ? __ldg(mask + w) : 0u, hi = w + 1 >= 0 && w + 1 < words ? __ldg(mask + w + 1) : 0u;
     return __funnelshift_r(lo, hi, at & 31);
 }
-// element c of the value row at `at`, of an 8-bit cache's key j
-template <bool EIGHT>
-__device__ __forceinline__ float value_at(const AttnArgs &a, const Item &im, long long at, int j, int c)
-{
-    if constexpr (EIGHT) return codes_to_float(static_cast<const unsigned char *>(a.v)[at + c], a.kind).x * scale_value(a.v_scales[attn_scale(a, im.b, im.h, j)]);
-    else return __bfloat162float(static_cast<const __nv_bfloat16 *>(a.v)[at + c]);
-}
-
 template <int KB, bool WHOLE, bool EIGHT, bool DRAFT>
 __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, int x, uint32_t tmem)
 {
@@ -357,7 +353,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
     const unsigned long long c2 = pair_of(c, c);
     uint32_t turn = 0, tiles_before = 0;            // tiles of S taken so far; key tiles of the items so far
     volatile int *const abort_flag = &sh.abort;
-    Walk walk;
+    Walk<DRAFT> walk;
     Item im;
     while (walk.next(t, im)) {
         const int pos = im.pos0 + x * t.ppt + place, tiles = min(x ? im.tiles[1] : im.tiles[0], im.end);
@@ -517,11 +513,23 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
                     if (DRAFT && j >= limit && !(mask_window(mask, a.mask_words, j - limit) & 1u)) continue;
                     const long long at = attn_row(a, im.b, im.h, im.sq.q_off, j);
                     if (at < 0) continue;
+                    if constexpr (EIGHT) {
+                        const unsigned char *v = static_cast<const unsigned char *>(a.v) + at + y * 32;
+                        const float by = scale_value(a.v_scales[attn_scale(a, im.b, im.h, j)]);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (!WHOLE && y * 32 + e >= D) break;
-                        const float ve = value_at<EIGHT>(a, im, at, j, y * 32 + e);
-                        if (!(fabsf(ve) < INFINITY)) o[e] += ve;
+                        for (int e = 0; e < 32; ++e) {
+                            if (!WHOLE && y * 32 + e >= D) break;
+                            const float ve = codes_to_float(v[e], a.kind).x * by;
+                            if (!(fabsf(ve) < INFINITY)) o[e] += ve;
+                        }
+                    } else {
+                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + at + y * 32;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            if (!WHOLE && y * 32 + e >= D) break;
+                            const float ve = __bfloat162float(v[e]);
+                            if (!(fabsf(ve) < INFINITY)) o[e] += ve;
+                        }
                     }
                 }
             }
@@ -562,7 +570,7 @@ __device__ __forceinline__ void softmax_warps(const TcAttnArgs &t, Shared &sh, i
 // ---- MMAs --------------------------------------------------------------------------------------
 // One warp issues for both query tiles in turn, which keeps them half a step apart: with a warp for each they fell into step, both
 // at their exponentials or both at their products (8,192 tokens of 32 heads: 11 % more time).
-template <int KB, bool WHOLE, bool EIGHT>
+template <int KB, bool WHOLE, bool EIGHT, bool DRAFT>
 __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, uint32_t tmem)
 {
     constexpr int NS = stages_for(KB, EIGHT), kStage = KB * kRegion;
@@ -575,7 +583,7 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
     const uint32_t o_idesc = umma_idesc_bf16(kTile, steps * 16) | kBTransposed;
     uint32_t entry = 0, clean_phase = 0;               // ring entries so far; parity per stage of the looked-through tiles
     uint32_t turn[2] = {0, 0}, outs[2] = {0, 0};       // tiles and items of each query tile so far
-    Walk walk;
+    Walk<DRAFT> walk;
     Item im;
     auto scores = [&](int x, int stage) {
         const uint64_t kd = k_desc0 + (uint64_t)((uint32_t)(stage * kStage) >> 4), qd = q_desc0 + (uint64_t)((uint32_t)(x * kStage) >> 4);
@@ -653,7 +661,7 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
 
 // ---- loads --------------------------------------------------------------------------------------
 // `ring`: of the tiles as the products take them, or of codes (EIGHT)
-template <int KB, bool EIGHT>
+template <int KB, bool EIGHT, bool DRAFT>
 __device__ __forceinline__ uint32_t load_warp(const TcAttnArgs &t, Shared &sh, const CUtensorMap *k_map, const CUtensorMap *v_map, uint8_t *ring)
 {
     constexpr int NS = EIGHT ? kRawStages : stages_for(KB, false), kStage = EIGHT ? raw_bytes(KB) : KB * kRegion;
@@ -662,7 +670,7 @@ __device__ __forceinline__ uint32_t load_warp(const TcAttnArgs &t, Shared &sh, c
     const int lane = threadIdx.x & 31;
     volatile int *const abort_flag = &sh.abort;
     uint32_t entry = 0;
-    Walk walk;
+    Walk<DRAFT> walk;
     Item im;
     const int boxes = kTile / t.box_rows;             // of a tile
     const uint32_t leader = elect_one();
@@ -759,17 +767,17 @@ __device__ __forceinline__ void load_queries(const TcAttnArgs &t, const Item &im
     asm volatile("cp.async.commit_group;" ::: "memory");
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
-template <int KB, bool EIGHT>
+template <int KB, bool EIGHT, bool DRAFT>
 __device__ __forceinline__ void helper_warp(const TcAttnArgs &t, Shared &sh, uint8_t *q_img, uint8_t *ring, int which)
 {
     constexpr int NS = stages_for(KB, EIGHT), kStage = KB * kRegion;
     const int lane = threadIdx.x & 31;
     volatile int *const abort_flag = &sh.abort;
     uint32_t entry = 0, look_phase = 0;
-    Walk walk;
+    Walk<DRAFT> walk;
     Item im;
     if (t.by_work && blockIdx.x == 0 && which == 1)
-        walk_line(t, lane, [&](int item, long long start, long long end) {
+        walk_line<DRAFT>(t, lane, [&](int item, long long start, long long end) {
             if (item < t.items) t.line[item] = start;
             if (item == t.items - 1) t.line[item + 1] = end;
             return false;
@@ -855,7 +863,7 @@ __device__ __forceinline__ void convert_tile(const uint8_t *raw, uint8_t *tile, 
         make(y, at ^ 32u);
     }
 }
-template <int KB>
+template <int KB, bool DRAFT>
 __device__ __forceinline__ void convert_warp(const TcAttnArgs &t, Shared &sh, const uint8_t *raw, uint8_t *ring, int which)
 {
     constexpr int NS = stages_for(KB, true), kStage = KB * kRegion;
@@ -863,7 +871,7 @@ __device__ __forceinline__ void convert_warp(const TcAttnArgs &t, Shared &sh, co
     const int lane = threadIdx.x & 31;
     volatile int *const abort_flag = &sh.abort;
     uint32_t entry = 0;
-    Walk walk;
+    Walk<DRAFT> walk;
     Item im;
     bool ok = true;
     while (ok && walk.next(t, im)) {
@@ -957,36 +965,36 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant_
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
+    if constexpr (EIGHT) {
+        if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    }
     if (warp < 8) {
-        if constexpr (EIGHT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         softmax_warps<KB, WHOLE, EIGHT, DRAFT>(t, sh, warp >> 2, tmem);
-    } else {
-        if constexpr (EIGHT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == 8) {
-            mma_warp<KB, WHOLE, EIGHT>(t, sh, q_img, ring, tmem);
-        } else if (warp == 9) {
-            if (lane == 0) {
-                tma_prefetch_desc(&k_map);
-                tma_prefetch_desc(&v_map);
-            }
-            const uint32_t issued = load_warp<KB, EIGHT>(t, sh, &k_map, &v_map, EIGHT ? raw : ring);
-            // nothing of this block may be in flight when it ends: the last MMAs (EIGHT: conversions) must have released their stages; after a
-            // failed wait, the loads already issued must still land
-            constexpr uint32_t LS = EIGHT ? kRawStages : NS;
-            uint64_t *const full = EIGHT ? sh.raw_full : sh.full, *const empty = EIGHT ? sh.raw_empty : sh.empty;
-            for (uint32_t e = issued > LS ? issued - LS : 0; e < issued; ++e) {
-                const int st = e % LS;
-                if (!warp_wait(&empty[st], (e / LS) & 1, &sh.abort)) {
-                    volatile int never = 0;
-                    warp_wait(&full[st], (e / LS) & 1, &never);
-                }
-            }
-            if (lane == 0 && *static_cast<volatile int *>(&sh.abort) && t.a.status) atomicOr(t.a.status, kStatusWaitExpired);
-        } else if (!EIGHT || warp < 12) {
-            helper_warp<KB, EIGHT>(t, sh, q_img, ring, warp - 10);
-        } else {
-            if constexpr (EIGHT) convert_warp<KB>(t, sh, raw, ring, warp - 12);
+    } else if (warp == 8) {
+        mma_warp<KB, WHOLE, EIGHT, DRAFT>(t, sh, q_img, ring, tmem);
+    } else if (warp == 9) {
+        if (lane == 0) {
+            tma_prefetch_desc(&k_map);
+            tma_prefetch_desc(&v_map);
         }
+        const uint32_t issued = load_warp<KB, EIGHT, DRAFT>(t, sh, &k_map, &v_map, EIGHT ? raw : ring);
+        // nothing of this block may be in flight when it ends: the last MMAs (EIGHT: conversions) must have released their stages; after a
+        // failed wait, the loads already issued must still land
+        constexpr uint32_t LS = EIGHT ? kRawStages : NS;
+        uint64_t *const full = EIGHT ? sh.raw_full : sh.full, *const empty = EIGHT ? sh.raw_empty : sh.empty;
+        for (uint32_t e = issued > LS ? issued - LS : 0; e < issued; ++e) {
+            const int st = e % LS;
+            if (!warp_wait(&empty[st], (e / LS) & 1, &sh.abort)) {
+                volatile int never = 0;
+                warp_wait(&full[st], (e / LS) & 1, &never);
+            }
+        }
+        if (lane == 0 && *static_cast<volatile int *>(&sh.abort) && t.a.status) atomicOr(t.a.status, kStatusWaitExpired);
+    } else if (!EIGHT || warp < 12) {
+        helper_warp<KB, EIGHT, DRAFT>(t, sh, q_img, ring, warp - 10);
+    } else if constexpr (EIGHT) {
+        convert_warp<KB, DRAFT>(t, sh, raw, ring, warp - 12);
     }
     tc_fence_before_sync();
     __syncthreads();
