@@ -786,7 +786,7 @@ def test_keep_draft(kind, layout):
 
 
 # ---- eviction --------------------------------------------------------------------------------------
-@pytest.mark.parametrize("budget,cap_pages", [(20, 6), (200, 40), (0, 3), (1000, 6), (2, 6)])
+@pytest.mark.parametrize("budget,cap_pages", [(20, 6), (200, 40), (300, 60), (0, 3), (1000, 6), (2, 6)])
 @pytest.mark.parametrize("layout", ["phsd", "pshd"])
 def test_evict8(budget, cap_pages, layout):
     """The rows' state as from the plain cache's eviction; codes and scales of every layer belong to the positions that stay."""
@@ -815,6 +815,48 @@ def test_evict8(budget, cap_pages, layout):
         rows = torch.tensor([row_of[int(p)] for p in outs[0][1][b, h, :keep]], dtype=torch.long, device="cuda")
         now, now_scales, _ = c.raw(l, kv, b, h, keep)
         assert torch.equal(now, codes[rows]) and torch.equal(now_scales, scales[rows])
+
+
+# ---- far places ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind,new", [("e4m3", 1), ("i8", 30), ("e4m3", 150)])
+def test_offsets_beyond_32_bits(kind, new):
+    """Pages a gigabyte apart: appended to, read back, attended over, kept of a draft."""
+    g, hk, hq, d, page, gap = gen(18), 2, 8, 64, 16, 1 << 30
+    n, num_pages, max_pages = 100, 12, 12
+    if new == 150:
+        n, num_pages, max_pages = 170, 12, 12
+    codes = [torch.empty(gap * (num_pages - 1) + hk * page * d, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros((num_pages, hk, page), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    table = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device="cuda").view(1, max_pages)
+    make = lambda m: wkv.PagedCache8(kind=kind, dtype="bf16", batch=1, n_q_heads=hq, n_kv_heads=hk, head_dim=d, page_size=page, num_pages=num_pages,
+                                     block_table=table, max_new=m, layout=(gap, page * d, d))
+    filling, cache = make(n), make(new)
+    layer = wkv.Layer8(cache, *codes, *scales)
+    k, v = (randn(g, 1, hk, n, d, dtype=torch.bfloat16) for _ in range(2))
+    none, lengths = torch.zeros((1, hk), dtype=torch.int32, device="cuda"), torch.full((1, hk), n, dtype=torch.int32, device="cuda")
+    wkv.wkv_append_kv_paged8(filling, layer, k, v, none)
+    rows = [torch.full((1, hk, n, d), 77.0, device="cuda") for _ in range(2)]
+    wkv.wkv_read_kv_paged8(filling, layer, lengths, rows[0], rows[1])
+    q = randn(g, 1, hq, new, d, dtype=torch.bfloat16)
+    out, ws = torch.full_like(q, 77.0), cache.alloc_workspace()
+    wkv.wkv_attend_paged8(cache, layer, q, lengths, out, ws)
+    torch.cuda.synchronize()
+    seen = (torch.arange(n)[None, :] <= torch.arange(new)[:, None] + n - new).cuda()
+    for h in range(hk):
+        for x, y in ((k, rows[0]), (v, rows[1])):
+            assert torch.equal(y[0, h].double(), cu.quantised(x[0, h], kind)[1])
+        for head in range(h * 4, h * 4 + 4):
+            ref, _, _, bd = cu.attention_seen(q[0, head], rows[0][0, h], rows[1][0, h], seen)
+            ou.assert_close(out[0, head], ref, ou.output_bound(ref, bd, torch.bfloat16), "out")
+    assert wkv.device_status(ws) == 0
+    masks = torch.zeros((1, new, (new + 31) // 32), dtype=torch.int32, device="cuda")
+    masks[0, -1, -1] = 1 << ((new - 1) % 32) if new % 32 else -2 ** 31     # the last token alone
+    kept = torch.zeros_like(lengths)
+    wkv.wkv_keep_draft_paged8(cache, masks, [layer], torch.tensor([new - 1], dtype=torch.int32, device="cuda"), lengths, kept)
+    last = torch.full((1, hk, 1, d), 77.0, device="cuda")
+    wkv.wkv_read_kv_paged8(filling, layer, kept, last, None, first=kept - 1)
+    torch.cuda.synchronize()
+    assert (kept == n - new + 1).all() and torch.equal(last[:, :, 0], rows[0][:, :, n - 1])
 
 
 # ---- a run of them together ----------------------------------------------------------------------------
