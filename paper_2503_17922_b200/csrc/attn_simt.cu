@@ -43,9 +43,11 @@ __device__ __forceinline__ void load_row_part(float *dst, const float *p, int d,
 
 // Stages of key tiles: with 16 rows the loads take as long as the arithmetic, and the next tile's come during this one's.  With more
 // rows a tile's values come during the product with its keys, and the next keys during that with the values, in half the memory.
-template <int DP, int ROWS>
+// EIGHT with 16 rows of more than 64 columns goes the second way too, as two blocks of an SM then convert under each other's products (four sequences of
+// 8,192 keys, 32 query heads on 8, d = 128, one token each: 203 us, with two stages and one block 353; at d = 64, with three blocks, both ways 111).
+template <int DP, int ROWS, bool EIGHT>
 struct SimtSmem {
-    static constexpr int kStages = ROWS == 16 && DP <= 128 ? 2 : 1;
+    static constexpr int kStages = ROWS == 16 && DP <= 128 && !(EIGHT && DP == 128) ? 2 : 1;
     float q[ROWS][DP + 4];
     float k[kStages][kKeys][DP + 4];
     float v[kStages][kKeys][DP];
@@ -63,13 +65,16 @@ struct WeightsSmem {
 
 // The keys or the values of a tile, on their way; rows from n on and rows without a page are zeros.  A row's vectors lie in neighbouring
 // threads, and a thread has EACH rows.  Their pages are looked up some work ahead, as that is a trip to memory.
-// EIGHT: the rows are codes, which become numbers on their way.
+// EIGHT: the rows are codes.  Four of them come into the place of the four numbers that they become there, in the thread that had them copied, once
+// they have landed.  (Four sequences of 8,192 keys,
+// 32 query heads on 8, d = 64, one token each: 111 us; converted on the way, with each load waited for, 134.)
 template <int DP, bool EIGHT>
 struct Fetch {
     static constexpr int kParts = DP / 4, kEach = kKeys * kParts / kThreads, kStep = kThreads / kParts;
     int page[kEach], slot[kEach];
     long long at[kEach];                   // element offsets, -1: none
     long long scale_at[EIGHT ? kEach : 1];
+    unsigned char by[2][EIGHT ? kEach : 1];                              // scales of the keys and of the values on their way
     __device__ __forceinline__ void look_up(const AttnArgs &a, int b, int n, int j0)
     {
         if (!a.table) return;
@@ -91,39 +96,39 @@ struct Fetch {
             if (threadIdx.x % kParts == 0) present[r] = at[x] >= 0;
         }
     }
-    __device__ __forceinline__ void issue(const AttnArgs &a, bool values, float *to, int stride) const
+    __device__ __forceinline__ void issue(const AttnArgs &a, bool values, float *to, int stride)
     {
+        typedef std::conditional_t<EIGHT, unsigned char, float> T;
         const int c = (int)(threadIdx.x % kParts) * 4;
-        const void *from = values ? a.v : a.k;
-        if constexpr (EIGHT) {
-            constexpr int kBatch = kEach < 8 ? kEach : 8;                // (loads first, a few at a time)
+        const T *from = static_cast<const T *>(values ? a.v : a.k);
 #pragma unroll
-            for (int x0 = 0; x0 < kEach; x0 += kBatch) {
-                unsigned w[kBatch];
-                float by[kBatch];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const bool have = at[x0 + u] >= 0 && c < a.d;
-                    w[u] = have ? *reinterpret_cast<const unsigned *>(static_cast<const unsigned char *>(from) + at[x0 + u] + c) : 0u;
-                    by[u] = have ? scale_value((values ? a.v_scales : a.k_scales)[scale_at[x0 + u]]) : 0.f;
-                }
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const float4 v = codes_to_float(w[u], a.kind);
-                    *reinterpret_cast<float4 *>(to + ((int)threadIdx.x / kParts + (x0 + u) * kStep) * stride + c) =
-                        make_float4(v.x * by[u], v.y * by[u], v.z * by[u], v.w * by[u]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int x = 0; x < kEach; ++x) {
-                const int r = (int)threadIdx.x / kParts + x * kStep;
-                const bool have = at[x] >= 0 && c < a.d;
-                const float *p = static_cast<const float *>(from) + (have ? at[x] + c : 0);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to + r * stride + c))), "l"(p), "r"(have ? 16 : 0) : "memory");
+        for (int x = 0; x < kEach; ++x) {
+            const int r = (int)threadIdx.x / kParts + x * kStep;
+            const bool have = at[x] >= 0 && c < a.d;
+            const T *p = from + (have ? at[x] + c : 0);
+            const uint32_t there = static_cast<uint32_t>(__cvta_generic_to_shared(to + r * stride + c));
+            if constexpr (EIGHT) {
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(there), "l"(p), "r"(have ? 4 : 0) : "memory");
+                by[values][x] = have ? (values ? a.v_scales : a.k_scales)[scale_at[x]] : 0;
+            } else {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(there), "l"(p), "r"(have ? 16 : 0) : "memory");
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");             // (an empty group with EIGHT: the waits count them)
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // EIGHT: what this thread issued has landed, and becomes numbers
+    __device__ __forceinline__ void convert(const AttnArgs &a, bool values, float *to, int stride)
+    {
+        if constexpr (EIGHT) {
+            const int c = (int)(threadIdx.x % kParts) * 4;
+#pragma unroll
+            for (int x = 0; x < kEach; ++x) {
+                float *row = to + ((int)threadIdx.x / kParts + x * kStep) * stride + c;
+                const float4 v = codes_to_float(*reinterpret_cast<const unsigned *>(row), a.kind);
+                const float f = scale_value(by[values][x]);
+                *reinterpret_cast<float4 *>(row) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+            }
+        }
     }
 };
 template <int DP, bool EIGHT>
@@ -191,11 +196,11 @@ __device__ __forceinline__ void logits(const float (&q)[ROWS][DP + 4], const flo
 
 // EIGHT: keys and values of 8 bits.  DRAFT: the rows go by their masks, as far as the new tokens' rows are concerned.
 template <int DP, int ROWS, bool EIGHT, bool DRAFT>
-__global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 64 && ROWS < 64 ? 3 : 1)) attn_simt_kernel(const __grid_constant__ AttnArgs a)
+__global__ void __launch_bounds__(kThreads, (ROWS == 64 && DP == 64) || (EIGHT && ROWS == 16 && DP == 128) ? 2 : (DP == 64 && ROWS < 64 ? 3 : 1)) attn_simt_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
-    SimtSmem<DP, ROWS> &sm = *reinterpret_cast<SimtSmem<DP, ROWS> *>(raw);
-    constexpr int RT = ROWS / 16, CT = DP / 64, NS = SimtSmem<DP, ROWS>::kStages;
+    SimtSmem<DP, ROWS, EIGHT> &sm = *reinterpret_cast<SimtSmem<DP, ROWS, EIGHT> *>(raw);
+    constexpr int RT = ROWS / 16, CT = DP / 64, NS = SimtSmem<DP, ROWS, EIGHT>::kStages;
     // The joining kernel may be placed now.  Another of this kind is not to be before this one ends: its blocks would crowd onto the
     // SMs that have room at that time.
     const bool clustered = a.clustered, parts = !clustered && (a.splits > 1 || a.logits);
@@ -243,6 +248,8 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
         rows_of.issue(a, false, &sm.k[t % NS][0][0], DP + 4);
     };
     auto fetch_values = [&](int t) { rows_of.issue(a, true, &sm.v[t % NS][0][0], DP); };
+    auto keys_landed = [&](int t) { rows_of.convert(a, false, &sm.k[t % NS][0][0], DP + 4); };
+    auto values_landed = [&](int t) { rows_of.convert(a, true, &sm.v[t % NS][0][0], DP); };
     if (t0 < t1) {
         rows_of.look_up(a, b, sq.n, t0 * kKeys);
         fetch_keys(t0);
@@ -252,12 +259,18 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
     load_queries<DP, ROWS>(a, sm.q, b, h, sq.q_off, row0, rows);
     if (NS == 1) {
         asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (t0 < t1) keys_landed(t0);
         __syncthreads();
     }
     const int plain = DRAFT ? base - 1 : base + row0 / a.G;              // every row attends to the keys before this one
     for (int t = t0; t < t1; ++t) {
         const int j0 = t * kKeys, st = t % NS;
         if (NS == 2) {
+            if (EIGHT) {                                                 // (before the next tile's scales come)
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                keys_landed(t);
+                values_landed(t);
+            }
             if (t + 1 < t1) {
                 fetch_keys(t + 1);
                 fetch_values(t + 1);
@@ -274,6 +287,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
         logits<DP, ROWS>(sm.q, sm.k[st], ty, tx, a.scale_log2, s);
         if (NS == 1) {
             asm volatile("cp.async.wait_group 0;" ::: "memory");
+            values_landed(t);
             __syncthreads();                                             // the values have landed for all, and nobody reads the keys any more
             if (t + 1 < t1) fetch_keys(t + 1);
         }
@@ -350,6 +364,7 @@ __global__ void __launch_bounds__(kThreads, ROWS == 64 && DP == 64 ? 2 : (DP == 
         if (guarded) product(std::true_type{});
         else product(std::false_type{});
         if (NS == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (NS == 1 && t + 1 < t1) keys_landed(t + 1);
         __syncthreads();                                                 // the next keys have landed for all, and nobody reads the values any more
         if (NS == 1 && t + 1 < t1) fetch_values(t + 1);
     }
@@ -608,7 +623,7 @@ int launch(K kernel, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t str
 template <int DP, int ROWS>
 int launch_dp(const AttnArgs &a, dim3 grid, cudaStream_t stream)
 {
-    constexpr size_t smem = sizeof(SimtSmem<DP, ROWS>);
+    const size_t smem = a.kind != kPlain ? sizeof(SimtSmem<DP, ROWS, true>) : sizeof(SimtSmem<DP, ROWS, false>);
     const int cluster = a.clustered ? a.splits : 1;
     if (a.kind != kPlain)
         return a.masks ? launch(attn_simt_kernel<DP, ROWS, true, true>, grid, smem, a, stream, "attention kernel (8-bit cache)", cluster)

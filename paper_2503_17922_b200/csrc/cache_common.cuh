@@ -167,6 +167,9 @@ struct PagedWorkspace {
 // With up to 16 rows, a power of two up to eight is preferred: those are clusters, which join their splits themselves, as long as
 // all of them run at once (32 sequences of 8 heads x 4-8 K rows: 267 us as clusters of eight, 188 as five splits and a joining
 // kernel; one sequence of 8 heads x 992 rows 8.8 and 12.6) and a block has no more than kClusterBytes of keys and values to read.
+// An 8-bit cache under fp32 queries costs a block the conversion of its tiles, not their bytes: there more than eight splits are taken where twice as many
+// can run and a cluster's blocks would have more than two tiles each (one token, 32 query heads on 8, d = 128: 8,000 keys 136 us in clusters, 67 in splits, 2,000 keys
+// 38 and 28; four sequences of 8,192 keys, for which ten splits are the most, 203 and 235).
 constexpr int kSplitBlocks = 2 * 148, kSplitKeys = 64, kSplitEven = 1024;
 constexpr long long kClusterBytes = 512 << 10;
 inline int plan_splits(const wkv_paged *c, const Paged &p, int tile, bool &clustered)
@@ -179,7 +182,8 @@ inline int plan_splits(const wkv_paged *c, const Paged &p, int tile, bool &clust
     long long power = 1;
     while (power < s && power < kClusterSplits) power *= 2;
     clustered = tile == 16 && blocks * power <= kSplitBlocks &&
-                (s <= power || 2ll * p.cap * c->head_dim * p.pool_eb / kClusterSplits <= kClusterBytes);
+                (s <= power || (p.pool_eb < p.eb && p.eb == 4 ? s < 2 * power || p.cap <= 2 * power * kSplitKeys
+                                                              : 2ll * p.cap * c->head_dim * p.pool_eb / kClusterSplits <= kClusterBytes));
     return (int)(clustered ? power : s);
 }
 // More rows than this go to the tensor-core kernel where it takes the shape (8 new tokens of 32 heads on 8, 32 rows: 4 sequences of 16,384
