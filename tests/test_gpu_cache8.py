@@ -505,6 +505,8 @@ ATTEND = [
     ("f32", "e4m3", 4, 2, 128, 16, "pshd", [[300, 10]], [1], False, (0, 0)),
     ("f32", "e4m3", 8, 1, 80, 16, "phsd", [[700]], [30], False, None),
     ("f32", "i8", 3, 3, 256, 16, "phsd", [[90, 80, 33]], [5], False, None),
+    ("f32", "e4m3", 8, 2, 128, 16, "phsd", [[2600, 2001]], [1], False, (0, 5)),
+    ("f32", "i8", 4, 1, 64, 24, "pshd", [[3001], [40]], [3, 1], True, None),
 ]
 
 
@@ -519,7 +521,7 @@ def test_attend8(case):
     a.check()
 
 
-@pytest.mark.parametrize("case", [ATTEND[i] for i in (0, 1, 2, 3, 4, 6, 8, 10, 12, 13, 14, 17, 18, 19)], ids=name_of)
+@pytest.mark.parametrize("case", [ATTEND[i] for i in (0, 1, 2, 3, 4, 6, 8, 10, 12, 13, 14, 17, 18, 19, 21, 22)], ids=name_of)
 def test_attend8_weights(case):
     a = Attend(*case[:10], hole=case[10])
     a.run(weights=True)
