@@ -3,6 +3,10 @@
 // A block takes kRows rows of one unit of one tensor.  Where they come from and go to is looked up once for each, a row per thread (window, table
 // entry), into shared memory; then a group of lanes takes a row, a vector to a lane, and a few rows at a time, loads first.  The row's
 // largest magnitude, by which its scale goes, is found over the lanes of the group: a row is read once.
+//
+// Bound by instructions: the conversion of 16 bytes, and their share of the row's maximum, scale and place.  Two layers of eight prompts of up to 12,289 rows,
+// 30 % kept, d = 128, bf16 into int8 codes, and all of it read back, 142 MB: 38.5 us in two launches, with one vector to a lane 44.  Reading back with 16 codes to a lane
+// instead of eight was slower.
 #include "cache8.cuh"
 
 #include <algorithm>

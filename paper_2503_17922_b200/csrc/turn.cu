@@ -9,6 +9,9 @@
 // piece is a vector of first partners with that of the second partners (HALF order), or a vector of whole pairs.  Cosines and sines
 // of a block's tokens and the weights are computed once into shared memory and serve all heads, as in the kernel without norms; the first
 // rows are on their way while the angles are computed.
+//
+// Bound by the instructions between load and store: 32,768 tokens, 32 query heads and 8 key heads of 128, bf16, three axes, 671 MB: 154-159 us = 4.3 TB/s with norms,
+// 81 % of issue slots busy; without norms 120 us = 5.6 TB/s.  With the tables read where they stand, neighbours in one bank, 177 us.  8 rows of 4 heads, d = 64, fp32, as every small call: 8 us, a launch and its trips to memory.
 #include "cache8.cuh"
 
 namespace wkv {
