@@ -25,10 +25,10 @@
 //
 // EIGHT: keys and values of 8 bits.  Warps 12-15 make bf16 tiles of them, exactly (a row's scale is a power of two), in the place where TMA otherwise puts
 // them; TMA's own tiles of codes have a ring in front of that.  What follows is the same.  Bound by those four warps' instructions beside the softmax's, on one
-// half-rate integer pipe and one instruction cache: four sequences of 8-16 K keys, 512 new tokens of 32 heads on 8, d = 128: 456-463 us (329 over bf16 rows; 386 in a copy that
+// half-rate integer pipe and one instruction cache: four sequences of 8-16 K keys, 512 new tokens of 32 heads on 8, d = 128: 456-464 us (329 over bf16 rows; 386 in a copy that
 // converts nothing); issue slots 49 % busy, tensor pipe 32 %.  The loop over a tile is kept small, as the softmax's code fills the cache: unrolled, 738 us.
 // DRAFT: the rows go by their masks, as far as the new tokens' rows are concerned: every row's keys reach to the unit's last one.  (16 drafts of 64 tokens over 4-8 K
-// rows of 8 bits, 32 heads on 8: 224-230 us; 197 in a copy that converts nothing.)
+// rows of 8 bits, 32 heads on 8: 224-231 us; 197 in a copy that converts nothing.)
 //
 // Blocks are persistent, one per SM; the items come in order of descending work and are dealt to the blocks back and forth.
 // Every wait is bounded; on expiry the block sets bit 0 of the status word, lets its loads land, frees its tensor memory and returns.
