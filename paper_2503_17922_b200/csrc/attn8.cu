@@ -10,9 +10,10 @@
 //
 // Codes become f16 in registers, exactly, an instruction or two to a pair, and scales stay out of the products: a logit is multiplied by
 // its key's 2^e, a weight by its value's.  Queries are scaled by a power of two per row, so that their largest element is in
-// 2^14 .. 2^15: exact down to 2^-29 of that.  Weights p 2^e go into the second product as f16, relative to the largest 2^e met so far
-// and times 2^15: rounded to 2^-12 of themselves down to 2^-29 of that, where bf16 has 2^-9.  Sums, maxima, logits and outputs are fp32,
-// the sum of the unrounded p.
+// 2^14 .. 2^15: exact down to 2^-29 of that.  Weights p 2^e go into the second product as f16, relative to a power of two per row, that of the
+// largest p 2^e that the row has met (its seen keys' alone: a scale that another row sees, or one of next to no weight, takes no bits), and times
+// 2^14: rounded to 2^-11 of themselves at most, half a step, down to 2^-28 of that, where bf16 has 2^-8.  Sums, maxima, logits and outputs are fp32, the sum of the
+// unrounded p.
 //
 // Which 16-byte chunk of a row a thread reads is free, as long as Q and K agree on the order of the columns: a thread reads whole chunks and takes them
 // apart into the operands of four (K) or eight (V) instructions.  Chunks are XORed with the row so that eight lanes meet eight
@@ -184,7 +185,12 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
             m[t][e] = -INFINITY;
             l[t][e] = 0.f;
         }
-    float v_ref = __uint_as_float((unsigned)(kScaleBias + kLeastExponent) << 23);      // O is in units of v_ref / 2^15
+    // O is in units of v_ref / 2^14, a power of two that the row's p 2^e (p relative to m) have not passed twofold.  Of a float the upper half
+    // says enough: two of them are compared by one instruction.
+    constexpr unsigned kLeastRef = (unsigned)(kScaleBias + kLeastExponent - 10) << 7, kMostRef = 253u << 7;
+    float v_ref[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) v_ref[t][0] = v_ref[t][1] = __uint_as_float(kLeastRef << 16);
 
     // ---- the ring of key tiles -----------------------------------------------------------------
     // A thread has a row of the tile: its place is looked up a tile ahead of its load, its scales a tile behind that: a trip to memory each.
@@ -327,16 +333,6 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
                         if (logits[n][y & 1] && j0 + g * 16 + quad + 8 * (y >> 1) < sq.n) logits[n][y & 1][t * kKeys + g * 16 + 8 * (y >> 1)] = s[g][n][y];
         }
         // ---- weights ---------------------------------------------------------------------------------
-        float v_top = fmaxf(fmaxf(v_scale[0][0], v_scale[0][1]), fmaxf(v_scale[1][0], v_scale[1][1]));
-#pragma unroll
-        for (int x = 4; x < 32; x <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, x));
-        float grow = 1.f;
-        if (v_top > v_ref) {                  // (the same in all lanes)
-            grow = v_ref / v_top;
-            v_ref = v_top;
-        }
-        // 2^15 / v_ref, a power of two by its bits
-        const float unit_of = __uint_as_float((269u << 23) - __float_as_uint(v_ref));
         uint32_t p[kGroups][NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -357,10 +353,9 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
                     for (int y = 0; y < 2; ++y) {
                         const float x = ex2(s[g][n][2 * y + e] - ref);
                         sum += x;
-                        w[g][2 * y + e] = x * (v_scale[g][y] * unit_of);
+                        w[g][2 * y + e] = x * v_scale[g][y];
                     }
                 l[n][e] = l[n][e] * keep[e] + sum;                       // this thread's keys; joined over the quads at the end
-                keep[e] *= grow;
             }
             if (masked) {
 #pragma unroll
@@ -368,6 +363,25 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
                         if (hidden >> ((g * NT + n) * 4 + y) & 1u) w[g][y] = 0.f;          // (0 times a NaN scale is not 0)
+            }
+            // the rows' largest p 2^e, upper halves side by side
+            const float w_top[2] = {fmaxf(fmaxf(w[0][0], w[0][2]), fmaxf(w[1][0], w[1][2])), fmaxf(fmaxf(w[0][1], w[0][3]), fmaxf(w[1][1], w[1][3]))};
+            unsigned tops = __byte_perm(__float_as_uint(w_top[0]), __float_as_uint(w_top[1]), 0x7632);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, x));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float before = v_ref[n][e] * keep[e];
+                const unsigned half = max(e ? tops >> 16 : tops & 0xffffu, __float_as_uint(before) >> 16) & 0xff80u;
+                const unsigned bits = min(max(half, kLeastRef), kMostRef) << 16;
+                v_ref[n][e] = __uint_as_float(bits);
+                const float inverse = __uint_as_float((254u << 23) - bits);
+                keep[e] = before * inverse;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    w[g][e] *= inverse * 16384.f;
+                    w[g][2 + e] *= inverse * 16384.f;
+                }
             }
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
@@ -468,12 +482,12 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
     constexpr int kPad = DP + 4;
     float *const all = reinterpret_cast<float *>(&sm.k[0][0]);             // [4][kRows][kPad]
     static_assert(4 * kRows * kPad * 4 <= sizeof(sm.k) + sizeof(sm.v), "the ring holds the warps' outputs");
-    const float by = v_ref * (1.f / 32768.f);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = n * 8 + 2 * ql + e;
+            const float by = v_ref[n][e] * (1.f / 16384.f);
             if (quad == 0) {
                 sm.m[warp][r] = m[n][e];
                 sm.l[warp][r] = l[n][e];
