@@ -654,10 +654,18 @@ int wkv_evict_kv_paged8(const wkv_paged *c, int32_t n_layers, const wkv_cache8 *
  */
 #define WKV_MAX_DRAFT 1024
 typedef struct {
-    uint32_t struct_size;      /* sizeof(wkv_draft), checked */
+    uint32_t struct_size;      /* sizeof(wkv_draft), or 16: without `before`; checked */
     int32_t words;             /* of a mask, >= max_new / 32 rounded up; max_new is at most WKV_MAX_DRAFT (WKV_ERR_LIMIT) */
     const uint32_t *masks;     /* DEVICE [B, max_new, words] or packed [T, words] */
+    const int32_t *before;     /* DEVICE int32 [B, H_kv] or NULL: every unit's rows in front of the draft */
 } wkv_draft;
+/*
+ * `before` is what the append took as `lengths`.  An append that runs out of rows drops a draft's last tokens, and its lengths_out ends at
+ * max_pages*page_size; how many it dropped can then be seen from `before` alone.  With `before`, the dropped tokens are seen by none and kept by
+ * none, and the rows in front of the draft stay as they are.  Without it the draft is taken to be the last rows of every unit, which is right only
+ * where lengths plus new tokens was max_pages*page_size at most in all of them: beyond, other rows would be taken for the draft's, attended to by its masks, and moved.
+ * Entries below 0, or below lengths less the new tokens, count as that, and those above lengths as lengths.
+ */
 /*
  * Masks of a draft that is a tree: token i hangs on token parents[i] of its sequence, or, where that is not in 0 .. i - 1, on the last
  * token in front of the draft.
@@ -686,8 +694,8 @@ int wkv_attend_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_dra
  * behind those in front of the draft; the others' rows are given up.  With a last[b] that is no token of the sequence none is kept.
  *   k_pools, v_pools    HOST arrays [n_layers] of DEVICE pool pointers, read and written; v_pools may be NULL
  *   last                DEVICE int32 [B]
- *   lengths             DEVICE int32 [B, H_kv]: rows of every unit, the draft's included
- *   lengths_out         DEVICE out, int32 [B, H_kv]; not `lengths` itself
+ *   lengths             DEVICE int32 [B, H_kv]: rows of every unit, the draft's included (those in front of it: draft->before)
+ *   lengths_out         DEVICE out, int32 [B, H_kv]; neither `lengths` nor `before` itself
  *   row_positions, row_weights   DEVICE or NULL, [B, H_kv, max_pages*page_size]: the rows' state, which moves with them
  * Rows whose page, or the one they would move to, is none are not moved.
  */

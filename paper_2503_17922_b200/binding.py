@@ -133,12 +133,17 @@ class WkvCache8(ctypes.Structure):
 
 
 class WkvDraft(ctypes.Structure):
-    """Mirror of `wkv_draft`."""
+    """Mirror of `wkv_draft` up to the masks."""
     _fields_ = [
         ("struct_size", ctypes.c_uint32),
         ("words", ctypes.c_int32),
         ("masks", ctypes.c_void_p),
     ]
+
+
+class WkvDraftBefore(WkvDraft):
+    """Mirror of the whole `wkv_draft`."""
+    _fields_ = [("before", ctypes.c_void_p)]
 
 
 class WkvError(RuntimeError):
@@ -1161,13 +1166,16 @@ def wkv_read_kv_paged8(cache: PagedCache8, layer: Layer8, lengths, k_out, v_out,
     prepare_read_kv_paged8(cache, layer, lengths, k_out, v_out, first, stream).run()
 
 
-def _check_draft(cache: PagedCache, masks) -> WkvDraft:
-    """Masks of drafted tokens, int32 [B, max_new, words] or packed [T, words], as a struct."""
+def _check_draft(cache: PagedCache, masks, before=None) -> WkvDraft:
+    """Masks of drafted tokens, int32 [B, max_new, words] or packed [T, words], as a struct; with the rows in front of them, int32 [B, H_kv]."""
     s, tokens = cache.shape, _chunk_tokens(cache)
     if masks is None or masks.dim() != (2 if cache.packed else 3):
         raise ValueError("masks: int32 [B, max_new, words] or packed [T, words] expected")
     _check_state(masks, ((tokens,) if cache.packed else (s.batch, s.max_new)) + (masks.shape[-1],), "int32", "masks")
-    return WkvDraft(ctypes.sizeof(WkvDraft), masks.shape[-1], _ptr(masks))
+    if before is None:
+        return WkvDraft(ctypes.sizeof(WkvDraft), masks.shape[-1], _ptr(masks))
+    _check_state(before, (s.batch, s.n_kv_heads), "int32", "before")
+    return WkvDraftBefore(ctypes.sizeof(WkvDraftBefore), masks.shape[-1], _ptr(masks), _ptr(before))
 
 
 def wkv_draft_masks(cache: PagedCache, parents, masks=None, first=None, positions=None, stream=None) -> None:
@@ -1195,17 +1203,18 @@ def _check_attend(cache: PagedCache, q, lengths, out, lse, weights_in=None, weig
     return _head_strides(q, cache.packed, "q"), _head_strides(out, cache.packed, "out")
 
 
-def prepare_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, lse=None, stream=None) -> PreparedCall:
-    """Attention of drafted tokens: as prepare_attend_paged, each new token to the rows in front of the draft and to the tokens that its mask names."""
-    _check_devices(cache.device, "draft attention", masks, q, k_pool, v_pool, lengths, out, workspace, lse)
+def prepare_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, lse=None, before=None, stream=None) -> PreparedCall:
+    """Attention of drafted tokens: as prepare_attend_paged, each new token to the rows in front of the draft and to the tokens that its mask names.
+    before: int32 [B, H_kv], the lengths that the append took; needed where a unit had no rows left for its whole draft."""
+    _check_devices(cache.device, "draft attention", masks, q, k_pool, v_pool, lengths, out, workspace, lse, before)
     _check_pool(cache, k_pool, "k_pool")
     _check_pool(cache, v_pool, "v_pool")
     qs, os_ = _check_attend(cache, q, lengths, out, lse)
-    draft = _check_draft(cache, masks)
+    draft = _check_draft(cache, masks, before)
     args = (ctypes.byref(cache.shape), ctypes.byref(draft), _ptr(q), qs, _ptr(k_pool), _ptr(v_pool), _ptr(lengths), _ptr(out), os_, _ptr(lse),
             _ptr(workspace), workspace.numel(), _stream(stream))
     return PreparedCall(lib().wkv_attend_draft_paged, "wkv_attend_draft_paged", args,
-                        (cache, draft, masks, q, qs, k_pool, v_pool, lengths, out, os_, lse, workspace))
+                        (cache, draft, masks, before, q, qs, k_pool, v_pool, lengths, out, os_, lse, workspace))
 
 
 def wkv_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, **kw) -> None:
@@ -1213,15 +1222,17 @@ def wkv_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths,
 
 
 def prepare_attend_paged8(cache: PagedCache8, layer: Layer8, q, lengths, out, workspace, lse=None, weights_in=None, weights_out=None, draft=None,
-                          stream=None) -> PreparedCall:
-    """Attention of the new tokens over the 8-bit cache: as prepare_attend_paged; `draft`: masks as in prepare_attend_draft_paged (without weights)."""
-    _check_devices(cache.device, "attention over the 8-bit cache", layer.tensors, q, lengths, out, workspace, lse, weights_in, weights_out, draft)
+                          before=None, stream=None) -> PreparedCall:
+    """Attention of the new tokens over the 8-bit cache: as prepare_attend_paged; `draft`, `before`: masks and rows as in prepare_attend_draft_paged (without weights)."""
+    _check_devices(cache.device, "attention over the 8-bit cache", layer.tensors, q, lengths, out, workspace, lse, weights_in, weights_out, draft, before)
+    if before is not None and draft is None:
+        raise ValueError("before: only with a draft")
     qs, os_ = _check_attend(cache, q, lengths, out, lse, weights_in, weights_out)
-    masks = _check_draft(cache, draft) if draft is not None else None
+    masks = _check_draft(cache, draft, before) if draft is not None else None
     args = (ctypes.byref(cache.shape), ctypes.byref(layer.struct), ctypes.byref(masks) if masks is not None else None, _ptr(q), qs, _ptr(lengths),
             _ptr(out), os_, _ptr(lse), _ptr(weights_in), _ptr(weights_out), _ptr(workspace), workspace.numel(), _stream(stream))
     return PreparedCall(lib().wkv_attend_paged8, "wkv_attend_paged8", args,
-                        (cache, layer, masks, draft, q, qs, lengths, out, os_, lse, weights_in, weights_out, workspace))
+                        (cache, layer, masks, draft, before, q, qs, lengths, out, os_, lse, weights_in, weights_out, workspace))
 
 
 def wkv_attend_paged8(cache: PagedCache8, layer: Layer8, q, lengths, out, workspace, **kw) -> None:
@@ -1250,21 +1261,22 @@ def wkv_evict_kv_paged8(cache: PagedCache8, layers: Sequence[Layer8], weights, p
                                      workspace.numel(), _stream(stream)), "wkv_evict_kv_paged8")
 
 
-def _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, *pools) -> WkvDraft:
-    _check_devices(cache.device, "draft", masks, last, lengths, lengths_out, row_positions, row_weights, *pools)
+def _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, before, *pools) -> WkvDraft:
+    _check_devices(cache.device, "draft", masks, last, lengths, lengths_out, row_positions, row_weights, before, *pools)
     units = (cache.shape.batch, cache.shape.n_kv_heads)
     _check_state(last, units[:1], "int32", "last")
     _check_state(lengths, units, "int32", "lengths")
     _check_state(lengths_out, units, "int32", "lengths_out")
     _check_state(row_positions, units + (cache.capacity,), "int32", "row_positions")
     _check_state(row_weights, units + (cache.capacity,), "float32", "row_weights")
-    return _check_draft(cache, masks)
+    return _check_draft(cache, masks, before)
 
 
 def wkv_keep_draft_paged(cache: PagedCache, masks, k_pools, v_pools, last, lengths, lengths_out, row_positions=None, row_weights=None,
-                         stream=None) -> None:
-    """Of every sequence's draft the path of token last[b] (int32 [B]; -1: nothing) stays, directly behind the rows in front of the draft."""
-    draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, k_pools, v_pools)
+                         before=None, stream=None) -> None:
+    """Of every sequence's draft the path of token last[b] (int32 [B]; -1: nothing) stays, directly behind the rows in front of the draft.
+    before: as in prepare_attend_draft_paged."""
+    draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, before, k_pools, v_pools)
     for pools, what in ((k_pools, "k_pools"), (v_pools, "v_pools")):
         if pools is not None and len(pools) != len(k_pools):
             raise ValueError(f"{what}: one pool per layer")
@@ -1275,9 +1287,9 @@ def wkv_keep_draft_paged(cache: PagedCache, masks, k_pools, v_pools, last, lengt
 
 
 def wkv_keep_draft_paged8(cache: PagedCache8, masks, layers: Sequence[Layer8], last, lengths, lengths_out, row_positions=None, row_weights=None,
-                          stream=None) -> None:
+                          before=None, stream=None) -> None:
     """The same in an 8-bit cache."""
-    draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, [x.tensors for x in layers])
+    draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, before, [x.tensors for x in layers])
     _check(lib().wkv_keep_draft_paged8(ctypes.byref(cache.shape), ctypes.byref(draft), len(layers), _layers8(layers), _ptr(last), _ptr(lengths),
                                        _ptr(lengths_out), _ptr(row_positions), _ptr(row_weights), _stream(stream)), "wkv_keep_draft_paged8")
 

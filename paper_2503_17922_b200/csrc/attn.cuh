@@ -49,6 +49,7 @@ struct AttnArgs {
     // drafted tokens: query i attends to the rows in front of the new ones and to those of them that its mask names
     const unsigned *masks;       // [batch][max_q][words] or packed [total_q][words], or null
     int mask_words;
+    const int *before;           // [units] rows in front of the draft, or null: a unit's rows less the new ones
 };
 constexpr int kPlain = 0, kE4m3 = 1 + WKV_CACHE_E4M3, kI8 = 1 + WKV_CACHE_I8;
 
@@ -88,6 +89,14 @@ __device__ __forceinline__ long long attn_scale(const AttnArgs &a, int b, int h,
 {
     const int pg = j / a.page_size, page = __ldg(a.table + (long long)b * a.max_pages + pg);
     return ((long long)page * a.hkv + h) * a.page_size + (j - pg * a.page_size);
+}
+// Rows in front of a unit's new tokens (negative where those are more than the unit has rows).  A draft's can be given: an append that ran out of rows has dropped
+// the last tokens, and the difference of rows and tokens is not where the first ones lie.  Never so few that a row behind them were none of the m.
+template <bool DRAFT>
+__device__ __forceinline__ int attn_before(const AttnArgs &a, const AttnSeq &s, int unit)
+{
+    const int rest = s.n - s.m;
+    return DRAFT && a.before ? min(max(a.before[unit], max(rest, 0)), s.n) : rest;
 }
 // the mask of query i of sequence b
 __device__ __forceinline__ const unsigned *attn_mask(const AttnArgs &a, const AttnSeq &s, int b, int i)
@@ -222,7 +231,7 @@ struct DraftArgs {
     int cap;
     int n_tensors;
     bool scaled;
-    const int *last, *lengths;
+    const int *last, *lengths, *before;      // before: or null, as in AttnArgs
     int *lengths_out, *row_positions;
     float *row_weights;
 };

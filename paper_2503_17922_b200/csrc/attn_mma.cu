@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(const __grid_constan
         return;
     }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane >> 2, ql = lane & 3;
-    const int base = sq.n - sq.m + 1;                                    // keys that query 0 attends to (may be negative)
+    const int base = attn_before<DRAFT>(a, sq, unit) + 1;                // keys that query 0 attends to (may be negative)
     const int most = DRAFT ? sq.n : min(base + (min(row0 + kRows, rows) - 1) / a.G, sq.n);
     const int all_tiles = (max(most, 0) + kKeys - 1) / kKeys;
     const int t0 = (int)((long long)all_tiles * split / splits), t1 = (int)((long long)all_tiles * (split + 1) / splits);

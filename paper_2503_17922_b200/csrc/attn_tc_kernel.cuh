@@ -113,7 +113,7 @@ __device__ __forceinline__ bool get_item(const TcAttnArgs &t, long long k, Item 
     const int per = 2 * t.ppt, pairs = (im.sq.m + per - 1) / per, pair = pairs - 1 - rank;
     if (pair < 0) return false;
     im.pos0 = pair * per;
-    im.base = im.sq.n - im.sq.m + 1;
+    im.base = attn_before<DRAFT>(a, im.sq, im.unit) + 1;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int first = im.pos0 + x * t.ppt;

@@ -107,10 +107,12 @@ Cache8Pages pages_of(const wkv_paged *c)
 }
 
 constexpr int kFewDraftRows = 64;
+constexpr size_t kDraftWithoutBefore = offsetof(wkv_draft, before);
+const int32_t *rows_before(const wkv_draft *d) { return d->struct_size == sizeof(wkv_draft) ? d->before : nullptr; }
 int check_draft(const wkv_paged *c, const wkv_draft *d)
 {
-    if (d->struct_size != sizeof(wkv_draft)) {
-        set_error_detail("draft: struct_size %u != %zu", d->struct_size, sizeof(wkv_draft));
+    if (d->struct_size != sizeof(wkv_draft) && d->struct_size != kDraftWithoutBefore) {
+        set_error_detail("draft: struct_size %u is neither %zu nor, up to the masks, %zu", d->struct_size, sizeof(wkv_draft), kDraftWithoutBefore);
         return WKV_ERR_SHAPE;
     }
     if (c->max_new > WKV_MAX_DRAFT) {
@@ -153,8 +155,8 @@ int keep_draft(const wkv_paged *c, const Paged &p, const wkv_draft *draft, const
     if (!draft) return missing("draft");
     if ((st = check_draft(c, draft)) != WKV_OK) return st;
     if (!last || !lengths || !lengths_out) return missing("last, lengths or lengths_out");
-    if (lengths_out == lengths) {
-        set_error_detail("lengths_out must not be lengths (other blocks still read them)");
+    if (lengths_out == lengths || lengths_out == rows_before(draft)) {
+        set_error_detail("lengths_out must not be lengths or the draft's before (other blocks still read them)");
         return WKV_ERR_SHAPE;
     }
     if ((st = check_pools_apart(c)) != WKV_OK) return st;
@@ -175,6 +177,7 @@ int keep_draft(const wkv_paged *c, const Paged &p, const wkv_draft *draft, const
     a.scaled = scaled;
     a.last = last;
     a.lengths = lengths;
+    a.before = rows_before(draft);
     a.lengths_out = lengths_out;
     a.row_positions = row_positions;
     a.row_weights = row_weights;
@@ -353,6 +356,7 @@ int wkv_attend_draft_paged(const wkv_paged *c, const wkv_draft *draft, const voi
         return st;
     a.masks = draft->masks;
     a.mask_words = draft->words;
+    a.before = rows_before(draft);
     // A small draft over a short cache: every 16 rows read the keys for themselves, split over the blocks of a cluster, where all of those
     // run at once.  (12 tokens of 32 heads on 8, d = 128: masks, attention and keeping over 992 rows 12.1 us, 22.3 on the tensor cores, 4,000 rows 23.0 and 31.2, 8,000
     // rows, where a block's share reaches kClusterBytes, 38.3 and 36.3.)
@@ -389,6 +393,7 @@ int wkv_attend_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_dra
     if (draft && !none) {
         a.masks = draft->masks;
         a.mask_words = draft->words;
+        a.before = rows_before(draft);
     }
     return launch_attend(c, p, w, a, static_cast<char *>(workspace), static_cast<cudaStream_t>(cuda_stream));
 }

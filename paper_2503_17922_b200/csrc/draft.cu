@@ -64,14 +64,16 @@ __global__ void __launch_bounds__(kThreads) keep_draft_kernel(const __grid_const
         m = min(min(max(a.cu_q[b + 1] - a.cu_q[b], 0), a.max_q), a.total_q - lo);
         off = lo;
     }
-    const int n = min(max(a.lengths[unit], 0), a.cap), before = n - m;            // rows in front of the draft (negative: its first tokens have no row)
+    const int n = min(max(a.lengths[unit], 0), a.cap);
+    // rows in front of the draft (negative: its first tokens have no row; given: its last ones may have none)
+    const int before = a.before ? min(max(a.before[unit], max(n - m, 0)), n) : n - m;
     const int last = a.last[b];
     const unsigned *mask = (unsigned)last < (unsigned)m ? a.masks + (off + last) * a.words : nullptr;
     // the path's tokens that have a row, in order
     int count = 0;
     for (int j0 = 0; j0 < m && mask; j0 += kThreads) {
         const int j = j0 + tid;
-        const bool on = j < m && before + j >= 0 && (mask[j >> 5] >> (j & 31) & 1u);
+        const bool on = j < m && before + j >= 0 && before + j < n && (mask[j >> 5] >> (j & 31) & 1u);
         const unsigned votes = __ballot_sync(0xffffffffu, on);
         if (lane == 0) counts[warp] = __popc(votes);
         __syncthreads();
