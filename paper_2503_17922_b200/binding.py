@@ -1058,19 +1058,33 @@ class Layer8:
     kept alive here."""
 
     def __init__(self, cache: PagedCache8, k_codes, v_codes, k_scales, v_scales):
+        self.tensors = (k_codes, v_codes, k_scales, v_scales)
+        self.type = cache.type
+        self._fits = None
+        self.check(cache)
+        self.struct = WkvCache8(ctypes.sizeof(WkvCache8), cache.type, _ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales))
+
+    def check(self, cache: PagedCache8) -> None:
+        """The layer's type is the cache's, and its pools hold every row that the cache's description reaches: the C side sees addresses only."""
+        if getattr(cache, "type", None) != self.type:
+            raise ValueError(f"layer: codes of another type than the cache's ({getattr(cache, 'kind', 'not of 8 bits')})")
         s = cache.shape
+        geometry = (s.num_pages, s.n_kv_heads, s.page_size, s.head_dim, s.page_stride, s.head_stride, s.row_stride)
+        if geometry == self._fits:                # (descriptions made anew for every step mostly differ in the new tokens alone)
+            return
+        k_codes, v_codes, k_scales, v_scales = self.tensors
         need = (s.num_pages - 1) * s.page_stride + (s.n_kv_heads - 1) * s.head_stride + (s.page_size - 1) * s.row_stride + s.head_dim
         for t, what in ((k_codes, "k_codes"), (v_codes, "v_codes")):
             if t is not None and hasattr(t, "untyped_storage") and (t.element_size() != 1 or t.untyped_storage().nbytes() - t.storage_offset() < need):
                 raise ValueError(f"{what}: {need} bytes of codes expected, got {tuple(t.shape)} of {t.dtype}")
         for t, what in ((k_scales, "k_scales"), (v_scales, "v_scales")):
             _check_state(t, (s.num_pages, s.n_kv_heads, s.page_size), "uint8", what)
-        self.tensors = (k_codes, v_codes, k_scales, v_scales)
-        self.type = cache.type
-        self.struct = WkvCache8(ctypes.sizeof(WkvCache8), cache.type, _ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales))
+        self._fits = geometry
 
 
-def _layers8(layers: Sequence[Layer8]):
+def _layers8(cache: PagedCache8, layers: Sequence[Layer8]):
+    for x in layers:
+        x.check(cache)
     return (WkvCache8 * len(layers))(*[x.struct for x in layers])
 
 
@@ -1117,6 +1131,7 @@ def wkv_norm_append_kv_paged(cache: PagedCache, k_new, v_new, lengths, k_pool, v
 def prepare_append_kv_paged8(cache: PagedCache8, layer: Layer8, k_new, v_new, lengths, q=None, q_out=None, positions=None, norm=None, rope=None,
                              axes=None, lengths_out=None, row_positions=None, row_weights=None, stream=None) -> PreparedCall:
     """New tokens into the 8-bit cache, quantised as they are written; tensors as in prepare_norm_append_kv_paged."""
+    layer.check(cache)
     return _prepare_append(cache, layer, "wkv_append_kv_paged8", None, k_new, v_new, lengths, q, q_out, positions, norm, rope, axes, lengths_out,
                            row_positions, row_weights, stream)
 
@@ -1135,7 +1150,7 @@ def prepare_gather_kv_paged8(prob: Problem, cache: PagedCache8, layers: Sequence
         for t in tensors or ():
             _check_kv_layout(prob, t, what)
     _check_state(window_idx, (s.batch, s.n_kv_heads, prob.k_max), "int32", "window_idx")
-    arrs = (_ptr_array(k_layers), _ptr_array(v_layers), _layers8(layers))
+    arrs = (_ptr_array(k_layers), _ptr_array(v_layers), _layers8(cache, layers))
     args = (ctypes.byref(s), ctypes.byref(cache.shape), len(layers), arrs[0], arrs[1], _ptr(window_idx), arrs[2], _stream(stream))
     return PreparedCall(lib().wkv_gather_kv_paged8, "wkv_gather_kv_paged8", args, (prob, cache, layers, k_layers, v_layers, window_idx, arrs))
 
@@ -1148,6 +1163,7 @@ def prepare_read_kv_paged8(cache: PagedCache8, layer: Layer8, lengths, k_out, v_
     """Rows first[b, h] .. lengths[b, h] - 1 of the 8-bit cache as what they stand for: k_out, v_out [B, H_kv, rows, d] of bf16 or fp32 (either may be
     None); first int32 [B, H_kv] or None."""
     s = cache.shape
+    layer.check(cache)
     _check_devices(cache.device, "rows of the 8-bit cache", layer.tensors, lengths, k_out, v_out, first)
     some = k_out if k_out is not None else v_out
     if some is None or some.dim() != 4 or str(some.dtype) not in ("torch.float32", "torch.bfloat16"):
@@ -1227,6 +1243,7 @@ def prepare_attend_paged8(cache: PagedCache8, layer: Layer8, q, lengths, out, wo
     _check_devices(cache.device, "attention over the 8-bit cache", layer.tensors, q, lengths, out, workspace, lse, weights_in, weights_out, draft, before)
     if before is not None and draft is None:
         raise ValueError("before: only with a draft")
+    layer.check(cache)
     qs, os_ = _check_attend(cache, q, lengths, out, lse, weights_in, weights_out)
     masks = _check_draft(cache, draft, before) if draft is not None else None
     args = (ctypes.byref(cache.shape), ctypes.byref(layer.struct), ctypes.byref(masks) if masks is not None else None, _ptr(q), qs, _ptr(lengths),
@@ -1256,7 +1273,7 @@ def wkv_evict_kv_paged8(cache: PagedCache8, layers: Sequence[Layer8], weights, p
     _check_devices(cache.device, "eviction", [x.tensors for x in layers], weights, positions, lengths, weights_out, positions_out, lengths_out, workspace,
                    budgets)
     _check_eviction(cache, weights, positions, lengths, weights_out, positions_out, lengths_out, budgets)
-    _check(lib().wkv_evict_kv_paged8(ctypes.byref(cache.shape), len(layers), _layers8(layers), budget, _ptr(budgets), recent, _ptr(weights),
+    _check(lib().wkv_evict_kv_paged8(ctypes.byref(cache.shape), len(layers), _layers8(cache, layers), budget, _ptr(budgets), recent, _ptr(weights),
                                      _ptr(positions), _ptr(lengths), _ptr(weights_out), _ptr(positions_out), _ptr(lengths_out), _ptr(workspace),
                                      workspace.numel(), _stream(stream)), "wkv_evict_kv_paged8")
 
@@ -1290,7 +1307,7 @@ def wkv_keep_draft_paged8(cache: PagedCache8, masks, layers: Sequence[Layer8], l
                           before=None, stream=None) -> None:
     """The same in an 8-bit cache."""
     draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, before, [x.tensors for x in layers])
-    _check(lib().wkv_keep_draft_paged8(ctypes.byref(cache.shape), ctypes.byref(draft), len(layers), _layers8(layers), _ptr(last), _ptr(lengths),
+    _check(lib().wkv_keep_draft_paged8(ctypes.byref(cache.shape), ctypes.byref(draft), len(layers), _layers8(cache, layers), _ptr(last), _ptr(lengths),
                                        _ptr(lengths_out), _ptr(row_positions), _ptr(row_weights), _stream(stream)), "wkv_keep_draft_paged8")
 
 

@@ -35,6 +35,53 @@ def test_keep_refuses_lengths_out_in_the_place_of_before(L):
     assert keep(whole(masks=None), P3) == NULL
 
 
+def test_a_layer_is_held_against_the_cache_of_every_call(L):
+    """A description with more pages, heads, rows or columns than the layer's pools have, other strides or another type is refused by every call that takes the
+    layer (on CPU tensors: a call that was not would go on to the library); one that differs in the new tokens alone is not."""
+    def describe(kind="i8", pages=20, hk=2, d=64, page=16, max_new=3, layout="phsd", cls=binding.PagedCache8):
+        kw = dict(kind=kind) if cls is binding.PagedCache8 else {}
+        return cls(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=hk, head_dim=d, page_size=page, num_pages=pages, max_new=max_new, layout=layout,
+                   block_table=torch.zeros((2, 9), dtype=torch.int32), **kw)
+    made = describe()
+    codes = [torch.zeros((20, 2, 16, 64), dtype=torch.uint8) for _ in range(2)]
+    one = binding.Layer8(made, *codes, made.alloc_scales(), made.alloc_scales())
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)
+    ws = torch.zeros(10, dtype=torch.uint8)
+
+    def calls(c):
+        hk, d, m, cap = c.shape.n_kv_heads, c.shape.head_dim, c.shape.max_new, c.capacity
+        bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+        k, q, lengths, masks = bf(2, hk, m, d), bf(2, 4, m, d), ints(2, hk), ints(2, m, 1)
+        weights = lambda: torch.zeros((2, hk, cap))
+        return [lambda: binding.prepare_append_kv_paged8(c, one, k, k, lengths, stream=0), lambda: binding.prepare_attend_paged8(c, one, q, lengths, q.clone(), ws, stream=0),
+                lambda: binding.prepare_read_kv_paged8(c, one, lengths, bf(2, hk, 5, d), None, stream=0),
+                lambda: binding.wkv_evict_kv_paged8(c, [one, one], weights(), ints(2, hk, cap), lengths, 5, 0, weights(), ints(2, hk, cap), ints(2, hk), ws),
+                lambda: binding.wkv_keep_draft_paged8(c, masks, [one], ints(2), lengths, ints(2, hk))]
+    others = [describe("e4m3"), describe(pages=21), describe(hk=4), describe(d=128), describe(page=32), describe(layout=(2 * 16 * 64, 16 * 64, 80)),
+              describe(layout=(2 * 16 * 64 + 64, 16 * 64, 64)), describe(cls=binding.PagedCache)]
+    for i, c in enumerate(others):
+        for j, call in enumerate(calls(c)):
+            with pytest.raises(ValueError):
+                call()
+                pytest.fail(f"description {i}, call {j} was not refused")
+    for c in (made, describe(max_new=7), describe(layout="pshd")):         # (the last: as many bytes)
+        one.check(c)
+        for call in calls(c)[:3]:
+            assert isinstance(call(), binding.PreparedCall)
+
+
+def test_the_gather_holds_its_layers_against_the_cache(L):
+    table = torch.zeros((1, 9), dtype=torch.int32)
+    make = lambda pages: binding.PagedCache8(kind="i8", dtype="bf16", batch=1, n_q_heads=2, n_kv_heads=2, head_dim=64, page_size=16, num_pages=pages, block_table=table)
+    cache, larger = make(9), make(10)
+    one = binding.Layer8(cache, *(torch.zeros((9, 2, 16, 64), dtype=torch.uint8) for _ in range(2)), cache.alloc_scales(), cache.alloc_scales())
+    prob = binding.Problem(dtype="bf16", batch=1, n_q_heads=2, n_kv_heads=2, head_dim=64, l_obs=8, window=8, task=0, top_p=0, max_seqlen=100, budgets=[40], device="cpu")
+    k, idx = torch.zeros((1, 2, 100, 64), dtype=torch.bfloat16), torch.zeros((1, 2, prob.k_max), dtype=torch.int32)
+    assert isinstance(binding.prepare_gather_kv_paged8(prob, cache, [one], [k], [k], idx, stream=0), binding.PreparedCall)
+    with pytest.raises(ValueError):
+        binding.prepare_gather_kv_paged8(prob, larger, [one], [k], [k], idx, stream=0)
+
+
 def test_python_face_refuses_other_rows_before(L):
     table = torch.zeros((2, 9), dtype=torch.int32)
     kw = dict(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=16, num_pages=20, block_table=table, max_new=3)
