@@ -153,7 +153,9 @@ int keep_draft(const wkv_paged *c, const Paged &p, const wkv_draft *draft, const
 {
     int st;
     if (!draft) return missing("draft");
-    if ((st = check_draft(c, draft)) != WKV_OK) return st;
+    // (no new tokens: there are no masks, and the lengths stay)
+    const bool none = c->cu_new_host && p.total_new == 0;
+    if (!none && (st = check_draft(c, draft)) != WKV_OK) return st;
     if (!last || !lengths || !lengths_out) return missing("last, lengths or lengths_out");
     if (lengths_out == lengths || lengths_out == rows_before(draft)) {
         set_error_detail("lengths_out must not be lengths or the draft's before (other blocks still read them)");
@@ -169,15 +171,15 @@ int keep_draft(const wkv_paged *c, const Paged &p, const wkv_draft *draft, const
     a.max_q = c->max_new;
     a.total_q = p.total_new;
     a.cu_q = c->cu_new_dev;
-    a.masks = draft->masks;
-    a.words = draft->words;
+    a.masks = none ? nullptr : draft->masks;
+    a.words = none ? 0 : draft->words;
     a.pages = pages_of(c);
     a.cap = p.cap;
     a.n_tensors = n_tensors;
     a.scaled = scaled;
     a.last = last;
     a.lengths = lengths;
-    a.before = rows_before(draft);
+    a.before = none ? nullptr : rows_before(draft);
     a.lengths_out = lengths_out;
     a.row_positions = row_positions;
     a.row_weights = row_weights;

@@ -135,3 +135,39 @@ def test_rows_in_front_of_a_draft_are_limited_to_the_draft():
     for head in range(2):
         ref, _, _, bd = cu.attention_seen(q[0, head], k, v, torch.ones((m, n), dtype=torch.bool, device="cuda"))
         ou.assert_close(outs[n][0, head], ref, ou.output_bound(ref, bd, torch.bfloat16), "all rows in front")
+
+
+# ---- batches without a token -----------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["plain", "e4m3"])
+@pytest.mark.parametrize("given", [False, True])
+def test_a_step_in_which_no_sequence_drafts(kind, given):
+    """Every call of a draft's step with packed tensors of no rows: nothing to attend or keep, and lengths stay."""
+    g, d, lengths = gen(33), 64, [[20, 3], [0, 64]]
+    c = cu.Cache8(g, kind, 2, 2, d, 16, 4) if kind != "plain" else ou.Cache(g, torch.bfloat16, 2, 2, d, 16, 4, fill=55.0)
+    c.fill(g, lengths)
+    if kind != "plain":
+        cache, (layer,) = c.describe("bf16", 4, 5, [0, 0, 0])
+        tensors = c.codes[0] + c.scales[0]
+    else:
+        cache = wkv.PagedCache(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=d, page_size=16, num_pages=c.num_pages, block_table=c.table, max_new=5,
+                               cu_new=[0, 0, 0])
+        tensors = c.k + c.v
+    held = [t.clone() for t in tensors]
+    empty = lambda *s, dtype=torch.bfloat16: torch.zeros((0, *s), dtype=dtype, device="cuda")
+    q, k, masks, ws = empty(4, d), empty(2, d), empty(1, dtype=torch.int32), cache.alloc_workspace()
+    before = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    grown, kept = torch.full_like(before, 77), torch.full_like(before, 77)
+    last, more = torch.tensor([-1, 0], dtype=torch.int32, device="cuda"), dict(before=before) if given else {}
+    wkv.wkv_draft_masks(cache, empty(dtype=torch.int32), masks)
+    if kind != "plain":
+        wkv.wkv_append_kv_paged8(cache, layer, k, k, before, lengths_out=grown)
+        wkv.wkv_attend_paged8(cache, layer, q, grown, q.clone(), ws, draft=masks, **more)
+        wkv.wkv_keep_draft_paged8(cache, masks, [layer], last, grown, kept, **more)
+    else:
+        wkv.wkv_append_kv_paged(cache, k, k, before, c.k[0], c.v[0], lengths_out=grown)
+        wkv.wkv_attend_draft_paged(cache, masks, q, c.k[0], c.v[0], grown, q.clone(), ws, **more)
+        wkv.wkv_keep_draft_paged(cache, masks, c.k, c.v, last, grown, kept, **more)
+    torch.cuda.synchronize()
+    assert torch.equal(grown, before) and torch.equal(kept, before)
+    for t, w in zip(tensors, held):
+        assert torch.equal(t, w)
