@@ -6,7 +6,7 @@ import torch
 import cache8_util as cu
 import operators_util as ou
 from paper_2503_17922_b200 import binding as wkv
-from test_gpu_cache8 import DT, cumulated, gen, name_of, randn, random_tree
+from test_gpu_cache8 import DT, Attend, cumulated, gen, name_of, randn, random_tree
 
 pytestmark = pytest.mark.gpu
 
@@ -24,6 +24,8 @@ CUT = [
     ("f32", "plain", 4, 2, 64, 16, 9, "phsd", [7, 7, 7], False),
     ("f32", "plain", 4, 2, 128, 16, 9, "pshd", [40, 33, 1], True),
     ("f32", "i8", 4, 2, 80, 16, 9, "phsd", [20, 20, 20], False),
+    ("bf16", "plain", 4, 2, 128, 16, 132, "phsd", [70, 64, 70], True),
+    ("bf16", "i8", 8, 2, 96, 32, 70, "pshd", [40, 40, 40], False),
 ]
 
 
@@ -171,3 +173,102 @@ def test_a_step_in_which_no_sequence_drafts(kind, given):
     assert torch.equal(grown, before) and torch.equal(kept, before)
     for t, w in zip(tensors, held):
         assert torch.equal(t, w)
+
+
+# ---- units whose work several blocks share -----------------------------------------------------------------
+# The tensor-core kernel cuts its items (256 query rows of a unit) into pieces where a unit can have 2,048 rows, and joins them: with up to 128 items by
+# one kernel, with more by another.  Everything here has more than 64 rows per unit, and so goes there.
+MANY = [[2200 + h for h in range(8)]] + [[100 + 13 * b + h for h in range(8)] for b in range(15)] + [[33] * 8]
+SHARED = [
+    # dtype, kind, hq, hk, d, page, layout, lengths, news, packed, tree, hole
+    ("bf16", "plain", 4, 1, 128, 16, "phsd", [[2300], [130], [70]], [70, 33, 70], True, True, (0, 3)),
+    ("bf16", "plain", 6, 2, 80, 24, "pshd", [[2050, 2100], [60, 61]], [60, 25], True, False, None),
+    ("bf16", "plain", 2, 2, 64, 8, "phsd", [[2500, 300]], [300], False, False, (0, 100)),
+    ("bf16", "e4m3", 8, 2, 96, 64, "pshd", [[3000, 2990], [40, 40]], [40, 40], False, False, None),
+    ("bf16", "i8", 4, 2, 80, 16, "phsd", [[2500, 2048], [700, 699]], [130, 100], True, True, (1, 2)),
+    ("bf16", "e4m3", 4, 1, 128, 128, "phsd", [[5000]], [1024], False, True, None),
+    ("bf16", "plain", 16, 8, 128, 16, "phsd", MANY, [40] + [33 + b % 8 for b in range(15)] + [33], True, True, (0, 60)),
+    ("bf16", "i8", 16, 8, 96, 32, "pshd", MANY, [40] + [b % 41 for b in range(0, 150, 10)] + [33], True, False, None),
+]
+
+
+@pytest.mark.parametrize("case", SHARED, ids=lambda c: "-".join(map(str, c[:7])))
+def test_shared_items_of_drafts(case):
+    """Trees, and masks of any form; sequences with no rows in front of their draft, rows that see nothing, lengths of zero."""
+    g, news, tree = gen(41), case[8], case[10]
+    sees = [cu.tree_of(random_tree(g, m)) if tree else torch.rand((m, m), generator=g) < 0.3 for m in news]
+    if not tree:
+        for s in sees:
+            s[:1] = False
+    a = Attend(*case[:10], sees=sees, hole=case[11])
+    units, pairs = len(news) * a.hk, -(-max(max(news), 1) // (2 * (128 // (a.hq // a.hk))))
+    assert a.c.cap >= 2048 and max(news) * a.hq // a.hk > 64 and (units * pairs > 128) == (case[7] is MANY)
+    a.run()
+    a.check()
+    first = a.out.clone()
+    a.run()
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, first)                                      # pieces are joined in an order of their own
+
+
+@pytest.mark.parametrize("kind,d", [("plain", 128), ("plain", 80), ("e4m3", 128), ("i8", 96)])
+@pytest.mark.parametrize("front", [True, False])
+def test_shared_items_do_not_see_other_branches(kind, d, front):
+    """NaN (plain: infinities too) in a token's row reaches its descendants and nobody else, in the pieces of a cut item as in a whole one."""
+    new = 70
+    n = 2300 if front else new
+    parents = random_tree(gen(42), new, 0.3)
+    sees = cu.tree_of(parents)
+    a = Attend("bf16", kind, 4, 1, d, 16, "phsd", [[n], [2300]], [new, new], False, sees=[sees, sees])
+    a.run()
+    a.check()
+    clean = a.out.clone()
+    token = new // 3
+    at = n - new + token
+    if kind == "plain":
+        a.c.slot(a.c.v[0], 0, 0, at)[3] = float("nan")
+        a.c.slot(a.c.v[0], 0, 0, at)[5] = -float("inf")
+    else:
+        codes, scales, _ = a.c.raw(0, 1, 0, 0, n)
+        if kind == "e4m3":
+            codes[at, 3] = 0x7f
+        else:
+            scales[at] = 255
+        a.c.put(0, 1, 0, 0, torch.arange(n), codes, scales)
+    a.run()
+    torch.cuda.synchronize()
+    on = sees[:, token].cuda()
+    assert torch.equal(a.out[0][:, ~on], clean[0][:, ~on]) and torch.equal(a.out[1], clean[1])
+    assert torch.isnan(a.out[0][:, on][..., 3]).all() and not torch.isnan(clean).any()
+    if kind == "plain":
+        assert (a.out[0][:, on][..., 5] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("kind", ["plain", "e4m3"])
+def test_shared_items_of_two_streams_and_a_captured_call(kind):
+    """Two calls at once with workspaces of their own, and a captured one replayed on other inputs, give what each gives alone."""
+    def make(seed):
+        sees = [cu.tree_of(random_tree(gen(seed), 70)) for _ in range(2)]
+        return Attend("bf16", kind, 8, 2, 128, 16, "phsd", [[2300, 2290], [300, 299]], [70, 70], False, sees=sees, seed=seed)
+    a, b = make(1), make(2)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                x.run()
+    a.check()
+    b.check()
+    want = b.out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run()
+    pools = (lambda x: x.c.k + x.c.v) if kind == "plain" else (lambda x: x.c.codes[0] + x.c.scales[0])
+    for x, y in [(a.q, b.q), (a.masks, b.masks), (a.c.table, b.c.table)] + list(zip(pools(a), pools(b))):
+        x.copy_(y)
+    for _ in range(2):
+        a.out.fill_(77.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a.out, want)
+    del graph
