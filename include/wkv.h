@@ -641,7 +641,7 @@ int wkv_gather_kv_paged8(const wkv_shape *s, const wkv_paged *c, int32_t n_layer
  */
 int wkv_read_kv_paged8(const wkv_paged *c, const wkv_cache8 *layer, const int32_t *first, const int32_t *lengths, int32_t out_dtype,
                        int32_t row_capacity, void *k_out, void *v_out, void *cuda_stream);
-/* Rows leave the cache by weight: as wkv_evict_kv_paged, codes and scales of all layers given (HOST array [n_layers], all of one type).
+/* Rows leave the cache by weight: as wkv_evict_kv_paged, codes and scales of all layers given (HOST array [n_layers], all of one type, no tensor twice).
  * Workspace of wkv_paged8_workspace_bytes(). */
 int wkv_evict_kv_paged8(const wkv_paged *c, int32_t n_layers, const wkv_cache8 *layers, int32_t budget, const int32_t *budgets,
                         int32_t recent, const float *weights, const int32_t *positions, const int32_t *lengths, float *weights_out,
@@ -692,7 +692,7 @@ int wkv_attend_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_dra
 /*
  * What is kept of a draft: the tokens that the mask of token last[b] names (its path, itself included), in their order, take the rows
  * behind those in front of the draft; the others' rows are given up.  With a last[b] that is no token of the sequence none is kept.
- *   k_pools, v_pools    HOST arrays [n_layers] of DEVICE pool pointers, read and written; v_pools may be NULL
+ *   k_pools, v_pools    HOST arrays [n_layers] of DEVICE pool pointers, read and written, each once; v_pools may be NULL
  *   last                DEVICE int32 [B]
  *   lengths             DEVICE int32 [B, H_kv]: rows of every unit, the draft's included (those in front of it: draft->before)
  *   lengths_out         DEVICE out, int32 [B, H_kv]; neither `lengths` nor `before` itself
@@ -702,7 +702,7 @@ int wkv_attend_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_dra
 int wkv_keep_draft_paged(const wkv_paged *c, const wkv_draft *draft, int32_t n_layers, void *const *k_pools, void *const *v_pools,
                          const int32_t *last, const int32_t *lengths, int32_t *lengths_out, int32_t *row_positions,
                          float *row_weights, void *cuda_stream);
-/* The same in an 8-bit cache, codes and scales (layers: HOST array [n_layers], all of one type). */
+/* The same in an 8-bit cache, codes and scales (layers: HOST array [n_layers], all of one type, no tensor twice). */
 int wkv_keep_draft_paged8(const wkv_paged *c, const wkv_draft *draft, int32_t n_layers, const wkv_cache8 *layers, const int32_t *last,
                           const int32_t *lengths, int32_t *lengths_out, int32_t *row_positions, float *row_weights,
                           void *cuda_stream);

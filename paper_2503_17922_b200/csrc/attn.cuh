@@ -206,6 +206,18 @@ struct PoolTable {
 struct ScaleTable {
     unsigned char *ptr[2 * WKV_MAX_GROUP_LAYERS];
 };
+// Rows are moved inside every tensor given: one that is given twice would be moved by two blocks at once.
+template <typename Table>
+inline int check_once(const Table &x, int n, const char *what)
+{
+    for (int i = 1; i < n; ++i)
+        for (int j = 0; j < i; ++j)
+            if (x.ptr[i] == x.ptr[j]) {
+                set_error_detail("%s: #%d and #%d are the same", what, j, i);
+                return WKV_ERR_SHAPE;
+            }
+    return WKV_OK;
+}
 int launch_evict(const EvictArgs &a, const PoolTable &pools, const ScaleTable &scales, cudaStream_t stream);
 // 8-bit cache: the gather into it, and rows read back
 struct Cache8Pages {

@@ -315,6 +315,7 @@ int wkv_evict_kv_paged8(const wkv_paged *c, int32_t n_layers, const wkv_cache8 *
                          workspace_bytes, a)) != WKV_OK)
         return st;
     a.scaled = true;
+    if ((st = check_once(pools, n_tensors, "pools")) != WKV_OK || (st = check_once(scales, n_tensors, "scales")) != WKV_OK) return st;
     return launch_evict(a, pools, scales, static_cast<cudaStream_t>(cuda_stream));
 }
 

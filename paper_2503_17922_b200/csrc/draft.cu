@@ -165,6 +165,9 @@ int launch_keep_draft(const DraftArgs &a, const PoolTable &pools, const ScaleTab
         set_error_detail("draft: %lld (unit, tensor) pairs, rows of %d bytes", blocks, a.d * a.elem_bytes);
         return WKV_ERR_LIMIT;
     }
+    int st = check_once(pools, a.n_tensors, "pools");
+    if (st == WKV_OK && a.scaled) st = check_once(scales, a.n_tensors, "scales");
+    if (st != WKV_OK) return st;
     const cudaError_t err = launch_pdl(keep_draft_kernel, dim3((unsigned)blocks), kThreads, 0, stream, 1, a, pools, scales);
     if (err == cudaSuccess) count_launches(1);
     return check_cuda(err, "draft kernel");

@@ -35,6 +35,21 @@ def test_keep_refuses_lengths_out_in_the_place_of_before(L):
     assert keep(whole(masks=None), P3) == NULL
 
 
+def test_a_tensor_given_twice_is_refused(L):
+    """Rows are moved inside every tensor, by blocks of its own: the same one twice would be moved by two at once."""
+    c, BIG = paged(), 1 << 40
+    ptrs = lambda *p: (ctypes.c_void_p * len(p))(*p)
+    keep = lambda k, v: L.wkv_keep_draft_paged(ref(c), ref(draft()), len(k), k, v, P, P, P2, None, None, None)
+    assert keep(ptrs(P), ptrs(P)) == SHAPE and keep(ptrs(P, P2), ptrs(P3, P)) == SHAPE and keep(ptrs(P, P), None) == SHAPE
+    P5, P6 = 0x5000, 0x6000
+    other = lambda **kw: layer(**{**dict(k_codes=P5, v_codes=P6, k_scales=P5, v_scales=P6), **kw})
+    for second in (layer(), other(k_codes=P), other(v_codes=P), other(k_scales=P4), other(v_scales=P4)):
+        two = (binding.WkvCache8 * 2)(layer(), second)
+        assert L.wkv_keep_draft_paged8(ref(c), ref(draft()), 2, two, P, P, P2, None, None, None) == SHAPE
+        assert L.wkv_evict_kv_paged8(ref(c), 2, two, 5, None, 0, P, P, P, P, P, P, P, BIG, None) == SHAPE
+        assert b"are the same" in L.wkv_last_error_detail()
+
+
 def test_a_layer_is_held_against_the_cache_of_every_call(L):
     """A description with more pages, heads, rows or columns than the layer's pools have, other strides or another type is refused by every call that takes the
     layer (on CPU tensors: a call that was not would go on to the library); one that differs in the new tokens alone is not."""
