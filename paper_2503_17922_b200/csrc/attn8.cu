@@ -186,11 +186,12 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
             l[t][e] = 0.f;
         }
     // O is in units of v_ref / 2^14, a power of two that the row's p 2^e (p relative to m) have not passed twofold.  Of a float the upper half
-    // says enough: two of them are compared by one instruction.
-    constexpr unsigned kLeastRef = (unsigned)(kScaleBias + kLeastExponent - 10) << 7, kMostRef = 253u << 7;
-    float v_ref[NT][2];
+    // says enough: those of a tile's two rows are one word, and compared by one instruction.
+    constexpr unsigned kLeastRef = (unsigned)(kScaleBias + kLeastExponent - 10) << 7, kMostRef = 253u << 7, kBoth = 0x10001u;
+    unsigned v_ref[NT];
+    auto ref_bits = [](unsigned both, int e) { return e ? both & 0xffff0000u : both << 16; };
 #pragma unroll
-    for (int t = 0; t < NT; ++t) v_ref[t][0] = v_ref[t][1] = __uint_as_float(kLeastRef << 16);
+    for (int t = 0; t < NT; ++t) v_ref[t] = kLeastRef * kBoth;
 
     // ---- the ring of key tiles -----------------------------------------------------------------
     // A thread has a row of the tile: its place is looked up a tile ahead of its load, its scales a tile behind that: a trip to memory each.
@@ -364,19 +365,19 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
                     for (int y = 0; y < 4; ++y)
                         if (hidden >> ((g * NT + n) * 4 + y) & 1u) w[g][y] = 0.f;          // (0 times a NaN scale is not 0)
             }
-            // the rows' largest p 2^e, upper halves side by side
+            // the rows' largest p 2^e
             const float w_top[2] = {fmaxf(fmaxf(w[0][0], w[0][2]), fmaxf(w[1][0], w[1][2])), fmaxf(fmaxf(w[0][1], w[0][3]), fmaxf(w[1][1], w[1][3]))};
             unsigned tops = __byte_perm(__float_as_uint(w_top[0]), __float_as_uint(w_top[1]), 0x7632);
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, x));
 #pragma unroll
+            for (int e = 0; e < 2; ++e) keep[e] *= __uint_as_float(ref_bits(v_ref[n], e));
+            tops = __vmaxu2(tops, __byte_perm(__float_as_uint(keep[0]), __float_as_uint(keep[1]), 0x7632));
+            v_ref[n] = __vminu2(__vmaxu2(tops, kLeastRef * kBoth), kMostRef * kBoth) & 0xff80ff80u;
+#pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float before = v_ref[n][e] * keep[e];
-                const unsigned half = max(e ? tops >> 16 : tops & 0xffffu, __float_as_uint(before) >> 16) & 0xff80u;
-                const unsigned bits = min(max(half, kLeastRef), kMostRef) << 16;
-                v_ref[n][e] = __uint_as_float(bits);
-                const float inverse = __uint_as_float((254u << 23) - bits);
-                keep[e] = before * inverse;
+                const float inverse = __uint_as_float((254u << 23) - ref_bits(v_ref[n], e));
+                keep[e] *= inverse;
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
                     w[g][e] *= inverse * 16384.f;
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, DP == 256 ? 1 : (DP == 64 && NT == 1
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int r = n * 8 + 2 * ql + e;
-            const float by = v_ref[n][e] * (1.f / 16384.f);
+            const float by = __uint_as_float(ref_bits(v_ref[n], e)) * (1.f / 16384.f);
             if (quad == 0) {
                 sm.m[warp][r] = m[n][e];
                 sm.l[warp][r] = l[n][e];

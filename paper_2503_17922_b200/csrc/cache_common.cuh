@@ -190,8 +190,8 @@ inline int plan_splits(const wkv_paged *c, const Paged &p, int tile, bool &clust
 // keys 171 us on the warp-level kernel, 88 here; one of 4,000 42 and 32).
 constexpr int kFewRows = 16;
 // Over the 8-bit cache the tensor-core kernel has the codes to convert, for one query tile as for two: more rows are left to the warp-level one, which reads the
-// keys once more for every 16 of them (16 drafts over 4-8 K rows of 8 heads, d = 128, 20 rows at most 82 us there and 166 on the tensor cores, 48
-// rows 117 and 172, 64 rows 135 and 175, 96 rows 176 and 178, 128 rows 221 and 179; one draft of 64 rows over 8 K 42 and 40).
+// keys once more for every 16 of them (16 drafts over 4-8 K rows of 8 heads, d = 128, 20 rows at most 87 us there and 157 on the tensor cores, 48
+// rows 123 and 163, 64 rows 142 and 165, 96 rows 185 and 168, 128 rows 233 and 170; one draft of 64 rows over 8 K 34 and 40).
 constexpr int kFewRows8 = 64;
 // Rows per unit whose logits are kept for the weights: 4 bytes for each beside the 2 * d * 2 of K and V, written and read.
 constexpr int kLogitRows = 16;
