@@ -683,7 +683,7 @@ int wkv_attend_draft_paged(const wkv_paged *c, const wkv_draft *draft, const voi
 /* Attention of new tokens over an 8-bit cache: as wkv_attend_paged; with a draft as wkv_attend_draft_paged (weights_in and weights_out
  * NULL then, WKV_ERR_UNSUPPORTED otherwise).  Workspace of wkv_paged8_workspace_bytes().
  * Precision: fp32 throughout with dtype fp32.  With bf16 the weights are rounded once, as operands of the second product: to bf16 where there are
- * more than 64 rows (position x head of the group), d <= 128 and page_size is a multiple of 8; otherwise weight x 2^e of the value to f16, by 2^-11 of itself at most, but by
+ * more than 64 rows (position x head of the group), d <= 128, at most 128 query heads per KV head and page_size a multiple of 8; otherwise weight x 2^e of the value to f16, by 2^-11 of itself at most, but by
  * no less than 2^-39 of the largest weight x 2^e of the row, and there an element of q counts to 2^-40 of the row's largest one.  Scales are those that calls write
  * (e from -100 to 100). */
 int wkv_attend_paged8(const wkv_paged *c, const wkv_cache8 *layer, const wkv_draft *draft, const void *q, const int64_t *q_strides,

@@ -20,8 +20,10 @@
 // different ones.
 //
 // Bound by the instructions that make operands of codes, half of them on the half-rate integer pipe, and by what few warps can hide: 32 sequences of 4-8 K rows of 8
-// heads, d = 128, one token of 32 heads (int8, 423 MB): 91 us = 4.6 TB/s, with the rows' weights 105-110; issue slots 53 % busy, integer pipe 47 %, tensor pipe 12 %, 11 warps
-// per SM.  With tiles of 64 keys, one group to a warp, 137 with weights.  One token over 992 rows of one sequence: 7.7 us.
+// heads, d = 128, one token of 32 heads (int8, 423 MB): 92 us = 4.6 TB/s, with the rows' weights 105-112; issue slots 54 % busy, integer pipe 46 %, tensor pipe 13 %, 11 warps
+// per SM: the ring of 70 KB per block of four warps admits three.  With tiles of 64 keys, one group to a warp, 137 with weights.  With one reference for all of a
+// warp's rows, seen keys or not, 0.7 % less time, with 16 rows 5 % less, and wrong where a row does not see the largest value (16 drafts over 4-8 K rows,
+// 64 rows at most: 142 and 135 us).  One token over 992 rows of one sequence: 7.7 us.
 #include "attn_cluster.cuh"
 #include "cache8.cuh"
 

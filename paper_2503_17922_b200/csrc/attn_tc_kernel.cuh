@@ -26,7 +26,9 @@
 // EIGHT: keys and values of 8 bits.  Warps 12-15 make bf16 tiles of them, exactly (a row's scale is a power of two), in the place where TMA otherwise puts
 // them; TMA's own tiles of codes have a ring in front of that.  What follows is the same.  Bound by those four warps' instructions beside the softmax's, on one
 // half-rate integer pipe and one instruction cache: four sequences of 8-16 K keys, 512 new tokens of 32 heads on 8, d = 128: 456-464 us (329 over bf16 rows; 386 in a copy that
-// converts nothing); issue slots 49 % busy, tensor pipe 32 %.  The loop over a tile is kept small, as the softmax's code fills the cache: unrolled, 738 us.
+// converts nothing: the rest of the difference, with rings of three and four stages where the plain form has one of five, is not explained); issue slots 49 % busy, tensor pipe
+// 32 %.  P is rounded to bf16 as in the plain form: 1.7e-3 from the 64-bit value over a whole output of the case above, where weights of fp32 would leave the output's own
+// 1.5e-3.  The loop over a tile is kept small, as the softmax's code fills the cache: unrolled, 738 us.
 // DRAFT: the rows go by their masks, as far as the new tokens' rows are concerned: every row's keys reach to the unit's last one.  (16 drafts of 64 tokens over 4-8 K
 // rows of 8 bits, 32 heads on 8: 224-231 us; 197 in a copy that converts nothing.)
 //
@@ -646,10 +648,7 @@ __device__ __forceinline__ void mma_warp(const TcAttnArgs &t, Shared &sh, uint8_
                     umma_bf16_ta_if(leader, o_tmem, s_tmem + ks * 8, vd + (uint64_t)((ks * 2048) >> 4), o_idesc, 1);
                 umma_commit_if(leader, &sh.pv_done[x]);
                 ++turn[x];
-                if (u + 1 < tiles[x]) {
-                    // (keys that are still being made are waited for no earlier: their stage may be the values' before)
-                    scores(x, k_stage);
-                }
+                if (u + 1 < tiles[x]) scores(x, k_stage);
             }
             umma_commit_if(leader, &sh.empty[v_stage]);
             if (more) {

@@ -4,9 +4,10 @@
 // entry), into shared memory; then a group of lanes takes a row, a vector to a lane, and a few rows at a time, loads first.  The row's
 // largest magnitude, by which its scale goes, is found over the lanes of the group: a row is read once.
 //
-// Bound by instructions: the conversion of 16 bytes, and their share of the row's maximum, scale and place.  Two layers of eight prompts of up to 12,289 rows,
-// 30 % kept, d = 128, bf16 into int8 codes, and all of it read back, 142 MB: 38.5 us in two launches, with one vector to a lane 44.  Reading back with 16 codes to a lane
-// instead of eight was slower.
+// Bound by waiting rather than by a pipe: of the gather's issue slots 47 % are busy, with 26 warps on an SM; places come before the first load, and two
+// rows of a group are in flight.  Two layers of eight prompts of up to 12,289 rows, 30 % kept, d = 128, bf16 into int8 codes, and all of it read back,
+// 142 MB: 38.5 us, of which the gather (one launch) 20.9 and the two reads (one per layer) 18.3, each timed alone; with one vector to a lane 44 in all.  Reading back with 16 codes to a
+// lane instead of eight was slower.
 #include "cache8.cuh"
 
 #include <algorithm>

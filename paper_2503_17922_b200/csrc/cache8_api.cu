@@ -361,7 +361,7 @@ int wkv_attend_draft_paged(const wkv_paged *c, const wkv_draft *draft, const voi
     a.mask_words = draft->words;
     a.before = rows_before(draft);
     // A small draft over a short cache: every 16 rows read the keys for themselves, split over the blocks of a cluster, where all of those
-    // run at once.  (12 tokens of 32 heads on 8, d = 128: masks, attention and keeping over 992 rows 12.1 us, 22.3 on the tensor cores, 4,000 rows 23.0 and 31.2, 8,000
+    // run at once.  (12 tokens of 32 heads on 8, d = 128: the attention over 992 rows 12.1 us, 22.3 on the tensor cores, 4,000 rows 23.0 and 31.2, 8,000
     // rows, where a block's share reaches kClusterBytes, 38.3 and 36.3.)
     bool clustered = false;
     const int splits = c->dtype == WKV_BF16 && p.rows_max > 16 && p.rows_max <= kFewDraftRows ? plan_splits(c, p, 16, clustered) : 0;

@@ -4,7 +4,8 @@
 // Keeping: a token's row moves to that of a lower number or stays, and a row that one token takes is an earlier token's or its own.  So every
 // thread walks over the path in ascending order with its own 16 bytes of the rows, a few rows read ahead: what it overwrites it has read before.
 //
-// Bound by latency, each a launch of a few microseconds: masks, attention and keeping of one draft of 12 tokens over 992 rows take 12.1 us together.
+// Bound by latency, a launch each: of one draft of 12 tokens over 992 rows the masks take 1.5-2.0 us and keeping a path of one layer 4.6 (2.7 where no row moves), of 16 drafts of up to 64 tokens
+// 2.0-2.1 and 3.2-3.6, each in a graph of 20.
 #include "attn.cuh"
 
 namespace wkv {

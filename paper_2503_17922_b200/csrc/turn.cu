@@ -11,7 +11,11 @@
 // rows are on their way while the angles are computed.
 //
 // Bound by the instructions between load and store: 32,768 tokens, 32 query heads and 8 key heads of 128, bf16, three axes, 671 MB: 154-159 us = 4.3 TB/s with norms,
-// 81 % of issue slots busy; without norms 120 us = 5.6 TB/s.  With the tables read where they stand, neighbours in one bank, 177 us.  8 rows of 4 heads, d = 64, fp32, as every small call: 8 us, a launch and its trips to memory.
+// 81 % of issue slots busy; without norms 120 us = 5.6 TB/s.  With the tables read where they stand, neighbours in one bank, 177 us.  1,024 tokens of 4 query and 2 key heads, d = 64, fp32, as
+// every small call: 8 us, a launch and its trips to memory.  An element is unpacked twice, once for the squares and once for its product, and the
+// tables are read for every row.
+// In HALF order the whole row goes by the largest vector that half the turned dimensions are a multiple of: of 32,768 tokens as above with 124 dimensions turned (vectors of
+// two) 405 us, with 126, 62 or 34 (single elements) 620-650.
 #include "cache8.cuh"
 
 namespace wkv {
