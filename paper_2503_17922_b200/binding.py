@@ -1219,7 +1219,7 @@ def _check_attend(cache: PagedCache, q, lengths, out, lse, weights_in=None, weig
     return _head_strides(q, cache.packed, "q"), _head_strides(out, cache.packed, "out")
 
 
-def prepare_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, lse=None, before=None, stream=None) -> PreparedCall:
+def prepare_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths, out, workspace, lse=None, stream=None, before=None) -> PreparedCall:
     """Attention of drafted tokens: as prepare_attend_paged, each new token to the rows in front of the draft and to the tokens that its mask names.
     before: int32 [B, H_kv], the lengths that the append took; needed where a unit had no rows left for its whole draft."""
     _check_devices(cache.device, "draft attention", masks, q, k_pool, v_pool, lengths, out, workspace, lse, before)
@@ -1238,7 +1238,7 @@ def wkv_attend_draft_paged(cache: PagedCache, masks, q, k_pool, v_pool, lengths,
 
 
 def prepare_attend_paged8(cache: PagedCache8, layer: Layer8, q, lengths, out, workspace, lse=None, weights_in=None, weights_out=None, draft=None,
-                          before=None, stream=None) -> PreparedCall:
+                          stream=None, before=None) -> PreparedCall:
     """Attention of the new tokens over the 8-bit cache: as prepare_attend_paged; `draft`, `before`: masks and rows as in prepare_attend_draft_paged (without weights)."""
     _check_devices(cache.device, "attention over the 8-bit cache", layer.tensors, q, lengths, out, workspace, lse, weights_in, weights_out, draft, before)
     if before is not None and draft is None:
@@ -1290,7 +1290,7 @@ def _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_wei
 
 
 def wkv_keep_draft_paged(cache: PagedCache, masks, k_pools, v_pools, last, lengths, lengths_out, row_positions=None, row_weights=None,
-                         before=None, stream=None) -> None:
+                         stream=None, before=None) -> None:
     """Of every sequence's draft the path of token last[b] (int32 [B]; -1: nothing) stays, directly behind the rows in front of the draft.
     before: as in prepare_attend_draft_paged."""
     draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, before, k_pools, v_pools)
@@ -1304,7 +1304,7 @@ def wkv_keep_draft_paged(cache: PagedCache, masks, k_pools, v_pools, last, lengt
 
 
 def wkv_keep_draft_paged8(cache: PagedCache8, masks, layers: Sequence[Layer8], last, lengths, lengths_out, row_positions=None, row_weights=None,
-                          before=None, stream=None) -> None:
+                          stream=None, before=None) -> None:
     """The same in an 8-bit cache."""
     draft = _keep_state(cache, masks, last, lengths, lengths_out, row_positions, row_weights, before, [x.tensors for x in layers])
     _check(lib().wkv_keep_draft_paged8(ctypes.byref(cache.shape), ctypes.byref(draft), len(layers), _layers8(cache, layers), _ptr(last), _ptr(lengths),

@@ -1,5 +1,6 @@
 """CPU-only checks of the rows in front of a draft and of a layer against its cache: struct mirrors and refusals before any device work."""
 import ctypes
+import inspect
 
 import pytest
 import torch
@@ -117,3 +118,9 @@ def test_python_face_refuses_other_rows_before(L):
             binding.wkv_keep_draft_paged8(cache, masks, [one], ints(2), lengths, ints(2, 2), before=before)
     with pytest.raises(ValueError):
         binding.prepare_attend_paged8(cache, one, q, lengths, q.clone(), ws, before=lengths)
+
+
+@pytest.mark.parametrize("call", [binding.prepare_attend_draft_paged, binding.prepare_attend_paged8, binding.wkv_keep_draft_paged, binding.wkv_keep_draft_paged8])
+def test_rows_before_come_behind_every_argument_that_was_there(call):
+    """A stream that is given by its place stays the stream."""
+    assert list(inspect.signature(call).parameters)[-2:] == ["stream", "before"]
